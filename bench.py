@@ -67,7 +67,10 @@ WORKLOADS = {
 ATTENTION_KERNELS = ("paged_decode_mfma_kernel", "paged_decode_short_kernel", "paged_decode_f32_kernel",
                      "paged_prefill_mfma_kernel", "paged_jagged_mfma_kernel", "paged_attention_f32_kernel", "paged_attention_generic_kernel")
 KERNELS = ATTENTION_KERNELS + ("paged_kv_append_kernel", "paged_kv_append_last_kernel", "paged_attention_merge_kernel",
-                               "paged_attention_merge_list_kernel")
+                               "paged_attention_merge_list_kernel") + (
+    # a step of drafted tokens
+    "paged_plan_step_kernel", "paged_release_blocks_kernel", "paged_rope_append_kernel", "paged_tree_accept_kernel",
+    "paged_attention_tree_generic_kernel")
 
 
 def read_kernels(binding, names):

@@ -246,6 +246,130 @@ pa_status paged_decode_step(const pa_kv_cache_desc* cache, const void* k_new, co
                             const pa_attn_mods* mods, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * ---------------------------------------------------------------------------
+ * A step of drafted tokens (a tree of candidates for each sequence, verified in one pass), on the GPU from end to end:
+ * plan the step, turn and append its keys, attend, keep what was accepted.  Each call stands alone as well: a decode or
+ * prefill program uses the plan and the rotary append in front of paged_attention_decode / _prefill.
+ *
+ * Rows of a step are packed: sequence s brings rows cu_q_lens[s] .. cu_q_lens[s+1]-1, its tokens in an order in which each
+ * follows (has a larger number than) its parent.  Token i of a sequence is appended at position ctx + i, the place
+ * of its K and V in the cache, whatever its place in the tree; what it is turned by is its depth, ctx + depth.
+ * ---------------------------------------------------------------------------
+ */
+
+/*
+ * Slots, positions, ancestor masks and pages of a step from the requests' lengths, in place and without the host
+ * (a captured graph can replay it): the device's own form of pa_pool_reserve for programs that keep the free list in
+ * device memory.  Use it OR a pa_pool for a table, not both.
+ * In: ctx_lens, new_lens int32[batch] (tokens in the cache; tokens that the step adds, 0 for none).  parents: NULL (each
+ * token follows the one before it) or int32[max_rows], packed by the prefix sums of new_lens: the number of the
+ * token's parent within its sequence; anything that is not a smaller number >= 0 makes the token a root (depth 0).
+ * State: block_table int32[batch, max_blocks] and num_blocks int32[batch], the mapped blocks of each row (row s maps
+ * blocks 0 .. num_blocks[s]-1); free_pages int32[..] and free_count int32[1], a stack.  The m-th page that the step
+ * lacks, in the order of sequences and blocks, is free_pages[free_count - 1 - m].
+ * Out: seq_lens = ctx_lens + new_lens and cu_q_lens int32[batch + 1], as paged_attention_prefill takes them; for each of
+ * max_rows rows seq_ids, positions (ctx + i), rope_positions (ctx + depth; may be NULL) and tree_mask (may be NULL):
+ * uint64[max_rows, mask_words], bit t = the row's token is token t or follows it.  Rows behind the last
+ * sequence's: seq_ids = positions = -1, rope_positions = 0, masks 0.
+ * shortage int32[2]: [0] pages that the free list lacks, [1] sequences whose blocks exceed max_blocks or whose tokens
+ * exceed the masks' bits, plus rows beyond max_rows.  Unless both are 0 nothing is granted: table, counts and free
+ * list stay as they were, seq_lens = ctx_lens, cu_q_lens = 0 (attention then has nothing to do); the rows' arrays describe
+ * the request all the same.  No output may overlap another array.
+ */
+pa_status paged_plan_step(const int32_t* ctx_lens, const int32_t* new_lens, int32_t batch, const int32_t* parents,
+                          int32_t page_size, int32_t* block_table, int32_t max_blocks, int32_t* num_blocks,
+                          const int32_t* free_pages, int32_t* free_count, int32_t max_rows, int32_t* seq_lens,
+                          int32_t* cu_q_lens, int32_t* seq_ids, int32_t* positions, int32_t* rope_positions,
+                          uint64_t* tree_mask, int32_t mask_words, int32_t* shortage, void* stream);
+
+/*
+ * The way back: sequence s keeps the blocks of its first keep_lens[s] tokens (0: none, a finished sequence), the others'
+ * entries become -1 and their pages return to the stack, the last one first, so that a plan for the same
+ * blocks takes the same pages again.  max_free: entries of free_pages.  A page that another row maps as well must not be
+ * given back (the device's list counts no references).
+ */
+pa_status paged_release_blocks(const int32_t* keep_lens, int32_t batch, int32_t page_size, int32_t* block_table,
+                               int32_t max_blocks, int32_t* num_blocks, int32_t* free_pages, int32_t* free_count,
+                               int32_t max_free, void* stream);
+
+/*
+ * Radians a position of the pairs of a rotary embedding, a pure host function: inv_freq (HOST, double[rotary_dim / 2])
+ * receives f_i = base^(-2 i / rotary_dim), scaled for contexts `factor` times as long as the `context` tokens that the
+ * base was made for, and mscale the factor on the turned coordinates.  scaling:
+ *   PA_ROPE_NONE    f_i
+ *   PA_ROPE_LINEAR  f_i / factor
+ *   PA_ROPE_BASE    base * factor^(r / (r - 2)) for base: the slowest pair is slowed by factor, the fastest not at all
+ *   PA_ROPE_PARTS   f_i for pairs that turn at least `fast` times in `context` tokens, f_i / factor for those that turn at
+ *                   most `slow` times, in between linearly in the turns
+ *   PA_ROPE_RAMP    the same linearly in the pair's number, from the number (rounded down) at which f would turn `fast`
+ *                   times to that (rounded up) at which it would turn `slow` times; mscale = 0.1 ln(factor) + 1
+ * Otherwise mscale = 1.  factor >= 1; 0 < slow < fast for the last two.
+ */
+typedef enum {
+    PA_ROPE_NONE = 0,
+    PA_ROPE_LINEAR = 1,
+    PA_ROPE_BASE = 2,
+    PA_ROPE_PARTS = 3,
+    PA_ROPE_RAMP = 4
+} pa_rope_scaling;
+pa_status pa_rope_frequencies(double* inv_freq, float* mscale, int32_t rotary_dim, double base, pa_rope_scaling scaling,
+                              double factor, double context, double slow, double fast);
+
+/*
+ * Rotary positions of q and k_new, and Algorithm 1, Assign, of the turned K rows and the V rows, in one pass.  Pair i of the
+ * first rotary_dim elements of a head, (i, i + rotary_dim / 2) or with interleaved != 0 (2 i, 2 i + 1), is turned by
+ * rope_positions[t] * inv_freq[i] (DEVICE double[rotary_dim / 2]; the angle is formed in 64 bits) and multiplied by mscale; the
+ * other elements are copied.  fp32 arithmetic, rounded once.
+ * q [T, Hq, d] -> q_out (may be q itself, with the same stride), both or neither NULL; k_new, v_new [T, Hkv, d], both or
+ * neither NULL: token t goes to position positions[t] of sequence seq_ids[t], as paged_kv_append takes them; a row with
+ * positions[t] < 0 (a padded batch), or whose block is not mapped, is not stored.  rope_positions int32[T] may
+ * be positions itself.  Strides: elements between tokens, multiples of 16 bytes, 0 = contiguous (heads are contiguous within
+ * a token), so the parts of one [T, Hq + 2 Hkv, d] projection are taken where they lie.  rotary_dim: even, at most
+ * head_dim; 0 turns nothing.  Types as the cache's.
+ */
+pa_status paged_rope_append(const pa_kv_cache_desc* cache, const void* q, int64_t q_stride, void* q_out,
+                            int64_t q_out_stride, int32_t num_q_heads, const void* k_new, int64_t k_stride,
+                            const void* v_new, int64_t v_stride, const int32_t* rope_positions, const int32_t* seq_ids,
+                            const int32_t* positions, int32_t T, const int32_t* block_table, int32_t batch,
+                            int32_t max_blocks, const double* inv_freq, int32_t rotary_dim, int32_t interleaved,
+                            float mscale, void* stream);
+
+/*
+ * Attention for trees of drafted tokens over the cache.  Sequence s brings n = cu_q_lens[s+1] - cu_q_lens[s] packed queries,
+ * whose K and V are its last n keys (seq_lens counts them; n <= seq_lens[s]).  A query sees every key of the context,
+ * j < seq_lens[s] - n, and of the drafted tokens those that its mask names: key seq_lens[s] - n + t if bit t (word t / 64, bit
+ * t % 64) of tree_mask[row] is set.  Any mask is taken, not only ancestors (a token need not see itself); bits from n
+ * on are ignored; a query without any visible key gives out = 0, lse = -inf.  Keys that no query of a
+ * sequence can see are masked by selection.
+ * tree_mask: uint64[total_q, mask_words], 64 * mask_words >= max_q_len (host upper bound of n).  q, out [total_q, Hq, d],
+ * lse NULL or float[total_q, Hq]; rows behind cu_q_lens[batch] are left as they were.  Workspace as for decode, of at least
+ * paged_attention_tree_workspace_bytes.  Any cache the library takes.  Results repeat bit for bit with the same arguments.
+ */
+size_t paged_attention_tree_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                            int32_t total_q, int32_t max_q_len, int32_t max_seq_len);
+pa_status paged_attention_tree(const pa_kv_cache_desc* cache, const void* q, void* out, float* lse,
+                               const int32_t* cu_q_lens, int32_t total_q, int32_t max_q_len, const uint64_t* tree_mask,
+                               int32_t mask_words, const int32_t* block_table, const int32_t* seq_lens, int32_t batch,
+                               int32_t num_q_heads, int32_t max_blocks, int32_t max_seq_len, float scale, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/*
+ * What stays of a verified step.  With tokens (the drafted tokens, int32 by packed row), targets (what the model chose
+ * behind each) and parents (as for the plan): the accepted path starts at the sequence's token 0, which is always
+ * kept (the token that the step before chose), and goes on to the first child of its last token whose token is
+ * that one's target, while there is one and the path has fewer than max_path tokens.  path int32[batch, max_path] receives
+ * the tokens' numbers, -1 behind them, path_lens int32[batch] their count and next_tokens (may be NULL) the last one's target.
+ * With all three NULL the caller's own rule has filled path and path_lens (numbers that climb; they are read only).
+ * Then K and V rows of the path move together: position ctx + path[i] -> ctx + i, ctx = seq_lens[s] - n; kept_lens (may be
+ * NULL, may be the plan's ctx_lens) = ctx + path_lens.  A sequence without drafted tokens: path_lens 0, next -1, kept =
+ * seq_lens.  max_q_len: host upper bound of n.  For further layers of a model call it again with their caches and the path found.
+ */
+pa_status paged_tree_accept(const pa_kv_cache_desc* cache, const int32_t* cu_q_lens, const int32_t* seq_lens, int32_t batch,
+                            int32_t max_q_len, const int32_t* parents, const int32_t* tokens, const int32_t* targets,
+                            int32_t* path, int32_t max_path, int32_t* path_lens, int32_t* next_tokens, int32_t* kept_lens,
+                            const int32_t* block_table, int32_t max_blocks, void* stream);
+
+/*
  * Debug utility: checks on the device the preconditions about device-side CONTENTS that the other entry points
  * assume and do not check.  counts (host, int64[3]) receives
  *   [0] block-table entries among the first ceil(seq_lens[s] / page_size) of a row that lie outside [0, num_pages)

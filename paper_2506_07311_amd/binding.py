@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -22,7 +22,8 @@ PA_DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 EXPORTS = (
     "paged_kv_append", "paged_kv_gather", "paged_attention_workspace_bytes", "paged_attention_decode",
     "paged_attention_prefill", "paged_attention_decode_mod", "paged_attention_prefill_mod", "paged_decode_step",
-    "paged_attention_decode_static", "pa_debug_check",
+    "paged_attention_decode_static", "paged_plan_step", "paged_release_blocks", "pa_rope_frequencies", "paged_rope_append",
+    "paged_attention_tree_workspace_bytes", "paged_attention_tree", "paged_tree_accept", "pa_debug_check",
     "pa_status_string", "pa_set_option", "pa_stream_read", "pa_profile_enable", "pa_profile_reset",
     "pa_profile_read",
     "pa_pool_create", "pa_pool_destroy", "pa_pool_set_growth", "pa_pool_reserve", "pa_pool_release", "pa_pool_share_prefix",
@@ -57,10 +58,12 @@ def load_library():
                 f"{path} is missing: build the HIP library first (python -m paper_2506_07311_amd.build). "
                 "There is no CPU fallback.")
         lib = ctypes.CDLL(path)
-        lib.paged_attention_workspace_bytes.restype = ctypes.c_size_t
+        sizes = ("paged_attention_workspace_bytes", "paged_attention_tree_workspace_bytes")
+        for name in sizes:
+            getattr(lib, name).restype = ctypes.c_size_t
         lib.pa_status_string.restype = ctypes.c_char_p
         for name in EXPORTS:
-            if name not in ("paged_attention_workspace_bytes", "pa_status_string"):
+            if name not in sizes and name != "pa_status_string":
                 getattr(lib, name).restype = ctypes.c_int
         _lib = lib
     return _lib
@@ -391,6 +394,272 @@ def paged_attention_prefill_mod(k_cache, v_cache, q, cu_q_lens, max_q_len: int, 
                                          _stream(stream))
     _check(st, "paged_attention_prefill_mod")
     return out
+
+
+# ---- a step of drafted tokens (see the block of that name in include/pagedattn.h) -----------------------------------
+
+def _together(what: str, *tensors) -> torch.device:
+    """All tensors on the current device, whose stream the call goes to."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise PagedAttnError(f"{what}: every tensor must be a device tensor")
+        if dev is not None and t.device != dev:
+            raise PagedAttnError(f"{what}: tensors on {dev} and {t.device}")
+        dev = t.device
+    if dev is not None and dev.index != torch.cuda.current_device():
+        raise PagedAttnError(f"{what}: tensors on {dev}, but the current device is cuda:{torch.cuda.current_device()}")
+    return dev
+
+
+def _shaped(t: torch.Tensor, what: str, shape, dtype=torch.int32) -> torch.Tensor:
+    if t.dtype != dtype or not t.is_contiguous() or not t.is_cuda or tuple(t.shape) != tuple(shape):
+        raise PagedAttnError(f"{what} must be a contiguous {dtype} device tensor of shape {list(shape)}, "
+                             f"got {t.dtype} {list(t.shape)}")
+    return t
+
+
+def _or_new(t, what, shape, device, dtype=torch.int32):
+    return torch.empty(shape, dtype=dtype, device=device) if t is None else _shaped(t, what, shape, dtype)
+
+
+class StepPlan(NamedTuple):
+    """What paged_plan_step leaves: the arguments of the calls that follow."""
+    seq_lens: torch.Tensor
+    cu_q_lens: torch.Tensor
+    seq_ids: torch.Tensor
+    positions: torch.Tensor
+    rope_positions: torch.Tensor
+    tree_mask: torch.Tensor
+    shortage: torch.Tensor
+
+
+def prepare_plan_step(ctx_lens, new_lens, block_table, num_blocks, free_pages, free_count, page_size: int, max_rows: int, *,
+                      parents=None, mask_words: int = 1, seq_lens=None, cu_q_lens=None, seq_ids=None, positions=None,
+                      rope_positions=None, tree_mask=None, shortage=None, stream=None) -> PreparedCall:
+    """paged_plan_step with its arguments marshalled once; the call returns a StepPlan.  Outputs are allocated unless
+    given (tree_mask: int64 [max_rows, mask_words], the bits of the header's uint64)."""
+    lib = load_library()
+    dev = _together("paged_plan_step", ctx_lens, new_lens, block_table, num_blocks, free_pages, free_count, parents, seq_lens,
+                    cu_q_lens, seq_ids, positions, rope_positions, tree_mask, shortage)
+    B = int(ctx_lens.shape[0])
+    _i32(block_table, "block_table"), _i32(free_pages, "free_pages")
+    if block_table.dim() != 2 or block_table.shape[0] != B or free_pages.dim() != 1:
+        raise PagedAttnError("block_table must be [batch, max_blocks], free_pages one-dimensional")
+    _shaped(ctx_lens, "ctx_lens", (B,)), _shaped(new_lens, "new_lens", (B,)), _shaped(num_blocks, "num_blocks", (B,))
+    _shaped(free_count, "free_count", (1,))
+    if parents is not None:
+        _shaped(parents, "parents", (max_rows,))
+    if tree_mask is not None:
+        mask_words = int(tree_mask.shape[-1])
+    plan = StepPlan(_or_new(seq_lens, "seq_lens", (B,), dev), _or_new(cu_q_lens, "cu_q_lens", (B + 1,), dev),
+                    _or_new(seq_ids, "seq_ids", (max_rows,), dev), _or_new(positions, "positions", (max_rows,), dev),
+                    _or_new(rope_positions, "rope_positions", (max_rows,), dev),
+                    _or_new(tree_mask, "tree_mask", (max_rows, mask_words), dev, torch.int64),
+                    _or_new(shortage, "shortage", (2,), dev))
+    args = (_p(ctx_lens), _p(new_lens), ctypes.c_int32(B), _p(parents), ctypes.c_int32(page_size), _p(block_table),
+            ctypes.c_int32(block_table.shape[1]), _p(num_blocks), _p(free_pages), _p(free_count), ctypes.c_int32(max_rows),
+            _p(plan.seq_lens), _p(plan.cu_q_lens), _p(plan.seq_ids), _p(plan.positions), _p(plan.rope_positions),
+            _p(plan.tree_mask if max_rows else None), ctypes.c_int32(mask_words), _p(plan.shortage), _stream(stream))
+    return PreparedCall(lib.paged_plan_step, args, (ctx_lens, new_lens, parents, block_table, num_blocks, free_pages,
+                                                    free_count, plan), "paged_plan_step", plan)
+
+
+def paged_plan_step(ctx_lens, new_lens, block_table, num_blocks, free_pages, free_count, page_size: int, max_rows: int,
+                    **kw) -> StepPlan:
+    """Slots, positions, ancestor masks and pages of a step from the requests' lengths; block_table, num_blocks and
+    free_count are updated in place.  Keyword arguments as for prepare_plan_step."""
+    return prepare_plan_step(ctx_lens, new_lens, block_table, num_blocks, free_pages, free_count, page_size, max_rows,
+                             **kw)()
+
+
+def prepare_release_blocks(keep_lens, block_table, num_blocks, free_pages, free_count, page_size: int, *,
+                           stream=None) -> PreparedCall:
+    lib = load_library()
+    _together("paged_release_blocks", keep_lens, block_table, num_blocks, free_pages, free_count)
+    B = int(keep_lens.shape[0])
+    _i32(block_table, "block_table"), _i32(free_pages, "free_pages")
+    if block_table.dim() != 2 or block_table.shape[0] != B or free_pages.dim() != 1:
+        raise PagedAttnError("block_table must be [batch, max_blocks], free_pages one-dimensional")
+    _shaped(keep_lens, "keep_lens", (B,)), _shaped(num_blocks, "num_blocks", (B,)), _shaped(free_count, "free_count", (1,))
+    args = (_p(keep_lens), ctypes.c_int32(B), ctypes.c_int32(page_size), _p(block_table), ctypes.c_int32(block_table.shape[1]),
+            _p(num_blocks), _p(free_pages), _p(free_count), ctypes.c_int32(free_pages.shape[0]), _stream(stream))
+    return PreparedCall(lib.paged_release_blocks, args, (keep_lens, block_table, num_blocks, free_pages, free_count),
+                        "paged_release_blocks")
+
+
+def paged_release_blocks(keep_lens, block_table, num_blocks, free_pages, free_count, page_size: int, *, stream=None) -> None:
+    """Gives the pages behind the first keep_lens[s] tokens of each sequence back to the free list, in place."""
+    prepare_release_blocks(keep_lens, block_table, num_blocks, free_pages, free_count, page_size, stream=stream)()
+
+
+PA_ROPE_SCALING = {"none": 0, "linear": 1, "base": 2, "parts": 3, "ramp": 4}
+
+
+def pa_rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                        context: float = 8192.0, slow: float = 1.0, fast: Optional[float] = None) -> Tuple[torch.Tensor, float]:
+    """(float64 [rotary_dim / 2] on the host, radians a position; factor on the turned coordinates).  ``fast`` defaults to 4
+    turns for "parts" and 32 for "ramp"."""
+    if scaling not in PA_ROPE_SCALING:
+        raise PagedAttnError(f"scaling must be one of {sorted(PA_ROPE_SCALING)}")
+    out = torch.empty(max(int(rotary_dim) // 2, 1), dtype=torch.float64)
+    mscale = ctypes.c_float(0.0)
+    fast = (32.0 if scaling == "ramp" else 4.0) if fast is None else fast
+    _check(load_library().pa_rope_frequencies(ctypes.c_void_p(out.data_ptr()), ctypes.byref(mscale), ctypes.c_int32(rotary_dim),
+                                              ctypes.c_double(base), ctypes.c_int(PA_ROPE_SCALING[scaling]),
+                                              ctypes.c_double(factor), ctypes.c_double(context), ctypes.c_double(slow),
+                                              ctypes.c_double(fast)), "pa_rope_frequencies")
+    return out, mscale.value
+
+
+def _rows(t: torch.Tensor, what: str, shape, dtype) -> torch.Tensor:
+    """[T, heads, d] whose tokens may lie apart (a part of one projection) but whose heads are contiguous."""
+    if t.dtype != dtype or not t.is_cuda or tuple(t.shape) != tuple(shape) or \
+            (t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]))):
+        raise PagedAttnError(f"{what} must be a {dtype} device tensor {list(shape)} with contiguous heads")
+    return t
+
+
+def _token_stride(t) -> ctypes.c_int64:
+    return ctypes.c_int64(0 if t is None or t.shape[0] < 2 else t.stride(0))
+
+
+def prepare_rope_append(k_cache, v_cache, q, k_new, v_new, rope_positions, seq_ids, positions, block_table, inv_freq, *,
+                        interleaved: bool = False, mscale: float = 1.0, q_out=None, head_major=False,
+                        stream=None) -> PreparedCall:
+    """paged_rope_append with its arguments marshalled once; the call returns ``q_out`` (allocated unless given; may be q).
+    q, or k_new and v_new with seq_ids, positions and block_table, may be None.  inv_freq: float64 [rotary_dim / 2] on the device."""
+    lib = load_library()
+    d = cache_desc(k_cache, v_cache, head_major)
+    dev = _together("paged_rope_append", k_cache, v_cache, q, k_new, v_new, rope_positions, seq_ids, positions, block_table,
+                    inv_freq, q_out)
+    T = int(rope_positions.shape[0])
+    _shaped(rope_positions, "rope_positions", (T,))
+    if inv_freq.dim() != 1:
+        raise PagedAttnError("inv_freq must be float64[rotary_dim / 2]")
+    _shaped(inv_freq, "inv_freq", inv_freq.shape, torch.float64)
+    Hq = 0
+    if q is not None:
+        Hq = int(q.shape[1]) if q.dim() == 3 else 0
+        _rows(q, "q", (T, Hq, d.head_dim), k_cache.dtype)
+        q_out = torch.empty((T, Hq, d.head_dim), dtype=q.dtype, device=dev) if q_out is None else \
+            _rows(q_out, "q_out", (T, Hq, d.head_dim), q.dtype)
+    elif q_out is not None:
+        raise PagedAttnError("q_out without q")
+    B = MB = 0
+    if k_new is not None:
+        if v_new is None or seq_ids is None or positions is None or block_table is None:
+            raise PagedAttnError("k_new needs v_new, seq_ids, positions and block_table")
+        _rows(k_new, "k_new", (T, d.num_kv_heads, d.head_dim), k_cache.dtype)
+        _rows(v_new, "v_new", (T, d.num_kv_heads, d.head_dim), k_cache.dtype)
+        _shaped(seq_ids, "seq_ids", (T,)), _shaped(positions, "positions", (T,)), _i32(block_table, "block_table")
+        if block_table.dim() != 2:
+            raise PagedAttnError("block_table must be [batch, max_blocks]")
+        B, MB = block_table.shape
+    elif v_new is not None:
+        raise PagedAttnError("v_new without k_new")
+    args = (ctypes.byref(d), _p(q), _token_stride(q), _p(q_out), _token_stride(q_out), ctypes.c_int32(Hq), _p(k_new),
+            _token_stride(k_new), _p(v_new), _token_stride(v_new), _p(rope_positions), _p(seq_ids), _p(positions),
+            ctypes.c_int32(T), _p(block_table), ctypes.c_int32(B), ctypes.c_int32(MB), _p(inv_freq),
+            ctypes.c_int32(2 * inv_freq.shape[0]), ctypes.c_int32(1 if interleaved else 0), ctypes.c_float(mscale),
+            _stream(stream))
+    return PreparedCall(lib.paged_rope_append, args, (d, k_cache, v_cache, q, q_out, k_new, v_new, rope_positions, seq_ids,
+                                                      positions, block_table, inv_freq), "paged_rope_append", q_out)
+
+
+def paged_rope_append(k_cache, v_cache, q, k_new, v_new, rope_positions, seq_ids, positions, block_table, inv_freq, **kw):
+    """Turns q and k_new by their positions, K and V into their pages.  Returns ``q_out``; keyword arguments as for
+    prepare_rope_append."""
+    return prepare_rope_append(k_cache, v_cache, q, k_new, v_new, rope_positions, seq_ids, positions, block_table, inv_freq,
+                               **kw)()
+
+
+def paged_attention_tree_workspace_bytes(batch: int, num_q_heads: int, num_kv_heads: int, head_dim: int, total_q: int,
+                                         max_q_len: int, max_seq_len: int) -> int:
+    return int(load_library().paged_attention_tree_workspace_bytes(
+        ctypes.c_int32(batch), ctypes.c_int32(num_q_heads), ctypes.c_int32(num_kv_heads), ctypes.c_int32(head_dim),
+        ctypes.c_int32(total_q), ctypes.c_int32(max_q_len), ctypes.c_int32(max_seq_len)))
+
+
+def prepare_attention_tree(k_cache, v_cache, q, cu_q_lens, max_q_len: int, tree_mask, block_table, seq_lens, max_seq_len: int,
+                           scale: float, *, out=None, lse=None, workspace=None, head_major=False,
+                           stream=None) -> PreparedCall:
+    """paged_attention_tree with its arguments marshalled once; the call returns ``out``.  tree_mask: int64 [total_q, words]."""
+    lib = load_library()
+    d = cache_desc(k_cache, v_cache, head_major)
+    dev = _together("paged_attention_tree", k_cache, v_cache, q, cu_q_lens, tree_mask, block_table, seq_lens, out, lse, workspace)
+    _dense(q, "q", k_cache.dtype)
+    if q.dim() != 3 or q.shape[2] != d.head_dim:
+        raise PagedAttnError("q must be [total_q, Hq, d]")
+    total_q, Hq, hd = q.shape
+    B = int(seq_lens.shape[0])
+    _shaped(seq_lens, "seq_lens", (B,)), _shaped(cu_q_lens, "cu_q_lens", (B + 1,)), _i32(block_table, "block_table")
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise PagedAttnError("block_table must be [batch, max_blocks]")
+    if tree_mask.dim() != 2:
+        raise PagedAttnError("tree_mask must be int64[total_q, words]")
+    words = int(tree_mask.shape[1])
+    _shaped(tree_mask, "tree_mask", (total_q, words), torch.int64)
+    out = torch.empty_like(q) if out is None else _shaped(out, "out", q.shape, q.dtype)
+    if lse is not None:
+        _shaped(lse, "lse", (total_q, Hq), torch.float32)
+    if workspace is None:
+        workspace = _workspace(None, paged_attention_tree_workspace_bytes(B, Hq, d.num_kv_heads, hd, total_q, max_q_len,
+                                                                          max_seq_len), dev)
+    args = (ctypes.byref(d), _p(q), _p(out), _p(lse), _p(cu_q_lens), ctypes.c_int32(total_q), ctypes.c_int32(max_q_len),
+            _p(tree_mask), ctypes.c_int32(words), _p(block_table), _p(seq_lens), ctypes.c_int32(B), ctypes.c_int32(Hq),
+            ctypes.c_int32(block_table.shape[1]), ctypes.c_int32(max_seq_len), ctypes.c_float(scale), _p(workspace),
+            ctypes.c_size_t(workspace.numel() * workspace.element_size()), _stream(stream))
+    return PreparedCall(lib.paged_attention_tree, args,
+                        (d, k_cache, v_cache, q, out, lse, cu_q_lens, tree_mask, block_table, seq_lens, workspace),
+                        "paged_attention_tree", out)
+
+
+def paged_attention_tree(k_cache, v_cache, q, cu_q_lens, max_q_len: int, tree_mask, block_table, seq_lens, max_seq_len: int,
+                         scale: float, **kw):
+    """Attention of trees of drafted tokens.  Returns ``out`` ([total_q, Hq, d], dtype of q); keyword arguments as for
+    prepare_attention_tree."""
+    return prepare_attention_tree(k_cache, v_cache, q, cu_q_lens, max_q_len, tree_mask, block_table, seq_lens, max_seq_len,
+                                  scale, **kw)()
+
+
+def prepare_tree_accept(k_cache, v_cache, cu_q_lens, seq_lens, max_q_len: int, block_table, path, path_lens, *, parents=None,
+                        tokens=None, targets=None, next_tokens=None, kept_lens=None, head_major=False,
+                        stream=None) -> PreparedCall:
+    """paged_tree_accept with its arguments marshalled once; the call returns (path, path_lens, next_tokens, kept_lens), the last
+    two allocated unless given.  path: int32 [batch, max_path].  Without parents, tokens and targets path and path_lens are read."""
+    lib = load_library()
+    d = cache_desc(k_cache, v_cache, head_major)
+    dev = _together("paged_tree_accept", k_cache, v_cache, cu_q_lens, seq_lens, block_table, path, path_lens, parents, tokens,
+                    targets, next_tokens, kept_lens)
+    B = int(seq_lens.shape[0])
+    _shaped(seq_lens, "seq_lens", (B,)), _shaped(cu_q_lens, "cu_q_lens", (B + 1,)), _i32(block_table, "block_table")
+    if path.dim() != 2 or block_table.dim() != 2 or block_table.shape[0] != B:
+        raise PagedAttnError("path must be [batch, max_path], block_table [batch, max_blocks]")
+    _shaped(path, "path", (B, path.shape[1])), _shaped(path_lens, "path_lens", (B,))
+    given = tokens is None
+    if (targets is None) != given or (parents is None) != given or (given and next_tokens is not None):
+        raise PagedAttnError("parents, tokens and targets come together, next_tokens with them")
+    if not given:
+        for t, what in ((parents, "parents"), (tokens, "tokens"), (targets, "targets")):
+            if _i32(t, what).dim() != 1 or t.shape != tokens.shape:
+                raise PagedAttnError("parents, tokens and targets must be int32[rows], equally long")
+        next_tokens = _or_new(next_tokens, "next_tokens", (B,), dev)
+    kept_lens = _or_new(kept_lens, "kept_lens", (B,), dev)
+    args = (ctypes.byref(d), _p(cu_q_lens), _p(seq_lens), ctypes.c_int32(B), ctypes.c_int32(max_q_len), _p(parents), _p(tokens),
+            _p(targets), _p(path), ctypes.c_int32(path.shape[1]), _p(path_lens), _p(next_tokens), _p(kept_lens),
+            _p(block_table), ctypes.c_int32(block_table.shape[1]), _stream(stream))
+    return PreparedCall(lib.paged_tree_accept, args, (d, k_cache, v_cache, cu_q_lens, seq_lens, block_table, path, path_lens,
+                                                      parents, tokens, targets, next_tokens, kept_lens), "paged_tree_accept",
+                        (path, path_lens, next_tokens, kept_lens))
+
+
+def paged_tree_accept(k_cache, v_cache, cu_q_lens, seq_lens, max_q_len: int, block_table, path, path_lens, **kw):
+    """Finds what stays of a verified tree and moves its K and V rows together.  Returns (path, path_lens, next_tokens,
+    kept_lens); keyword arguments as for prepare_tree_accept."""
+    return prepare_tree_accept(k_cache, v_cache, cu_q_lens, seq_lens, max_q_len, block_table, path, path_lens, **kw)()
 
 
 def pa_debug_check(k_cache, v_cache, block_table, seq_lens, seq_ids=None, positions=None, *, head_major=False,

@@ -32,6 +32,10 @@ struct Options {
 };
 thread_local Options g_opt;       // per host thread: a thread's knobs shape only the calls it makes itself
 
+}  // namespace
+
+bool portable_kernels_only() { return g_opt.force_generic != 0; }
+
 // Compute units of the current device (the tile-stream decode launches one workgroup per CU by default).
 int32_t device_cus()
 {
@@ -45,6 +49,8 @@ int32_t device_cus()
     }
     return cached[dev];
 }
+
+namespace {
 
 struct ProfileRecord {
     std::string kernel;

@@ -240,6 +240,81 @@ int64_t prefill_list_items(const AttnArgs& a);
 pa_status launch_merge(const AttnArgs& a, hipStream_t stream);
 
 // ---------------------------------------------------------------------------------------------
+// A step of drafted tokens (validated arguments of the entry points, see pagedattn.h).
+// ---------------------------------------------------------------------------------------------
+int32_t device_cus();          // compute units of the current device
+bool portable_kernels_only();  // the calling thread's "force_generic"
+
+struct StepPlanArgs {
+    const int32_t* ctx_lens;
+    const int32_t* new_lens;
+    const int32_t* parents;
+    const int32_t* free_pages;
+    int32_t batch, page_size, max_blocks, max_rows, mask_words;
+    int32_t* block_table;
+    int32_t* num_blocks;
+    int32_t* free_count;
+    int32_t* seq_lens;
+    int32_t* cu_q_lens;
+    int32_t* seq_ids;
+    int32_t* positions;
+    int32_t* rope_positions;
+    uint64_t* tree_mask;
+    int32_t* shortage;
+};
+pa_status launch_plan_step(const StepPlanArgs& p, hipStream_t stream);
+pa_status launch_release_blocks(const int32_t* keep_lens, int32_t batch, int32_t page_size, int32_t* block_table,
+                                int32_t max_blocks, int32_t* num_blocks, int32_t* free_pages, int32_t* free_count,
+                                int32_t max_free, hipStream_t stream);
+
+struct RopeArgs {
+    const void* q;
+    void* q_out;
+    const void* k_new;
+    const void* v_new;
+    int64_t q_stride, q_out_stride, k_stride, v_stride;
+    const double* inv_freq;
+    const int32_t* rope_positions;
+    const int32_t* seq_ids;
+    const int32_t* positions;
+    const int32_t* block_table;
+    int32_t T, num_q_heads, batch, max_blocks, rotary_dim;
+    bool interleaved;
+    float mscale;
+};
+pa_status launch_rope_append(const pa_kv_cache_desc* c, const RopeArgs& r, hipStream_t stream);
+
+struct TreeArgs {
+    CacheView cache;
+    pa_dtype dtype;
+    const void* q;               // [total_q, Hq, d]
+    void* out;
+    float* lse;                  // or null
+    const int32_t* cu_q_lens;
+    const int32_t* seq_lens;
+    const uint64_t* tree_mask;   // [total_q, mask_words]
+    const int32_t* block_table;
+    int32_t mask_words, batch, total_q, max_q_len, num_q_heads, max_blocks, max_seq_len;
+    float scale;
+};
+pa_status launch_tree_generic(const TreeArgs& a, hipStream_t stream);
+
+struct TreeAcceptArgs {
+    const int32_t* cu_q_lens;
+    const int32_t* seq_lens;
+    const int32_t* parents;
+    const int32_t* tokens;
+    const int32_t* targets;
+    const int32_t* block_table;
+    int32_t* path;
+    int32_t* path_lens;
+    int32_t* next_tokens;
+    int32_t* kept_lens;
+    int32_t batch, max_path, cap, max_blocks;   // cap <= max_path: most tokens a path can have
+};
+pa_status launch_tree_accept(const pa_kv_cache_desc* c, const TreeAcceptArgs& t, hipStream_t stream);
+
+// ---------------------------------------------------------------------------------------------
 // Small device helpers.
 // ---------------------------------------------------------------------------------------------
 #if defined(__HIPCC__)

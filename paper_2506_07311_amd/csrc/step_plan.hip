@@ -1,0 +1,484 @@
+// Bookkeeping of a step of drafted tokens on the GPU: slots, positions, ancestor masks and pages from request lengths
+// (paged_plan_step), pages back to the free list (paged_release_blocks), and the accepted path of a verified tree with
+// its K and V rows moved together (paged_tree_accept).  All three move a few kilobytes; what counts is that a step
+// needs no round trip to the host, and the launches' own latency.
+#include "common.h"
+
+namespace pa {
+
+namespace {
+
+// ---- plan and release ----------------------------------------------------------------------------------------------
+constexpr int kPlanThreads = 256;
+constexpr int kReleaseThreads = 1024;
+
+// Inclusive sum over the workgroup (N threads) of one value a thread; `total` gets the whole sum.  sm: N / 64 words,
+// free for the next call on return.
+template <int N>
+__device__ __forceinline__ int32_t group_scan(int32_t v, int32_t* sm, int32_t& total)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int32_t up = __shfl_up(v, o, 64);
+        if (lane >= o) v += up;
+    }
+    if (lane == 63) sm[wave] = v;
+    __syncthreads();
+    total = 0;
+    int32_t before = 0;
+#pragma unroll
+    for (int w = 0; w < N / 64; ++w) {
+        const int32_t x = sm[w];
+        if (w < wave) before += x;
+        total += x;
+    }
+    __syncthreads();
+    return v + before;
+}
+
+// The sequence of a block of them that item m belongs to: the first whose inclusive sum exceeds it (m < the last sum).
+template <int N>
+__device__ __forceinline__ int32_t find_in(const int32_t* ends, int32_t m)
+{
+    int32_t lo = 0, hi = N - 1;
+    while (lo < hi) {
+        const int32_t mid = (lo + hi) >> 1;
+        if (ends[mid] > m) hi = mid; else lo = mid + 1;
+    }
+    return lo;
+}
+
+struct PlanArgs {
+    const int32_t* ctx_lens;
+    const int32_t* new_lens;
+    const int32_t* parents;      // or null: every token follows the one before it
+    const int32_t* free_pages;
+    int32_t* block_table;
+    int32_t* num_blocks;
+    int32_t* free_count;
+    int32_t* seq_lens;
+    int32_t* cu_q_lens;
+    int32_t* seq_ids;
+    int32_t* positions;
+    int32_t* rope_positions;     // or null
+    uint64_t* tree_mask;         // or null
+    int32_t* shortage;
+    int32_t batch, max_blocks, log2_page, max_rows, mask_words;
+};
+
+__device__ __forceinline__ int32_t blocks_for(int32_t tokens, int32_t log2_page)
+{
+    return (int32_t)(((int64_t)tokens + (1 << log2_page) - 1) >> log2_page);
+}
+
+// Workgroup 0: everything that is one value a sequence, and the pages.  It alone writes what it and the others read
+// nothing of but itself (counts, table, free list), so that a call can work in place in one launch; the others derive the
+// rows' values from ctx_lens and new_lens, whether the request is granted or not.
+__device__ __forceinline__ void plan_sequences(const PlanArgs& a)
+{
+    __shared__ int32_t sm[kPlanThreads / 64];
+    __shared__ int32_t sm_end[kPlanThreads];
+    const int tid = threadIdx.x;
+    const int32_t count = a.free_count[0];
+    int32_t need_all = 0, long_all = 0, rows_all = 0;
+    for (int32_t s0 = 0; s0 < a.batch; s0 += kPlanThreads) {
+        const int32_t s = s0 + tid;
+        int32_t need = 0, late = 0, rows = 0;
+        if (s < a.batch) {
+            rows = max(a.new_lens[s], 0);
+            const int32_t want = blocks_for(a.ctx_lens[s] + rows, a.log2_page);
+            need = max(want - a.num_blocks[s], 0);
+            late = want > a.max_blocks || (a.tree_mask && rows > 64 * a.mask_words) ? 1 : 0;
+        }
+        int32_t t;
+        group_scan<kPlanThreads>(need, sm, t);
+        need_all += t;
+        group_scan<kPlanThreads>(late, sm, t);
+        long_all += t;
+        group_scan<kPlanThreads>(rows, sm, t);
+        rows_all += t;
+    }
+    if (rows_all > a.max_rows) long_all += rows_all - a.max_rows;
+    const bool ok = need_all <= count && long_all == 0;
+    int32_t rows_before = 0, pages_before = 0;
+    for (int32_t s0 = 0; s0 < a.batch; s0 += kPlanThreads) {
+        const int32_t s = s0 + tid;
+        int32_t need = 0, rows = 0, ctx = 0;
+        if (s < a.batch) {
+            rows = max(a.new_lens[s], 0);
+            ctx = a.ctx_lens[s];
+            need = max(blocks_for(ctx + rows, a.log2_page) - a.num_blocks[s], 0);
+        }
+        int32_t rows_here, pages_here;
+        const int32_t row_end = group_scan<kPlanThreads>(rows, sm, rows_here);
+        sm_end[tid] = group_scan<kPlanThreads>(need, sm, pages_here);
+        if (s < a.batch) {
+            a.cu_q_lens[s + 1] = ok ? rows_before + row_end : 0;
+            a.seq_lens[s] = ok ? ctx + rows : ctx;
+        }
+        __syncthreads();
+        if (ok) {
+            for (int32_t m = tid; m < pages_here; m += kPlanThreads) {
+                const int32_t f = find_in<kPlanThreads>(sm_end, m);
+                const int32_t at = m - (f ? sm_end[f - 1] : 0);
+                a.block_table[(int64_t)(s0 + f) * a.max_blocks + a.num_blocks[s0 + f] + at] =
+                    a.free_pages[count - 1 - pages_before - m];
+            }
+            __syncthreads();                                 // (the counts have been read)
+            if (need > 0) a.num_blocks[s] += need;
+        }
+        rows_before += rows_here;
+        pages_before += pages_here;
+        __syncthreads();
+    }
+    if (tid == 0) {
+        a.cu_q_lens[0] = 0;
+        if (ok) a.free_count[0] = count - need_all;
+        a.shortage[0] = max(need_all - count, 0);
+        a.shortage[1] = long_all;
+    }
+    for (int32_t r = min(rows_all, a.max_rows) + tid; r < a.max_rows; r += kPlanThreads) {
+        a.seq_ids[r] = -1;
+        a.positions[r] = -1;
+        if (a.rope_positions) a.rope_positions[r] = 0;
+        if (a.tree_mask)
+            for (int32_t w = 0; w < a.mask_words; ++w) a.tree_mask[(int64_t)r * a.mask_words + w] = 0;
+    }
+}
+
+// One wave: the rows of sequence s, 64 at a time.  The mask and the depth of a token come from its chain of parents: for
+// up to 64 tokens by doubling (after round k a lane holds the union of the 2^k nearest and points 2^k up: 6 rounds of lane
+// moves), beyond that by walking up, once a word.
+__device__ __forceinline__ void plan_rows(const PlanArgs& a, int32_t s)
+{
+    const int lane = threadIdx.x & 63;
+    int32_t start = 0;
+    for (int32_t i = lane; i < s; i += 64) start += max(a.new_lens[i], 0);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) start += __shfl_xor(start, o, 64);
+    const int32_t n = max(a.new_lens[s], 0), ctx = a.ctx_lens[s];
+    for (int32_t base = 0; base < n; base += 64) {
+        const int32_t i = base + lane;
+        const int64_t r = (int64_t)start + i;
+        const bool live = i < n && r < a.max_rows;
+        int32_t depth = i;
+        if (n <= 64 && a.parents) {
+            int32_t up = live ? a.parents[r] : -1;
+            if (up < 0 || up >= i) up = -1;
+            uint64_t bits = 1ull << lane;
+            depth = up >= 0 ? 1 : 0;
+            while (__any(up >= 0)) {
+                const int from = up >= 0 ? up : lane;
+                const uint64_t b = __shfl((unsigned long long)bits, from, 64);
+                const int32_t d = __shfl(depth, from, 64), u = __shfl(up, from, 64);
+                if (up >= 0) {
+                    bits |= b;
+                    depth += d;
+                    up = u;
+                }
+            }
+            if (live && a.tree_mask) {
+                a.tree_mask[r * a.mask_words] = bits;
+                for (int32_t w = 1; w < a.mask_words; ++w) a.tree_mask[r * a.mask_words + w] = 0;
+            }
+        } else if (live && a.parents) {
+            auto above = [&](int32_t k) {
+                const int64_t row = (int64_t)start + k;
+                const int32_t u = a.parents[row];
+                return u >= 0 && u < k ? u : -1;
+            };
+            depth = -1;
+            for (int32_t k = i; k >= 0; k = above(k)) ++depth;
+            if (a.tree_mask)
+                for (int32_t w = 0; w < a.mask_words; ++w) {
+                    uint64_t bits = 0;
+                    for (int32_t k = i; k >= 64 * w; k = above(k))
+                        if (k >> 6 == w) bits |= 1ull << (k & 63);
+                    a.tree_mask[r * a.mask_words + w] = bits;
+                }
+        } else if (live && a.tree_mask) {
+            for (int32_t w = 0; w < a.mask_words; ++w) {
+                const int32_t k = i - 64 * w;                // bits 0 .. k of the word
+                a.tree_mask[r * a.mask_words + w] = k < 0 ? 0 : k >= 63 ? ~0ull : (2ull << k) - 1;
+            }
+        }
+        if (live) {
+            a.seq_ids[r] = s;
+            a.positions[r] = ctx + i;
+            if (a.rope_positions) a.rope_positions[r] = ctx + depth;
+        }
+    }
+}
+
+__global__ __launch_bounds__(kPlanThreads) void paged_plan_step_kernel(PlanArgs a)
+{
+    if (blockIdx.x == 0) {
+        plan_sequences(a);
+        return;
+    }
+    const int32_t s = ((int32_t)blockIdx.x - 1) * (kPlanThreads / 64) + (int32_t)(threadIdx.x >> 6);
+    if (s < a.batch) plan_rows(a, s);
+}
+
+// Blocks of a sequence beyond ceil(keep_lens / P) go back to the end of the free list, the last one first: a plan that asks
+// for the same blocks again gets the same pages.  One workgroup: the list is one.
+__global__ __launch_bounds__(kReleaseThreads) void paged_release_blocks_kernel(
+    const int32_t* __restrict__ keep_lens, int32_t* __restrict__ block_table, int32_t* __restrict__ num_blocks,
+    int32_t* __restrict__ free_pages, int32_t* __restrict__ free_count, int32_t batch, int32_t max_blocks,
+    int32_t log2_page, int32_t max_free)
+{
+    __shared__ int32_t sm[kReleaseThreads / 64];
+    __shared__ int32_t sm_end[kReleaseThreads];
+    const int tid = threadIdx.x;
+    auto gone = [&](int32_t s) {
+        return s < batch ? max(min(num_blocks[s], max_blocks) - blocks_for(max(keep_lens[s], 0), log2_page), 0) : 0;
+    };
+    const int32_t count = free_count[0];
+    int32_t all = 0;
+    for (int32_t s0 = 0; s0 < batch; s0 += kReleaseThreads) {
+        int32_t t;
+        group_scan<kReleaseThreads>(gone(s0 + tid), sm, t);
+        all += t;
+    }
+    int32_t before = 0;
+    for (int32_t s0 = 0; s0 < batch; s0 += kReleaseThreads) {
+        int32_t here;
+        const int32_t mine = gone(s0 + tid);
+        sm_end[tid] = group_scan<kReleaseThreads>(mine, sm, here);
+        __syncthreads();
+        for (int32_t m = tid; m < here; m += kReleaseThreads) {
+            const int32_t f = find_in<kReleaseThreads>(sm_end, m);
+            const int32_t at = m - (f ? sm_end[f - 1] : 0);
+            int32_t* const entry = block_table + (int64_t)(s0 + f) * max_blocks +
+                                   blocks_for(max(keep_lens[s0 + f], 0), log2_page) + at;
+            const int64_t to = (int64_t)count + all - 1 - before - m;
+            if (to < max_free) free_pages[to] = *entry;
+            *entry = -1;
+        }
+        __syncthreads();
+        if (mine > 0) num_blocks[s0 + tid] = blocks_for(max(keep_lens[s0 + tid], 0), log2_page);
+        before += here;
+        __syncthreads();
+    }
+    if (tid == 0) free_count[0] = min(count + all, max_free);
+}
+
+// ---- acceptance ----------------------------------------------------------------------------------------------------
+constexpr int kAcceptThreads = 256;
+
+struct AcceptArgs {
+    const int32_t* cu_q_lens;
+    const int32_t* seq_lens;
+    const int32_t* parents;      // with tokens and targets: the path is found here; all null: it is given
+    const int32_t* tokens;
+    const int32_t* targets;
+    const int32_t* block_table;
+    int32_t* path;               // [batch, max_path]
+    int32_t* path_lens;
+    int32_t* next_tokens;        // or null
+    int32_t* kept_lens;          // or null
+    uint4* k_cache;
+    uint4* v_cache;
+    int64_t page_stride_v, token_stride_v, head_stride_v;   // in 16-byte pieces
+    int32_t max_path, cap, max_blocks, log2_page, num_kv_heads, vec_per_head, num_pages;   // cap: most tokens of a path
+};
+
+// The path through the tree: node 0, then of the last one's children with the token the model chose there the first, while
+// there is one.  Wave 0; sm_path and the result are the same on every lane.
+__device__ __forceinline__ int32_t walk_tree(const AcceptArgs& a, int32_t row0, int32_t n, int32_t* sm_path, int32_t& next)
+{
+    const int lane = threadIdx.x & 63;
+    int32_t count = 0, cur = 0;
+    if (n <= 64) {                                           // the whole tree in one wave's registers
+        const bool live = lane < n;
+        const int32_t up = live ? a.parents[row0 + lane] : -1;
+        const int32_t token = live ? a.tokens[row0 + lane] : -1;
+        const int32_t target = live ? a.targets[row0 + lane] : -1;
+        for (;;) {
+            if (lane == 0) sm_path[count] = cur;
+            ++count;
+            next = __builtin_amdgcn_readlane(target, cur);
+            if (count == a.cap) return count;
+            const uint64_t hit = __ballot(live && lane > cur && up == cur && token == next);
+            if (!hit) return count;
+            cur = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)hit) - 1);
+        }
+    }
+    for (;;) {
+        if (lane == 0) sm_path[count] = cur;
+        ++count;
+        next = a.targets[row0 + cur];
+        if (count == a.cap) return count;
+        int32_t found = -1;
+        for (int32_t base = cur + 1; base < n && found < 0; base += 64) {
+            const int32_t c = base + lane;
+            const uint64_t hit = __ballot(c < n && a.parents[row0 + min(c, n - 1)] == cur && a.tokens[row0 + min(c, n - 1)] == next);
+            if (hit) found = base + __ffsll((unsigned long long)hit) - 1;
+        }
+        if (found < 0) return count;
+        cur = __builtin_amdgcn_readfirstlane(found);
+    }
+}
+
+// Grid (sequences, pieces of a token's K and V rows / 256).  A thread moves one 16-byte piece of all the path's rows, eight at a
+// time and in the path's order: a path climbs (path[i] >= i, and each further than the one before), so no row is
+// written before it has been read.
+__global__ __launch_bounds__(kAcceptThreads) void paged_tree_accept_kernel(AcceptArgs a)
+{
+    extern __shared__ int32_t sm_path[];                     // [cap]
+    __shared__ int32_t sm_len;
+    const int32_t s = blockIdx.x;
+    const int32_t row0 = a.cu_q_lens[s], n = a.cu_q_lens[s + 1] - row0;
+    const int32_t ctx = a.seq_lens[s] - n;
+    if (n <= 0) {                                            // (nothing drafted: nothing to keep)
+        if (blockIdx.y == 0) {
+            for (int32_t i = threadIdx.x; a.tokens && i < a.max_path; i += kAcceptThreads) a.path[(int64_t)s * a.max_path + i] = -1;
+            if (threadIdx.x == 0) {
+                if (a.tokens) a.path_lens[s] = 0;
+                if (a.tokens && a.next_tokens) a.next_tokens[s] = -1;
+                if (a.kept_lens) a.kept_lens[s] = ctx;
+            }
+        }
+        return;
+    }
+    if (threadIdx.x < 64) {
+        int32_t len, next = -1;
+        if (a.tokens) {
+            len = walk_tree(a, row0, n, sm_path, next);
+        } else {
+            len = min(max(a.path_lens[s], 0), min(n, a.cap));
+            for (int32_t i = threadIdx.x; i < len; i += 64)
+                sm_path[i] = min(max(a.path[(int64_t)s * a.max_path + i], 0), n - 1);
+        }
+        if (threadIdx.x == 0) {
+            sm_len = len;
+            if (blockIdx.y == 0) {
+                if (a.tokens) a.path_lens[s] = len;
+                if (a.tokens && a.next_tokens) a.next_tokens[s] = next;
+                if (a.kept_lens) a.kept_lens[s] = ctx + len;
+            }
+        }
+    }
+    __syncthreads();
+    const int32_t len = sm_len;
+    if (a.tokens && blockIdx.y == 0)
+        for (int32_t i = threadIdx.x; i < a.max_path; i += kAcceptThreads)
+            a.path[(int64_t)s * a.max_path + i] = i < len ? sm_path[i] : -1;
+    const int32_t piece = (int32_t)blockIdx.y * kAcceptThreads + threadIdx.x;
+    const int32_t per_pool = a.num_kv_heads * a.vec_per_head;
+    if (piece >= 2 * per_pool) return;
+    uint4* const pool = piece < per_pool ? a.k_cache : a.v_cache;
+    const int32_t p = piece < per_pool ? piece : piece - per_pool;
+    const int64_t in_token = (int64_t)(p / a.vec_per_head) * a.head_stride_v + p % a.vec_per_head;
+    const int32_t* const table = a.block_table + (int64_t)s * a.max_blocks;
+    auto at = [&](int32_t t) -> int64_t {                    // piece of token t, -1: it has no page
+        if (t < 0 || (t >> a.log2_page) >= a.max_blocks) return -1;
+        const int32_t page = table[t >> a.log2_page];
+        if (page < 0 || page >= a.num_pages) return -1;
+        return (int64_t)page * a.page_stride_v + (int64_t)(t & ((1 << a.log2_page) - 1)) * a.token_stride_v + in_token;
+    };
+    constexpr int kBatch = 8;
+    for (int32_t i0 = 0; i0 < len; i0 += kBatch) {
+        uint4 row[kBatch];
+        int64_t to[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int32_t i = i0 + u;
+            to[u] = -1;
+            if (i < len && sm_path[i] != i) {
+                const int64_t from = at(ctx + sm_path[i]);
+                to[u] = from < 0 ? -1 : at(ctx + i);
+                if (to[u] >= 0) row[u] = pool[from];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+            if (to[u] >= 0) pool[to[u]] = row[u];
+    }
+}
+
+int log2_of(int32_t page_size)
+{
+    int l = 0;
+    while ((1 << l) < page_size) ++l;
+    return l;
+}
+
+}  // namespace
+
+pa_status launch_plan_step(const StepPlanArgs& p, hipStream_t stream)
+{
+    PlanArgs a;
+    a.ctx_lens = p.ctx_lens;
+    a.new_lens = p.new_lens;
+    a.parents = p.parents;
+    a.free_pages = p.free_pages;
+    a.block_table = p.block_table;
+    a.num_blocks = p.num_blocks;
+    a.free_count = p.free_count;
+    a.seq_lens = p.seq_lens;
+    a.cu_q_lens = p.cu_q_lens;
+    a.seq_ids = p.seq_ids;
+    a.positions = p.positions;
+    a.rope_positions = p.rope_positions;
+    a.tree_mask = p.tree_mask;
+    a.shortage = p.shortage;
+    a.batch = p.batch;
+    a.max_blocks = p.max_blocks;
+    a.log2_page = log2_of(p.page_size);
+    a.max_rows = p.max_rows;
+    a.mask_words = p.mask_words;
+    const uint32_t wgs = 1 + (uint32_t)((p.batch + kPlanThreads / 64 - 1) / (kPlanThreads / 64));
+    ProfileScope prof("paged_plan_step_kernel", stream);
+    hipLaunchKernelGGL(paged_plan_step_kernel, dim3(wgs), dim3(kPlanThreads), 0, stream, a);
+    return launch_status();
+}
+
+pa_status launch_release_blocks(const int32_t* keep_lens, int32_t batch, int32_t page_size, int32_t* block_table,
+                                int32_t max_blocks, int32_t* num_blocks, int32_t* free_pages, int32_t* free_count,
+                                int32_t max_free, hipStream_t stream)
+{
+    ProfileScope prof("paged_release_blocks_kernel", stream);
+    hipLaunchKernelGGL(paged_release_blocks_kernel, dim3(1), dim3(kReleaseThreads), 0, stream, keep_lens, block_table,
+                       num_blocks, free_pages, free_count, batch, max_blocks, log2_of(page_size), max_free);
+    return launch_status();
+}
+
+pa_status launch_tree_accept(const pa_kv_cache_desc* c, const TreeAcceptArgs& t, hipStream_t stream)
+{
+    const CacheView v = make_view(c);
+    const int32_t epv = c->dtype == PA_DTYPE_F32 ? 4 : 8;     // elements per 16-byte piece
+    AcceptArgs a;
+    a.cu_q_lens = t.cu_q_lens;
+    a.seq_lens = t.seq_lens;
+    a.parents = t.parents;
+    a.tokens = t.tokens;
+    a.targets = t.targets;
+    a.block_table = t.block_table;
+    a.path = t.path;
+    a.path_lens = t.path_lens;
+    a.next_tokens = t.next_tokens;
+    a.kept_lens = t.kept_lens;
+    a.k_cache = (uint4*)c->k_cache;
+    a.v_cache = (uint4*)c->v_cache;
+    a.page_stride_v = c->page_stride / epv;
+    a.token_stride_v = c->token_stride / epv;
+    a.head_stride_v = c->head_stride / epv;
+    a.max_path = t.max_path;
+    a.cap = t.cap;
+    a.max_blocks = t.max_blocks;
+    a.log2_page = v.log2_page;
+    a.num_kv_heads = c->num_kv_heads;
+    a.vec_per_head = c->head_dim / epv;
+    a.num_pages = c->num_pages;
+    const int64_t pieces = 2LL * a.num_kv_heads * a.vec_per_head;
+    const int64_t groups = (pieces + kAcceptThreads - 1) / kAcceptThreads;
+    if (groups > 65535) return PA_ERR_UNSUPPORTED;
+    ProfileScope prof("paged_tree_accept_kernel", stream);
+    hipLaunchKernelGGL(paged_tree_accept_kernel, dim3((uint32_t)t.batch, (uint32_t)groups), dim3(kAcceptThreads),
+                       (size_t)t.cap * sizeof(int32_t), stream, a);
+    return launch_status();
+}
+
+}  // namespace pa
