@@ -70,7 +70,7 @@ KERNELS = ATTENTION_KERNELS + ("paged_kv_append_kernel", "paged_kv_append_last_k
                                "paged_attention_merge_list_kernel") + (
     # a step of drafted tokens
     "paged_plan_step_kernel", "paged_release_blocks_kernel", "paged_rope_append_kernel", "paged_tree_accept_kernel",
-    "paged_attention_tree_generic_kernel")
+    "paged_attention_tree_generic_kernel", "paged_attention_tree_mfma_kernel", "paged_attention_tree_merge_kernel")
 
 
 def read_kernels(binding, names):

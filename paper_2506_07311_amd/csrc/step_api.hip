@@ -113,8 +113,12 @@ pa_status paged_rope_append(const pa_kv_cache_desc* cache, const void* q, int64_
 size_t paged_attention_tree_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                             int32_t total_q, int32_t max_q_len, int32_t max_seq_len)
 {
-    (void)batch, (void)num_q_heads, (void)num_kv_heads, (void)head_dim, (void)total_q, (void)max_q_len, (void)max_seq_len;
-    return 256;
+    if (batch <= 0 || num_kv_heads <= 0 || num_q_heads < num_kv_heads || head_dim <= 0 || total_q <= 0 || max_q_len < 0 ||
+        max_seq_len < 0)
+        return 256;
+    const TreePlan p = plan_tree(batch, num_q_heads, num_kv_heads, head_dim, max_q_len, max_seq_len);
+    const size_t bytes = p.part_o_bytes + p.part_lse_bytes;
+    return bytes > 0 ? bytes : 256;
 }
 
 pa_status paged_attention_tree(const pa_kv_cache_desc* cache, const void* q, void* out, float* lse,
@@ -139,6 +143,7 @@ pa_status paged_attention_tree(const pa_kv_cache_desc* cache, const void* q, voi
     if ((uintptr_t)workspace & 255) return PA_ERR_INVALID_ARG;
     TreeArgs a = {make_view(cache), cache->dtype, q, out, lse, cu_q_lens, seq_lens, tree_mask, block_table, mask_words, batch, total_q,
                   max_q_len, num_q_heads, max_blocks, max_seq_len, scale};
+    if (!portable_kernels_only() && tree_mfma_supported(a)) return launch_tree_mfma(a, workspace, stream_of(stream));
     return launch_tree_generic(a, stream_of(stream));
 }
 

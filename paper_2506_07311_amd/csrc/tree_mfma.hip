@@ -1,0 +1,83 @@
+// Matrix-core attention of drafted trees (tree_mfma_impl.h) at up to 128 columns, and its plan.
+#include "tree_mfma_impl.h"
+
+namespace pa {
+
+pa_status launch_tree_d256(const TreeKernelArgs& a, pa_dtype dtype, int row_waves, hipStream_t stream);
+pa_status launch_tree_d128(const TreeKernelArgs& a, pa_dtype dtype, int row_waves, hipStream_t stream)
+{
+    return launch_tree_dim<128>(a, dtype, row_waves, stream);
+}
+pa_status launch_tree_d96(const TreeKernelArgs& a, pa_dtype dtype, int row_waves, hipStream_t stream);
+pa_status launch_tree_d64(const TreeKernelArgs& a, pa_dtype dtype, int row_waves, hipStream_t stream);
+
+namespace {
+
+int32_t columns_of(int32_t d) { return d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : 256; }
+
+size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+
+}  // namespace
+
+// Up to 64 rows a (sequence, KV head) two waves share 32 rows.  The tiles are shared by as many workgroups as the machine holds
+// at once; on contexts of up to kPlainTiles tiles a row block is one workgroup's and there is no merge.
+TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t max_q_len, int32_t max_seq_len)
+{
+    constexpr int32_t kPlainTiles = 8;
+    TreePlan p;
+    const int64_t rows = (int64_t)max_q_len * (num_q_heads / num_kv_heads);
+    p.row_waves = rows <= 64 ? 2 : 4;
+    const int64_t blocks = (rows + 32 * p.row_waves - 1) / (32 * p.row_waves);
+    p.row_blocks = blocks < 1 ? 1 : (int32_t)blocks;
+    const int64_t tiles = ((int64_t)max_seq_len + prefill::kBN - 1) / prefill::kBN;
+    p.wgs = 0;
+    p.part_o_bytes = p.part_lse_bytes = 0;
+    if (tiles > kPlainTiles) {
+        const int64_t slots = (int64_t)device_cus() * (columns_of(head_dim) > 128 ? 1 : 2);
+        const int64_t most = (batch * blocks * tiles + 3) / 4;
+        int64_t wgs = slots / num_kv_heads;
+        if (wgs > most) wgs = most;
+        p.wgs = wgs < 1 ? 1 : (int32_t)wgs;
+        const size_t part_rows = (size_t)p.wgs * num_kv_heads * 2 * 32 * p.row_waves;
+        p.part_o_bytes = align256(part_rows * columns_of(head_dim) * sizeof(float));
+        p.part_lse_bytes = align256(part_rows * sizeof(float));
+    }
+    return p;
+}
+
+bool tree_mfma_supported(const TreeArgs& a)
+{
+    return a.dtype != PA_DTYPE_F32 && a.cache.page_size >= 16;
+}
+
+pa_status launch_tree_mfma(const TreeArgs& t, void* workspace, hipStream_t stream)
+{
+    const TreePlan p = plan_tree(t.batch, t.num_q_heads, t.cache.num_kv_heads, t.cache.head_dim, t.max_q_len, t.max_seq_len);
+    TreeKernelArgs a;
+    a.cache = t.cache;
+    a.q = (const uint16_t*)t.q;
+    a.out = (uint16_t*)t.out;
+    a.lse = t.lse;
+    a.cu_q_lens = t.cu_q_lens;
+    a.seq_lens = t.seq_lens;
+    a.tree_mask = t.tree_mask;
+    a.block_table = t.block_table;
+    a.part_o = reinterpret_cast<float*>(workspace);
+    a.part_lse = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + p.part_o_bytes);
+    a.mask_words = t.mask_words;
+    a.batch = t.batch;
+    a.num_q_heads = t.num_q_heads;
+    a.max_blocks = t.max_blocks;
+    a.group = t.num_q_heads / t.cache.num_kv_heads;
+    a.wgs = p.wgs;
+    a.row_blocks = p.row_blocks;
+    a.scale = t.scale;
+    switch (columns_of(t.cache.head_dim)) {
+        case 64: return launch_tree_d64(a, t.dtype, p.row_waves, stream);
+        case 96: return launch_tree_d96(a, t.dtype, p.row_waves, stream);
+        case 128: return launch_tree_d128(a, t.dtype, p.row_waves, stream);
+    }
+    return launch_tree_d256(a, t.dtype, p.row_waves, stream);
+}
+
+}  // namespace pa

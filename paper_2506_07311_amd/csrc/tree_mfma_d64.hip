@@ -1,0 +1,11 @@
+// Matrix-core attention of drafted trees (tree_mfma_impl.h) in 64 columns.
+#include "tree_mfma_impl.h"
+
+namespace pa {
+
+pa_status launch_tree_d64(const TreeKernelArgs& a, pa_dtype dtype, int row_waves, hipStream_t stream)
+{
+    return launch_tree_dim<64>(a, dtype, row_waves, stream);
+}
+
+}  // namespace pa

@@ -1,0 +1,576 @@
+// Attention of trees of drafted tokens on the matrix cores: bf16 / fp16 pools, pages of 16 tokens and more, any head_dim the
+// library takes (computed in DP = 64, 96, 128 or 256 columns).  Internal header: the kernel templates.
+//
+// A sequence's n drafted queries and the G query heads of a KV head are n * G rows that all see the context and differ
+// in the last n keys only.  The context's K and V are read once for all of them, so up to about 200 rows the call is bound by
+// that read, not by its 4 * rows * d flops a key; what the kernel is built for is to keep it going.
+//   * A workgroup of four waves owns RB = 32 * WR rows of one (sequence, KV head) and walks keys in tiles of 64, whose K and V
+//     rows the load unit writes straight into LDS through the block table, one tile ahead (two buffers).  Rows are stored in
+//     16-byte pieces swizzled so that neither kind of operand read meets a bank conflict.
+//   * WR = 4: a wave takes 32 rows and all 64 keys.  WR = 2 (up to 64 rows): two waves share 32 rows and halve the tile, their
+//     results meet in LDS at the end.
+//   * Both products are transposed (v_mfma_f32_32x32x16, lane % 32 = row), so softmax statistics are a lane's own:
+//         S^T[key, row] = K Q^T,   O^T[column, row] += V^T P^T.
+//   * Softmax is online in the log2 domain against a reference that trails the maximum: weights are taken with the
+//     reference as it stands, and only where a lane's sum leaves the range that 16-bit operands carry is it raised and O
+//     rescaled.  Weights enter as two 16-bit terms (p = hi + lo, off by 2^-17 of a weight): one term alone would add an
+//     error as large as the output's own rounding, and its matrix work hides behind the read.
+//   * A key is masked by selection: key len - n + t of a tile is seen by a row if bit t of the row's words is set, 32 bits at a
+//     time; tiles that end in the context take no mask at all.  An infinity or a NaN in a V row that some rows of a tile
+//     do not see would reach them through a product with a weight of zero.  It always leaves its mark on an accumulator, so
+//     they are looked at once, at the end, and such a piece of work is done again key by key (CAREFUL).
+//   * Work is the batch's key tiles in a row (sequence, row block, tile), cut evenly over the workgroups of a KV head whatever the
+//     lengths are; what a cut leaves unfinished goes to the workspace, and a second launch merges it.  On short contexts
+//     a workgroup takes a whole row block and there is no second launch.
+#pragma once
+
+#include "prefill_tiles.h"
+
+namespace pa {
+
+struct TreeKernelArgs {
+    CacheView cache;
+    const uint16_t* q;
+    uint16_t* out;
+    float* lse;
+    const int32_t* cu_q_lens;
+    const int32_t* seq_lens;
+    const uint64_t* tree_mask;
+    const int32_t* block_table;
+    float* part_o;               // [KV head][workgroup][2][RB][DP], normalised
+    float* part_lse;             // [KV head][workgroup][2][RB], log2 domain
+    int32_t mask_words, batch, num_q_heads, max_blocks, group;
+    int32_t wgs;                 // workgroups of a KV head that share the tiles; 0: one a (sequence, row block)
+    int32_t row_blocks;          // most row blocks of a sequence
+    float scale;
+};
+
+namespace {
+
+using namespace prefill;
+
+constexpr int32_t kTreeMinTiles = 4;   // fewest tiles of a workgroup that shares them
+
+template <int DP>
+struct TreeGeo {
+    static constexpr int kRowB = DP > 128 ? 512 : DP > 64 ? 256 : 128;   // bytes of a row in LDS
+    static constexpr int kTileB = kBN * kRowB;                           // K part of a buffer; V follows
+    static constexpr int kBufB = 2 * kTileB;
+    static constexpr int kKS = DP / 16;                                  // steps of a score product
+    static constexpr int kT = DP / 32;                                   // 32-column blocks of O
+    static constexpr int kLoads = kTileB / 4096;                         // load instructions of a wave and pool a tile
+    static constexpr int kOcc = DP > 128 ? 1 : 2;                        // workgroups of a compute unit
+};
+
+// Byte offset inside its LDS row r of logical 16-byte piece L (rows of 512 bytes swizzle each half by itself; of rows of
+// 128 bytes two share the banks).
+template <int DP>
+__device__ __forceinline__ int tree_piece(int L, int r)
+{
+    if (DP <= 64) return 16 * (L ^ (((r & 2) << 1) | ((r >> 2) & 3)));
+    return 16 * ((L & 16) | ((L & 15) ^ swz(r)));
+}
+
+// V^T operand of 32 columns and 16 keys from row-major V: two transpose loads (keys 0-3 / 4-7 of a lane's contraction slots).
+__device__ __forceinline__ uint4 tree_v_frag(const char* lo, const char* hi)
+{
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    struct pair {
+        s16x4 lo, hi;
+    } r;
+    r.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lo));
+    r.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(hi));
+    return __builtin_bit_cast(uint4, r);
+}
+
+// A row's view of 32 keys from key0 on: bit i = key key0 + i is visible.
+__device__ __forceinline__ uint32_t visible_keys(const uint64_t* __restrict__ mask, int32_t words, int32_t key0, int32_t ctx,
+                                                 int32_t len)
+{
+    const int32_t node = key0 - ctx;
+    uint32_t bits;
+    if (node <= -32) {
+        bits = ~0u;
+    } else if (node < 0) {
+        bits = ((uint32_t)mask[0] << -node) | ((1u << -node) - 1u);
+    } else {
+        const int32_t w = node >> 6, sh = node & 63;
+        const uint64_t lo = w < words ? mask[w] >> sh : 0;
+        const uint64_t hi = sh && w + 1 < words ? mask[w + 1] << (64 - sh) : 0;
+        bits = (uint32_t)(lo | hi);
+    }
+    const int32_t left = len - key0;
+    return left >= 32 ? bits : left <= 0 ? 0u : bits & ((1u << left) - 1u);
+}
+
+template <typename E>
+__device__ __forceinline__ void tree_pack(uint4& w, uint4& wl, const f32x16& p, int r0)
+{
+    w.x = E::pack(p[r0 + 0], p[r0 + 1]);
+    w.y = E::pack(p[r0 + 2], p[r0 + 3]);
+    w.z = E::pack(p[r0 + 4], p[r0 + 5]);
+    w.w = E::pack(p[r0 + 6], p[r0 + 7]);
+    wl.x = E::pack(p[r0 + 0] - E::lo_of(w.x), p[r0 + 1] - E::hi_of(w.x));
+    wl.y = E::pack(p[r0 + 2] - E::lo_of(w.y), p[r0 + 3] - E::hi_of(w.y));
+    wl.z = E::pack(p[r0 + 4] - E::lo_of(w.z), p[r0 + 5] - E::hi_of(w.z));
+    wl.w = E::pack(p[r0 + 6] - E::lo_of(w.w), p[r0 + 7] - E::hi_of(w.w));
+}
+
+// Weights of 32 keys; s holds raw scores.  vis (MASK): this lane's keys, score r is bit 8 (r / 4) + r % 4.
+template <bool MASK, int T>
+__device__ __forceinline__ void tree_softmax(f32x16& p, const f32x16& s, f32x16 (&o)[T], float& m, float& l, float sc, uint32_t vis)
+{
+    float psum = 0.f;
+    auto score = [&](int r) {                                // in the log2 domain (whatever the sign of the scale)
+        const float x = s[r] * sc;
+        return !MASK || (vis >> (8 * (r / 4) + r % 4)) & 1u ? x : -INFINITY;
+    };
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        p[r] = __builtin_amdgcn_exp2f(MASK ? score(r) - m : __builtin_fmaf(s[r], sc, -m));
+        psum += p[r];
+    }
+    if (__any(!(psum <= kWeightSumMax))) {                   // also the NaN or infinity of a fresh reference
+        float top = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, score(r));
+        const float m_new = fmaxf(m, row_max<2>(top));
+        const float use = m_new == -INFINITY ? 0.f : m_new;  // (no key so far)
+        const float alpha = __builtin_amdgcn_exp2f(m - use);
+#pragma unroll
+        for (int t = 0; t < T; ++t) o[t] *= alpha;
+        l *= alpha;
+        m = m_new;
+        psum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            p[r] = __builtin_amdgcn_exp2f(score(r) - use);
+            psum += p[r];
+        }
+    }
+    l += psum;
+}
+
+// O^T += V^T P^T for 32 keys of which V may hold values that are not finite: key by key on the vector unit, each added only to the
+// rows that see it.  vh = V's rows of the 32 keys; vis = their bits.
+template <typename E, int DP, int T>
+__device__ __forceinline__ void tree_pv_by_key(f32x16 (&o)[T], f32x16 p, const char* vh, uint32_t vis, int ql, int hh)
+{
+#pragma unroll 1
+    for (int i = 0; i < 32; ++i) {
+        const int key = 8 * (i >> 3) + 4 * (i & 1) + ((i >> 1) & 3);
+        const float w = __shfl(p[0], ql + 32 * (i & 1), 64);
+        const bool seen = (vis >> key) & 1u;
+        const char* const row = vh + key * TreeGeo<DP>::kRowB + 8 * hh;
+#pragma unroll
+        for (int c = 0; c < 4 * T; ++c) {
+            const uint2 v = *reinterpret_cast<const uint2*>(row + tree_piece<DP>(c, key));
+            o[c / 4][4 * (c % 4) + 0] = seen ? __builtin_fmaf(w, E::lo_of(v.x), o[c / 4][4 * (c % 4) + 0]) : o[c / 4][4 * (c % 4) + 0];
+            o[c / 4][4 * (c % 4) + 1] = seen ? __builtin_fmaf(w, E::hi_of(v.x), o[c / 4][4 * (c % 4) + 1]) : o[c / 4][4 * (c % 4) + 1];
+            o[c / 4][4 * (c % 4) + 2] = seen ? __builtin_fmaf(w, E::lo_of(v.y), o[c / 4][4 * (c % 4) + 2]) : o[c / 4][4 * (c % 4) + 2];
+            o[c / 4][4 * (c % 4) + 3] = seen ? __builtin_fmaf(w, E::hi_of(v.y), o[c / 4][4 * (c % 4) + 3]) : o[c / 4][4 * (c % 4) + 3];
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (i & 1) p = __builtin_shufflevector(p, p, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15, 0);   // the next pair's weight
+    }
+}
+
+// A workgroup's piece of work: key tiles [tile_begin, tile_end) of row block rb of sequence s.
+struct TreeItem {
+    int32_t s, rb, row0, n, len, tile_begin, tile_end;
+    int64_t slot;                // >= 0: a partial
+};
+
+// Returns whether it has to be done again with CAREFUL (the same on every thread).
+template <int WR, bool CAREFUL, typename E, int DP>
+__device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, const TreeKernelArgs& a, const TreeItem& it, int32_t kvh)
+{
+    typedef TreeGeo<DP> Geo;
+    constexpr int RB = 32 * WR, KW = 4 / WR, ROWB = Geo::kRowB, T = Geo::kT, KS = Geo::kKS;
+    constexpr int HALVES = 2 / KW;                           // 32-key halves of a tile that a wave takes
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));                            // (what follows from it is not kept across pieces of work)
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int ql = lane & 31, hh = lane >> 5;
+    const int rw = wave % WR, kw = wave / WR;
+    const int32_t d = a.cache.head_dim, G = a.group, len = it.len, ctx = it.len - it.n, n_rows = it.n * G;
+    const int32_t r_lane = it.rb * RB + 32 * rw + ql;
+    const int32_t r = min(r_lane, n_rows - 1);
+    const int32_t qi = r / G, h = kvh * G + r % G;
+    const bool live = it.rb * RB + 32 * rw < n_rows;         // this wave has rows (wave-uniform)
+    const uint64_t* const mask = a.tree_mask + (int64_t)(it.row0 + qi) * a.mask_words;
+    const int32_t* const table = a.block_table + (int64_t)it.s * a.max_blocks;
+    const int32_t last_key = len - 1;
+
+    // Q as B operand: lane % 32 = row, step ks covers 8 elements of either lane half; 0 behind head_dim
+    const uint16_t* const qrow = a.q + ((int64_t)(it.row0 + qi) * a.num_q_heads + h) * d;
+    uint4 qf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        qf[ks] = uint4{0, 0, 0, 0};
+        if (16 * ks + 8 * hh < d) qf[ks] = *reinterpret_cast<const uint4*>(qrow + 16 * ks + 8 * hh);
+    }
+
+    // operand offsets: K piece 2 ks + hh of row ql; V pieces of the 32 columns t for the lane's transpose-load row, key 4 hh + j
+    // (and 8 on) of a 16-key step, columns 4 qq .. + 3 of the 16-column block dblk
+    uint32_t kx[KS], vx[2 * T];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) kx[ks] = ql * ROWB + tree_piece<DP>(2 * ks + hh, ql);
+    {
+        const int j = (lane & 15) >> 2, qq = lane & 3, dblk = (lane >> 4) & 1;
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            const int piece = 4 * t + 2 * dblk + (qq >> 1);
+            vx[2 * t] = (4 * hh + j) * ROWB + tree_piece<DP>(piece, 4 * hh + j) + 8 * (qq & 1);
+            vx[2 * t + 1] = (4 * hh + j + 8) * ROWB + tree_piece<DP>(piece, 4 * hh + j + 8) + 8 * (qq & 1);
+        }
+    }
+
+    // fetch role: instruction i of a wave fills rows RPI * (wave + 4 i) .. of the tile, a lane the piece at position lane % PPR of
+    // row RPI * (wave + 4 i) + lane / PPR (pieces that head_dim does not have repeat others).  The swizzle repeats every 16
+    // rows: at 512 bytes a row two instructions in a row differ.
+    constexpr int RPI = 1024 / ROWB, PPR = ROWB / 16;
+    const int frow = RPI * wave + lane / PPR;
+    uint32_t lane_off[2];
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+        int piece = tree_piece<DP>(lane % PPR, frow + 4 * RPI * v) / 16;   // (the swizzle undoes itself)
+        piece %= d / 8;
+        lane_off[v] = (uint32_t)(kvh * a.cache.head_stride * 2) + 16 * piece;
+    }
+    const uint32_t lds0 = lds_address(buf) + 1024 * wave;
+    PageIds ids;
+    auto fetch = [&](int b, int32_t t0) {
+#pragma unroll
+        for (int i = 0; i < Geo::kLoads; ++i) {
+            constexpr int STEP = 4 * RPI;                    // rows between a wave's instructions: 32, 16, 8
+            const int g = STEP >= 32 ? 0 : i * STEP / 16;
+            int32_t page;
+            if (STEP == 32) page = i == 0 ? (wave < 2 ? ids.p0 : ids.p1) : (wave < 2 ? ids.p2 : ids.p3);
+            else page = g == 0 ? ids.p0 : g == 1 ? ids.p1 : g == 2 ? ids.p2 : ids.p3;
+            const int32_t slot = min(t0 + frow + STEP * i, last_key) & (a.cache.page_size - 1);
+            int64_t page_off = (int64_t)page * a.cache.page_stride * 2;
+            asm volatile("" : "+s"(page_off));               // stays in scalar registers
+            const uint32_t off = (uint32_t)slot * (uint32_t)(a.cache.token_stride * 2) + lane_off[ROWB == 512 ? i & 1 : 0];
+            load_to_lds16(lds0 + b * Geo::kBufB, 4096 * i, reinterpret_cast<const char*>(a.cache.k) + page_off, off);
+            load_to_lds16(lds0 + b * Geo::kBufB, 4096 * i + Geo::kTileB, reinterpret_cast<const char*>(a.cache.v) + page_off, off);
+        }
+    };
+
+    f32x16 o[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) o[t] = (f32x16)(0.f);
+    float m = -INFINITY, l = 0.f;
+    const float sc = a.scale * kLog2e;
+
+    load_ids<true>(ids, a.cache, table, it.tile_begin * kBN, 0, last_key);
+    fetch(0, it.tile_begin * kBN);
+    if (it.tile_begin + 1 < it.tile_end) load_ids<true>(ids, a.cache, table, (it.tile_begin + 1) * kBN, 0, last_key);
+    wait_tile_loads();
+    __syncthreads();
+    int b = 0;
+    for (int32_t t = it.tile_begin; t < it.tile_end; ++t, b ^= 1) {
+        if (t + 1 < it.tile_end) {
+            fetch(b ^ 1, (t + 1) * kBN);
+            if (t + 2 < it.tile_end) load_ids<true>(ids, a.cache, table, (t + 2) * kBN, 0, last_key);
+        }
+        const char* const kbuf = buf + b * Geo::kBufB;
+#pragma unroll 1
+        for (int i = 0; i < HALVES; ++i) {
+            const int half = KW == 2 ? kw : i;
+            const int32_t key0 = t * kBN + 32 * half;
+            if (!live || key0 >= len) continue;              // (wave-uniform)
+            f32x16 s = (f32x16)(0.f), p;
+            const char* const kh = kbuf + 32 * half * ROWB;
+            const char* const vh = kh + Geo::kTileB;
+            // (scheduling barriers keep the operand reads of one phase from piling up in registers ahead of another)
+            uint4 ka[4], va[T], vb[T];
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) ka[ks] = *reinterpret_cast<const uint4*>(kh + kx[ks]);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                s = E::mfma32(ka[ks & 3], qf[ks], s);
+                if (ks + 4 < KS) ka[ks & 3] = *reinterpret_cast<const uint4*>(kh + kx[ks + 4]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (!CAREFUL) {
+#pragma unroll
+                for (int c = 0; c < T; ++c) va[c] = tree_v_frag(vh + vx[2 * c], vh + vx[2 * c + 1]);
+            }
+            uint32_t vis = ~0u;
+            if (key0 + 32 > ctx) {                           // (wave-uniform: drafted keys, or the end)
+                vis = visible_keys(mask, a.mask_words, key0, ctx, len);
+                tree_softmax<true, T>(p, s, o, m, l, sc, vis >> (4 * hh));
+            } else {
+                tree_softmax<false, T>(p, s, o, m, l, sc, 0u);
+            }
+            if (CAREFUL) {
+                tree_pv_by_key<E, DP, T>(o, p, vh, vis, ql, hh);
+                continue;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            uint4 w, wl;
+            tree_pack<E>(w, wl, p, 0);
+#pragma unroll
+            for (int c = 0; c < T; ++c) {
+                vb[c] = tree_v_frag(vh + 16 * ROWB + vx[2 * c], vh + 16 * ROWB + vx[2 * c + 1]);
+                o[c] = E::mfma32(va[c], w, o[c]);
+                o[c] = E::mfma32(va[c], wl, o[c]);
+            }
+            tree_pack<E>(w, wl, p, 8);
+#pragma unroll
+            for (int c = 0; c < T; ++c) {
+                o[c] = E::mfma32(vb[c], w, o[c]);
+                o[c] = E::mfma32(vb[c], wl, o[c]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        wait_tile_loads();
+        __syncthreads();
+    }
+
+    if (!CAREFUL) {
+        bool odd = false;
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) odd |= !(__builtin_fabsf(o[t][i]) <= 3.402823466e38f);
+        const bool any = __any(odd);
+        if (lane == 0) flags[wave] = any ? 1u : 0u;
+        __syncthreads();
+        const uint32_t again = flags[0] | flags[1] | flags[2] | flags[3];
+        __syncthreads();
+        if (again) return true;
+    }
+    l += __shfl_xor(l, 32, 64);
+    if (KW == 2) {                                           // the two waves of 32 rows meet (the tile buffers are free)
+        float4* const po = reinterpret_cast<float4*>(buf) + rw * (T * 4 + 1) * 64;
+        if (kw == 1) {
+#pragma unroll
+            for (int i = 0; i < 4 * T; ++i)
+                po[i * 64 + lane] = float4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
+            po[4 * T * 64 + lane] = float4{m, l, 0.f, 0.f};
+        }
+        __syncthreads();
+        if (kw == 0) {
+            const float4 ml = po[4 * T * 64 + lane];
+            const float top = fmaxf(m, ml.x), use = top == -INFINITY ? 0.f : top;
+            const float wa = __builtin_amdgcn_exp2f(m - use), wb = __builtin_amdgcn_exp2f(ml.x - use);
+            l = l * wa + ml.y * wb;
+            m = top;
+#pragma unroll
+            for (int i = 0; i < 4 * T; ++i) {
+                const float4 v = po[i * 64 + lane];
+                o[i / 4][4 * (i % 4)] = o[i / 4][4 * (i % 4)] * wa + v.x * wb;
+                o[i / 4][4 * (i % 4) + 1] = o[i / 4][4 * (i % 4) + 1] * wa + v.y * wb;
+                o[i / 4][4 * (i % 4) + 2] = o[i / 4][4 * (i % 4) + 2] * wa + v.z * wb;
+                o[i / 4][4 * (i % 4) + 3] = o[i / 4][4 * (i % 4) + 3] * wa + v.w * wb;
+            }
+        }
+        __syncthreads();                                     // (before the next piece of work loads over them)
+        if (kw == 1) return false;
+    }
+    if (r_lane >= n_rows) return false;
+    const float inv = l > 0.f ? 1.f / l : 0.f;               // (a NaN among the scores is in O as well)
+    const float lse2 = l <= 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l);
+    if (it.slot >= 0) {
+        const int64_t row = it.slot * RB + 32 * rw + ql;
+        float* const po = a.part_o + row * DP;
+#pragma unroll
+        for (int i = 0; i < 4 * T; ++i)
+            *reinterpret_cast<float4*>(po + 8 * i + 4 * hh) = float4{o[i / 4][4 * (i % 4)] * inv, o[i / 4][4 * (i % 4) + 1] * inv,
+                                                                     o[i / 4][4 * (i % 4) + 2] * inv, o[i / 4][4 * (i % 4) + 3] * inv};
+        if (hh == 0) a.part_lse[row] = lse2;
+        return false;
+    }
+    const int64_t row = (int64_t)(it.row0 + qi) * a.num_q_heads + h;
+    uint16_t* const orow = a.out + row * d;
+#pragma unroll
+    for (int i = 0; i < 4 * T; ++i) {
+        if (8 * i >= d) continue;                            // columns behind head_dim
+        *reinterpret_cast<uint2*>(orow + 8 * i + 4 * hh) =
+            uint2{E::pack(o[i / 4][4 * (i % 4)] * inv, o[i / 4][4 * (i % 4) + 1] * inv),
+                  E::pack(o[i / 4][4 * (i % 4) + 2] * inv, o[i / 4][4 * (i % 4) + 3] * inv)};
+    }
+    if (a.lse && hh == 0) a.lse[row] = lse2 * kLn2;
+    return false;
+}
+
+// Row blocks and key tiles of sequence i.
+struct TreeSeq {
+    int32_t row0, n, len, blocks, tiles;
+};
+template <int RB>
+__device__ __forceinline__ TreeSeq tree_seq(const TreeKernelArgs& a, int32_t i)
+{
+    TreeSeq q = {0, 0, 0, 0, 0};
+    if (i < a.batch) {
+        q.row0 = a.cu_q_lens[i];
+        q.n = a.cu_q_lens[i + 1] - q.row0;
+        q.len = a.seq_lens[i];
+        q.blocks = q.n > 0 ? (q.n * a.group + RB - 1) / RB : 0;
+        q.tiles = (q.len + kBN - 1) / kBN;
+    }
+    return q;
+}
+
+// All key tiles of the call (one KV head), and the workgroups that share them.
+template <int RB>
+__device__ __forceinline__ int64_t tree_tiles(const TreeKernelArgs& a, int lane, int64_t& wgs)
+{
+    int64_t all = 0;
+    for (int32_t i0 = 0; i0 < a.batch; i0 += 64) {
+        const TreeSeq q = tree_seq<RB>(a, i0 + lane);
+        all += wave_total_moves(q.blocks * q.tiles);
+    }
+    wgs = all / kTreeMinTiles;
+    wgs = wgs > a.wgs ? a.wgs : wgs < 1 ? 1 : wgs;
+    return all;
+}
+
+template <int WR, typename E, int DP>
+__global__ __launch_bounds__(256, TreeGeo<DP>::kOcc) void paged_attention_tree_mfma_kernel(TreeKernelArgs a)
+{
+    constexpr int RB = 32 * WR;
+    __shared__ __attribute__((aligned(1024))) char buf[2 * TreeGeo<DP>::kBufB];
+    __shared__ uint32_t flags[4];
+    const int lane = threadIdx.x & 63;
+    const int32_t hkv = a.cache.num_kv_heads;
+    const int32_t kvh = (int32_t)(blockIdx.x % (uint32_t)hkv), x = (int32_t)(blockIdx.x / (uint32_t)hkv);
+    // what is shared by the whole call: tiles [t, t_end) of all sequences' row blocks in a row, or one row block's
+    int32_t s = 0, rb = 0;
+    int64_t t = 0, t_end = 1, first = 0;
+    if (a.wgs == 0) {
+        s = x / a.row_blocks;
+        rb = x % a.row_blocks;
+    } else {
+        int64_t wgs;
+        const int64_t all = tree_tiles<RB>(a, lane, wgs);
+        if (x >= wgs) return;
+        t = (int64_t)x * all / wgs;
+        t_end = (int64_t)(x + 1) * all / wgs;
+        // the sequence of tile t and its first tile
+        for (int32_t i0 = 0; i0 < a.batch; i0 += 64) {
+            const TreeSeq q = tree_seq<RB>(a, i0 + lane);
+            const int32_t mine = q.blocks * q.tiles, inc = wave_scan_moves(mine);
+            const uint64_t hit = __ballot(first + inc > t);
+            if (hit) {
+                const int f = __ffsll((unsigned long long)hit) - 1;
+                s = i0 + f;
+                first += __builtin_amdgcn_readlane(inc, f) - __builtin_amdgcn_readlane(mine, f);
+                break;
+            }
+            first += __builtin_amdgcn_readlane(inc, 63);
+        }
+    }
+    while (t < t_end) {
+        const TreeSeq q = tree_seq<RB>(a, s);
+        TreeItem it;
+        it.s = s;
+        it.row0 = q.row0;
+        it.n = q.n;
+        it.len = q.len;
+        if (a.wgs == 0) {
+            if (rb >= q.blocks || q.tiles <= 0) return;
+            it.rb = rb;
+            it.tile_begin = 0;
+            it.tile_end = q.tiles;
+            it.slot = -1;
+            t = t_end;
+        } else {
+            const int32_t mine = q.blocks * q.tiles;
+            if (t >= first + mine) {                         // (nothing, or nothing more, of this one)
+                first += mine;
+                if (++s >= a.batch) return;
+                continue;
+            }
+            const int32_t at = (int32_t)(t - first);
+            it.rb = at / q.tiles;
+            it.tile_begin = at % q.tiles;
+            it.tile_end = (int32_t)min((int64_t)q.tiles, it.tile_begin + (t_end - t));
+            const bool whole = it.tile_begin == 0 && it.tile_end == q.tiles;
+            it.slot = whole ? -1 : ((int64_t)kvh * a.wgs + x) * 2 + (it.tile_begin == 0 ? 1 : 0);
+            t += it.tile_end - it.tile_begin;
+        }
+        if (tree_piece_of_work<WR, false, E, DP>(buf, flags, a, it, kvh)) tree_piece_of_work<WR, true, E, DP>(buf, flags, a, it, kvh);
+    }
+}
+
+// The pieces of a row block that workgroups' ends cut, merged by their log-sum-exps.  Grid (sequences x row blocks x RB / 32, KV
+// heads): 32 rows each, a thread four columns of some of them.
+template <int WR, typename E, int DP>
+__global__ __launch_bounds__(256) void paged_attention_tree_merge_kernel(TreeKernelArgs a)
+{
+    constexpr int RB = 32 * WR, CPR = DP / 4;
+    const int lane = threadIdx.x & 63;
+    const int32_t kvh = blockIdx.y, r0 = 32 * (int32_t)(blockIdx.x % WR);
+    const int32_t u = (int32_t)(blockIdx.x / WR), s = u / a.row_blocks, rb = u % a.row_blocks;
+    const TreeSeq own = tree_seq<RB>(a, s);
+    if (rb >= own.blocks || rb * RB + r0 >= own.n * a.group || own.tiles <= 0) return;
+    int64_t wgs, first = 0;
+    const int64_t all = tree_tiles<RB>(a, lane, wgs);
+    for (int32_t i0 = 0; i0 < s; i0 += 64) {
+        const TreeSeq q = tree_seq<RB>(a, i0 + lane);
+        first += wave_total_moves(i0 + lane < s ? q.blocks * q.tiles : 0);
+    }
+    const int64_t begin = first + (int64_t)rb * own.tiles, end = begin + own.tiles;
+    const int64_t w_first = ((begin + 1) * wgs - 1) / all, w_last = (end * wgs - 1) / all;   // workgroups of its first and last tile
+    if (w_first == w_last) return;
+    const int32_t pieces = (int32_t)(w_last - w_first) + 1, n_rows = own.n * a.group, d = a.cache.head_dim;
+    const int64_t slot0 = ((int64_t)kvh * a.wgs + w_first) * 2;
+    auto row_of = [&](int32_t k, int32_t row) { return (slot0 + 2 * (int64_t)k + (k == 0 ? 1 : 0)) * RB + row; };
+    for (int32_t i = threadIdx.x; i < 32 * CPR; i += 256) {
+        const int32_t row = r0 + i / CPR, c = 4 * (i % CPR), r = rb * RB + row;
+        if (r >= n_rows) continue;
+        float top = -INFINITY, sum = 0.f;
+        for (int32_t k = 0; k < pieces; ++k) top = fmaxf(top, a.part_lse[row_of(k, row)]);
+        const float use = top == -INFINITY ? 0.f : top;
+        float4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int32_t k = 0; k < pieces; ++k) {
+            const float w = __builtin_amdgcn_exp2f(a.part_lse[row_of(k, row)] - use);
+            const float4 v = *reinterpret_cast<const float4*>(a.part_o + row_of(k, row) * DP + c);
+            sum += w;
+            if (!(w == 0.f)) {                               // (a piece that the row sees nothing of)
+                acc.x = __builtin_fmaf(w, v.x, acc.x);
+                acc.y = __builtin_fmaf(w, v.y, acc.y);
+                acc.z = __builtin_fmaf(w, v.z, acc.z);
+                acc.w = __builtin_fmaf(w, v.w, acc.w);
+            }
+        }
+        if (c >= d) continue;
+        const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+        const int64_t out_row = (int64_t)(own.row0 + r / a.group) * a.num_q_heads + kvh * a.group + r % a.group;
+        *reinterpret_cast<uint2*>(a.out + out_row * d + c) = uint2{E::pack(acc.x * inv, acc.y * inv), E::pack(acc.z * inv, acc.w * inv)};
+        if (a.lse && c == 0) a.lse[out_row] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    }
+}
+
+template <int WR, typename E, int DP>
+pa_status launch_tree_of(const TreeKernelArgs& a, hipStream_t stream)
+{
+    const int64_t units = (int64_t)a.batch * a.row_blocks;
+    const int64_t grid = (a.wgs > 0 ? a.wgs : units) * a.cache.num_kv_heads;
+    if (grid > 0x7fffffffLL || units * WR > 0x7fffffffLL || a.cache.num_kv_heads > 65535) return PA_ERR_UNSUPPORTED;
+    {
+        ProfileScope prof("paged_attention_tree_mfma_kernel", stream);
+        hipLaunchKernelGGL((paged_attention_tree_mfma_kernel<WR, E, DP>), dim3((uint32_t)grid), dim3(256), 0, stream, a);
+        const pa_status st = launch_status();
+        if (st != PA_OK || a.wgs == 0) return st;
+    }
+    ProfileScope prof("paged_attention_tree_merge_kernel", stream);
+    hipLaunchKernelGGL((paged_attention_tree_merge_kernel<WR, E, DP>), dim3((uint32_t)(units * WR), (uint32_t)a.cache.num_kv_heads),
+                       dim3(256), 0, stream, a);
+    return launch_status();
+}
+
+template <int DP>
+pa_status launch_tree_dim(const TreeKernelArgs& a, pa_dtype dtype, int row_waves, hipStream_t stream)
+{
+    if (dtype == PA_DTYPE_BF16)
+        return row_waves == 2 ? launch_tree_of<2, ElemBf16, DP>(a, stream) : launch_tree_of<4, ElemBf16, DP>(a, stream);
+    return row_waves == 2 ? launch_tree_of<2, ElemF16, DP>(a, stream) : launch_tree_of<4, ElemF16, DP>(a, stream);
+}
+
+}  // namespace
+
+}  // namespace pa
