@@ -19,27 +19,30 @@ size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 }  // namespace
 
-// Up to 64 rows a (sequence, KV head) two waves share 32 rows.  The tiles are shared by as many workgroups as the machine holds
-// at once; on contexts of up to kPlainTiles tiles a row block is one workgroup's and there is no merge.
+// Up to 64 rows a (sequence, KV head) two waves share 32 rows, up to 128 at head_dims up to 128 as well, with eight waves; beyond
+// that a workgroup takes 256 rows (128 above head_dim 128, where a wave's O and Q fill its registers).  The tiles are shared by
+// as many workgroups as the machine holds at once; on contexts of up to kPlainTiles tiles a row block is one workgroup's
+// and there is no merge.
 TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t max_q_len, int32_t max_seq_len)
 {
     constexpr int32_t kPlainTiles = 8;
     TreePlan p;
     const int64_t rows = (int64_t)max_q_len * (num_q_heads / num_kv_heads);
-    p.row_waves = rows <= 64 ? 2 : 4;
+    const int32_t columns = columns_of(head_dim);
+    p.row_waves = rows <= 64 ? 2 : rows <= 128 || columns > 128 ? 4 : 8;
     const int64_t blocks = (rows + 32 * p.row_waves - 1) / (32 * p.row_waves);
     p.row_blocks = blocks < 1 ? 1 : (int32_t)blocks;
     const int64_t tiles = ((int64_t)max_seq_len + prefill::kBN - 1) / prefill::kBN;
     p.wgs = 0;
     p.part_o_bytes = p.part_lse_bytes = 0;
     if (tiles > kPlainTiles) {
-        const int64_t slots = (int64_t)device_cus() * (columns_of(head_dim) > 128 ? 1 : 2);
+        const int64_t slots = (int64_t)device_cus() * (columns == 64 && p.row_waves == 2 ? 2 : 1);
         const int64_t most = (batch * blocks * tiles + 3) / 4;
         int64_t wgs = slots / num_kv_heads;
         if (wgs > most) wgs = most;
-        p.wgs = wgs < 1 ? 1 : (int32_t)wgs;
+        p.wgs = wgs < 1 ? 1 : wgs > kTreeMaxPieces ? kTreeMaxPieces : (int32_t)wgs;
         const size_t part_rows = (size_t)p.wgs * num_kv_heads * 2 * 32 * p.row_waves;
-        p.part_o_bytes = align256(part_rows * columns_of(head_dim) * sizeof(float));
+        p.part_o_bytes = align256(part_rows * columns * sizeof(float));
         p.part_lse_bytes = align256(part_rows * sizeof(float));
     }
     return p;

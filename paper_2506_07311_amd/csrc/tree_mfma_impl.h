@@ -58,9 +58,42 @@ struct TreeGeo {
     static constexpr int kBufB = 2 * kTileB;
     static constexpr int kKS = DP / 16;                                  // steps of a score product
     static constexpr int kT = DP / 32;                                   // 32-column blocks of O
-    static constexpr int kLoads = kTileB / 4096;                         // load instructions of a wave and pool a tile
-    static constexpr int kOcc = DP > 128 ? 1 : 2;                        // workgroups of a compute unit
 };
+
+// A workgroup's waves: WR beside each other in rows, KW along a tile's keys.  Buffers as LDS holds them: what is in flight
+// beside the tile being computed has to cover the memory's latency at its full rate, about 100 KB a compute unit.
+template <int WR, int DP>
+struct TreeShape {
+    static constexpr int kKW = WR == 2 || (WR == 4 && DP <= 128) ? 2 : 1;
+    static constexpr int kWaves = WR * kKW;
+    static constexpr int kOcc = DP <= 64 && kWaves == 4 ? 2 : 1;         // workgroups of a compute unit
+    static constexpr int kBufs = DP > 128 ? 2 : DP > 64 ? 4 : kOcc == 2 ? 4 : 8;
+    static constexpr int kLoads = TreeGeo<DP>::kTileB / (1024 * kWaves); // load instructions of a wave and pool a tile
+};
+
+// This wave's loads to LDS have landed but for the last n tiles' (kLoads of either pool each).  In order, so what the
+// compiler has issued in between makes it wait for more, not for less.
+template <int LOADS>
+__device__ __forceinline__ void wait_tiles_but(int n)
+{
+    // (vmcnt is split: bits 3..0 and 15..14; counts beyond its 63 do not occur)
+#define PA_WAIT_BUT(N)                                                                                        \
+    {                                                                                                         \
+        constexpr int V = 2 * LOADS * N < 63 ? 2 * LOADS * N : 63;                                            \
+        __builtin_amdgcn_s_waitcnt(0x0F70 | (V & 15) | ((V >> 4) << 14));                                     \
+        break;                                                                                                \
+    }
+    switch (n) {
+        case 0: PA_WAIT_BUT(0)
+        case 1: PA_WAIT_BUT(1)
+        case 2: PA_WAIT_BUT(2)
+        case 3: PA_WAIT_BUT(3)
+        case 4: PA_WAIT_BUT(4)
+        case 5: PA_WAIT_BUT(5)
+        default: PA_WAIT_BUT(6)                              // eight buffers
+    }
+#undef PA_WAIT_BUT
+}
 
 // Byte offset inside its LDS row r of logical 16-byte piece L (rows of 512 bytes swizzle each half by itself; of rows of
 // 128 bytes two share the banks).
@@ -116,25 +149,21 @@ __device__ __forceinline__ void tree_pack(uint4& w, uint4& wl, const f32x16& p, 
     wl.w = E::pack(p[r0 + 6] - E::lo_of(w.w), p[r0 + 7] - E::hi_of(w.w));
 }
 
-// Weights of 32 keys; s holds raw scores.  vis (MASK): this lane's keys, score r is bit 8 (r / 4) + r % 4.
-template <bool MASK, int T>
-__device__ __forceinline__ void tree_softmax(f32x16& p, const f32x16& s, f32x16 (&o)[T], float& m, float& l, float sc, uint32_t vis)
+// Weights of 32 keys from their raw scores (-inf: not seen); sc > 0.
+template <int T>
+__device__ __forceinline__ void tree_softmax(f32x16& p, const f32x16& s, f32x16 (&o)[T], float& m, float& l, float sc)
 {
     float psum = 0.f;
-    auto score = [&](int r) {                                // in the log2 domain (whatever the sign of the scale)
-        const float x = s[r] * sc;
-        return !MASK || (vis >> (8 * (r / 4) + r % 4)) & 1u ? x : -INFINITY;
-    };
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-        p[r] = __builtin_amdgcn_exp2f(MASK ? score(r) - m : __builtin_fmaf(s[r], sc, -m));
+        p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc, -m));
         psum += p[r];
     }
     if (__any(!(psum <= kWeightSumMax))) {                   // also the NaN or infinity of a fresh reference
         float top = -INFINITY;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, score(r));
-        const float m_new = fmaxf(m, row_max<2>(top));
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[r]);
+        const float m_new = fmaxf(m, row_max<2>(top) * sc);
         const float use = m_new == -INFINITY ? 0.f : m_new;  // (no key so far)
         const float alpha = __builtin_amdgcn_exp2f(m - use);
 #pragma unroll
@@ -144,7 +173,7 @@ __device__ __forceinline__ void tree_softmax(f32x16& p, const f32x16& s, f32x16 
         psum = 0.f;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            p[r] = __builtin_amdgcn_exp2f(score(r) - use);
+            p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc, -use));
             psum += p[r];
         }
     }
@@ -186,7 +215,8 @@ template <int WR, bool CAREFUL, typename E, int DP>
 __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, const TreeKernelArgs& a, const TreeItem& it, int32_t kvh)
 {
     typedef TreeGeo<DP> Geo;
-    constexpr int RB = 32 * WR, KW = 4 / WR, ROWB = Geo::kRowB, T = Geo::kT, KS = Geo::kKS;
+    typedef TreeShape<WR, DP> Shape;
+    constexpr int RB = 32 * WR, KW = Shape::kKW, NW = Shape::kWaves, NB = Shape::kBufs, ROWB = Geo::kRowB, T = Geo::kT, KS = Geo::kKS;
     constexpr int HALVES = 2 / KW;                           // 32-key halves of a tile that a wave takes
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));                            // (what follows from it is not kept across pieces of work)
@@ -202,13 +232,19 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
     const int32_t* const table = a.block_table + (int64_t)it.s * a.max_blocks;
     const int32_t last_key = len - 1;
 
-    // Q as B operand: lane % 32 = row, step ks covers 8 elements of either lane half; 0 behind head_dim
+    // Q as B operand: lane % 32 = row, step ks covers 8 elements of either lane half; 0 behind head_dim.  The scale that the scores
+    // get is positive, so that masking commutes with it: a negative one's sign goes to Q, and for a scale of 0 Q is 0.
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+    const float sc = a.scale == 0.f ? 1.f : __builtin_fabsf(a.scale) * kLog2e;
     const uint16_t* const qrow = a.q + ((int64_t)(it.row0 + qi) * a.num_q_heads + h) * d;
     uint4 qf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
         qf[ks] = uint4{0, 0, 0, 0};
-        if (16 * ks + 8 * hh < d) qf[ks] = *reinterpret_cast<const uint4*>(qrow + 16 * ks + 8 * hh);
+        if (16 * ks + 8 * hh < d && a.scale != 0.f) {
+            const uint4 v = *reinterpret_cast<const uint4*>(qrow + 16 * ks + 8 * hh);
+            qf[ks] = uint4{v.x ^ flip, v.y ^ flip, v.z ^ flip, v.w ^ flip};
+        }
     }
 
     // operand offsets: K piece 2 ks + hh of row ql; V pieces of the 32 columns t for the lane's transpose-load row, key 4 hh + j
@@ -226,34 +262,32 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
         }
     }
 
-    // fetch role: instruction i of a wave fills rows RPI * (wave + 4 i) .. of the tile, a lane the piece at position lane % PPR of
-    // row RPI * (wave + 4 i) + lane / PPR (pieces that head_dim does not have repeat others).  The swizzle repeats every 16
-    // rows: at 512 bytes a row two instructions in a row differ.
-    constexpr int RPI = 1024 / ROWB, PPR = ROWB / 16;
+    // fetch role: instruction i of a wave fills rows RPI * (wave + NW i) .. of the tile, a lane the piece at position lane % PPR of
+    // row RPI * (wave + NW i) + lane / PPR (pieces that head_dim does not have repeat others).  The swizzle repeats every 16
+    // rows: with 8 rows between a wave's instructions, two in a row differ.
+    constexpr int RPI = 1024 / ROWB, PPR = ROWB / 16, STEP = NW * RPI;
     const int frow = RPI * wave + lane / PPR;
-    uint32_t lane_off[2];
+    uint32_t lane_off[STEP == 8 ? 2 : 1];
 #pragma unroll
-    for (int v = 0; v < 2; ++v) {
-        int piece = tree_piece<DP>(lane % PPR, frow + 4 * RPI * v) / 16;   // (the swizzle undoes itself)
+    for (int v = 0; v < (STEP == 8 ? 2 : 1); ++v) {
+        int piece = tree_piece<DP>(lane % PPR, frow + 8 * v) / 16;         // (the swizzle undoes itself)
         piece %= d / 8;
         lane_off[v] = (uint32_t)(kvh * a.cache.head_stride * 2) + 16 * piece;
     }
     const uint32_t lds0 = lds_address(buf) + 1024 * wave;
+    const int32_t page16 = (RPI * wave) >> 4;                // group of 16 rows (one page) of the wave's first instruction
     PageIds ids;
     auto fetch = [&](int b, int32_t t0) {
 #pragma unroll
-        for (int i = 0; i < Geo::kLoads; ++i) {
-            constexpr int STEP = 4 * RPI;                    // rows between a wave's instructions: 32, 16, 8
-            const int g = STEP >= 32 ? 0 : i * STEP / 16;
-            int32_t page;
-            if (STEP == 32) page = i == 0 ? (wave < 2 ? ids.p0 : ids.p1) : (wave < 2 ? ids.p2 : ids.p3);
-            else page = g == 0 ? ids.p0 : g == 1 ? ids.p1 : g == 2 ? ids.p2 : ids.p3;
+        for (int i = 0; i < Shape::kLoads; ++i) {
+            const int g = page16 + STEP * i / 16;            // (STEP < 16: the wave's rows stay in a group of its instruction)
+            const int32_t page = g == 0 ? ids.p0 : g == 1 ? ids.p1 : g == 2 ? ids.p2 : ids.p3;
             const int32_t slot = min(t0 + frow + STEP * i, last_key) & (a.cache.page_size - 1);
             int64_t page_off = (int64_t)page * a.cache.page_stride * 2;
             asm volatile("" : "+s"(page_off));               // stays in scalar registers
-            const uint32_t off = (uint32_t)slot * (uint32_t)(a.cache.token_stride * 2) + lane_off[ROWB == 512 ? i & 1 : 0];
-            load_to_lds16(lds0 + b * Geo::kBufB, 4096 * i, reinterpret_cast<const char*>(a.cache.k) + page_off, off);
-            load_to_lds16(lds0 + b * Geo::kBufB, 4096 * i + Geo::kTileB, reinterpret_cast<const char*>(a.cache.v) + page_off, off);
+            const uint32_t off = (uint32_t)slot * (uint32_t)(a.cache.token_stride * 2) + lane_off[STEP == 8 ? i & 1 : 0];
+            load_to_lds16(lds0 + b * Geo::kBufB, 1024 * NW * i, reinterpret_cast<const char*>(a.cache.k) + page_off, off);
+            load_to_lds16(lds0 + b * Geo::kBufB, 1024 * NW * i + Geo::kTileB, reinterpret_cast<const char*>(a.cache.v) + page_off, off);
         }
     };
 
@@ -261,18 +295,23 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
 #pragma unroll
     for (int t = 0; t < T; ++t) o[t] = (f32x16)(0.f);
     float m = -INFINITY, l = 0.f;
-    const float sc = a.scale * kLog2e;
 
-    load_ids<true>(ids, a.cache, table, it.tile_begin * kBN, 0, last_key);
-    fetch(0, it.tile_begin * kBN);
-    if (it.tile_begin + 1 < it.tile_end) load_ids<true>(ids, a.cache, table, (it.tile_begin + 1) * kBN, 0, last_key);
-    wait_tile_loads();
-    __syncthreads();
+    // NB - 1 tiles ahead (a piece of work has a tile at least); the page ids of the tile that is fetched next are loaded a tile before
+    int32_t ahead = it.tile_begin;                           // the tile to fetch next
+    load_ids<true>(ids, a.cache, table, ahead * kBN, 0, last_key);
+#pragma unroll 1
+    for (int i = 0; i < NB - 1 && ahead < it.tile_end; ++i) {
+        fetch(i, ahead * kBN);
+        if (++ahead < it.tile_end) load_ids<true>(ids, a.cache, table, ahead * kBN, 0, last_key);
+    }
     int b = 0;
-    for (int32_t t = it.tile_begin; t < it.tile_end; ++t, b ^= 1) {
-        if (t + 1 < it.tile_end) {
-            fetch(b ^ 1, (t + 1) * kBN);
-            if (t + 2 < it.tile_end) load_ids<true>(ids, a.cache, table, (t + 2) * kBN, 0, last_key);
+#pragma unroll 1
+    for (int32_t t = it.tile_begin; t < it.tile_end; ++t) {
+        wait_tiles_but<Shape::kLoads>(NB == 2 ? 0 : min(ahead - t - 1, NB - 2));
+        __syncthreads();                                     // tile t is there, and tile t - 1 done with
+        if (ahead < it.tile_end) {
+            fetch(b == 0 ? NB - 1 : b - 1, ahead * kBN);
+            if (++ahead < it.tile_end) load_ids<true>(ids, a.cache, table, ahead * kBN, 0, last_key);
         }
         const char* const kbuf = buf + b * Geo::kBufB;
 #pragma unroll 1
@@ -300,10 +339,11 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
             uint32_t vis = ~0u;
             if (key0 + 32 > ctx) {                           // (wave-uniform: drafted keys, or the end)
                 vis = visible_keys(mask, a.mask_words, key0, ctx, len);
-                tree_softmax<true, T>(p, s, o, m, l, sc, vis >> (4 * hh));
-            } else {
-                tree_softmax<false, T>(p, s, o, m, l, sc, 0u);
+                const uint32_t own = vis >> (4 * hh);        // score r is key 8 (r / 4) + 4 hh + r % 4
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = (own >> (8 * (r / 4) + r % 4)) & 1u ? s[r] : -INFINITY;
             }
+            tree_softmax<T>(p, s, o, m, l, sc);
             if (CAREFUL) {
                 tree_pv_by_key<E, DP, T>(o, p, vh, vis, ql, hh);
                 continue;
@@ -325,10 +365,10 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        wait_tile_loads();
-        __syncthreads();
+        b = b == NB - 1 ? 0 : b + 1;
     }
 
+    bool again = false;
     if (!CAREFUL) {
         bool odd = false;
 #pragma unroll
@@ -337,13 +377,15 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
             for (int i = 0; i < 16; ++i) odd |= !(__builtin_fabsf(o[t][i]) <= 3.402823466e38f);
         const bool any = __any(odd);
         if (lane == 0) flags[wave] = any ? 1u : 0u;
-        __syncthreads();
-        const uint32_t again = flags[0] | flags[1] | flags[2] | flags[3];
-        __syncthreads();
+    }
+    __syncthreads();                                         // (the tile buffers are free)
+    if (!CAREFUL) {
+#pragma unroll
+        for (int w = 0; w < NW; ++w) again |= flags[w] != 0;
         if (again) return true;
     }
     l += __shfl_xor(l, 32, 64);
-    if (KW == 2) {                                           // the two waves of 32 rows meet (the tile buffers are free)
+    if (KW == 2) {                                           // the two waves of 32 rows meet
         float4* const po = reinterpret_cast<float4*>(buf) + rw * (T * 4 + 1) * 64;
         if (kw == 1) {
 #pragma unroll
@@ -429,11 +471,11 @@ __device__ __forceinline__ int64_t tree_tiles(const TreeKernelArgs& a, int lane,
 }
 
 template <int WR, typename E, int DP>
-__global__ __launch_bounds__(256, TreeGeo<DP>::kOcc) void paged_attention_tree_mfma_kernel(TreeKernelArgs a)
+__global__ __launch_bounds__((64 * TreeShape<WR, DP>::kWaves), (TreeShape<WR, DP>::kOcc * TreeShape<WR, DP>::kWaves / 4)) void paged_attention_tree_mfma_kernel(TreeKernelArgs a)
 {
     constexpr int RB = 32 * WR;
-    __shared__ __attribute__((aligned(1024))) char buf[2 * TreeGeo<DP>::kBufB];
-    __shared__ uint32_t flags[4];
+    __shared__ __attribute__((aligned(1024))) char buf[TreeShape<WR, DP>::kBufs * TreeGeo<DP>::kBufB];
+    __shared__ uint32_t flags[8];
     const int lane = threadIdx.x & 63;
     const int32_t hkv = a.cache.num_kv_heads;
     const int32_t kvh = (int32_t)(blockIdx.x % (uint32_t)hkv), x = (int32_t)(blockIdx.x / (uint32_t)hkv);
@@ -496,15 +538,21 @@ __global__ __launch_bounds__(256, TreeGeo<DP>::kOcc) void paged_attention_tree_m
     }
 }
 
-// The pieces of a row block that workgroups' ends cut, merged by their log-sum-exps.  Grid (sequences x row blocks x RB / 32, KV
-// heads): 32 rows each, a thread four columns of some of them.
+// The pieces of a row block that workgroups' ends cut, merged by their log-sum-exps.  Grid (sequences x row blocks x RB / 8, KV
+// heads): 8 rows each (a call of few sequences still spreads over the machine).  Statistics first, all at once, and their weights
+// into LDS; then a thread's columns, with the loads of four pieces in flight.
+constexpr int kTreeMergeRows = 8;
+constexpr int kTreeMaxPieces = 512;
+
 template <int WR, typename E, int DP>
 __global__ __launch_bounds__(256) void paged_attention_tree_merge_kernel(TreeKernelArgs a)
 {
-    constexpr int RB = 32 * WR, CPR = DP / 4;
+    constexpr int RB = 32 * WR, CPR = DP / 4, PARTS = RB / kTreeMergeRows, RM = kTreeMergeRows;
+    __shared__ float weight[kTreeMaxPieces * RM];
+    __shared__ float sm_top[RM], sm_sum[RM];
     const int lane = threadIdx.x & 63;
-    const int32_t kvh = blockIdx.y, r0 = 32 * (int32_t)(blockIdx.x % WR);
-    const int32_t u = (int32_t)(blockIdx.x / WR), s = u / a.row_blocks, rb = u % a.row_blocks;
+    const int32_t kvh = blockIdx.y, r0 = RM * (int32_t)(blockIdx.x % PARTS);
+    const int32_t u = (int32_t)(blockIdx.x / PARTS), s = u / a.row_blocks, rb = u % a.row_blocks;
     const TreeSeq own = tree_seq<RB>(a, s);
     if (rb >= own.blocks || rb * RB + r0 >= own.n * a.group || own.tiles <= 0) return;
     int64_t wgs, first = 0;
@@ -519,29 +567,43 @@ __global__ __launch_bounds__(256) void paged_attention_tree_merge_kernel(TreeKer
     const int32_t pieces = (int32_t)(w_last - w_first) + 1, n_rows = own.n * a.group, d = a.cache.head_dim;
     const int64_t slot0 = ((int64_t)kvh * a.wgs + w_first) * 2;
     auto row_of = [&](int32_t k, int32_t row) { return (slot0 + 2 * (int64_t)k + (k == 0 ? 1 : 0)) * RB + row; };
-    for (int32_t i = threadIdx.x; i < 32 * CPR; i += 256) {
-        const int32_t row = r0 + i / CPR, c = 4 * (i % CPR), r = rb * RB + row;
-        if (r >= n_rows) continue;
+    for (int32_t i = threadIdx.x; i < pieces * RM; i += 256) weight[i] = a.part_lse[row_of(i / RM, r0 + i % RM)];
+    __syncthreads();
+    if (threadIdx.x < RM) {
         float top = -INFINITY, sum = 0.f;
-        for (int32_t k = 0; k < pieces; ++k) top = fmaxf(top, a.part_lse[row_of(k, row)]);
+        for (int32_t k = 0; k < pieces; ++k) top = fmaxf(top, weight[k * RM + threadIdx.x]);
         const float use = top == -INFINITY ? 0.f : top;
-        float4 acc = {0.f, 0.f, 0.f, 0.f};
         for (int32_t k = 0; k < pieces; ++k) {
-            const float w = __builtin_amdgcn_exp2f(a.part_lse[row_of(k, row)] - use);
-            const float4 v = *reinterpret_cast<const float4*>(a.part_o + row_of(k, row) * DP + c);
+            const float w = __builtin_amdgcn_exp2f(weight[k * RM + threadIdx.x] - use);
+            weight[k * RM + threadIdx.x] = w;
             sum += w;
-            if (!(w == 0.f)) {                               // (a piece that the row sees nothing of)
-                acc.x = __builtin_fmaf(w, v.x, acc.x);
-                acc.y = __builtin_fmaf(w, v.y, acc.y);
-                acc.z = __builtin_fmaf(w, v.z, acc.z);
-                acc.w = __builtin_fmaf(w, v.w, acc.w);
+        }
+        sm_top[threadIdx.x] = top;
+        sm_sum[threadIdx.x] = sum;
+    }
+    __syncthreads();
+    for (int32_t i = threadIdx.x; i < RM * CPR; i += 256) {
+        const int32_t row = i / CPR, c = 4 * (i % CPR), r = rb * RB + r0 + row;
+        if (r >= n_rows || c >= d) continue;
+        float4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int32_t k0 = 0; k0 < pieces; k0 += 4) {
+            float4 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const float4*>(a.part_o + row_of(min(k0 + k, pieces - 1), r0 + row) * DP + c);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (k0 + k >= pieces) break;
+                const float w = weight[(k0 + k) * RM + row];
+                acc.x = __builtin_fmaf(w, v[k].x, acc.x);
+                acc.y = __builtin_fmaf(w, v[k].y, acc.y);
+                acc.z = __builtin_fmaf(w, v[k].z, acc.z);
+                acc.w = __builtin_fmaf(w, v[k].w, acc.w);
             }
         }
-        if (c >= d) continue;
-        const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+        const float sum = sm_sum[row], inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
         const int64_t out_row = (int64_t)(own.row0 + r / a.group) * a.num_q_heads + kvh * a.group + r % a.group;
         *reinterpret_cast<uint2*>(a.out + out_row * d + c) = uint2{E::pack(acc.x * inv, acc.y * inv), E::pack(acc.z * inv, acc.w * inv)};
-        if (a.lse && c == 0) a.lse[out_row] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+        if (a.lse && c == 0) a.lse[out_row] = sum == 0.f ? -INFINITY : (sm_top[row] + __builtin_amdgcn_logf(sum)) * kLn2;
     }
 }
 
@@ -550,25 +612,34 @@ pa_status launch_tree_of(const TreeKernelArgs& a, hipStream_t stream)
 {
     const int64_t units = (int64_t)a.batch * a.row_blocks;
     const int64_t grid = (a.wgs > 0 ? a.wgs : units) * a.cache.num_kv_heads;
-    if (grid > 0x7fffffffLL || units * WR > 0x7fffffffLL || a.cache.num_kv_heads > 65535) return PA_ERR_UNSUPPORTED;
+    constexpr int PARTS = 32 * WR / kTreeMergeRows;
+    if (grid > 0x7fffffffLL || units * PARTS > 0x7fffffffLL || a.cache.num_kv_heads > 65535) return PA_ERR_UNSUPPORTED;
     {
         ProfileScope prof("paged_attention_tree_mfma_kernel", stream);
-        hipLaunchKernelGGL((paged_attention_tree_mfma_kernel<WR, E, DP>), dim3((uint32_t)grid), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((paged_attention_tree_mfma_kernel<WR, E, DP>), dim3((uint32_t)grid),
+                           dim3(64 * TreeShape<WR, DP>::kWaves), 0, stream, a);
         const pa_status st = launch_status();
         if (st != PA_OK || a.wgs == 0) return st;
     }
     ProfileScope prof("paged_attention_tree_merge_kernel", stream);
-    hipLaunchKernelGGL((paged_attention_tree_merge_kernel<WR, E, DP>), dim3((uint32_t)(units * WR), (uint32_t)a.cache.num_kv_heads),
+    hipLaunchKernelGGL((paged_attention_tree_merge_kernel<WR, E, DP>), dim3((uint32_t)(units * PARTS), (uint32_t)a.cache.num_kv_heads),
                        dim3(256), 0, stream, a);
     return launch_status();
+}
+
+template <typename E, int DP>
+pa_status launch_tree_rows(const TreeKernelArgs& a, int row_waves, hipStream_t stream)
+{
+    if (row_waves == 2) return launch_tree_of<2, E, DP>(a, stream);
+    if constexpr (DP <= 128)
+        if (row_waves == 8) return launch_tree_of<8, E, DP>(a, stream);
+    return launch_tree_of<4, E, DP>(a, stream);
 }
 
 template <int DP>
 pa_status launch_tree_dim(const TreeKernelArgs& a, pa_dtype dtype, int row_waves, hipStream_t stream)
 {
-    if (dtype == PA_DTYPE_BF16)
-        return row_waves == 2 ? launch_tree_of<2, ElemBf16, DP>(a, stream) : launch_tree_of<4, ElemBf16, DP>(a, stream);
-    return row_waves == 2 ? launch_tree_of<2, ElemF16, DP>(a, stream) : launch_tree_of<4, ElemF16, DP>(a, stream);
+    return dtype == PA_DTYPE_BF16 ? launch_tree_rows<ElemBf16, DP>(a, row_waves, stream) : launch_tree_rows<ElemF16, DP>(a, row_waves, stream);
 }
 
 }  // namespace
