@@ -33,6 +33,8 @@ struct TreeKernelArgs {
     const uint16_t* q;
     uint16_t* out;
     float* lse;
+    // (kernel arguments of their own: the compiler has to know that nothing else points there, or page ids come by vector loads,
+    // and each wait for one is a wait for every tile in flight: 16 x 16 tokens on 131072 2512 us)
     const int32_t* cu_q_lens;
     const int32_t* seq_lens;
     const uint64_t* tree_mask;
@@ -71,28 +73,14 @@ struct TreeShape {
     static constexpr int kLoads = TreeGeo<DP>::kTileB / (1024 * kWaves); // load instructions of a wave and pool a tile
 };
 
-// This wave's loads to LDS have landed but for the last n tiles' (kLoads of either pool each).  In order, so what the
-// compiler has issued in between makes it wait for more, not for less.
-template <int LOADS>
-__device__ __forceinline__ void wait_tiles_but(int n)
+// This wave's loads to LDS have landed but for the last N tiles' (LOADS of either pool each).  In order, so what the compiler
+// has issued in between makes it wait for more, not for less.
+template <int LOADS, int N>
+__device__ __forceinline__ void wait_tiles_but()
 {
-    // (vmcnt is split: bits 3..0 and 15..14; counts beyond its 63 do not occur)
-#define PA_WAIT_BUT(N)                                                                                        \
-    {                                                                                                         \
-        constexpr int V = 2 * LOADS * N < 63 ? 2 * LOADS * N : 63;                                            \
-        __builtin_amdgcn_s_waitcnt(0x0F70 | (V & 15) | ((V >> 4) << 14));                                     \
-        break;                                                                                                \
-    }
-    switch (n) {
-        case 0: PA_WAIT_BUT(0)
-        case 1: PA_WAIT_BUT(1)
-        case 2: PA_WAIT_BUT(2)
-        case 3: PA_WAIT_BUT(3)
-        case 4: PA_WAIT_BUT(4)
-        case 5: PA_WAIT_BUT(5)
-        default: PA_WAIT_BUT(6)                              // eight buffers
-    }
-#undef PA_WAIT_BUT
+    constexpr int V = 2 * LOADS * N;
+    static_assert(V < 64, "more loads than the counter holds");
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (V & 15) | ((V >> 4) << 14));   // vmcnt: bits 3..0 and 15..14
 }
 
 // Byte offset inside its LDS row r of logical 16-byte piece L (rows of 512 bytes swizzle each half by itself; of rows of
@@ -275,15 +263,19 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
         lane_off[v] = (uint32_t)(kvh * a.cache.head_stride * 2) + 16 * piece;
     }
     const uint32_t lds0 = lds_address(buf) + 1024 * wave;
-    const int32_t page16 = (RPI * wave) >> 4;                // group of 16 rows (one page) of the wave's first instruction
-    PageIds ids;
+    int32_t pages[Shape::kLoads];                            // of the rows of each instruction (16 rows and more lie in one page)
+    auto load_pages = [&](int32_t t0) {
+#pragma unroll
+        for (int i = 0; i < Shape::kLoads; ++i) {
+            const int32_t key = __builtin_amdgcn_readfirstlane(t0 + RPI * wave + STEP * i);
+            pages[i] = table[min(key, last_key) >> a.cache.log2_page];
+        }
+    };
     auto fetch = [&](int b, int32_t t0) {
 #pragma unroll
         for (int i = 0; i < Shape::kLoads; ++i) {
-            const int g = page16 + STEP * i / 16;            // (STEP < 16: the wave's rows stay in a group of its instruction)
-            const int32_t page = g == 0 ? ids.p0 : g == 1 ? ids.p1 : g == 2 ? ids.p2 : ids.p3;
             const int32_t slot = min(t0 + frow + STEP * i, last_key) & (a.cache.page_size - 1);
-            int64_t page_off = (int64_t)page * a.cache.page_stride * 2;
+            int64_t page_off = (int64_t)pages[i] * a.cache.page_stride * 2;
             asm volatile("" : "+s"(page_off));               // stays in scalar registers
             const uint32_t off = (uint32_t)slot * (uint32_t)(a.cache.token_stride * 2) + lane_off[STEP == 8 ? i & 1 : 0];
             load_to_lds16(lds0 + b * Geo::kBufB, 1024 * NW * i, reinterpret_cast<const char*>(a.cache.k) + page_off, off);
@@ -298,20 +290,24 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
 
     // NB - 1 tiles ahead (a piece of work has a tile at least); the page ids of the tile that is fetched next are loaded a tile before
     int32_t ahead = it.tile_begin;                           // the tile to fetch next
-    load_ids<true>(ids, a.cache, table, ahead * kBN, 0, last_key);
+    load_pages(ahead * kBN);
 #pragma unroll 1
     for (int i = 0; i < NB - 1 && ahead < it.tile_end; ++i) {
         fetch(i, ahead * kBN);
-        if (++ahead < it.tile_end) load_ids<true>(ids, a.cache, table, ahead * kBN, 0, last_key);
+        if (++ahead < it.tile_end) load_pages(ahead * kBN);
     }
     int b = 0;
 #pragma unroll 1
     for (int32_t t = it.tile_begin; t < it.tile_end; ++t) {
-        wait_tiles_but<Shape::kLoads>(NB == 2 ? 0 : min(ahead - t - 1, NB - 2));
+        const int32_t after = ahead - t - 1;                 // tiles in flight behind this one
+        constexpr int MANY = NB - 2, SOME = MANY > 3 ? 3 : MANY > 1 ? 1 : 0;
+        if (after >= MANY) wait_tiles_but<Shape::kLoads, MANY>();
+        else if (after >= SOME) wait_tiles_but<Shape::kLoads, SOME>();
+        else wait_tiles_but<Shape::kLoads, 0>();
         __syncthreads();                                     // tile t is there, and tile t - 1 done with
         if (ahead < it.tile_end) {
             fetch(b == 0 ? NB - 1 : b - 1, ahead * kBN);
-            if (++ahead < it.tile_end) load_ids<true>(ids, a.cache, table, ahead * kBN, 0, last_key);
+            if (++ahead < it.tile_end) load_pages(ahead * kBN);
         }
         const char* const kbuf = buf + b * Geo::kBufB;
 #pragma unroll 1
@@ -322,20 +318,23 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
             f32x16 s = (f32x16)(0.f), p;
             const char* const kh = kbuf + 32 * half * ROWB;
             const char* const vh = kh + Geo::kTileB;
-            // (scheduling barriers keep the operand reads of one phase from piling up in registers ahead of another)
-            uint4 ka[4], va[T], vb[T];
+            // The operand reads are kept four ahead of their products and V's first step comes behind K's last: left to itself the
+            // compiler waits for each read in front of the product that takes it.
+            uint4 va[T], vb[T];
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks) ka[ks] = *reinterpret_cast<const uint4*>(kh + kx[ks]);
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                s = E::mfma32(ka[ks & 3], qf[ks], s);
-                if (ks + 4 < KS) ka[ks & 3] = *reinterpret_cast<const uint4*>(kh + kx[ks + 4]);
-            }
-            __builtin_amdgcn_sched_barrier(0);
+            for (int ks = 0; ks < KS; ++ks) s = E::mfma32(*reinterpret_cast<const uint4*>(kh + kx[ks]), qf[ks], s);
             if (!CAREFUL) {
 #pragma unroll
                 for (int c = 0; c < T; ++c) va[c] = tree_v_frag(vh + vx[2 * c], vh + vx[2 * c + 1]);
             }
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                if (ks + 4 < KS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                else __builtin_amdgcn_sched_group_barrier(0x100, (T + 1) / 2, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
             uint32_t vis = ~0u;
             if (key0 + 32 > ctx) {                           // (wave-uniform: drafted keys, or the end)
                 vis = visible_keys(mask, a.mask_words, key0, ctx, len);
@@ -353,15 +352,23 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
             tree_pack<E>(w, wl, p, 0);
 #pragma unroll
             for (int c = 0; c < T; ++c) {
-                vb[c] = tree_v_frag(vh + 16 * ROWB + vx[2 * c], vh + 16 * ROWB + vx[2 * c + 1]);
                 o[c] = E::mfma32(va[c], w, o[c]);
                 o[c] = E::mfma32(va[c], wl, o[c]);
             }
+#pragma unroll
+            for (int c = 0; c < T; ++c) vb[c] = tree_v_frag(vh + 16 * ROWB + vx[2 * c], vh + 16 * ROWB + vx[2 * c + 1]);
             tree_pack<E>(w, wl, p, 8);
 #pragma unroll
             for (int c = 0; c < T; ++c) {
                 o[c] = E::mfma32(vb[c], w, o[c]);
                 o[c] = E::mfma32(vb[c], wl, o[c]);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+#pragma unroll
+            for (int c = 0; c < 2 * T; ++c) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x002, 32 / T, 1);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -471,8 +478,14 @@ __device__ __forceinline__ int64_t tree_tiles(const TreeKernelArgs& a, int lane,
 }
 
 template <int WR, typename E, int DP>
-__global__ __launch_bounds__((64 * TreeShape<WR, DP>::kWaves), (TreeShape<WR, DP>::kOcc * TreeShape<WR, DP>::kWaves / 4)) void paged_attention_tree_mfma_kernel(TreeKernelArgs a)
+__global__ __launch_bounds__((64 * TreeShape<WR, DP>::kWaves), (TreeShape<WR, DP>::kOcc * TreeShape<WR, DP>::kWaves / 4)) void paged_attention_tree_mfma_kernel(
+    TreeKernelArgs a, const int32_t* __restrict__ cu_q_lens, const int32_t* __restrict__ seq_lens,
+    const int32_t* __restrict__ block_table, const uint64_t* __restrict__ tree_mask)
 {
+    a.cu_q_lens = cu_q_lens;
+    a.seq_lens = seq_lens;
+    a.block_table = block_table;
+    a.tree_mask = tree_mask;
     constexpr int RB = 32 * WR;
     __shared__ __attribute__((aligned(1024))) char buf[TreeShape<WR, DP>::kBufs * TreeGeo<DP>::kBufB];
     __shared__ uint32_t flags[8];
@@ -545,8 +558,14 @@ constexpr int kTreeMergeRows = 8;
 constexpr int kTreeMaxPieces = 512;
 
 template <int WR, typename E, int DP>
-__global__ __launch_bounds__(256) void paged_attention_tree_merge_kernel(TreeKernelArgs a)
+__global__ __launch_bounds__(256) void paged_attention_tree_merge_kernel(
+    TreeKernelArgs a, const int32_t* __restrict__ cu_q_lens, const int32_t* __restrict__ seq_lens,
+    const int32_t* __restrict__ block_table, const uint64_t* __restrict__ tree_mask)
 {
+    a.cu_q_lens = cu_q_lens;
+    a.seq_lens = seq_lens;
+    a.block_table = block_table;
+    a.tree_mask = tree_mask;
     constexpr int RB = 32 * WR, CPR = DP / 4, PARTS = RB / kTreeMergeRows, RM = kTreeMergeRows;
     __shared__ float weight[kTreeMaxPieces * RM];
     __shared__ float sm_top[RM], sm_sum[RM];
@@ -617,13 +636,13 @@ pa_status launch_tree_of(const TreeKernelArgs& a, hipStream_t stream)
     {
         ProfileScope prof("paged_attention_tree_mfma_kernel", stream);
         hipLaunchKernelGGL((paged_attention_tree_mfma_kernel<WR, E, DP>), dim3((uint32_t)grid),
-                           dim3(64 * TreeShape<WR, DP>::kWaves), 0, stream, a);
+                           dim3(64 * TreeShape<WR, DP>::kWaves), 0, stream, a, a.cu_q_lens, a.seq_lens, a.block_table, a.tree_mask);
         const pa_status st = launch_status();
         if (st != PA_OK || a.wgs == 0) return st;
     }
     ProfileScope prof("paged_attention_tree_merge_kernel", stream);
     hipLaunchKernelGGL((paged_attention_tree_merge_kernel<WR, E, DP>), dim3((uint32_t)(units * PARTS), (uint32_t)a.cache.num_kv_heads),
-                       dim3(256), 0, stream, a);
+                       dim3(256), 0, stream, a, a.cu_q_lens, a.seq_lens, a.block_table, a.tree_mask);
     return launch_status();
 }
 
