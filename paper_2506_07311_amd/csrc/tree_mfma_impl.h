@@ -39,7 +39,7 @@ struct TreeKernelArgs {
     const int32_t* seq_lens;
     const uint64_t* tree_mask;
     const int32_t* block_table;
-    float* part_o;               // [KV head][workgroup][2][RB][DP], normalised
+    float* part_o;               // [KV head][workgroup][2][WR][DP / 8][lane][4], normalised
     float* part_lse;             // [KV head][workgroup][2][RB], log2 domain
     int32_t mask_words, batch, num_q_heads, max_blocks, group;
     int32_t wgs;                 // workgroups of a KV head that share the tiles; 0: one a (sequence, row block)
@@ -51,7 +51,10 @@ namespace {
 
 using namespace prefill;
 
-constexpr int32_t kTreeMinTiles = 4;   // fewest tiles of a workgroup that shares them
+constexpr int32_t kTreeMinTiles = 4;     // fewest tiles of a workgroup that shares them
+constexpr int32_t kTreePieceTiles = 4;   // what a piece of work costs besides its tiles, in tiles
+constexpr int32_t kTreeMaxChunk = 12;    // most tiles of a workgroup that has one piece of work
+constexpr int32_t kTreeMaxPieces = 256;  // workgroups that share a row block
 
 template <int DP>
 struct TreeGeo {
@@ -220,34 +223,13 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
     const int32_t* const table = a.block_table + (int64_t)it.s * a.max_blocks;
     const int32_t last_key = len - 1;
 
-    // Q as B operand: lane % 32 = row, step ks covers 8 elements of either lane half; 0 behind head_dim.  The scale that the scores
-    // get is positive, so that masking commutes with it: a negative one's sign goes to Q, and for a scale of 0 Q is 0.
-    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
-    const float sc = a.scale == 0.f ? 1.f : __builtin_fabsf(a.scale) * kLog2e;
+    // Q as B operand: lane % 32 = row, step ks covers 8 elements of either lane half; 0 behind head_dim
     const uint16_t* const qrow = a.q + ((int64_t)(it.row0 + qi) * a.num_q_heads + h) * d;
     uint4 qf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
         qf[ks] = uint4{0, 0, 0, 0};
-        if (16 * ks + 8 * hh < d && a.scale != 0.f) {
-            const uint4 v = *reinterpret_cast<const uint4*>(qrow + 16 * ks + 8 * hh);
-            qf[ks] = uint4{v.x ^ flip, v.y ^ flip, v.z ^ flip, v.w ^ flip};
-        }
-    }
-
-    // operand offsets: K piece 2 ks + hh of row ql; V pieces of the 32 columns t for the lane's transpose-load row, key 4 hh + j
-    // (and 8 on) of a 16-key step, columns 4 qq .. + 3 of the 16-column block dblk
-    uint32_t kx[KS], vx[2 * T];
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) kx[ks] = ql * ROWB + tree_piece<DP>(2 * ks + hh, ql);
-    {
-        const int j = (lane & 15) >> 2, qq = lane & 3, dblk = (lane >> 4) & 1;
-#pragma unroll
-        for (int t = 0; t < T; ++t) {
-            const int piece = 4 * t + 2 * dblk + (qq >> 1);
-            vx[2 * t] = (4 * hh + j) * ROWB + tree_piece<DP>(piece, 4 * hh + j) + 8 * (qq & 1);
-            vx[2 * t + 1] = (4 * hh + j + 8) * ROWB + tree_piece<DP>(piece, 4 * hh + j + 8) + 8 * (qq & 1);
-        }
+        if (16 * ks + 8 * hh < d) qf[ks] = *reinterpret_cast<const uint4*>(qrow + 16 * ks + 8 * hh);
     }
 
     // fetch role: instruction i of a wave fills rows RPI * (wave + NW i) .. of the tile, a lane the piece at position lane % PPR of
@@ -263,19 +245,19 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
         lane_off[v] = (uint32_t)(kvh * a.cache.head_stride * 2) + 16 * piece;
     }
     const uint32_t lds0 = lds_address(buf) + 1024 * wave;
-    int32_t pages[Shape::kLoads];                            // of the rows of each instruction (16 rows and more lie in one page)
-    auto load_pages = [&](int32_t t0) {
+    int32_t pages[NB - 1][Shape::kLoads];                    // of the rows of each instruction (16 rows and more lie in one page)
+    auto load_pages = [&](int b, int32_t t0) {
 #pragma unroll
         for (int i = 0; i < Shape::kLoads; ++i) {
             const int32_t key = __builtin_amdgcn_readfirstlane(t0 + RPI * wave + STEP * i);
-            pages[i] = table[min(key, last_key) >> a.cache.log2_page];
+            pages[b][i] = table[min(key, last_key) >> a.cache.log2_page];
         }
     };
-    auto fetch = [&](int b, int32_t t0) {
+    auto fetch = [&](int b, int p, int32_t t0) {
 #pragma unroll
         for (int i = 0; i < Shape::kLoads; ++i) {
             const int32_t slot = min(t0 + frow + STEP * i, last_key) & (a.cache.page_size - 1);
-            int64_t page_off = (int64_t)pages[i] * a.cache.page_stride * 2;
+            int64_t page_off = (int64_t)pages[p][i] * a.cache.page_stride * 2;
             asm volatile("" : "+s"(page_off));               // stays in scalar registers
             const uint32_t off = (uint32_t)slot * (uint32_t)(a.cache.token_stride * 2) + lane_off[STEP == 8 ? i & 1 : 0];
             load_to_lds16(lds0 + b * Geo::kBufB, 1024 * NW * i, reinterpret_cast<const char*>(a.cache.k) + page_off, off);
@@ -283,20 +265,54 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
         }
     };
 
+    // The first NB - 1 tiles (a piece of work has a tile at least), the page ids of all of them in one trip.  Q is waited for
+    // behind the first of them: what is issued between a load and its wait is waited for as well.
+#pragma unroll
+    for (int i = 0; i < NB - 1; ++i) load_pages(i, min(it.tile_begin + i, it.tile_end - 1) * kBN);
+    fetch(0, 0, it.tile_begin * kBN);
+    // operand offsets: K piece 2 ks + hh of row ql; V pieces of the 32 columns t for the lane's transpose-load row, key 4 hh + j
+    // (and 8 on) of a 16-key step, columns 4 qq .. + 3 of the 16-column block dblk
+    uint32_t kx[KS], vx[2 * T];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) kx[ks] = ql * ROWB + tree_piece<DP>(2 * ks + hh, ql);
+    {
+        const int j = (lane & 15) >> 2, qq = lane & 3, dblk = (lane >> 4) & 1;
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            const int piece = 4 * t + 2 * dblk + (qq >> 1);
+            vx[2 * t] = (4 * hh + j) * ROWB + tree_piece<DP>(piece, 4 * hh + j) + 8 * (qq & 1);
+            vx[2 * t + 1] = (4 * hh + j + 8) * ROWB + tree_piece<DP>(piece, 4 * hh + j + 8) + 8 * (qq & 1);
+        }
+    }
+    // The scale that the scores get is positive, so that masking commutes with it: a negative one's sign goes to Q, and for a scale of 0
+    // Q is 0.
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u, hold = a.scale == 0.f ? 0u : ~0u;
+    const float sc = a.scale == 0.f ? 1.f : __builtin_fabsf(a.scale) * kLog2e;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+        qf[ks] = uint4{(qf[ks].x ^ flip) & hold, (qf[ks].y ^ flip) & hold, (qf[ks].z ^ flip) & hold, (qf[ks].w ^ flip) & hold};
+    int32_t ahead = it.tile_begin + 1;                       // the tile to fetch next
+#pragma unroll
+    for (int i = 1; i < NB - 1; ++i) {
+        if (ahead < it.tile_end) fetch(i, i, ahead++ * kBN);
+    }
+    if (ahead < it.tile_end) load_pages(0, ahead * kBN);
+
     f32x16 o[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) o[t] = (f32x16)(0.f);
     float m = -INFINITY, l = 0.f;
 
-    // NB - 1 tiles ahead (a piece of work has a tile at least); the page ids of the tile that is fetched next are loaded a tile before
-    int32_t ahead = it.tile_begin;                           // the tile to fetch next
-    load_pages(ahead * kBN);
-#pragma unroll 1
-    for (int i = 0; i < NB - 1 && ahead < it.tile_end; ++i) {
-        fetch(i, ahead * kBN);
-        if (++ahead < it.tile_end) load_pages(ahead * kBN);
-    }
     int b = 0;
+    // With eight waves two share a SIMD, and the load unit takes a third of a tile's time for its instructions: the second
+    // four waves issue theirs behind their products, so that either half has the unit and the matrix cores in turn.
+    const bool late = NW == 8 && wave >= 4;
+    auto issue = [&]() {
+        if (ahead < it.tile_end) {
+            fetch(b == 0 ? NB - 1 : b - 1, 0, ahead * kBN);
+            if (++ahead < it.tile_end) load_pages(0, ahead * kBN);   // (a tile before they are needed)
+        }
+    };
 #pragma unroll 1
     for (int32_t t = it.tile_begin; t < it.tile_end; ++t) {
         const int32_t after = ahead - t - 1;                 // tiles in flight behind this one
@@ -305,10 +321,7 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
         else if (after >= SOME) wait_tiles_but<Shape::kLoads, SOME>();
         else wait_tiles_but<Shape::kLoads, 0>();
         __syncthreads();                                     // tile t is there, and tile t - 1 done with
-        if (ahead < it.tile_end) {
-            fetch(b == 0 ? NB - 1 : b - 1, ahead * kBN);
-            if (++ahead < it.tile_end) load_pages(ahead * kBN);
-        }
+        if (!late) issue();
         const char* const kbuf = buf + b * Geo::kBufB;
 #pragma unroll 1
         for (int i = 0; i < HALVES; ++i) {
@@ -372,6 +385,7 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
             }
             __builtin_amdgcn_sched_barrier(0);
         }
+        if (late) issue();
         b = b == NB - 1 ? 0 : b + 1;
     }
 
@@ -419,19 +433,19 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
         __syncthreads();                                     // (before the next piece of work loads over them)
         if (kw == 1) return false;
     }
-    if (r_lane >= n_rows) return false;
+    if (!live) return false;
     const float inv = l > 0.f ? 1.f / l : 0.f;               // (a NaN among the scores is in O as well)
     const float lse2 = l <= 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l);
-    if (it.slot >= 0) {
-        const int64_t row = it.slot * RB + 32 * rw + ql;
-        float* const po = a.part_o + row * DP;
+    if (it.slot >= 0) {                                      // a partial, lane by lane: whole lines a store
+        float4* const po = reinterpret_cast<float4*>(a.part_o) + (it.slot * WR + rw) * (4 * T * 64) + lane;
 #pragma unroll
         for (int i = 0; i < 4 * T; ++i)
-            *reinterpret_cast<float4*>(po + 8 * i + 4 * hh) = float4{o[i / 4][4 * (i % 4)] * inv, o[i / 4][4 * (i % 4) + 1] * inv,
-                                                                     o[i / 4][4 * (i % 4) + 2] * inv, o[i / 4][4 * (i % 4) + 3] * inv};
-        if (hh == 0) a.part_lse[row] = lse2;
+            po[i * 64] = float4{o[i / 4][4 * (i % 4)] * inv, o[i / 4][4 * (i % 4) + 1] * inv, o[i / 4][4 * (i % 4) + 2] * inv,
+                                o[i / 4][4 * (i % 4) + 3] * inv};
+        if (hh == 0) a.part_lse[it.slot * RB + 32 * rw + ql] = lse2;
         return false;
     }
+    if (r_lane >= n_rows) return false;
     const int64_t row = (int64_t)(it.row0 + qi) * a.num_q_heads + h;
     uint16_t* const orow = a.out + row * d;
 #pragma unroll
@@ -463,18 +477,35 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeKernelArgs& a, int32_t i)
     return q;
 }
 
-// All key tiles of the call (one KV head), and the workgroups that share them.
+// How a KV head's workgroups share the call's key tiles.  Where they are few, every row block is cut into chunks of about `chunk`
+// tiles, one a workgroup.  Otherwise (chunk == 0) all tiles stand in a row, each row block's behind kTreePieceTiles places for what a
+// piece of work costs besides its tiles, and workgroup x of wgs takes places [x all / wgs, (x + 1) all / wgs).
+struct TreeShare {
+    int64_t all;
+    int32_t wgs, chunk;
+};
 template <int RB>
-__device__ __forceinline__ int64_t tree_tiles(const TreeKernelArgs& a, int lane, int64_t& wgs)
+__device__ __forceinline__ TreeShare tree_share(const TreeKernelArgs& a, int lane)
 {
-    int64_t all = 0;
+    int64_t tiles = 0, blocks = 0;
     for (int32_t i0 = 0; i0 < a.batch; i0 += 64) {
         const TreeSeq q = tree_seq<RB>(a, i0 + lane);
-        all += wave_total_moves(q.blocks * q.tiles);
+        tiles += wave_total_moves(q.blocks * q.tiles);
+        blocks += wave_total_moves(q.blocks);
     }
-    wgs = all / kTreeMinTiles;
-    wgs = wgs > a.wgs ? a.wgs : wgs < 1 ? 1 : wgs;
-    return all;
+    TreeShare r = {tiles + kTreePieceTiles * blocks, 1, 0};
+    if (blocks < a.wgs) {
+        const int64_t c = (tiles + a.wgs - blocks - 1) / (a.wgs - blocks);
+        if (c <= kTreeMaxChunk) r.chunk = (int32_t)(c < kTreeMinTiles ? kTreeMinTiles : c);
+    }
+    const int64_t n = r.all / (kTreeMinTiles + kTreePieceTiles);
+    r.wgs = n > a.wgs ? a.wgs : n < 1 ? 1 : (int32_t)n;
+    return r;
+}
+// Places of a row block of the sequence: chunks, or tiles and what comes before them.
+__device__ __forceinline__ int32_t tree_places(const TreeShare& r, const TreeSeq& q)
+{
+    return q.blocks == 0 ? 0 : r.chunk > 0 ? (q.tiles + r.chunk - 1) / r.chunk : q.tiles + kTreePieceTiles;
 }
 
 template <int WR, typename E, int DP>
@@ -492,127 +523,153 @@ __global__ __launch_bounds__((64 * TreeShape<WR, DP>::kWaves), (TreeShape<WR, DP
     const int lane = threadIdx.x & 63;
     const int32_t hkv = a.cache.num_kv_heads;
     const int32_t kvh = (int32_t)(blockIdx.x % (uint32_t)hkv), x = (int32_t)(blockIdx.x / (uint32_t)hkv);
-    // what is shared by the whole call: tiles [t, t_end) of all sequences' row blocks in a row, or one row block's
-    int32_t s = 0, rb = 0;
+    // this workgroup's places [t, t_end), the sequence of the first and that one's first place
+    int32_t s = 0;
     int64_t t = 0, t_end = 1, first = 0;
-    if (a.wgs == 0) {
+    TreeShare share = {0, 0, 0};
+    TreeSeq q = {0, 0, 0, 0, 0};
+    if (a.wgs == 0) {                                        // one row block
         s = x / a.row_blocks;
-        rb = x % a.row_blocks;
+        q = tree_seq<RB>(a, s);
+        if (x % a.row_blocks >= q.blocks || q.tiles <= 0) return;
     } else {
-        int64_t wgs;
-        const int64_t all = tree_tiles<RB>(a, lane, wgs);
-        if (x >= wgs) return;
-        t = (int64_t)x * all / wgs;
-        t_end = (int64_t)(x + 1) * all / wgs;
-        // the sequence of tile t and its first tile
+        share = tree_share<RB>(a, lane);
+        if (share.chunk > 0) {
+            t = x;
+            t_end = t + 1;
+        } else {
+            if (x >= share.wgs) return;
+            t = (int64_t)x * share.all / share.wgs;
+            t_end = (int64_t)(x + 1) * share.all / share.wgs;
+        }
+        bool found = false;
         for (int32_t i0 = 0; i0 < a.batch; i0 += 64) {
-            const TreeSeq q = tree_seq<RB>(a, i0 + lane);
-            const int32_t mine = q.blocks * q.tiles, inc = wave_scan_moves(mine);
+            const TreeSeq own = tree_seq<RB>(a, i0 + lane);
+            const int32_t mine = own.blocks * tree_places(share, own), inc = wave_scan_moves(mine);
             const uint64_t hit = __ballot(first + inc > t);
             if (hit) {
                 const int f = __ffsll((unsigned long long)hit) - 1;
                 s = i0 + f;
                 first += __builtin_amdgcn_readlane(inc, f) - __builtin_amdgcn_readlane(mine, f);
+                q.row0 = __builtin_amdgcn_readlane(own.row0, f);
+                q.n = __builtin_amdgcn_readlane(own.n, f);
+                q.len = __builtin_amdgcn_readlane(own.len, f);
+                q.blocks = __builtin_amdgcn_readlane(own.blocks, f);
+                q.tiles = __builtin_amdgcn_readlane(own.tiles, f);
+                found = true;
                 break;
             }
             first += __builtin_amdgcn_readlane(inc, 63);
         }
+        if (!found) return;
     }
     while (t < t_end) {
-        const TreeSeq q = tree_seq<RB>(a, s);
         TreeItem it;
         it.s = s;
         it.row0 = q.row0;
         it.n = q.n;
         it.len = q.len;
         if (a.wgs == 0) {
-            if (rb >= q.blocks || q.tiles <= 0) return;
-            it.rb = rb;
+            it.rb = x % a.row_blocks;
             it.tile_begin = 0;
             it.tile_end = q.tiles;
             it.slot = -1;
             t = t_end;
         } else {
-            const int32_t mine = q.blocks * q.tiles;
-            if (t >= first + mine) {                         // (nothing, or nothing more, of this one)
-                first += mine;
+            const int32_t places = tree_places(share, q);
+            if (t >= first + (int64_t)q.blocks * places) {   // (nothing, or nothing more, of this one)
+                first += (int64_t)q.blocks * places;
                 if (++s >= a.batch) return;
+                q = tree_seq<RB>(a, s);
                 continue;
             }
-            const int32_t at = (int32_t)(t - first);
-            it.rb = at / q.tiles;
-            it.tile_begin = at % q.tiles;
-            it.tile_end = (int32_t)min((int64_t)q.tiles, it.tile_begin + (t_end - t));
+            const int32_t at = (int32_t)((t - first) % places);
+            it.rb = (int32_t)((t - first) / places);
+            if (share.chunk > 0) {
+                it.tile_begin = (int32_t)((int64_t)at * q.tiles / places);
+                it.tile_end = (int32_t)((int64_t)(at + 1) * q.tiles / places);
+                t = t_end;
+            } else {
+                const int32_t to = (int32_t)min((int64_t)places, at + (t_end - t));
+                it.tile_begin = max(at - kTreePieceTiles, 0);
+                it.tile_end = max(to - kTreePieceTiles, 0);
+                t += to - at;
+            }
             const bool whole = it.tile_begin == 0 && it.tile_end == q.tiles;
             it.slot = whole ? -1 : ((int64_t)kvh * a.wgs + x) * 2 + (it.tile_begin == 0 ? 1 : 0);
-            t += it.tile_end - it.tile_begin;
+            if (it.tile_begin == it.tile_end) continue;      // (places before the tiles alone)
         }
         if (tree_piece_of_work<WR, false, E, DP>(buf, flags, a, it, kvh)) tree_piece_of_work<WR, true, E, DP>(buf, flags, a, it, kvh);
     }
 }
 
-// The pieces of a row block that workgroups' ends cut, merged by their log-sum-exps.  Grid (sequences x row blocks x RB / 8, KV
-// heads): 8 rows each (a call of few sequences still spreads over the machine).  Statistics first, all at once, and their weights
-// into LDS; then a thread's columns, with the loads of four pieces in flight.
-constexpr int kTreeMergeRows = 8;
-constexpr int kTreeMaxPieces = 512;
+// The pieces of a row block that were cut, merged by their log-sum-exps.  Grid (sequences x row blocks x WR x kTreeMergeParts, KV
+// heads): 32 rows and a part of their columns each, in the partials' own order, so that a call of few sequences spreads over the
+// machine as well.  Statistics first, all at once, and their weights into LDS; then a thread's four columns, the loads of
+// four pieces in flight.
+constexpr int kTreeMergeParts = 4;
 
 template <int WR, typename E, int DP>
 __global__ __launch_bounds__(256) void paged_attention_tree_merge_kernel(
-    TreeKernelArgs a, const int32_t* __restrict__ cu_q_lens, const int32_t* __restrict__ seq_lens,
-    const int32_t* __restrict__ block_table, const uint64_t* __restrict__ tree_mask)
+    TreeKernelArgs a, const int32_t* __restrict__ cu_q_lens, const int32_t* __restrict__ seq_lens)
 {
     a.cu_q_lens = cu_q_lens;
     a.seq_lens = seq_lens;
-    a.block_table = block_table;
-    a.tree_mask = tree_mask;
-    constexpr int RB = 32 * WR, CPR = DP / 4, PARTS = RB / kTreeMergeRows, RM = kTreeMergeRows;
-    __shared__ float weight[kTreeMaxPieces * RM];
-    __shared__ float sm_top[RM], sm_sum[RM];
+    constexpr int RB = 32 * WR, T = DP / 32, PIECES = 4 * T / kTreeMergeParts;
+    extern __shared__ float weight[];                        // [pieces][32]
+    __shared__ float sm_top[32], sm_sum[32];
     const int lane = threadIdx.x & 63;
-    const int32_t kvh = blockIdx.y, r0 = RM * (int32_t)(blockIdx.x % PARTS);
-    const int32_t u = (int32_t)(blockIdx.x / PARTS), s = u / a.row_blocks, rb = u % a.row_blocks;
+    const int32_t kvh = blockIdx.y, part = (int32_t)(blockIdx.x % kTreeMergeParts);
+    const int32_t rw = (int32_t)(blockIdx.x / kTreeMergeParts) % WR;
+    const int32_t u = (int32_t)(blockIdx.x / (kTreeMergeParts * WR)), s = u / a.row_blocks, rb = u % a.row_blocks;
     const TreeSeq own = tree_seq<RB>(a, s);
-    if (rb >= own.blocks || rb * RB + r0 >= own.n * a.group || own.tiles <= 0) return;
-    int64_t wgs, first = 0;
-    const int64_t all = tree_tiles<RB>(a, lane, wgs);
+    const int32_t n_rows = own.n * a.group, r0 = rb * RB + 32 * rw, d = a.cache.head_dim;
+    if (rb >= own.blocks || r0 >= n_rows || own.tiles <= 0) return;
+    const TreeShare share = tree_share<RB>(a, lane);
+    int64_t first = 0;
     for (int32_t i0 = 0; i0 < s; i0 += 64) {
         const TreeSeq q = tree_seq<RB>(a, i0 + lane);
-        first += wave_total_moves(i0 + lane < s ? q.blocks * q.tiles : 0);
+        first += wave_total_moves(i0 + lane < s ? q.blocks * tree_places(share, q) : 0);
     }
-    const int64_t begin = first + (int64_t)rb * own.tiles, end = begin + own.tiles;
-    const int64_t w_first = ((begin + 1) * wgs - 1) / all, w_last = (end * wgs - 1) / all;   // workgroups of its first and last tile
+    const int32_t places = tree_places(share, own);
+    const int64_t begin = first + (int64_t)rb * places, end = begin + places;
+    int64_t w_first = begin, w_last = end - 1;               // workgroups of its first and last tile
+    if (share.chunk == 0) {
+        w_first = ((begin + kTreePieceTiles + 1) * share.wgs - 1) / share.all;
+        w_last = (end * share.wgs - 1) / share.all;
+    }
     if (w_first == w_last) return;
-    const int32_t pieces = (int32_t)(w_last - w_first) + 1, n_rows = own.n * a.group, d = a.cache.head_dim;
+    const int32_t pieces = (int32_t)(w_last - w_first) + 1;
     const int64_t slot0 = ((int64_t)kvh * a.wgs + w_first) * 2;
-    auto row_of = [&](int32_t k, int32_t row) { return (slot0 + 2 * (int64_t)k + (k == 0 ? 1 : 0)) * RB + row; };
-    for (int32_t i = threadIdx.x; i < pieces * RM; i += 256) weight[i] = a.part_lse[row_of(i / RM, r0 + i % RM)];
+    auto slot = [&](int32_t k) { return slot0 + 2 * (int64_t)k + (k == 0 ? 1 : 0); };
+    for (int32_t i = threadIdx.x; i < pieces * 32; i += 256) weight[i] = a.part_lse[slot(i >> 5) * RB + 32 * rw + (i & 31)];
     __syncthreads();
-    if (threadIdx.x < RM) {
+    if (threadIdx.x < 32) {
         float top = -INFINITY, sum = 0.f;
-        for (int32_t k = 0; k < pieces; ++k) top = fmaxf(top, weight[k * RM + threadIdx.x]);
+        for (int32_t k = 0; k < pieces; ++k) top = fmaxf(top, weight[k * 32 + threadIdx.x]);
         const float use = top == -INFINITY ? 0.f : top;
         for (int32_t k = 0; k < pieces; ++k) {
-            const float w = __builtin_amdgcn_exp2f(weight[k * RM + threadIdx.x] - use);
-            weight[k * RM + threadIdx.x] = w;
+            const float w = __builtin_amdgcn_exp2f(weight[k * 32 + threadIdx.x] - use);
+            weight[k * 32 + threadIdx.x] = w;
             sum += w;
         }
         sm_top[threadIdx.x] = top;
         sm_sum[threadIdx.x] = sum;
     }
     __syncthreads();
-    for (int32_t i = threadIdx.x; i < RM * CPR; i += 256) {
-        const int32_t row = i / CPR, c = 4 * (i % CPR), r = rb * RB + r0 + row;
+    for (int32_t i = threadIdx.x; i < PIECES * 64; i += 256) {
+        const int32_t j = part * PIECES * 64 + i, row = j & 31, c = 8 * (j >> 6) + 4 * ((j >> 5) & 1), r = r0 + row;
         if (r >= n_rows || c >= d) continue;
+        const float4* const po = reinterpret_cast<const float4*>(a.part_o) + rw * (4 * T * 64) + j;
         float4 acc = {0.f, 0.f, 0.f, 0.f};
         for (int32_t k0 = 0; k0 < pieces; k0 += 4) {
             float4 v[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const float4*>(a.part_o + row_of(min(k0 + k, pieces - 1), r0 + row) * DP + c);
+            for (int k = 0; k < 4; ++k) v[k] = po[slot(min(k0 + k, pieces - 1)) * (WR * 4 * T * 64)];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 if (k0 + k >= pieces) break;
-                const float w = weight[(k0 + k) * RM + row];
+                const float w = weight[(k0 + k) * 32 + row];
                 acc.x = __builtin_fmaf(w, v[k].x, acc.x);
                 acc.y = __builtin_fmaf(w, v[k].y, acc.y);
                 acc.z = __builtin_fmaf(w, v[k].z, acc.z);
@@ -631,7 +688,7 @@ pa_status launch_tree_of(const TreeKernelArgs& a, hipStream_t stream)
 {
     const int64_t units = (int64_t)a.batch * a.row_blocks;
     const int64_t grid = (a.wgs > 0 ? a.wgs : units) * a.cache.num_kv_heads;
-    constexpr int PARTS = 32 * WR / kTreeMergeRows;
+    constexpr int PARTS = WR * kTreeMergeParts;
     if (grid > 0x7fffffffLL || units * PARTS > 0x7fffffffLL || a.cache.num_kv_heads > 65535) return PA_ERR_UNSUPPORTED;
     {
         ProfileScope prof("paged_attention_tree_mfma_kernel", stream);
@@ -642,7 +699,7 @@ pa_status launch_tree_of(const TreeKernelArgs& a, hipStream_t stream)
     }
     ProfileScope prof("paged_attention_tree_merge_kernel", stream);
     hipLaunchKernelGGL((paged_attention_tree_merge_kernel<WR, E, DP>), dim3((uint32_t)(units * PARTS), (uint32_t)a.cache.num_kv_heads),
-                       dim3(256), 0, stream, a, a.cu_q_lens, a.seq_lens, a.block_table, a.tree_mask);
+                       dim3(256), (size_t)a.wgs * 32 * sizeof(float), stream, a, a.cu_q_lens, a.seq_lens);
     return launch_status();
 }
 
