@@ -16,11 +16,12 @@ LIB = os.path.join(HERE, "libpagedattn.so")
 SOURCES = ["api.hip", "kv_copy.hip", "attention_generic.hip", "attention_f32.hip", "merge.hip", "decode_mfma.hip", "decode_mfma_d64.hip",
            "decode_mfma_d256.hip", "prefill_mfma.hip", "prefill_mfma_d64.hip", "prefill_mfma_d256.hip",
            "prefill_mfma_odd.hip", "jagged_mfma.hip", "page_pool.hip", "step_api.hip", "step_plan.hip",
-           "rope_append.hip", "tree_generic.hip", "tree_mfma.hip", "tree_mfma_d64.hip", "tree_mfma_d96.hip", "tree_mfma_d256.hip"]
+           "rope_append.hip", "tree_generic.hip", "tree_mfma.hip", "tree_mfma_d64.hip", "tree_mfma_d96.hip", "tree_mfma_d256.hip",
+           "tree_f32.hip"]
 HEADERS = [os.path.join(CSRC, "common.h"), os.path.join(CSRC, "prefill_tiles.h"),
            os.path.join(CSRC, "decode_mfma_impl.h"), os.path.join(CSRC, "prefill_mfma_impl.h"),
            os.path.join(HERE, "..", "include", "pagedattn.h"), os.path.join(HERE, "..", "include", "pagedattn_mods.h")]
-TREE_HEADER = os.path.join(CSRC, "tree_mfma_impl.h")
+TREE_HEADERS = [os.path.join(CSRC, "tree_share.h"), os.path.join(CSRC, "tree_mfma_impl.h")]
 # packed-fp32 VALU forms are disabled on purpose (they have produced wrong results on these machines)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang",
          "-packed-fp32-ops", "-Wall", "-Wno-unused-function", "-Wno-unknown-warning-option"]
@@ -36,7 +37,7 @@ def _hipcc() -> str:
 def _compile(src: str, force: bool) -> str:
     obj = os.path.join(OBJ, src.replace(".hip", ".o"))
     path = os.path.join(CSRC, src)
-    deps = [path] + HEADERS + ([TREE_HEADER] if src.startswith("tree_mfma") else [])
+    deps = [path] + HEADERS + (TREE_HEADERS if src.startswith("tree_") else [])
     if not force and os.path.exists(obj) and os.path.getmtime(obj) >= max(os.path.getmtime(p) for p in deps):
         return obj
     cmd = [_hipcc(), *FLAGS, "-c", path, "-o", obj]

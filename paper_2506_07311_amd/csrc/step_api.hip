@@ -116,9 +116,12 @@ size_t paged_attention_tree_workspace_bytes(int32_t batch, int32_t num_q_heads, 
     if (batch <= 0 || num_kv_heads <= 0 || num_q_heads < num_kv_heads || head_dim <= 0 || total_q <= 0 || max_q_len < 0 ||
         max_seq_len < 0)
         return 256;
-    const TreePlan p = plan_tree(batch, num_q_heads, num_kv_heads, head_dim, max_q_len, max_seq_len);
-    const size_t bytes = p.part_o_bytes + p.part_lse_bytes;
-    return bytes > 0 ? bytes : 256;
+    size_t most = 256;                                       // (the type is not known here)
+    for (const bool f32 : {false, true}) {
+        const TreePlan p = plan_tree(batch, num_q_heads, num_kv_heads, head_dim, max_q_len, max_seq_len, f32);
+        if (p.part_o_bytes + p.part_lse_bytes > most) most = p.part_o_bytes + p.part_lse_bytes;
+    }
+    return most;
 }
 
 pa_status paged_attention_tree(const pa_kv_cache_desc* cache, const void* q, void* out, float* lse,

@@ -11,37 +11,41 @@ pa_status launch_tree_d128(const TreeKernelArgs& a, pa_dtype dtype, int row_wave
 pa_status launch_tree_d96(const TreeKernelArgs& a, pa_dtype dtype, int row_waves, hipStream_t stream);
 pa_status launch_tree_d64(const TreeKernelArgs& a, pa_dtype dtype, int row_waves, hipStream_t stream);
 
+pa_status launch_tree_f32(const TreeKernelArgs& a, int row_waves, hipStream_t stream);
+
 namespace {
 
-int32_t columns_of(int32_t d) { return d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : 256; }
+int32_t columns_of(int32_t d, bool f32) { return d <= 64 ? 64 : d <= 96 && !f32 ? 96 : d <= 128 ? 128 : 256; }
 
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 }  // namespace
 
-// Up to 64 rows a (sequence, KV head) two waves share 32 rows, up to 128 at head_dims up to 128 as well, with eight waves; beyond
-// that a workgroup takes 256 rows (128 above head_dim 128, where a wave's O and Q fill its registers).  The tiles are shared by
-// as many workgroups as the machine holds at once; on contexts of up to kPlainTiles tiles a row block is one workgroup's
-// and there is no merge.
-TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t max_q_len, int32_t max_seq_len)
+// 16-bit pools: up to 64 rows a (sequence, KV head) two waves share 32 rows, up to 128 at head_dims up to 128 as well, with eight
+// waves; beyond that a workgroup takes 256 rows (128 above head_dim 128, where a wave's O and Q fill its registers).  fp32 pools: 16 rows a
+// wave, 16, 32 or 64 a workgroup.  The tiles are shared by as many workgroups as the machine holds at once; on contexts of
+// up to kPlainTiles tiles a row block is one workgroup's and there is no merge.
+TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t max_q_len, int32_t max_seq_len, bool f32)
 {
     constexpr int32_t kPlainTiles = 8;
     TreePlan p;
     const int64_t rows = (int64_t)max_q_len * (num_q_heads / num_kv_heads);
-    const int32_t columns = columns_of(head_dim);
-    p.row_waves = rows <= 64 ? 2 : rows <= 128 || columns > 128 ? 4 : 8;
-    const int64_t blocks = (rows + 32 * p.row_waves - 1) / (32 * p.row_waves);
+    const int32_t columns = columns_of(head_dim, f32), wave_rows = f32 ? 16 : 32;
+    if (f32) p.row_waves = rows <= 16 && columns <= 128 ? 1 : rows <= 32 ? 2 : 4;
+    else p.row_waves = rows <= 64 ? 2 : rows <= 128 || columns > 128 ? 4 : 8;
+    const int64_t blocks = (rows + wave_rows * p.row_waves - 1) / (wave_rows * p.row_waves);
     p.row_blocks = blocks < 1 ? 1 : (int32_t)blocks;
-    const int64_t tiles = ((int64_t)max_seq_len + prefill::kBN - 1) / prefill::kBN;
+    const int32_t tile = f32 && columns > 128 ? 32 : prefill::kBN;
+    const int64_t tiles = ((int64_t)max_seq_len + tile - 1) / tile;
     p.wgs = 0;
     p.part_o_bytes = p.part_lse_bytes = 0;
     if (tiles > kPlainTiles) {
-        const int64_t slots = (int64_t)device_cus() * (columns == 64 && p.row_waves == 2 ? 2 : 1);
+        const int64_t slots = (int64_t)device_cus() * (columns == 64 && p.row_waves == 2 && !f32 ? 2 : 1);
         const int64_t most = (batch * blocks * tiles + 3) / 4;
         int64_t wgs = slots / num_kv_heads;
         if (wgs > most) wgs = most;
         p.wgs = wgs < 1 ? 1 : wgs > kTreeMaxPieces ? kTreeMaxPieces : (int32_t)wgs;
-        const size_t part_rows = (size_t)p.wgs * num_kv_heads * 2 * 32 * p.row_waves;
+        const size_t part_rows = (size_t)p.wgs * num_kv_heads * 2 * wave_rows * p.row_waves;
         p.part_o_bytes = align256(part_rows * columns * sizeof(float));
         p.part_lse_bytes = align256(part_rows * sizeof(float));
     }
@@ -50,16 +54,17 @@ TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int
 
 bool tree_mfma_supported(const TreeArgs& a)
 {
-    return a.dtype != PA_DTYPE_F32 && a.cache.page_size >= 16;
+    return a.cache.page_size >= 16;
 }
 
 pa_status launch_tree_mfma(const TreeArgs& t, void* workspace, hipStream_t stream)
 {
-    const TreePlan p = plan_tree(t.batch, t.num_q_heads, t.cache.num_kv_heads, t.cache.head_dim, t.max_q_len, t.max_seq_len);
+    const TreePlan p = plan_tree(t.batch, t.num_q_heads, t.cache.num_kv_heads, t.cache.head_dim, t.max_q_len, t.max_seq_len,
+                                 t.dtype == PA_DTYPE_F32);
     TreeKernelArgs a;
     a.cache = t.cache;
-    a.q = (const uint16_t*)t.q;
-    a.out = (uint16_t*)t.out;
+    a.q = t.q;
+    a.out = t.out;
     a.lse = t.lse;
     a.cu_q_lens = t.cu_q_lens;
     a.seq_lens = t.seq_lens;
@@ -75,7 +80,8 @@ pa_status launch_tree_mfma(const TreeArgs& t, void* workspace, hipStream_t strea
     a.wgs = p.wgs;
     a.row_blocks = p.row_blocks;
     a.scale = t.scale;
-    switch (columns_of(t.cache.head_dim)) {
+    if (t.dtype == PA_DTYPE_F32) return launch_tree_f32(a, p.row_waves, stream);
+    switch (columns_of(t.cache.head_dim, false)) {
         case 64: return launch_tree_d64(a, t.dtype, p.row_waves, stream);
         case 96: return launch_tree_d96(a, t.dtype, p.row_waves, stream);
         case 128: return launch_tree_d128(a, t.dtype, p.row_waves, stream);

@@ -24,37 +24,11 @@
 //     a workgroup takes a whole row block and there is no second launch.
 #pragma once
 
-#include "prefill_tiles.h"
+#include "tree_share.h"
 
 namespace pa {
 
-struct TreeKernelArgs {
-    CacheView cache;
-    const uint16_t* q;
-    uint16_t* out;
-    float* lse;
-    // (kernel arguments of their own: the compiler has to know that nothing else points there, or page ids come by vector loads,
-    // and each wait for one is a wait for every tile in flight: 16 x 16 tokens on 131072 2512 us)
-    const int32_t* cu_q_lens;
-    const int32_t* seq_lens;
-    const uint64_t* tree_mask;
-    const int32_t* block_table;
-    float* part_o;               // [KV head][workgroup][2][WR][DP / 8][lane][4], normalised
-    float* part_lse;             // [KV head][workgroup][2][RB], log2 domain
-    int32_t mask_words, batch, num_q_heads, max_blocks, group;
-    int32_t wgs;                 // workgroups of a KV head that share the tiles; 0: one a (sequence, row block)
-    int32_t row_blocks;          // most row blocks of a sequence
-    float scale;
-};
-
 namespace {
-
-using namespace prefill;
-
-constexpr int32_t kTreeMinTiles = 4;     // fewest tiles of a workgroup that shares them
-constexpr int32_t kTreePieceTiles = 4;   // what a piece of work costs besides its tiles, in tiles
-constexpr int32_t kTreeMaxChunk = 12;    // most tiles of a workgroup that has one piece of work
-constexpr int32_t kTreeMaxPieces = 256;  // workgroups that share a row block
 
 template <int DP>
 struct TreeGeo {
@@ -76,16 +50,6 @@ struct TreeShape {
     static constexpr int kLoads = TreeGeo<DP>::kTileB / (1024 * kWaves); // load instructions of a wave and pool a tile
 };
 
-// This wave's loads to LDS have landed but for the last N tiles' (LOADS of either pool each).  In order, so what the compiler
-// has issued in between makes it wait for more, not for less.
-template <int LOADS, int N>
-__device__ __forceinline__ void wait_tiles_but()
-{
-    constexpr int V = 2 * LOADS * N;
-    static_assert(V < 64, "more loads than the counter holds");
-    __builtin_amdgcn_s_waitcnt(0x0F70 | (V & 15) | ((V >> 4) << 14));   // vmcnt: bits 3..0 and 15..14
-}
-
 // Byte offset inside its LDS row r of logical 16-byte piece L (rows of 512 bytes swizzle each half by itself; of rows of
 // 128 bytes two share the banks).
 template <int DP>
@@ -105,26 +69,6 @@ __device__ __forceinline__ uint4 tree_v_frag(const char* lo, const char* hi)
     r.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lo));
     r.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(hi));
     return __builtin_bit_cast(uint4, r);
-}
-
-// A row's view of 32 keys from key0 on: bit i = key key0 + i is visible.
-__device__ __forceinline__ uint32_t visible_keys(const uint64_t* __restrict__ mask, int32_t words, int32_t key0, int32_t ctx,
-                                                 int32_t len)
-{
-    const int32_t node = key0 - ctx;
-    uint32_t bits;
-    if (node <= -32) {
-        bits = ~0u;
-    } else if (node < 0) {
-        bits = ((uint32_t)mask[0] << -node) | ((1u << -node) - 1u);
-    } else {
-        const int32_t w = node >> 6, sh = node & 63;
-        const uint64_t lo = w < words ? mask[w] >> sh : 0;
-        const uint64_t hi = sh && w + 1 < words ? mask[w + 1] << (64 - sh) : 0;
-        bits = (uint32_t)(lo | hi);
-    }
-    const int32_t left = len - key0;
-    return left >= 32 ? bits : left <= 0 ? 0u : bits & ((1u << left) - 1u);
 }
 
 template <typename E>
@@ -195,12 +139,6 @@ __device__ __forceinline__ void tree_pv_by_key(f32x16 (&o)[T], f32x16 p, const c
     }
 }
 
-// A workgroup's piece of work: key tiles [tile_begin, tile_end) of row block rb of sequence s.
-struct TreeItem {
-    int32_t s, rb, row0, n, len, tile_begin, tile_end;
-    int64_t slot;                // >= 0: a partial
-};
-
 // Returns whether it has to be done again with CAREFUL (the same on every thread).
 template <int WR, bool CAREFUL, typename E, int DP>
 __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, const TreeKernelArgs& a, const TreeItem& it, int32_t kvh)
@@ -224,7 +162,7 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
     const int32_t last_key = len - 1;
 
     // Q as B operand: lane % 32 = row, step ks covers 8 elements of either lane half; 0 behind head_dim
-    const uint16_t* const qrow = a.q + ((int64_t)(it.row0 + qi) * a.num_q_heads + h) * d;
+    const uint16_t* const qrow = static_cast<const uint16_t*>(a.q) + ((int64_t)(it.row0 + qi) * a.num_q_heads + h) * d;
     uint4 qf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
@@ -304,15 +242,6 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
     float m = -INFINITY, l = 0.f;
 
     int b = 0;
-    // With eight waves two share a SIMD, and the load unit takes a third of a tile's time for its instructions: the second
-    // four waves issue theirs behind their products, so that either half has the unit and the matrix cores in turn.
-    const bool late = NW == 8 && wave >= 4;
-    auto issue = [&]() {
-        if (ahead < it.tile_end) {
-            fetch(b == 0 ? NB - 1 : b - 1, 0, ahead * kBN);
-            if (++ahead < it.tile_end) load_pages(0, ahead * kBN);   // (a tile before they are needed)
-        }
-    };
 #pragma unroll 1
     for (int32_t t = it.tile_begin; t < it.tile_end; ++t) {
         const int32_t after = ahead - t - 1;                 // tiles in flight behind this one
@@ -321,7 +250,10 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
         else if (after >= SOME) wait_tiles_but<Shape::kLoads, SOME>();
         else wait_tiles_but<Shape::kLoads, 0>();
         __syncthreads();                                     // tile t is there, and tile t - 1 done with
-        if (!late) issue();
+        if (ahead < it.tile_end) {
+            fetch(b == 0 ? NB - 1 : b - 1, 0, ahead * kBN);
+            if (++ahead < it.tile_end) load_pages(0, ahead * kBN);   // (a tile before they are needed)
+        }
         const char* const kbuf = buf + b * Geo::kBufB;
 #pragma unroll 1
         for (int i = 0; i < HALVES; ++i) {
@@ -385,7 +317,6 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        if (late) issue();
         b = b == NB - 1 ? 0 : b + 1;
     }
 
@@ -447,7 +378,7 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
     }
     if (r_lane >= n_rows) return false;
     const int64_t row = (int64_t)(it.row0 + qi) * a.num_q_heads + h;
-    uint16_t* const orow = a.out + row * d;
+    uint16_t* const orow = static_cast<uint16_t*>(a.out) + row * d;
 #pragma unroll
     for (int i = 0; i < 4 * T; ++i) {
         if (8 * i >= d) continue;                            // columns behind head_dim
@@ -459,257 +390,29 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
     return false;
 }
 
-// Row blocks and key tiles of sequence i.
-struct TreeSeq {
-    int32_t row0, n, len, blocks, tiles;
-};
-template <int RB>
-__device__ __forceinline__ TreeSeq tree_seq(const TreeKernelArgs& a, int32_t i)
-{
-    TreeSeq q = {0, 0, 0, 0, 0};
-    if (i < a.batch) {
-        q.row0 = a.cu_q_lens[i];
-        q.n = a.cu_q_lens[i + 1] - q.row0;
-        q.len = a.seq_lens[i];
-        q.blocks = q.n > 0 ? (q.n * a.group + RB - 1) / RB : 0;
-        q.tiles = (q.len + kBN - 1) / kBN;
-    }
-    return q;
-}
-
-// How a KV head's workgroups share the call's key tiles.  Where they are few, every row block is cut into chunks of about `chunk`
-// tiles, one a workgroup.  Otherwise (chunk == 0) all tiles stand in a row, each row block's behind kTreePieceTiles places for what a
-// piece of work costs besides its tiles, and workgroup x of wgs takes places [x all / wgs, (x + 1) all / wgs).
-struct TreeShare {
-    int64_t all;
-    int32_t wgs, chunk;
-};
-template <int RB>
-__device__ __forceinline__ TreeShare tree_share(const TreeKernelArgs& a, int lane)
-{
-    int64_t tiles = 0, blocks = 0;
-    for (int32_t i0 = 0; i0 < a.batch; i0 += 64) {
-        const TreeSeq q = tree_seq<RB>(a, i0 + lane);
-        tiles += wave_total_moves(q.blocks * q.tiles);
-        blocks += wave_total_moves(q.blocks);
-    }
-    TreeShare r = {tiles + kTreePieceTiles * blocks, 1, 0};
-    if (blocks < a.wgs) {
-        const int64_t c = (tiles + a.wgs - blocks - 1) / (a.wgs - blocks);
-        if (c <= kTreeMaxChunk) r.chunk = (int32_t)(c < kTreeMinTiles ? kTreeMinTiles : c);
-    }
-    const int64_t n = r.all / (kTreeMinTiles + kTreePieceTiles);
-    r.wgs = n > a.wgs ? a.wgs : n < 1 ? 1 : (int32_t)n;
-    return r;
-}
-// Places of a row block of the sequence: chunks, or tiles and what comes before them.
-__device__ __forceinline__ int32_t tree_places(const TreeShare& r, const TreeSeq& q)
-{
-    return q.blocks == 0 ? 0 : r.chunk > 0 ? (q.tiles + r.chunk - 1) / r.chunk : q.tiles + kTreePieceTiles;
-}
-
 template <int WR, typename E, int DP>
-__global__ __launch_bounds__((64 * TreeShape<WR, DP>::kWaves), (TreeShape<WR, DP>::kOcc * TreeShape<WR, DP>::kWaves / 4)) void paged_attention_tree_mfma_kernel(
-    TreeKernelArgs a, const int32_t* __restrict__ cu_q_lens, const int32_t* __restrict__ seq_lens,
-    const int32_t* __restrict__ block_table, const uint64_t* __restrict__ tree_mask)
-{
-    a.cu_q_lens = cu_q_lens;
-    a.seq_lens = seq_lens;
-    a.block_table = block_table;
-    a.tree_mask = tree_mask;
-    constexpr int RB = 32 * WR;
-    __shared__ __attribute__((aligned(1024))) char buf[TreeShape<WR, DP>::kBufs * TreeGeo<DP>::kBufB];
-    __shared__ uint32_t flags[8];
-    const int lane = threadIdx.x & 63;
-    const int32_t hkv = a.cache.num_kv_heads;
-    const int32_t kvh = (int32_t)(blockIdx.x % (uint32_t)hkv), x = (int32_t)(blockIdx.x / (uint32_t)hkv);
-    // this workgroup's places [t, t_end), the sequence of the first and that one's first place
-    int32_t s = 0;
-    int64_t t = 0, t_end = 1, first = 0;
-    TreeShare share = {0, 0, 0};
-    TreeSeq q = {0, 0, 0, 0, 0};
-    if (a.wgs == 0) {                                        // one row block
-        s = x / a.row_blocks;
-        q = tree_seq<RB>(a, s);
-        if (x % a.row_blocks >= q.blocks || q.tiles <= 0) return;
-    } else {
-        share = tree_share<RB>(a, lane);
-        if (share.chunk > 0) {
-            t = x;
-            t_end = t + 1;
-        } else {
-            if (x >= share.wgs) return;
-            t = (int64_t)x * share.all / share.wgs;
-            t_end = (int64_t)(x + 1) * share.all / share.wgs;
-        }
-        bool found = false;
-        for (int32_t i0 = 0; i0 < a.batch; i0 += 64) {
-            const TreeSeq own = tree_seq<RB>(a, i0 + lane);
-            const int32_t mine = own.blocks * tree_places(share, own), inc = wave_scan_moves(mine);
-            const uint64_t hit = __ballot(first + inc > t);
-            if (hit) {
-                const int f = __ffsll((unsigned long long)hit) - 1;
-                s = i0 + f;
-                first += __builtin_amdgcn_readlane(inc, f) - __builtin_amdgcn_readlane(mine, f);
-                q.row0 = __builtin_amdgcn_readlane(own.row0, f);
-                q.n = __builtin_amdgcn_readlane(own.n, f);
-                q.len = __builtin_amdgcn_readlane(own.len, f);
-                q.blocks = __builtin_amdgcn_readlane(own.blocks, f);
-                q.tiles = __builtin_amdgcn_readlane(own.tiles, f);
-                found = true;
-                break;
-            }
-            first += __builtin_amdgcn_readlane(inc, 63);
-        }
-        if (!found) return;
-    }
-    while (t < t_end) {
-        TreeItem it;
-        it.s = s;
-        it.row0 = q.row0;
-        it.n = q.n;
-        it.len = q.len;
-        if (a.wgs == 0) {
-            it.rb = x % a.row_blocks;
-            it.tile_begin = 0;
-            it.tile_end = q.tiles;
-            it.slot = -1;
-            t = t_end;
-        } else {
-            const int32_t places = tree_places(share, q);
-            if (t >= first + (int64_t)q.blocks * places) {   // (nothing, or nothing more, of this one)
-                first += (int64_t)q.blocks * places;
-                if (++s >= a.batch) return;
-                q = tree_seq<RB>(a, s);
-                continue;
-            }
-            const int32_t at = (int32_t)((t - first) % places);
-            it.rb = (int32_t)((t - first) / places);
-            if (share.chunk > 0) {
-                it.tile_begin = (int32_t)((int64_t)at * q.tiles / places);
-                it.tile_end = (int32_t)((int64_t)(at + 1) * q.tiles / places);
-                t = t_end;
-            } else {
-                const int32_t to = (int32_t)min((int64_t)places, at + (t_end - t));
-                it.tile_begin = max(at - kTreePieceTiles, 0);
-                it.tile_end = max(to - kTreePieceTiles, 0);
-                t += to - at;
-            }
-            const bool whole = it.tile_begin == 0 && it.tile_end == q.tiles;
-            it.slot = whole ? -1 : ((int64_t)kvh * a.wgs + x) * 2 + (it.tile_begin == 0 ? 1 : 0);
-            if (it.tile_begin == it.tile_end) continue;      // (places before the tiles alone)
-        }
-        if (tree_piece_of_work<WR, false, E, DP>(buf, flags, a, it, kvh)) tree_piece_of_work<WR, true, E, DP>(buf, flags, a, it, kvh);
-    }
-}
-
-// The pieces of a row block that were cut, merged by their log-sum-exps.  Grid (sequences x row blocks x WR x kTreeMergeParts, KV
-// heads): 32 rows and a part of their columns each, in the partials' own order, so that a call of few sequences spreads over the
-// machine as well.  Statistics first, all at once, and their weights into LDS; then a thread's four columns, the loads of
-// four pieces in flight.
-constexpr int kTreeMergeParts = 4;
-
-template <int WR, typename E, int DP>
-__global__ __launch_bounds__(256) void paged_attention_tree_merge_kernel(
-    TreeKernelArgs a, const int32_t* __restrict__ cu_q_lens, const int32_t* __restrict__ seq_lens)
-{
-    a.cu_q_lens = cu_q_lens;
-    a.seq_lens = seq_lens;
-    constexpr int RB = 32 * WR, T = DP / 32, PIECES = 4 * T / kTreeMergeParts;
-    extern __shared__ float weight[];                        // [pieces][32]
-    __shared__ float sm_top[32], sm_sum[32];
-    const int lane = threadIdx.x & 63;
-    const int32_t kvh = blockIdx.y, part = (int32_t)(blockIdx.x % kTreeMergeParts);
-    const int32_t rw = (int32_t)(blockIdx.x / kTreeMergeParts) % WR;
-    const int32_t u = (int32_t)(blockIdx.x / (kTreeMergeParts * WR)), s = u / a.row_blocks, rb = u % a.row_blocks;
-    const TreeSeq own = tree_seq<RB>(a, s);
-    const int32_t n_rows = own.n * a.group, r0 = rb * RB + 32 * rw, d = a.cache.head_dim;
-    if (rb >= own.blocks || r0 >= n_rows || own.tiles <= 0) return;
-    const TreeShare share = tree_share<RB>(a, lane);
-    int64_t first = 0;
-    for (int32_t i0 = 0; i0 < s; i0 += 64) {
-        const TreeSeq q = tree_seq<RB>(a, i0 + lane);
-        first += wave_total_moves(i0 + lane < s ? q.blocks * tree_places(share, q) : 0);
-    }
-    const int32_t places = tree_places(share, own);
-    const int64_t begin = first + (int64_t)rb * places, end = begin + places;
-    int64_t w_first = begin, w_last = end - 1;               // workgroups of its first and last tile
-    if (share.chunk == 0) {
-        w_first = ((begin + kTreePieceTiles + 1) * share.wgs - 1) / share.all;
-        w_last = (end * share.wgs - 1) / share.all;
-    }
-    if (w_first == w_last) return;
-    const int32_t pieces = (int32_t)(w_last - w_first) + 1;
-    const int64_t slot0 = ((int64_t)kvh * a.wgs + w_first) * 2;
-    auto slot = [&](int32_t k) { return slot0 + 2 * (int64_t)k + (k == 0 ? 1 : 0); };
-    for (int32_t i = threadIdx.x; i < pieces * 32; i += 256) weight[i] = a.part_lse[slot(i >> 5) * RB + 32 * rw + (i & 31)];
-    __syncthreads();
-    if (threadIdx.x < 32) {
-        float top = -INFINITY, sum = 0.f;
-        for (int32_t k = 0; k < pieces; ++k) top = fmaxf(top, weight[k * 32 + threadIdx.x]);
-        const float use = top == -INFINITY ? 0.f : top;
-        for (int32_t k = 0; k < pieces; ++k) {
-            const float w = __builtin_amdgcn_exp2f(weight[k * 32 + threadIdx.x] - use);
-            weight[k * 32 + threadIdx.x] = w;
-            sum += w;
-        }
-        sm_top[threadIdx.x] = top;
-        sm_sum[threadIdx.x] = sum;
-    }
-    __syncthreads();
-    for (int32_t i = threadIdx.x; i < PIECES * 64; i += 256) {
-        const int32_t j = part * PIECES * 64 + i, row = j & 31, c = 8 * (j >> 6) + 4 * ((j >> 5) & 1), r = r0 + row;
-        if (r >= n_rows || c >= d) continue;
-        const float4* const po = reinterpret_cast<const float4*>(a.part_o) + rw * (4 * T * 64) + j;
-        float4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int32_t k0 = 0; k0 < pieces; k0 += 4) {
-            float4 v[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = po[slot(min(k0 + k, pieces - 1)) * (WR * 4 * T * 64)];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (k0 + k >= pieces) break;
-                const float w = weight[(k0 + k) * 32 + row];
-                acc.x = __builtin_fmaf(w, v[k].x, acc.x);
-                acc.y = __builtin_fmaf(w, v[k].y, acc.y);
-                acc.z = __builtin_fmaf(w, v[k].z, acc.z);
-                acc.w = __builtin_fmaf(w, v[k].w, acc.w);
-            }
-        }
-        const float sum = sm_sum[row], inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
-        const int64_t out_row = (int64_t)(own.row0 + r / a.group) * a.num_q_heads + kvh * a.group + r % a.group;
-        *reinterpret_cast<uint2*>(a.out + out_row * d + c) = uint2{E::pack(acc.x * inv, acc.y * inv), E::pack(acc.z * inv, acc.w * inv)};
-        if (a.lse && c == 0) a.lse[out_row] = sum == 0.f ? -INFINITY : (sm_top[row] + __builtin_amdgcn_logf(sum)) * kLn2;
-    }
-}
-
-template <int WR, typename E, int DP>
-pa_status launch_tree_of(const TreeKernelArgs& a, hipStream_t stream)
-{
-    const int64_t units = (int64_t)a.batch * a.row_blocks;
-    const int64_t grid = (a.wgs > 0 ? a.wgs : units) * a.cache.num_kv_heads;
-    constexpr int PARTS = WR * kTreeMergeParts;
-    if (grid > 0x7fffffffLL || units * PARTS > 0x7fffffffLL || a.cache.num_kv_heads > 65535) return PA_ERR_UNSUPPORTED;
+struct Tree16 {
+    typedef TreeShape<WR, DP> Shape;
+    static constexpr int kRows = 32 * WR, kWaveRows = 32, kColumns = DP, kTile = kBN, kWaves = Shape::kWaves, kOcc = Shape::kOcc;
+    static constexpr int kLds = Shape::kBufs * TreeGeo<DP>::kBufB;
+    template <bool CAREFUL>
+    static __device__ __forceinline__ bool work(char* buf, uint32_t* flags, const TreeKernelArgs& a, const TreeItem& it, int32_t kvh)
     {
-        ProfileScope prof("paged_attention_tree_mfma_kernel", stream);
-        hipLaunchKernelGGL((paged_attention_tree_mfma_kernel<WR, E, DP>), dim3((uint32_t)grid),
-                           dim3(64 * TreeShape<WR, DP>::kWaves), 0, stream, a, a.cu_q_lens, a.seq_lens, a.block_table, a.tree_mask);
-        const pa_status st = launch_status();
-        if (st != PA_OK || a.wgs == 0) return st;
+        return tree_piece_of_work<WR, CAREFUL, E, DP>(buf, flags, a, it, kvh);
     }
-    ProfileScope prof("paged_attention_tree_merge_kernel", stream);
-    hipLaunchKernelGGL((paged_attention_tree_merge_kernel<WR, E, DP>), dim3((uint32_t)(units * PARTS), (uint32_t)a.cache.num_kv_heads),
-                       dim3(256), (size_t)a.wgs * 32 * sizeof(float), stream, a, a.cu_q_lens, a.seq_lens);
-    return launch_status();
-}
+    static __device__ __forceinline__ void store(void* out, int64_t at, float4 v)
+    {
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = uint2{E::pack(v.x, v.y), E::pack(v.z, v.w)};
+    }
+};
 
 template <typename E, int DP>
 pa_status launch_tree_rows(const TreeKernelArgs& a, int row_waves, hipStream_t stream)
 {
-    if (row_waves == 2) return launch_tree_of<2, E, DP>(a, stream);
+    if (row_waves == 2) return launch_tree_of<Tree16<2, E, DP>>(a, stream);
     if constexpr (DP <= 128)
-        if (row_waves == 8) return launch_tree_of<8, E, DP>(a, stream);
-    return launch_tree_of<4, E, DP>(a, stream);
+        if (row_waves == 8) return launch_tree_of<Tree16<8, E, DP>>(a, stream);
+    return launch_tree_of<Tree16<4, E, DP>>(a, stream);
 }
 
 template <int DP>
