@@ -54,7 +54,136 @@ struct Elem<PA_DTYPE_F16> {
     static __device__ __forceinline__ uint16_t put(float x) { return (uint16_t)float_to_f16_bits(x); }
 };
 
-// One workgroup a token: cosines and sines of its pairs into LDS, then element by element over the heads.
+// Where token t goes in the pools: nowhere (-1) without a position or a page.
+__device__ __forceinline__ int64_t slot_of(const RopeKernelArgs& a, int32_t t)
+{
+    const int32_t pos = a.positions[t], s = a.seq_ids[t];
+    if (pos < 0 || s < 0 || s >= a.batch || (pos >> a.log2_page) >= a.max_blocks) return -1;
+    const int32_t page = a.block_table[(int64_t)s * a.max_blocks + (pos >> a.log2_page)];
+    if (page < 0 || page >= a.num_pages) return -1;
+    return (int64_t)page * a.page_stride + (int64_t)(pos & ((1 << a.log2_page) - 1)) * a.token_stride;
+}
+
+// mscale times cosine and sine of pair i of a token.
+__device__ __forceinline__ float2 turn_of(const RopeKernelArgs& a, int32_t t, int32_t i)
+{
+    const double turns = (double)a.rope_positions[t] * (a.inv_freq[i] * 0.15915494309189535);
+    float sn, cs;
+    sincospif((float)(2.0 * (turns - rint(turns))), &sn, &cs);
+    return float2{cs * a.mscale, sn * a.mscale};
+}
+
+// 16 bytes at a time, where the turned part divides into such pieces.  A workgroup takes TOKENS tokens, or a part of one's heads where
+// there are few: cosines and sines once for all heads into LDS, then a thread's pieces: two of a pair of halves, one of neighbours, one to
+// copy.  Bound by reading and writing q, K and V once; a thread's first piece is on its way while the angles are formed.
+template <pa_dtype DT, bool INTER, int TOKENS>
+__global__ __launch_bounds__(kThreads) void paged_rope_append_wide_kernel(RopeKernelArgs a)
+{
+    typedef Elem<DT> E;
+    typedef typename E::T T;
+    constexpr int V = 16 / sizeof(T);
+    __shared__ __attribute__((aligned(16))) float sm_c[TOKENS][128], sm_s[TOKENS][128];
+    __shared__ int64_t sm_slot[TOKENS];
+    const int32_t d = a.head_dim, half = a.half, t0 = (int32_t)blockIdx.x * TOKENS, tokens = min(TOKENS, a.T - t0);
+    const int32_t turned = INTER ? 2 * half / V : half / V;  // pieces of a head that turn, then those to copy
+    const int32_t pieces = turned + (d - 2 * half) / V, copies = d / V;
+    const int32_t q_tasks = a.q_heads * pieces, k_tasks = a.kv_heads * pieces, all = q_tasks + k_tasks + a.kv_heads * copies;
+    const int32_t mine = (all * tokens + (int32_t)gridDim.y - 1) / (int32_t)gridDim.y, begin = mine * (int32_t)blockIdx.y;
+    const int32_t end = min(begin + mine, all * tokens);
+
+    struct Piece {
+        const T* src;            // of the piece's first element
+        int32_t token, u;        // u: number of the piece in its head; -1: to copy
+        int32_t what;            // 0: q, 1: K, 2: V
+        int64_t at;              // where it goes within its token
+    };
+    auto locate = [&](int32_t i) {
+        Piece p;
+        p.token = TOKENS == 1 ? 0 : i / all;
+        int32_t j = i - p.token * all;
+        p.what = j < q_tasks ? 0 : j < q_tasks + k_tasks ? 1 : 2;
+        j -= p.what == 0 ? 0 : p.what == 1 ? q_tasks : q_tasks + k_tasks;
+        const int32_t n = p.what == 2 ? copies : pieces, h = j / n;
+        p.u = j - h * n;
+        int32_t first = p.u * V;                             // element of the head
+        if (p.what == 2 || p.u >= turned) {
+            if (p.what != 2) first = 2 * half + (p.u - turned) * V;
+            p.u = -1;
+        }
+        const int64_t t = t0 + p.token;
+        const T* const base = p.what == 0 ? (const T*)a.q + t * a.q_stride : p.what == 1 ? (const T*)a.k_new + t * a.k_stride
+                                                                                           : (const T*)a.v_new + t * a.v_stride;
+        p.src = base + (int64_t)h * d + first;
+        p.at = (p.what == 0 ? (int64_t)h * d : h * a.head_stride) + first;
+        return p;
+    };
+    struct Pair {
+        uint4 x, y;
+    };
+    auto load = [&](const Piece& p) {
+        Pair v;
+        v.x = *reinterpret_cast<const uint4*>(p.src);
+        v.y = v.x;
+        if (!INTER && p.u >= 0) v.y = *reinterpret_cast<const uint4*>(p.src + half);
+        return v;
+    };
+    Piece p;
+    Pair v;
+    int32_t i = begin + threadIdx.x;
+    if (i < end) {
+        p = locate(i);
+        v = load(p);
+    }
+    if (a.kv_heads > 0 && (int)threadIdx.x < tokens) sm_slot[threadIdx.x] = slot_of(a, t0 + threadIdx.x);
+    for (int32_t k = threadIdx.x; k < tokens * half; k += kThreads) {
+        const int32_t t = k / half, pair = k - t * half;
+        const float2 cs = turn_of(a, t0 + t, pair);
+        sm_c[t][pair] = cs.x;
+        sm_s[t][pair] = cs.y;
+    }
+    __syncthreads();
+    while (i < end) {
+        T* dst = nullptr;
+        if (p.what == 0) dst = (T*)a.q_out + (int64_t)(t0 + p.token) * a.q_out_stride + p.at;
+        else if (sm_slot[p.token] >= 0) dst = (T*)(p.what == 1 ? a.k_cache : a.v_cache) + sm_slot[p.token] + p.at;
+        if (dst) {
+            if (p.u >= 0) {
+                T x[V], y[V];
+                __builtin_memcpy(x, &v.x, 16);
+                __builtin_memcpy(y, &v.y, 16);
+                if (INTER) {
+                    const int32_t at = p.u * (V / 2);
+#pragma unroll
+                    for (int e = 0; e < V; e += 2) {
+                        const float c = sm_c[p.token][at + e / 2], s = sm_s[p.token][at + e / 2];
+                        const float fx = E::get(x[e]), fy = E::get(x[e + 1]);
+                        x[e] = E::put(fx * c - fy * s);
+                        x[e + 1] = E::put(fx * s + fy * c);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float c = sm_c[p.token][p.u * V + e], s = sm_s[p.token][p.u * V + e];
+                        const float fx = E::get(x[e]), fy = E::get(y[e]);
+                        x[e] = E::put(fx * c - fy * s);
+                        y[e] = E::put(fx * s + fy * c);
+                    }
+                    __builtin_memcpy(&v.y, y, 16);
+                    *reinterpret_cast<uint4*>(dst + half) = v.y;
+                }
+                __builtin_memcpy(&v.x, x, 16);
+            }
+            *reinterpret_cast<uint4*>(dst) = v.x;
+        }
+        i += kThreads;
+        if (i < end) {
+            p = locate(i);
+            v = load(p);
+        }
+    }
+}
+
+// Pair by pair, whatever the turned part: a workgroup a token.
 template <pa_dtype DT, bool INTER>
 __global__ __launch_bounds__(kThreads) void paged_rope_append_kernel(RopeKernelArgs a)
 {
@@ -63,22 +192,8 @@ __global__ __launch_bounds__(kThreads) void paged_rope_append_kernel(RopeKernelA
     __shared__ float2 sm_cs[128];                            // head_dim is at most 256
     const int32_t t = blockIdx.x;
     const int32_t d = a.head_dim, half = a.half;
-    if ((int)threadIdx.x < half) {
-        const double turns = (double)a.rope_positions[t] * (a.inv_freq[threadIdx.x] * 0.15915494309189535);
-        float sn, cs;
-        sincospif((float)(2.0 * (turns - rint(turns))), &sn, &cs);
-        sm_cs[threadIdx.x] = float2{cs * a.mscale, sn * a.mscale};
-    }
-    // where the token goes: nowhere without a position or a page
-    int64_t slot = -1;
-    if (a.kv_heads > 0) {
-        const int32_t pos = a.positions[t], s = a.seq_ids[t];
-        if (pos >= 0 && s >= 0 && s < a.batch && (pos >> a.log2_page) < a.max_blocks) {
-            const int32_t page = a.block_table[(int64_t)s * a.max_blocks + (pos >> a.log2_page)];
-            if (page >= 0 && page < a.num_pages)
-                slot = (int64_t)page * a.page_stride + (int64_t)(pos & ((1 << a.log2_page) - 1)) * a.token_stride;
-        }
-    }
+    if ((int)threadIdx.x < half) sm_cs[threadIdx.x] = turn_of(a, t, threadIdx.x);
+    const int64_t slot = a.kv_heads > 0 ? slot_of(a, t) : -1;
     __syncthreads();
     const int32_t units = half + (d - 2 * half);             // pairs, then single elements
     auto turn = [&](const T* src, T* dst, int32_t u) {
@@ -107,13 +222,31 @@ __global__ __launch_bounds__(kThreads) void paged_rope_append_kernel(RopeKernelA
     }
 }
 
+template <pa_dtype DT, bool INTER>
+void launch_layout(const RopeKernelArgs& a, hipStream_t stream)
+{
+    constexpr int V = DT == PA_DTYPE_F32 ? 4 : 8;
+    if ((INTER ? 2 * a.half : a.half) % V != 0) {
+        hipLaunchKernelGGL((paged_rope_append_kernel<DT, INTER>), dim3(a.T), dim3(kThreads), 0, stream, a);
+        return;
+    }
+    // Four tokens a workgroup once that leaves each compute unit four of them; where tokens are few, a thread takes a piece or two.
+    constexpr int kTokens = 4;
+    if (a.T >= 4096) {
+        hipLaunchKernelGGL((paged_rope_append_wide_kernel<DT, INTER, kTokens>), dim3((a.T + kTokens - 1) / kTokens), dim3(kThreads), 0, stream, a);
+        return;
+    }
+    const int32_t pieces = (a.q_heads + a.kv_heads) * ((INTER ? 2 * a.half : a.half) / V + (a.head_dim - 2 * a.half) / V) +
+                           a.kv_heads * a.head_dim / V;
+    const int32_t parts = a.T >= 512 ? 1 : (pieces + kThreads - 1) / kThreads;
+    hipLaunchKernelGGL((paged_rope_append_wide_kernel<DT, INTER, 1>), dim3(a.T, parts), dim3(kThreads), 0, stream, a);
+}
+
 template <pa_dtype DT>
 void launch_dtype(const RopeKernelArgs& a, bool inter, hipStream_t stream)
 {
-    if (inter)
-        hipLaunchKernelGGL((paged_rope_append_kernel<DT, true>), dim3(a.T), dim3(kThreads), 0, stream, a);
-    else
-        hipLaunchKernelGGL((paged_rope_append_kernel<DT, false>), dim3(a.T), dim3(kThreads), 0, stream, a);
+    if (inter) launch_layout<DT, true>(a, stream);
+    else launch_layout<DT, false>(a, stream);
 }
 
 }  // namespace
