@@ -365,36 +365,42 @@ __global__ __launch_bounds__(kAcceptThreads) void paged_tree_accept_kernel(Accep
     if (a.tokens && blockIdx.y == 0)
         for (int32_t i = threadIdx.x; i < a.max_path; i += kAcceptThreads)
             a.path[(int64_t)s * a.max_path + i] = i < len ? sm_path[i] : -1;
+    // 64 rows' places at a time, a thread each, then every thread's piece of them
+    __shared__ int64_t sm_from[64], sm_to[64];               // 16-byte pieces into a pool; to < 0: nothing to move
     const int32_t piece = (int32_t)blockIdx.y * kAcceptThreads + threadIdx.x;
     const int32_t per_pool = a.num_kv_heads * a.vec_per_head;
-    if (piece >= 2 * per_pool) return;
     uint4* const pool = piece < per_pool ? a.k_cache : a.v_cache;
     const int32_t p = piece < per_pool ? piece : piece - per_pool;
     const int64_t in_token = (int64_t)(p / a.vec_per_head) * a.head_stride_v + p % a.vec_per_head;
     const int32_t* const table = a.block_table + (int64_t)s * a.max_blocks;
-    auto at = [&](int32_t t) -> int64_t {                    // piece of token t, -1: it has no page
+    auto place = [&](int32_t t) -> int64_t {                 // of token t, -1: it has no page
         if (t < 0 || (t >> a.log2_page) >= a.max_blocks) return -1;
         const int32_t page = table[t >> a.log2_page];
         if (page < 0 || page >= a.num_pages) return -1;
-        return (int64_t)page * a.page_stride_v + (int64_t)(t & ((1 << a.log2_page) - 1)) * a.token_stride_v + in_token;
+        return (int64_t)page * a.page_stride_v + (int64_t)(t & ((1 << a.log2_page) - 1)) * a.token_stride_v;
     };
     constexpr int kBatch = 8;
-    for (int32_t i0 = 0; i0 < len; i0 += kBatch) {
-        uint4 row[kBatch];
-        int64_t to[kBatch];
+    for (int32_t base = 0; base < len; base += 64) {
+        const int32_t rows = min(len - base, 64);
+        if ((int)threadIdx.x < rows) {
+            const int32_t i = base + threadIdx.x;
+            const int64_t from = place(ctx + sm_path[i]), to = place(ctx + i);
+            sm_from[threadIdx.x] = from;
+            sm_to[threadIdx.x] = from < 0 || sm_path[i] == i ? -1 : to;
+        }
+        __syncthreads();
+        if (piece < 2 * per_pool) {
+            for (int32_t i0 = 0; i0 < rows; i0 += kBatch) {
+                uint4 row[kBatch];
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            const int32_t i = i0 + u;
-            to[u] = -1;
-            if (i < len && sm_path[i] != i) {
-                const int64_t from = at(ctx + sm_path[i]);
-                to[u] = from < 0 ? -1 : at(ctx + i);
-                if (to[u] >= 0) row[u] = pool[from];
+                for (int u = 0; u < kBatch; ++u)
+                    if (i0 + u < rows && sm_to[i0 + u] >= 0) row[u] = pool[sm_from[i0 + u] + in_token];
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u)
+                    if (i0 + u < rows && sm_to[i0 + u] >= 0) pool[sm_to[i0 + u] + in_token] = row[u];
             }
         }
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u)
-            if (to[u] >= 0) pool[to[u]] = row[u];
+        __syncthreads();
     }
 }
 
