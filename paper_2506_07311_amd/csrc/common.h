@@ -303,7 +303,7 @@ struct TreePlan {
     int32_t row_waves;           // waves of a workgroup beside each other in rows: 2, 4 or 8 of 32 rows; fp32 1, 2 or 4 of 16
     int32_t row_blocks;          // most row blocks of a sequence
     int32_t wgs;                 // workgroups of a KV head that share all key tiles; 0: one a row block, no partials
-    size_t part_o_bytes, part_lse_bytes;
+    size_t part_o_bytes, part_lse_bytes, cuts_bytes;
 };
 TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t max_q_len, int32_t max_seq_len, bool f32);
 bool tree_mfma_supported(const TreeArgs& a);

@@ -119,7 +119,8 @@ size_t paged_attention_tree_workspace_bytes(int32_t batch, int32_t num_q_heads, 
     size_t most = 256;                                       // (the type is not known here)
     for (const bool f32 : {false, true}) {
         const TreePlan p = plan_tree(batch, num_q_heads, num_kv_heads, head_dim, max_q_len, max_seq_len, f32);
-        if (p.part_o_bytes + p.part_lse_bytes > most) most = p.part_o_bytes + p.part_lse_bytes;
+        const size_t bytes = p.part_o_bytes + p.part_lse_bytes + p.cuts_bytes;
+        if (bytes > most) most = bytes;
     }
     return most;
 }

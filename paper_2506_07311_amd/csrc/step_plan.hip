@@ -9,7 +9,6 @@ namespace pa {
 namespace {
 
 // ---- plan and release ----------------------------------------------------------------------------------------------
-constexpr int kPlanThreads = 256;
 constexpr int kReleaseThreads = 1024;
 
 // Inclusive sum over the workgroup (N threads) of one value a thread; `total` gets the whole sum.  sm: N / 64 words,
@@ -75,58 +74,57 @@ __device__ __forceinline__ int32_t blocks_for(int32_t tokens, int32_t log2_page)
 // Workgroup 0: everything that is one value a sequence, and the pages.  It alone writes what it and the others read
 // nothing of but itself (counts, table, free list), so that a call can work in place in one launch; the others derive the
 // rows' values from ctx_lens and new_lens, whether the request is granted or not.
+template <int N>
 __device__ __forceinline__ void plan_sequences(const PlanArgs& a)
 {
-    __shared__ int32_t sm[kPlanThreads / 64];
-    __shared__ int32_t sm_end[kPlanThreads];
+    __shared__ int32_t sm[N / 64];
+    __shared__ int32_t sm_end[N];
     const int tid = threadIdx.x;
     const int32_t count = a.free_count[0];
-    int32_t need_all = 0, long_all = 0, rows_all = 0;
-    for (int32_t s0 = 0; s0 < a.batch; s0 += kPlanThreads) {
-        const int32_t s = s0 + tid;
-        int32_t need = 0, late = 0, rows = 0;
+    int32_t need = 0, rows = 0, ctx = 0, have = 0, row_end = 0, need_end = 0, rows_here = 0, pages_here = 0;
+    bool late = false;
+    auto look = [&](int32_t s) {                             // this thread's sequence, and the sums up to it
+        need = rows = 0;
+        late = false;
         if (s < a.batch) {
             rows = max(a.new_lens[s], 0);
-            const int32_t want = blocks_for(a.ctx_lens[s] + rows, a.log2_page);
-            need = max(want - a.num_blocks[s], 0);
-            late = want > a.max_blocks || (a.tree_mask && rows > 64 * a.mask_words) ? 1 : 0;
+            ctx = a.ctx_lens[s];
+            have = a.num_blocks[s];
+            const int32_t want = blocks_for(ctx + rows, a.log2_page);
+            need = max(want - have, 0);
+            late = want > a.max_blocks || (a.tree_mask && rows > 64 * a.mask_words);
         }
-        int32_t t;
-        group_scan<kPlanThreads>(need, sm, t);
-        need_all += t;
-        group_scan<kPlanThreads>(late, sm, t);
-        long_all += t;
-        group_scan<kPlanThreads>(rows, sm, t);
-        rows_all += t;
+        row_end = group_scan<N>(rows, sm, rows_here);
+        need_end = group_scan<N>(need, sm, pages_here);
+    };
+    int32_t need_all = 0, long_all = 0, rows_all = 0;
+    for (int32_t s0 = 0; s0 < a.batch; s0 += N) {
+        look(s0 + tid);
+        need_all += pages_here;
+        rows_all += rows_here;
+        long_all += __syncthreads_count(late);
     }
     if (rows_all > a.max_rows) long_all += rows_all - a.max_rows;
     const bool ok = need_all <= count && long_all == 0;
     int32_t rows_before = 0, pages_before = 0;
-    for (int32_t s0 = 0; s0 < a.batch; s0 += kPlanThreads) {
+    for (int32_t s0 = 0; s0 < a.batch; s0 += N) {
         const int32_t s = s0 + tid;
-        int32_t need = 0, rows = 0, ctx = 0;
-        if (s < a.batch) {
-            rows = max(a.new_lens[s], 0);
-            ctx = a.ctx_lens[s];
-            need = max(blocks_for(ctx + rows, a.log2_page) - a.num_blocks[s], 0);
-        }
-        int32_t rows_here, pages_here;
-        const int32_t row_end = group_scan<kPlanThreads>(rows, sm, rows_here);
-        sm_end[tid] = group_scan<kPlanThreads>(need, sm, pages_here);
+        if (a.batch > N) look(s);                            // (one block of sequences is still at hand)
+        sm_end[tid] = need_end;
         if (s < a.batch) {
             a.cu_q_lens[s + 1] = ok ? rows_before + row_end : 0;
             a.seq_lens[s] = ok ? ctx + rows : ctx;
         }
         __syncthreads();
         if (ok) {
-            for (int32_t m = tid; m < pages_here; m += kPlanThreads) {
-                const int32_t f = find_in<kPlanThreads>(sm_end, m);
+            for (int32_t m = tid; m < pages_here; m += N) {
+                const int32_t f = find_in<N>(sm_end, m);
                 const int32_t at = m - (f ? sm_end[f - 1] : 0);
                 a.block_table[(int64_t)(s0 + f) * a.max_blocks + a.num_blocks[s0 + f] + at] =
                     a.free_pages[count - 1 - pages_before - m];
             }
             __syncthreads();                                 // (the counts have been read)
-            if (need > 0) a.num_blocks[s] += need;
+            if (need > 0) a.num_blocks[s] = have + need;
         }
         rows_before += rows_here;
         pages_before += pages_here;
@@ -138,7 +136,7 @@ __device__ __forceinline__ void plan_sequences(const PlanArgs& a)
         a.shortage[0] = max(need_all - count, 0);
         a.shortage[1] = long_all;
     }
-    for (int32_t r = min(rows_all, a.max_rows) + tid; r < a.max_rows; r += kPlanThreads) {
+    for (int32_t r = min(rows_all, a.max_rows) + tid; r < a.max_rows; r += N) {
         a.seq_ids[r] = -1;
         a.positions[r] = -1;
         if (a.rope_positions) a.rope_positions[r] = 0;
@@ -211,13 +209,15 @@ __device__ __forceinline__ void plan_rows(const PlanArgs& a, int32_t s)
     }
 }
 
-__global__ __launch_bounds__(kPlanThreads) void paged_plan_step_kernel(PlanArgs a)
+// (N threads: as many sequences at a time)
+template <int N>
+__global__ __launch_bounds__(N) void paged_plan_step_kernel(PlanArgs a)
 {
     if (blockIdx.x == 0) {
-        plan_sequences(a);
+        plan_sequences<N>(a);
         return;
     }
-    const int32_t s = ((int32_t)blockIdx.x - 1) * (kPlanThreads / 64) + (int32_t)(threadIdx.x >> 6);
+    const int32_t s = ((int32_t)blockIdx.x - 1) * (N / 64) + (int32_t)(threadIdx.x >> 6);
     if (s < a.batch) plan_rows(a, s);
 }
 
@@ -435,9 +435,9 @@ pa_status launch_plan_step(const StepPlanArgs& p, hipStream_t stream)
     a.log2_page = log2_of(p.page_size);
     a.max_rows = p.max_rows;
     a.mask_words = p.mask_words;
-    const uint32_t wgs = 1 + (uint32_t)((p.batch + kPlanThreads / 64 - 1) / (kPlanThreads / 64));
     ProfileScope prof("paged_plan_step_kernel", stream);
-    hipLaunchKernelGGL(paged_plan_step_kernel, dim3(wgs), dim3(kPlanThreads), 0, stream, a);
+    if (p.batch <= 256) hipLaunchKernelGGL(paged_plan_step_kernel<256>, dim3(1 + (p.batch + 3) / 4), dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL(paged_plan_step_kernel<1024>, dim3(1 + (p.batch + 15) / 16), dim3(1024), 0, stream, a);
     return launch_status();
 }
 

@@ -38,7 +38,7 @@ TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int
     const int32_t tile = f32 && columns > 128 ? 32 : prefill::kBN;
     const int64_t tiles = ((int64_t)max_seq_len + tile - 1) / tile;
     p.wgs = 0;
-    p.part_o_bytes = p.part_lse_bytes = 0;
+    p.part_o_bytes = p.part_lse_bytes = p.cuts_bytes = 0;
     if (tiles > kPlainTiles) {
         const int64_t slots = (int64_t)device_cus() * (columns == 64 && p.row_waves == 2 && !f32 ? 2 : 1);
         const int64_t most = (batch * blocks * tiles + 3) / 4;
@@ -48,6 +48,7 @@ TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int
         const size_t part_rows = (size_t)p.wgs * num_kv_heads * 2 * wave_rows * p.row_waves;
         p.part_o_bytes = align256(part_rows * columns * sizeof(float));
         p.part_lse_bytes = align256(part_rows * sizeof(float));
+        p.cuts_bytes = align256((size_t)num_kv_heads * batch * p.row_blocks * sizeof(int2));
     }
     return p;
 }
@@ -72,6 +73,7 @@ pa_status launch_tree_mfma(const TreeArgs& t, void* workspace, hipStream_t strea
     a.block_table = t.block_table;
     a.part_o = reinterpret_cast<float*>(workspace);
     a.part_lse = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + p.part_o_bytes);
+    a.cuts = reinterpret_cast<int2*>(reinterpret_cast<char*>(a.part_lse) + p.part_lse_bytes);
     a.mask_words = t.mask_words;
     a.batch = t.batch;
     a.num_q_heads = t.num_q_heads;

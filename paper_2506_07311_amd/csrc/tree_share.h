@@ -24,6 +24,7 @@ struct TreeKernelArgs {
     const int32_t* block_table;
     float* part_o;               // [KV head][workgroup][2][wave of rows][rows x columns as the wave holds them], normalised
     float* part_lse;             // [KV head][workgroup][2][row], log2 domain
+    int2* cuts;                  // [KV head][sequence][row block]: first workgroup and number of pieces
     int32_t mask_words, batch, num_q_heads, max_blocks, group;
     int32_t wgs;                 // workgroups of a KV head that share the tiles; 0: one a (sequence, row block)
     int32_t row_blocks;          // most row blocks of a sequence
@@ -101,11 +102,11 @@ struct TreeShare {
     int32_t wgs, chunk;
 };
 template <typename S>
-__device__ __forceinline__ TreeShare tree_share(const TreeKernelArgs& a, int lane)
+__device__ __forceinline__ TreeShare tree_share(const TreeKernelArgs& a, int lane, const TreeSeq& own)   // own: sequence `lane`
 {
     int64_t tiles = 0, blocks = 0;
     for (int32_t i0 = 0; i0 < a.batch; i0 += 64) {
-        const TreeSeq q = tree_seq<S>(a, i0 + lane);
+        const TreeSeq q = i0 == 0 ? own : tree_seq<S>(a, i0 + lane);
         tiles += wave_total_moves(q.blocks * q.tiles);
         blocks += wave_total_moves(q.blocks);
     }
@@ -148,7 +149,8 @@ __global__ __launch_bounds__(64 * S::kWaves, S::kOcc * S::kWaves / 4) void paged
         q = tree_seq<S>(a, s);
         if (x % a.row_blocks >= q.blocks || q.tiles <= 0) return;
     } else {
-        share = tree_share<S>(a, lane);
+        const TreeSeq start = tree_seq<S>(a, lane);
+        share = tree_share<S>(a, lane, start);
         if (share.chunk > 0) {
             t = x;
             t_end = t + 1;
@@ -159,7 +161,7 @@ __global__ __launch_bounds__(64 * S::kWaves, S::kOcc * S::kWaves / 4) void paged
         }
         bool found = false;
         for (int32_t i0 = 0; i0 < a.batch; i0 += 64) {
-            const TreeSeq own = tree_seq<S>(a, i0 + lane);
+            const TreeSeq own = i0 == 0 ? start : tree_seq<S>(a, i0 + lane);
             const int32_t mine = own.blocks * tree_places(share, own), inc = wave_scan_moves(mine);
             const uint64_t hit = __ballot(first + inc > t);
             if (hit) {
@@ -213,6 +215,14 @@ __global__ __launch_bounds__(64 * S::kWaves, S::kOcc * S::kWaves / 4) void paged
             const bool whole = it.tile_begin == 0 && it.tile_end == q.tiles;
             it.slot = whole ? -1 : ((int64_t)kvh * a.wgs + x) * 2 + (it.tile_begin == 0 ? 1 : 0);
             if (it.tile_begin == it.tile_end) continue;      // (places before the tiles alone)
+            if (it.tile_begin == 0 && threadIdx.x == 0) {    // what the merge has to know: workgroups up to the last tile's
+                int32_t pieces = places;
+                if (share.chunk == 0) {
+                    const int64_t end = first + (int64_t)(it.rb + 1) * places;
+                    pieces = (int32_t)((end * share.wgs - 1) / share.all) - x + 1;
+                }
+                a.cuts[((int64_t)kvh * a.batch + s) * a.row_blocks + it.rb] = int2{x, pieces};
+            }
         }
         if (S::template work<false>(buf, flags, a, it, kvh)) S::template work<true>(buf, flags, a, it, kvh);
     }
@@ -233,29 +243,16 @@ __global__ __launch_bounds__(256) void paged_attention_tree_merge_kernel(
     constexpr int RB = S::kRows, RW = S::kWaveRows, WR = RB / RW, VECS = RW * S::kColumns / 4, MINE = VECS / kTreeMergeParts;
     extern __shared__ float weight[];                        // [pieces][RW]
     __shared__ float sm_top[RW], sm_sum[RW];
-    const int lane = threadIdx.x & 63;
     const int32_t kvh = blockIdx.y, part = (int32_t)(blockIdx.x % kTreeMergeParts);
     const int32_t rw = (int32_t)(blockIdx.x / kTreeMergeParts) % WR;
     const int32_t u = (int32_t)(blockIdx.x / (kTreeMergeParts * WR)), s = u / a.row_blocks, rb = u % a.row_blocks;
+    const int2 cut = a.cuts[((int64_t)kvh * a.batch + s) * a.row_blocks + rb];
     const TreeSeq own = tree_seq<S>(a, s);
     const int32_t n_rows = own.n * a.group, r0 = rb * RB + RW * rw, d = a.cache.head_dim;
-    if (rb >= own.blocks || r0 >= n_rows || own.tiles <= 0) return;
-    const TreeShare share = tree_share<S>(a, lane);
-    int64_t first = 0;
-    for (int32_t i0 = 0; i0 < s; i0 += 64) {
-        const TreeSeq q = tree_seq<S>(a, i0 + lane);
-        first += wave_total_moves(i0 + lane < s ? q.blocks * tree_places(share, q) : 0);
-    }
-    const int32_t places = tree_places(share, own);
-    const int64_t begin = first + (int64_t)rb * places, end = begin + places;
-    int64_t w_first = begin, w_last = end - 1;               // workgroups of its first and last tile
-    if (share.chunk == 0) {
-        w_first = ((begin + kTreePieceTiles + 1) * share.wgs - 1) / share.all;
-        w_last = (end * share.wgs - 1) / share.all;
-    }
-    if (w_first == w_last) return;
-    const int32_t pieces = (int32_t)(w_last - w_first) + 1;
-    const int64_t slot0 = ((int64_t)kvh * a.wgs + w_first) * 2;
+    if (rb >= own.blocks || r0 >= n_rows || own.tiles <= 0) return;   // (and then the cut is no one's)
+    const int32_t pieces = cut.y;
+    if (pieces == 1) return;
+    const int64_t slot0 = ((int64_t)kvh * a.wgs + cut.x) * 2;
     auto slot = [&](int32_t k) { return slot0 + 2 * (int64_t)k + (k == 0 ? 1 : 0); };
     for (int32_t i = threadIdx.x; i < pieces * RW; i += 256) weight[i] = a.part_lse[slot(i / RW) * RB + RW * rw + i % RW];
     __syncthreads();
