@@ -40,8 +40,8 @@ TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int
     p.wgs = 0;
     p.part_o_bytes = p.part_lse_bytes = p.cuts_bytes = 0;
     if (tiles > kPlainTiles) {
-        const int64_t slots = (int64_t)device_cus() * (columns == 64 && p.row_waves == 2 && !f32 ? 2 : 1);
-        const int64_t most = (batch * blocks * tiles + 3) / 4;
+        const int64_t slots = (int64_t)device_cus() * (columns <= 128 && p.row_waves == 2 && !f32 ? 2 : 1);
+        const int64_t most = (batch * blocks * tiles + kTreeMinTiles - 1) / kTreeMinTiles;
         int64_t wgs = slots / num_kv_heads;
         if (wgs > most) wgs = most;
         p.wgs = wgs < 1 ? 1 : wgs > kTreeMaxPieces ? kTreeMaxPieces : (int32_t)wgs;

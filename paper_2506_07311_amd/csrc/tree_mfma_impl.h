@@ -45,8 +45,8 @@ template <int WR, int DP>
 struct TreeShape {
     static constexpr int kKW = WR == 2 || (WR == 4 && DP <= 128) ? 2 : 1;
     static constexpr int kWaves = WR * kKW;
-    static constexpr int kOcc = DP <= 64 && kWaves == 4 ? 2 : 1;         // workgroups of a compute unit
-    static constexpr int kBufs = DP > 128 ? 2 : DP > 64 ? 4 : kOcc == 2 ? 4 : 8;
+    static constexpr int kOcc = DP <= 128 && kWaves == 4 ? 2 : 1;        // workgroups of a compute unit
+    static constexpr int kBufs = DP > 128 ? 2 : (DP > 64 ? 4 : 8) / kOcc;
     static constexpr int kLoads = TreeGeo<DP>::kTileB / (1024 * kWaves); // load instructions of a wave and pool a tile
 };
 

@@ -35,7 +35,7 @@ namespace {
 
 using namespace prefill;
 
-constexpr int32_t kTreeMinTiles = 4;     // fewest tiles of a workgroup that shares them
+constexpr int32_t kTreeMinTiles = 2;     // fewest tiles of a workgroup that shares them
 constexpr int32_t kTreePieceTiles = 4;   // what a piece of work costs besides its tiles, in tiles
 constexpr int32_t kTreeMaxChunk = 12;    // most tiles of a workgroup that has one piece of work
 constexpr int32_t kTreeMaxPieces = 256;  // workgroups that share a row block
@@ -229,23 +229,21 @@ __global__ __launch_bounds__(64 * S::kWaves, S::kOcc * S::kWaves / 4) void paged
 }
 
 // The pieces of a row block that were cut, merged by their log-sum-exps.  Grid (sequences x row blocks x row waves x
-// kTreeMergeParts, KV heads): a wave's rows and a part of their columns each, in the partials' own order, so that a call of few sequences spreads over the
-// machine as well.  Statistics first, all at once, and their weights into LDS; then a thread's four columns, the loads of
-// four pieces in flight.
-constexpr int kTreeMergeParts = 4;
-
-template <typename S>
+// PARTS, KV heads): a wave's rows and a part of their columns each, in the partials' own order, so that a call of few sequences spreads over the
+// machine as well.  Statistics first, all at once, and their weights into LDS.
+template <typename S, int PARTS>
 __global__ __launch_bounds__(256) void paged_attention_tree_merge_kernel(
     TreeKernelArgs a, const int32_t* __restrict__ cu_q_lens, const int32_t* __restrict__ seq_lens)
 {
     a.cu_q_lens = cu_q_lens;
     a.seq_lens = seq_lens;
-    constexpr int RB = S::kRows, RW = S::kWaveRows, WR = RB / RW, VECS = RW * S::kColumns / 4, MINE = VECS / kTreeMergeParts;
+    constexpr int RB = S::kRows, RW = S::kWaveRows, WR = RB / RW, VECS = RW * S::kColumns / 4, MINE = VECS / PARTS, LINES = MINE / 64;
     extern __shared__ float weight[];                        // [pieces][RW]
-    __shared__ float sm_top[RW], sm_sum[RW];
-    const int32_t kvh = blockIdx.y, part = (int32_t)(blockIdx.x % kTreeMergeParts);
-    const int32_t rw = (int32_t)(blockIdx.x / kTreeMergeParts) % WR;
-    const int32_t u = (int32_t)(blockIdx.x / (kTreeMergeParts * WR)), s = u / a.row_blocks, rb = u % a.row_blocks;
+    __shared__ float sm_top[RW], sm_sum[RW], sm_red[256 / RW][RW];
+    __shared__ float4 sm_acc[4][LINES][64];
+    const int32_t kvh = blockIdx.y, part = (int32_t)(blockIdx.x % PARTS);
+    const int32_t rw = (int32_t)(blockIdx.x / PARTS) % WR;
+    const int32_t u = (int32_t)(blockIdx.x / (PARTS * WR)), s = u / a.row_blocks, rb = u % a.row_blocks;
     const int2 cut = a.cuts[((int64_t)kvh * a.batch + s) * a.row_blocks + rb];
     const TreeSeq own = tree_seq<S>(a, s);
     const int32_t n_rows = own.n * a.group, r0 = rb * RB + RW * rw, d = a.cache.head_dim;
@@ -254,46 +252,91 @@ __global__ __launch_bounds__(256) void paged_attention_tree_merge_kernel(
     if (pieces == 1) return;
     const int64_t slot0 = ((int64_t)kvh * a.wgs + cut.x) * 2;
     auto slot = [&](int32_t k) { return slot0 + 2 * (int64_t)k + (k == 0 ? 1 : 0); };
-    for (int32_t i = threadIdx.x; i < pieces * RW; i += 256) weight[i] = a.part_lse[slot(i / RW) * RB + RW * rw + i % RW];
-    __syncthreads();
-    if (threadIdx.x < RW) {
-        float top = -INFINITY, sum = 0.f;
-        for (int32_t k = 0; k < pieces; ++k) top = fmaxf(top, weight[k * RW + threadIdx.x]);
-        const float use = top == -INFINITY ? 0.f : top;
-        for (int32_t k = 0; k < pieces; ++k) {
-            const float w = __builtin_amdgcn_exp2f(weight[k * RW + threadIdx.x] - use);
-            weight[k * RW + threadIdx.x] = w;
-            sum += w;
+    // (256 / RW threads a row)
+    constexpr int GROUPS = 256 / RW;
+    const int32_t srow = threadIdx.x % RW, group = threadIdx.x / RW;
+    float top = -INFINITY;
+    for (int32_t k0 = group; k0 < pieces; k0 += 8 * GROUPS) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = a.part_lse[slot(min(k0 + i * GROUPS, pieces - 1)) * RB + RW * rw + srow];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (k0 + i * GROUPS < pieces) weight[(k0 + i * GROUPS) * RW + srow] = x[i];
+            top = fmaxf(top, x[i]);
         }
-        sm_top[threadIdx.x] = top;
-        sm_sum[threadIdx.x] = sum;
+    }
+    sm_red[group][srow] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) top = fmaxf(top, sm_red[i][srow]);
+    __syncthreads();
+    const float use = top == -INFINITY ? 0.f : top;
+    float wsum = 0.f;
+    for (int32_t k = group; k < pieces; k += GROUPS) {       // (the thread's own)
+        const float w = __builtin_amdgcn_exp2f(weight[k * RW + srow] - use);
+        weight[k * RW + srow] = w;
+        wsum += w;
+    }
+    sm_red[group][srow] = wsum;
+    __syncthreads();
+    if (group == 0) {
+        wsum = 0.f;
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i) wsum += sm_red[i][srow];
+        sm_top[srow] = top;
+        sm_sum[srow] = wsum;
     }
     __syncthreads();
-    for (int32_t i = threadIdx.x; i < MINE; i += 256) {
-        // float4 j of a wave's partial: lane j % 64 holds row j % RW, four columns of every 4 * 64 / RW
-        const int32_t j = part * MINE + i, row = j % RW, c = 4 * (j / RW), r = r0 + row;
+    // float4 j of a wave's partial: lane j % 64 holds row j % RW, four columns of every 4 * 64 / RW.  Each of the four waves takes
+    // every fourth piece, several pieces at a time; then they meet in LDS.
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane % RW;
+    const float4* const po = reinterpret_cast<const float4*>(a.part_o) + rw * VECS + part * MINE + lane;
+    float4 acc[LINES];
+#pragma unroll
+    for (int i = 0; i < LINES; ++i) acc[i] = float4{0.f, 0.f, 0.f, 0.f};
+    constexpr int DEEP = LINES > 2 ? 2 : 8 / LINES;          // pieces at a time
+    for (int32_t k0 = wave; k0 < pieces; k0 += 4 * DEEP) {
+        float4 v[DEEP][LINES];
+#pragma unroll
+        for (int k = 0; k < DEEP; ++k)
+#pragma unroll
+            for (int i = 0; i < LINES; ++i) v[k][i] = po[slot(min(k0 + 4 * k, pieces - 1)) * (WR * VECS) + 64 * i];
+#pragma unroll
+        for (int k = 0; k < DEEP; ++k) {
+            if (k0 + 4 * k >= pieces) break;
+            const float w = weight[(k0 + 4 * k) * RW + row];
+#pragma unroll
+            for (int i = 0; i < LINES; ++i)
+                acc[i] = float4{__builtin_fmaf(w, v[k][i].x, acc[i].x), __builtin_fmaf(w, v[k][i].y, acc[i].y),
+                                __builtin_fmaf(w, v[k][i].z, acc[i].z), __builtin_fmaf(w, v[k][i].w, acc[i].w)};
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < LINES; ++i) sm_acc[wave][i][lane] = acc[i];
+    __syncthreads();
+    for (int32_t i = wave; i < LINES; i += 4) {
+        const int32_t j = part * MINE + 64 * i + lane, c = 4 * (j / RW), r = r0 + row;
         if (r >= n_rows || c >= d) continue;
-        const float4* const po = reinterpret_cast<const float4*>(a.part_o) + rw * VECS + j;
-        float4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int32_t k0 = 0; k0 < pieces; k0 += 4) {
-            float4 v[4];
+        float4 x = sm_acc[0][i][lane];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = po[slot(min(k0 + k, pieces - 1)) * (WR * VECS)];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (k0 + k >= pieces) break;
-                const float w = weight[(k0 + k) * RW + row];
-                acc.x = __builtin_fmaf(w, v[k].x, acc.x);
-                acc.y = __builtin_fmaf(w, v[k].y, acc.y);
-                acc.z = __builtin_fmaf(w, v[k].z, acc.z);
-                acc.w = __builtin_fmaf(w, v[k].w, acc.w);
-            }
+        for (int k = 1; k < 4; ++k) {
+            const float4 y = sm_acc[k][i][lane];
+            x = float4{x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w};
         }
         const float sum = sm_sum[row], inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
         const int64_t out_row = (int64_t)(own.row0 + r / a.group) * a.num_q_heads + kvh * a.group + r % a.group;
-        S::store(a.out, out_row * d + c, float4{acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv});
+        S::store(a.out, out_row * d + c, float4{x.x * inv, x.y * inv, x.z * inv, x.w * inv});
         if (a.lse && c == 0) a.lse[out_row] = sum == 0.f ? -INFINITY : (sm_top[row] + __builtin_amdgcn_logf(sum)) * kLn2;
     }
+}
+
+template <typename S, int PARTS>
+void launch_tree_merge(const TreeKernelArgs& a, hipStream_t stream)
+{
+    const uint32_t x = (uint32_t)((int64_t)a.batch * a.row_blocks * (S::kRows / S::kWaveRows) * PARTS);
+    hipLaunchKernelGGL((paged_attention_tree_merge_kernel<S, PARTS>), dim3(x, (uint32_t)a.cache.num_kv_heads), dim3(256),
+                       (size_t)a.wgs * S::kWaveRows * sizeof(float), stream, a, a.cu_q_lens, a.seq_lens);
 }
 
 template <typename S>
@@ -301,8 +344,12 @@ pa_status launch_tree_of(const TreeKernelArgs& a, hipStream_t stream)
 {
     const int64_t units = (int64_t)a.batch * a.row_blocks;
     const int64_t grid = (a.wgs > 0 ? a.wgs : units) * a.cache.num_kv_heads;
-    constexpr int PARTS = S::kRows / S::kWaveRows * kTreeMergeParts;
-    if (grid > 0x7fffffffLL || units * PARTS > 0x7fffffffLL || a.cache.num_kv_heads > 65535) return PA_ERR_UNSUPPORTED;
+    // A merging workgroup takes a quarter of a wave's columns, or one line of 64 vectors of them where there are few (us with quarters /
+    // lines: 2 x 8 tokens on 1500, 512 workgroups, 16.1 / 15.3, 1 x 8 on 100000 with 8 / 1 heads 41.6 / 39.3; 8 x 16 on 128 to
+    // 2048, 2048 workgroups, 22.1 / 24.4).
+    constexpr int LINES = S::kWaveRows * S::kColumns / 256;
+    const int64_t waves = units * (S::kRows / S::kWaveRows);
+    if (grid > 0x7fffffffLL || waves * LINES > 0x7fffffffLL || a.cache.num_kv_heads > 65535) return PA_ERR_UNSUPPORTED;
     {
         ProfileScope prof("paged_attention_tree_mfma_kernel", stream);
         hipLaunchKernelGGL((paged_attention_tree_mfma_kernel<S>), dim3((uint32_t)grid),
@@ -311,8 +358,8 @@ pa_status launch_tree_of(const TreeKernelArgs& a, hipStream_t stream)
         if (st != PA_OK || a.wgs == 0) return st;
     }
     ProfileScope prof("paged_attention_tree_merge_kernel", stream);
-    hipLaunchKernelGGL((paged_attention_tree_merge_kernel<S>), dim3((uint32_t)(units * PARTS), (uint32_t)a.cache.num_kv_heads),
-                       dim3(256), (size_t)a.wgs * S::kWaveRows * sizeof(float), stream, a, a.cu_q_lens, a.seq_lens);
+    if (waves * LINES * a.cache.num_kv_heads <= 512) launch_tree_merge<S, LINES>(a, stream);
+    else launch_tree_merge<S, 4>(a, stream);
     return launch_status();
 }
 
