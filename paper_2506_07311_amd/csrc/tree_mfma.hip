@@ -3,13 +3,13 @@
 
 namespace pa {
 
-pa_status launch_tree_d256(const TreeKernelArgs& a, pa_dtype dtype, int row_waves, hipStream_t stream);
-pa_status launch_tree_d128(const TreeKernelArgs& a, pa_dtype dtype, int row_waves, hipStream_t stream)
+pa_status launch_tree_d256(const TreeKernelArgs& a, pa_dtype dtype, const TreePlan& p, hipStream_t stream);
+pa_status launch_tree_d128(const TreeKernelArgs& a, pa_dtype dtype, const TreePlan& p, hipStream_t stream)
 {
-    return launch_tree_dim<128>(a, dtype, row_waves, stream);
+    return launch_tree_dim<128>(a, dtype, p, stream);
 }
-pa_status launch_tree_d96(const TreeKernelArgs& a, pa_dtype dtype, int row_waves, hipStream_t stream);
-pa_status launch_tree_d64(const TreeKernelArgs& a, pa_dtype dtype, int row_waves, hipStream_t stream);
+pa_status launch_tree_d96(const TreeKernelArgs& a, pa_dtype dtype, const TreePlan& p, hipStream_t stream);
+pa_status launch_tree_d64(const TreeKernelArgs& a, pa_dtype dtype, const TreePlan& p, hipStream_t stream);
 
 pa_status launch_tree_f32(const TreeKernelArgs& a, int row_waves, hipStream_t stream);
 
@@ -27,7 +27,7 @@ size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 // up to kPlainTiles tiles a row block is one workgroup's and there is no merge.
 TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t max_q_len, int32_t max_seq_len, bool f32)
 {
-    constexpr int32_t kPlainTiles = 8;
+    constexpr int32_t kPlainTiles = 8, kOneTermKeys = 1024;   // (see tree_mfma_impl.h)
     TreePlan p;
     const int64_t rows = (int64_t)max_q_len * (num_q_heads / num_kv_heads);
     const int32_t columns = columns_of(head_dim, f32), wave_rows = f32 ? 16 : 32;
@@ -37,6 +37,7 @@ TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int
     p.row_blocks = blocks < 1 ? 1 : (int32_t)blocks;
     const int32_t tile = f32 && columns > 128 ? 32 : prefill::kBN;
     const int64_t tiles = ((int64_t)max_seq_len + tile - 1) / tile;
+    p.two_terms = max_seq_len < kOneTermKeys;
     p.wgs = 0;
     p.part_o_bytes = p.part_lse_bytes = p.cuts_bytes = 0;
     if (tiles > kPlainTiles) {
@@ -84,11 +85,11 @@ pa_status launch_tree_mfma(const TreeArgs& t, void* workspace, hipStream_t strea
     a.scale = t.scale;
     if (t.dtype == PA_DTYPE_F32) return launch_tree_f32(a, p.row_waves, stream);
     switch (columns_of(t.cache.head_dim, false)) {
-        case 64: return launch_tree_d64(a, t.dtype, p.row_waves, stream);
-        case 96: return launch_tree_d96(a, t.dtype, p.row_waves, stream);
-        case 128: return launch_tree_d128(a, t.dtype, p.row_waves, stream);
+        case 64: return launch_tree_d64(a, t.dtype, p, stream);
+        case 96: return launch_tree_d96(a, t.dtype, p, stream);
+        case 128: return launch_tree_d128(a, t.dtype, p, stream);
     }
-    return launch_tree_d256(a, t.dtype, p.row_waves, stream);
+    return launch_tree_d256(a, t.dtype, p, stream);
 }
 
 }  // namespace pa

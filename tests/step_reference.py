@@ -67,9 +67,11 @@ def rope(x, positions, inv_freq, interleaved, mscale):
     return out
 
 
-def tree_attention(k, v, q, mask, ctx, scale):
-    """One sequence: k, v [len, hkv, d], q [n, hq, d], mask [n, n] (query, drafted key).  Returns out, lse."""
+def tree_attention(k, v, q, mask, ctx, scale, spread=False):
+    """One sequence: k, v [len, hkv, d], q [n, hq, d], mask [n, n] (query, drafted key).  Returns out, lse; and with spread
+    sqrt(sum p^2 v^2) / sum p, what independent relative errors of the weights p, of deviation 1, do to out."""
     n, hq, d = q.shape
+    wide = np.zeros((n, hq, d))
     G = hq // k.shape[1]
     seen = np.concatenate([np.ones((n, ctx), bool), np.asarray(mask, bool)], 1)
     out, lse = np.zeros((n, hq, d)), np.full((n, hq), -np.inf)
@@ -83,7 +85,8 @@ def tree_attention(k, v, q, mask, ctx, scale):
             p = np.exp(x - m)
             out[i, h] = p @ v[j, h // G] / p.sum()
             lse[i, h] = m + np.log(p.sum())
-    return out, lse
+            wide[i, h] = np.sqrt(p ** 2 @ v[j, h // G] ** 2) / p.sum()
+    return (out, lse, wide) if spread else (out, lse)
 
 
 def accept(parents, tokens, targets, max_path):
