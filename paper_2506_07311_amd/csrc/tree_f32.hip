@@ -68,7 +68,7 @@ __device__ __forceinline__ bool Tree32<WR, DP>::work(char* buf, uint32_t* flags,
     // row (pieces that head_dim does not have repeat others)
     constexpr int RPI = 1024 / ROWB, PPR = ROWB / 16, STEP = NW * RPI;
     const int frow = RPI * wave + lane / PPR;
-    const uint32_t head_off = (uint32_t)(kvh * a.cache.head_stride * 4), lds0 = lds_address(buf) + 1024 * wave;
+    const uint32_t lds0 = lds_address(buf) + 1024 * wave;
     int32_t pages[NB - 1][kLoads];
     auto load_pages = [&](int b, int32_t t0) {
 #pragma unroll
@@ -82,9 +82,9 @@ __device__ __forceinline__ bool Tree32<WR, DP>::work(char* buf, uint32_t* flags,
         for (int i = 0; i < kLoads; ++i) {
             const int row = frow + STEP * i;
             const int32_t slot = min(t0 + row, last_key) & (a.cache.page_size - 1);
-            int64_t page_off = (int64_t)pages[p][i] * a.cache.page_stride * 4;
+            int64_t page_off = ((int64_t)pages[p][i] * a.cache.page_stride + kvh * a.cache.head_stride) * 4;
             asm volatile("" : "+s"(page_off));               // stays in scalar registers
-            const uint32_t off = (uint32_t)slot * (uint32_t)(a.cache.token_stride * 4) + head_off;
+            const uint32_t off = (uint32_t)slot * (uint32_t)(a.cache.token_stride * 4);
             const uint32_t pk = (uint32_t)piece_k(lane % PPR, row) % (uint32_t)(d / 4), pv = (uint32_t)piece_v(lane % PPR, row) % (uint32_t)(d / 4);
             load_to_lds16(lds0 + b * kBufB, 1024 * NW * i, reinterpret_cast<const char*>(a.cache.k) + page_off, off + 16 * pk);
             load_to_lds16(lds0 + b * kBufB, 1024 * NW * i + kTileB, reinterpret_cast<const char*>(a.cache.v) + page_off, off + 16 * pv);
@@ -259,20 +259,20 @@ __device__ __forceinline__ bool Tree32<WR, DP>::work(char* buf, uint32_t* flags,
 }
 
 template <int DP>
-pa_status launch_rows(const TreeKernelArgs& a, int row_waves, hipStream_t stream)
+pa_status launch_rows(const TreeKernelArgs& a, bool merge, int row_waves, hipStream_t stream)
 {
     if constexpr (DP <= 128)
-        if (row_waves == 1) return launch_tree_of<Tree32<1, DP>>(a, stream);
-    if (row_waves == 2) return launch_tree_of<Tree32<2, DP>>(a, stream);
-    return launch_tree_of<Tree32<4, DP>>(a, stream);
+        if (row_waves == 1) return launch_tree_of<Tree32<1, DP>>(a, merge, stream);
+    if (row_waves == 2) return launch_tree_of<Tree32<2, DP>>(a, merge, stream);
+    return launch_tree_of<Tree32<4, DP>>(a, merge, stream);
 }
 
 }  // namespace
 
-pa_status launch_tree_f32(const TreeKernelArgs& a, int row_waves, hipStream_t stream)
+pa_status launch_tree_f32(const TreeKernelArgs& a, bool merge, int row_waves, hipStream_t stream)
 {
     const int32_t d = a.cache.head_dim;
-    return d <= 64 ? launch_rows<64>(a, row_waves, stream) : d <= 128 ? launch_rows<128>(a, row_waves, stream) : launch_rows<256>(a, row_waves, stream);
+    return d <= 64 ? launch_rows<64>(a, merge, row_waves, stream) : d <= 128 ? launch_rows<128>(a, merge, row_waves, stream) : launch_rows<256>(a, merge, row_waves, stream);
 }
 
 }  // namespace pa

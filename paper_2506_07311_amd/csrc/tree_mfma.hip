@@ -3,15 +3,15 @@
 
 namespace pa {
 
-pa_status launch_tree_d256(const TreeKernelArgs& a, pa_dtype dtype, const TreePlan& p, hipStream_t stream);
-pa_status launch_tree_d128(const TreeKernelArgs& a, pa_dtype dtype, const TreePlan& p, hipStream_t stream)
+pa_status launch_tree_d256(const TreeKernelArgs& a, bool merge, pa_dtype dtype, const TreePlan& p, hipStream_t stream);
+pa_status launch_tree_d128(const TreeKernelArgs& a, bool merge, pa_dtype dtype, const TreePlan& p, hipStream_t stream)
 {
-    return launch_tree_dim<128>(a, dtype, p, stream);
+    return launch_tree_dim<128>(a, merge, dtype, p, stream);
 }
-pa_status launch_tree_d96(const TreeKernelArgs& a, pa_dtype dtype, const TreePlan& p, hipStream_t stream);
-pa_status launch_tree_d64(const TreeKernelArgs& a, pa_dtype dtype, const TreePlan& p, hipStream_t stream);
+pa_status launch_tree_d96(const TreeKernelArgs& a, bool merge, pa_dtype dtype, const TreePlan& p, hipStream_t stream);
+pa_status launch_tree_d64(const TreeKernelArgs& a, bool merge, pa_dtype dtype, const TreePlan& p, hipStream_t stream);
 
-pa_status launch_tree_f32(const TreeKernelArgs& a, int row_waves, hipStream_t stream);
+pa_status launch_tree_f32(const TreeKernelArgs& a, bool merge, int row_waves, hipStream_t stream);
 
 namespace {
 
@@ -56,7 +56,8 @@ TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int
 
 bool tree_mfma_supported(const TreeArgs& a)
 {
-    return a.cache.page_size >= 16;
+    // (a lane's offset within a page is one of 32 bits)
+    return a.cache.page_size >= 16 && a.cache.token_stride * a.cache.page_size < ((int64_t)1 << 29);
 }
 
 pa_status launch_tree_mfma(const TreeArgs& t, void* workspace, hipStream_t stream)
@@ -83,13 +84,22 @@ pa_status launch_tree_mfma(const TreeArgs& t, void* workspace, hipStream_t strea
     a.wgs = p.wgs;
     a.row_blocks = p.row_blocks;
     a.scale = t.scale;
-    if (t.dtype == PA_DTYPE_F32) return launch_tree_f32(a, p.row_waves, stream);
-    switch (columns_of(t.cache.head_dim, false)) {
-        case 64: return launch_tree_d64(a, t.dtype, p, stream);
-        case 96: return launch_tree_d96(a, t.dtype, p, stream);
-        case 128: return launch_tree_d128(a, t.dtype, p, stream);
+    auto launch = [&](bool merge) {
+        if (t.dtype == PA_DTYPE_F32) return launch_tree_f32(a, merge, p.row_waves, stream);
+        switch (columns_of(t.cache.head_dim, false)) {
+            case 64: return launch_tree_d64(a, merge, t.dtype, p, stream);
+            case 96: return launch_tree_d96(a, merge, t.dtype, p, stream);
+            case 128: return launch_tree_d128(a, merge, t.dtype, p, stream);
+        }
+        return launch_tree_d256(a, merge, t.dtype, p, stream);
+    };
+    {
+        ProfileScope prof("paged_attention_tree_mfma_kernel", stream);
+        const pa_status st = launch(false);
+        if (st != PA_OK || p.wgs == 0) return st;
     }
-    return launch_tree_d256(a, t.dtype, p, stream);
+    ProfileScope prof("paged_attention_tree_merge_kernel", stream);
+    return launch(true);
 }
 
 }  // namespace pa

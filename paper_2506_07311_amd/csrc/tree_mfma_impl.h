@@ -185,7 +185,7 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
     for (int v = 0; v < (STEP == 8 ? 2 : 1); ++v) {
         int piece = tree_piece<DP>(lane % PPR, frow + 8 * v) / 16;         // (the swizzle undoes itself)
         piece %= d / 8;
-        lane_off[v] = (uint32_t)(kvh * a.cache.head_stride * 2) + 16 * piece;
+        lane_off[v] = 16 * piece;
     }
     const uint32_t lds0 = lds_address(buf) + 1024 * wave;
     int32_t pages[NB - 1][Shape::kLoads];                    // of the rows of each instruction (16 rows and more lie in one page)
@@ -200,7 +200,7 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
 #pragma unroll
         for (int i = 0; i < Shape::kLoads; ++i) {
             const int32_t slot = min(t0 + frow + STEP * i, last_key) & (a.cache.page_size - 1);
-            int64_t page_off = (int64_t)pages[p][i] * a.cache.page_stride * 2;
+            int64_t page_off = ((int64_t)pages[p][i] * a.cache.page_stride + kvh * a.cache.head_stride) * 2;
             asm volatile("" : "+s"(page_off));               // stays in scalar registers
             const uint32_t off = (uint32_t)slot * (uint32_t)(a.cache.token_stride * 2) + lane_off[STEP == 8 ? i & 1 : 0];
             load_to_lds16(lds0 + b * Geo::kBufB, 1024 * NW * i, reinterpret_cast<const char*>(a.cache.k) + page_off, off);
@@ -412,25 +412,25 @@ struct Tree16 {
 };
 
 template <bool TWO, typename E, int DP>
-pa_status launch_tree_rows(const TreeKernelArgs& a, int row_waves, hipStream_t stream)
+pa_status launch_tree_rows(const TreeKernelArgs& a, bool merge, int row_waves, hipStream_t stream)
 {
     if constexpr (DP <= 128)
-        if (row_waves == 8) return launch_tree_of<Tree16<8, TWO, E, DP>>(a, stream);
-    return launch_tree_of<Tree16<4, TWO, E, DP>>(a, stream);
+        if (row_waves == 8) return launch_tree_of<Tree16<8, TWO, E, DP>>(a, merge, stream);
+    return launch_tree_of<Tree16<4, TWO, E, DP>>(a, merge, stream);
 }
 
 template <typename E, int DP>
-pa_status launch_tree_type(const TreeKernelArgs& a, int row_waves, bool two_terms, hipStream_t stream)
+pa_status launch_tree_type(const TreeKernelArgs& a, bool merge, int row_waves, bool two_terms, hipStream_t stream)
 {
-    if (row_waves == 2) return launch_tree_of<Tree16<2, true, E, DP>>(a, stream);
-    return two_terms ? launch_tree_rows<true, E, DP>(a, row_waves, stream) : launch_tree_rows<false, E, DP>(a, row_waves, stream);
+    if (row_waves == 2) return launch_tree_of<Tree16<2, true, E, DP>>(a, merge, stream);
+    return two_terms ? launch_tree_rows<true, E, DP>(a, merge, row_waves, stream) : launch_tree_rows<false, E, DP>(a, merge, row_waves, stream);
 }
 
 template <int DP>
-pa_status launch_tree_dim(const TreeKernelArgs& a, pa_dtype dtype, const TreePlan& p, hipStream_t stream)
+pa_status launch_tree_dim(const TreeKernelArgs& a, bool merge, pa_dtype dtype, const TreePlan& p, hipStream_t stream)
 {
-    return dtype == PA_DTYPE_BF16 ? launch_tree_type<ElemBf16, DP>(a, p.row_waves, p.two_terms, stream)
-                                  : launch_tree_type<ElemF16, DP>(a, p.row_waves, p.two_terms, stream);
+    return dtype == PA_DTYPE_BF16 ? launch_tree_type<ElemBf16, DP>(a, merge, p.row_waves, p.two_terms, stream)
+                                  : launch_tree_type<ElemF16, DP>(a, merge, p.row_waves, p.two_terms, stream);
 }
 
 }  // namespace

@@ -88,7 +88,7 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeKernelArgs& a, int32_t i)
         q.row0 = a.cu_q_lens[i];
         q.n = a.cu_q_lens[i + 1] - q.row0;
         q.len = a.seq_lens[i];
-        q.blocks = q.n > 0 ? (q.n * a.group + S::kRows - 1) / S::kRows : 0;
+        q.blocks = q.n > 0 ? min((q.n * a.group + S::kRows - 1) / S::kRows, a.row_blocks) : 0;   // (n keeps to its bound)
         q.tiles = (q.len + S::kTile - 1) / S::kTile;
     }
     return q;
@@ -339,27 +339,25 @@ void launch_tree_merge(const TreeKernelArgs& a, hipStream_t stream)
                        (size_t)a.wgs * S::kWaveRows * sizeof(float), stream, a, a.cu_q_lens, a.seq_lens);
 }
 
+// The attention kernel, or the merge behind it.
 template <typename S>
-pa_status launch_tree_of(const TreeKernelArgs& a, hipStream_t stream)
+pa_status launch_tree_of(const TreeKernelArgs& a, bool merge, hipStream_t stream)
 {
     const int64_t units = (int64_t)a.batch * a.row_blocks;
     const int64_t grid = (a.wgs > 0 ? a.wgs : units) * a.cache.num_kv_heads;
-    // A merging workgroup takes a quarter of a wave's columns, or one line of 64 vectors of them where there are few (us with quarters /
-    // lines: 2 x 8 tokens on 1500, 512 workgroups, 16.1 / 15.3, 1 x 8 on 100000 with 8 / 1 heads 41.6 / 39.3; 8 x 16 on 128 to
-    // 2048, 2048 workgroups, 22.1 / 24.4).
-    constexpr int LINES = S::kWaveRows * S::kColumns / 256;
+    // A merging workgroup takes four lines of 64 vectors of a wave's columns (a quarter of them at 128 columns of 32 rows), or one where
+    // there are few (us with four / one: 2 x 8 tokens on 1500, 512 workgroups, 16.1 / 15.3, 1 x 8 on 100000 with 8 / 1
+    // heads 41.6 / 39.3; 8 x 16 on 128 to 2048, 2048 workgroups, 22.1 / 24.4).
+    constexpr int LINES = S::kWaveRows * S::kColumns / 256, PARTS = LINES > 4 ? LINES / 4 : 1;
     const int64_t waves = units * (S::kRows / S::kWaveRows);
     if (grid > 0x7fffffffLL || waves * LINES > 0x7fffffffLL || a.cache.num_kv_heads > 65535) return PA_ERR_UNSUPPORTED;
-    {
-        ProfileScope prof("paged_attention_tree_mfma_kernel", stream);
-        hipLaunchKernelGGL((paged_attention_tree_mfma_kernel<S>), dim3((uint32_t)grid),
-                           dim3(64 * S::kWaves), 0, stream, a, a.cu_q_lens, a.seq_lens, a.block_table, a.tree_mask);
-        const pa_status st = launch_status();
-        if (st != PA_OK || a.wgs == 0) return st;
+    if (merge) {
+        if (waves * LINES * a.cache.num_kv_heads <= 512) launch_tree_merge<S, LINES>(a, stream);
+        else launch_tree_merge<S, PARTS>(a, stream);
+    } else {
+        hipLaunchKernelGGL((paged_attention_tree_mfma_kernel<S>), dim3((uint32_t)grid), dim3(64 * S::kWaves), 0, stream, a,
+                           a.cu_q_lens, a.seq_lens, a.block_table, a.tree_mask);
     }
-    ProfileScope prof("paged_attention_tree_merge_kernel", stream);
-    if (waves * LINES * a.cache.num_kv_heads <= 512) launch_tree_merge<S, LINES>(a, stream);
-    else launch_tree_merge<S, 4>(a, stream);
     return launch_status();
 }
 
