@@ -274,7 +274,8 @@ pa_status paged_decode_step(const pa_kv_cache_desc* cache, const void* k_new, co
  * shortage int32[2]: [0] pages that the free list lacks, [1] sequences whose blocks exceed max_blocks or whose tokens
  * exceed the masks' bits, plus rows beyond max_rows.  Unless both are 0 nothing is granted: table, counts and free
  * list stay as they were, seq_lens = ctx_lens, cu_q_lens = 0 (attention then has nothing to do); the rows' arrays describe
- * the request all the same.  No output may overlap another array.
+ * the request all the same, so a table whose entries from num_blocks[s] on are -1 keeps an append of them within the
+ * sequence's own pages.  No output may overlap another array.  batch 0: nothing is done.
  */
 pa_status paged_plan_step(const int32_t* ctx_lens, const int32_t* new_lens, int32_t batch, const int32_t* parents,
                           int32_t page_size, int32_t* block_table, int32_t max_blocks, int32_t* num_blocks,
@@ -344,6 +345,9 @@ pa_status paged_rope_append(const pa_kv_cache_desc* cache, const void* q, int64_
  * tree_mask: uint64[total_q, mask_words], 64 * mask_words >= max_q_len (host upper bound of n).  q, out [total_q, Hq, d],
  * lse NULL or float[total_q, Hq]; rows behind cu_q_lens[batch] are left as they were.  Workspace as for decode, of at least
  * paged_attention_tree_workspace_bytes.  Any cache the library takes.  Results repeat bit for bit with the same arguments.
+ * fp32 arithmetic; of 16-bit pools the weights (at most 1) enter the product with V as two 16-bit terms, exact to 2^-16 or
+ * better, but with more than 64 rows (max_q_len x query heads of a KV head) and max_seq_len >= 1024 as one: each weight is then
+ * off by half a step of its type, of a sum whose own rounding to the output is as large.
  */
 size_t paged_attention_tree_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                             int32_t total_q, int32_t max_q_len, int32_t max_seq_len);
@@ -361,7 +365,7 @@ pa_status paged_attention_tree(const pa_kv_cache_desc* cache, const void* q, voi
  * the tokens' numbers, -1 behind them, path_lens int32[batch] their count and next_tokens (may be NULL) the last one's target.
  * With all three NULL the caller's own rule has filled path and path_lens (numbers that climb; they are read only).
  * Then K and V rows of the path move together: position ctx + path[i] -> ctx + i, ctx = seq_lens[s] - n; kept_lens (may be
- * NULL, may be the plan's ctx_lens) = ctx + path_lens.  A sequence without drafted tokens: path_lens 0, next -1, kept =
+ * NULL, may be the plan's ctx_lens, not seq_lens) = ctx + path_lens.  A sequence without drafted tokens: path_lens 0, next -1, kept =
  * seq_lens.  max_q_len: host upper bound of n.  For further layers of a model call it again with their caches and the path found.
  */
 pa_status paged_tree_accept(const pa_kv_cache_desc* cache, const int32_t* cu_q_lens, const int32_t* seq_lens, int32_t batch,

@@ -31,6 +31,7 @@ pa_status paged_plan_step(const int32_t* ctx_lens, const int32_t* new_lens, int3
         return PA_ERR_INVALID_ARG;
     if (max_rows > 0 && (!seq_ids || !positions)) return PA_ERR_INVALID_ARG;
     if (tree_mask && (mask_words == 0 || ((uintptr_t)tree_mask & 7))) return PA_ERR_INVALID_ARG;
+    if (seq_lens == ctx_lens || seq_lens == new_lens) return PA_ERR_INVALID_ARG;   // (read while they are written)
     StepPlanArgs p = {ctx_lens, new_lens, parents, free_pages, batch, page_size, max_blocks, max_rows, mask_words, block_table,
                       num_blocks, free_count, seq_lens, cu_q_lens, seq_ids, positions, rope_positions, tree_mask, shortage};
     return launch_plan_step(p, stream_of(stream));
@@ -162,6 +163,7 @@ pa_status paged_tree_accept(const pa_kv_cache_desc* cache, const int32_t* cu_q_l
     if (!tokens != !targets || !tokens != !parents || (!tokens && next_tokens)) return PA_ERR_INVALID_ARG;
     if (batch == 0) return PA_OK;
     if (!cu_q_lens || !seq_lens || !path || !path_lens || !block_table || max_blocks == 0) return PA_ERR_INVALID_ARG;
+    if (kept_lens == seq_lens) return PA_ERR_INVALID_ARG;     // (read while they are written)
     const int32_t cap = max_path < max_q_len ? max_path : max_q_len > 0 ? max_q_len : 1;
     if (cap > kMaxPath) return PA_ERR_UNSUPPORTED;
     TreeAcceptArgs t = {cu_q_lens, seq_lens, parents, tokens, targets, block_table, path, path_lens, next_tokens, kept_lens, batch,

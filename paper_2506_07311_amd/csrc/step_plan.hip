@@ -66,9 +66,9 @@ struct PlanArgs {
     int32_t batch, max_blocks, log2_page, max_rows, mask_words;
 };
 
-__device__ __forceinline__ int32_t blocks_for(int32_t tokens, int32_t log2_page)
+__device__ __forceinline__ int32_t blocks_for(int64_t tokens, int32_t log2_page)
 {
-    return (int32_t)(((int64_t)tokens + (1 << log2_page) - 1) >> log2_page);
+    return (int32_t)((tokens + (1 << log2_page) - 1) >> log2_page);
 }
 
 // Workgroup 0: everything that is one value a sequence, and the pages.  It alone writes what it and the others read
@@ -90,9 +90,10 @@ __device__ __forceinline__ void plan_sequences(const PlanArgs& a)
             rows = max(a.new_lens[s], 0);
             ctx = a.ctx_lens[s];
             have = a.num_blocks[s];
-            const int32_t want = blocks_for(ctx + rows, a.log2_page);
+            const int64_t tokens = (int64_t)ctx + rows;
+            const int32_t want = blocks_for(tokens, a.log2_page);
             need = max(want - have, 0);
-            late = want > a.max_blocks || (a.tree_mask && rows > 64 * a.mask_words);
+            late = want > a.max_blocks || tokens > 0x7fffffff || (a.tree_mask && rows > 64LL * a.mask_words);
         }
         row_end = group_scan<N>(rows, sm, rows_here);
         need_end = group_scan<N>(need, sm, pages_here);

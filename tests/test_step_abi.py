@@ -39,12 +39,13 @@ def call(fn, args, **change):
 
 
 def test_plan_refusals(lib):
+    L = ctypes.c_void_p(0x6000)                                   # (lengths that are written are not those that are read)
     a = dict(ctx=P, new=P, batch=i32(2), parents=NULL, page=i32(16), table=P, max_blocks=i32(4), num=P, free=P, count=P, rows=i32(8),
-             seq_lens=P, cu=P, ids=P, pos=P, rope=NULL, mask=P, words=i32(1), shortage=P, stream=NULL)
+             seq_lens=L, cu=P, ids=P, pos=P, rope=NULL, mask=P, words=i32(1), shortage=P, stream=NULL)
     for bad in (dict(batch=i32(-1)), dict(page=i32(0)), dict(page=i32(12)), dict(max_blocks=i32(0)), dict(max_blocks=i32(-1)),
                 dict(rows=i32(-1)), dict(words=i32(0)), dict(words=i32(-1)), dict(mask=ctypes.c_void_p(0x4004)), dict(ctx=NULL),
                 dict(new=NULL), dict(table=NULL), dict(num=NULL), dict(free=NULL), dict(count=NULL), dict(seq_lens=NULL),
-                dict(cu=NULL), dict(ids=NULL), dict(pos=NULL), dict(shortage=NULL)):
+                dict(cu=NULL), dict(ids=NULL), dict(pos=NULL), dict(shortage=NULL), dict(seq_lens=P), dict(ctx=L), dict(new=L)):
         assert call(lib.paged_plan_step, a, **bad) == INVALID, bad
     assert call(lib.paged_plan_step, a, batch=i32(0)) == 0
     r = dict(keep=P, batch=i32(2), page=i32(16), table=P, max_blocks=i32(4), num=P, free=P, count=P, max_free=i32(9), stream=NULL)
@@ -96,11 +97,11 @@ def test_tree_workspace_bound(lib):
 
 def test_accept_refusals(lib):
     a = dict(cache=desc(), cu=P, lens=P, batch=i32(2), max_q=i32(8), parents=P, tokens=P, targets=P, path=P, max_path=i32(8),
-             path_lens=P, nxt=P, kept=P, table=P, max_blocks=i32(4), stream=NULL)
+             path_lens=P, nxt=P, kept=ctypes.c_void_p(0x6000), table=P, max_blocks=i32(4), stream=NULL)
     fn = lib.paged_tree_accept
     for bad in (dict(batch=i32(-1)), dict(max_q=i32(-1)), dict(max_path=i32(0)), dict(parents=NULL), dict(tokens=NULL),
                 dict(targets=NULL), dict(parents=NULL, tokens=NULL, targets=NULL), dict(path=NULL), dict(path_lens=NULL),
-                dict(cu=NULL), dict(lens=NULL), dict(table=NULL), dict(max_blocks=i32(0)), dict(cache=desc(k_cache=0))):
+                dict(cu=NULL), dict(lens=NULL), dict(table=NULL), dict(max_blocks=i32(0)), dict(cache=desc(k_cache=0)), dict(kept=P)):
         assert call(fn, a, **bad) == INVALID, bad
     assert call(fn, a, max_q=i32(9000), max_path=i32(9000)) == UNSUPPORTED
     assert call(fn, a, batch=i32(0)) == 0
