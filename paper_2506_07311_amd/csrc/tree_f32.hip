@@ -3,11 +3,18 @@
 // As for the 16-bit pools (tree_mfma_impl.h), in v_mfma_f32_16x16x4 tiles, lane % 16 = row:
 //     S^T[key, row] = K Q^T,   O^T[column, row] += V^T P^T.
 // An fp32 product costs 16 times a 16-bit one, so the call is bound by its 4 * rows * d flops a key from about 16 rows a (sequence,
-// KV head) on, and waves of 16 rows waste the fewest of them on rows that are not there; up to 16 rows the four waves of a
-// workgroup take 16 of a tile's 64 keys each, up to 32 two waves share 16 rows.  Since any order of a contraction's index serves, a lane
-// reads 16 bytes of a K row for four products (product e takes element e of each lane's four), and P^T is the second
-// product's operand as the first one leaves it: step r takes keys 4 g + r, of lane group g.  A tile's K rows are swizzled for
+// KV head) on, and waves of 16 rows waste the fewest of them on rows that are not there.  A workgroup's eight waves, two a matrix
+// core, take 128 rows, or 64 or 32 with two or four waves beside each other along a tile's 64 keys; up to 16 rows four waves
+// take 16 keys each (more would find no keys), and above 128 columns there are four, since a wave's O and Q fill its registers.
+// What a wave takes of a tile it takes at once: all its score products, their softmax, all products with V, so that few gaps
+// are left between matrix instructions.  Since any order of a contraction's index serves, a lane reads 16 bytes of a K row for
+// four products (product e takes element e of each lane's four), and P^T is the second product's operand as the first one leaves
+// it: step r takes keys 4 g + r, of lane group g.  Operands are read ahead of their products.  A tile's K rows are swizzled for
 // reads of one 16-byte piece of 16 rows, its V rows for reads of 16 columns of rows 4 apart.
+//
+// us (TFLOP/s, of the 157 that the matrix cores have) with 32 / 8 heads of 128: 8 x 64 tokens on 2048 174 (99), 8 x 16 65 (66), 8 x 8
+// 45; with four waves, 64 rows and operands read when needed 232, 88, 54; eight waves alone 232, 81, 51; operands ahead 193, 69,
+// 45; 32 keys at once 181, 65, 45.
 #include "tree_share.h"
 
 namespace pa {
@@ -18,9 +25,10 @@ typedef mfma_f32x4 f32x4;
 
 template <int WR, int DP>
 struct Tree32 {
-    static constexpr int kWaves = 4, kOcc = 1, kRows = 16 * WR, kWaveRows = 16, kColumns = DP;
+    static constexpr int kWaves = WR > 1 && DP <= 128 ? 8 : 4, kOcc = 1, kRows = 16 * WR, kWaveRows = 16, kColumns = DP;
     static constexpr int kTile = DP > 128 ? 32 : 64;
-    static constexpr int kKW = 4 / WR < kTile / 16 ? 4 / WR : kTile / 16;        // waves that share 16 rows
+    static constexpr int kKW = kWaves / WR < kTile / 16 ? kWaves / WR : kTile / 16;        // waves that share 16 rows
+    static constexpr int kSubs = kTile / 16 / kKW;                               // times 16 keys of a tile that a wave takes
     static constexpr int kRowB = 4 * DP, kTileB = kTile * kRowB, kBufB = 2 * kTileB;
     static constexpr int kBufs = DP > 64 ? 2 : 4, kLds = kBufs * kBufB;
     static constexpr int kLoads = kTileB / (1024 * kWaves);
@@ -40,7 +48,7 @@ template <int WR, int DP>
 template <bool CAREFUL>
 __device__ __forceinline__ bool Tree32<WR, DP>::work(char* buf, uint32_t* flags, const TreeKernelArgs& a, const TreeItem& it, int32_t kvh)
 {
-    constexpr int RB = kRows, KW = kKW, NW = kWaves, NB = kBufs, ROWB = kRowB, J = DP / 16;
+    constexpr int RB = kRows, KW = kKW, NW = kWaves, NB = kBufs, ROWB = kRowB, J = DP / 16, N = kSubs;
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));                            // (what follows from it is not kept across pieces of work)
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -123,36 +131,70 @@ __device__ __forceinline__ bool Tree32<WR, DP>::work(char* buf, uint32_t* flags,
         }
         const char* const kbuf = buf + b * kBufB;
 #pragma unroll 1
-        for (int sub = kw; sub < kTile / 16; sub += KW) {
+        for (int sub = kw * N; sub < kTile / 16; sub += KW * N) {
             const int32_t key0 = t * kTile + 16 * sub;
             if (!live || key0 >= len) break;                 // (wave-uniform)
             const char* const kh = kbuf + 16 * sub * ROWB;
-            f32x4 s0 = (f32x4)(0.f), s1 = (f32x4)(0.f);
+            const char* const vh = kh + kTileB;
+            constexpr int AHEAD = 4;
+            f32x4 kf[AHEAD];
+            auto read_k = [&](int i) {                       // 16 keys after 16 keys
+                const int j = i % J;
+                return *reinterpret_cast<const f32x4*>(kh + (16 * (i / J) + ql) * ROWB + 16 * piece_k(4 * j + g, ql));
+            };
+            float vf[2][J];
+            auto read_v = [&](int i) {
+                const int key = 4 * g + i % 4;
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const f32x4 kf = *reinterpret_cast<const f32x4*>(kh + ql * ROWB + 16 * piece_k(4 * j + g, ql));
-                s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[0], qf[j][0], s0, 0, 0, 0);
-                s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[1], qf[j][1], s1, 0, 0, 0);
-                s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[2], qf[j][2], s0, 0, 0, 0);
-                s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[3], qf[j][3], s1, 0, 0, 0);
+                for (int c = 0; c < J; ++c)
+                    vf[i & 1][c] = *reinterpret_cast<const float*>(vh + (16 * (i / 4) + key) * ROWB + 16 * piece_v(4 * c + (ql >> 2), key) + 4 * (ql & 3));
+            };
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) kf[i] = read_k(i);
+            f32x4 s[N], p[N];
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                f32x4 s0 = (f32x4)(0.f), s1 = (f32x4)(0.f);
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    const int i = u * J + j;
+                    const f32x4 k = kf[i % AHEAD];
+                    s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[0], qf[j][0], s0, 0, 0, 0);
+                    s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[1], qf[j][1], s1, 0, 0, 0);
+                    s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[2], qf[j][2], s0, 0, 0, 0);
+                    s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[3], qf[j][3], s1, 0, 0, 0);
+                    if (i + AHEAD < N * J) kf[i % AHEAD] = read_k(i + AHEAD);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                s[u] = s0 + s1;
             }
-            f32x4 s = s0 + s1, p;
-            uint32_t vis = ~0u;
-            if (key0 + 16 > ctx) {                           // (wave-uniform: drafted keys, or the end)
-                vis = visible_keys(mask, a.mask_words, key0, ctx, len);
+            if (!CAREFUL) read_v(0);
+            __builtin_amdgcn_sched_barrier(0);
+            uint32_t vis[(N + 1) / 2];                       // 32 keys each
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[i] = (vis >> (4 * g + i)) & 1u ? s[i] : -INFINITY;
+            for (int u = 0; u < N; u += 2) vis[u / 2] = ~0u;
+            if (key0 + 16 * N > ctx) {                       // (wave-uniform: drafted keys, or the end)
+#pragma unroll
+                for (int u = 0; u < N; u += 2) vis[u / 2] = visible_keys(mask, a.mask_words, key0 + 16 * u, ctx, len);
+#pragma unroll
+                for (int u = 0; u < N; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[u][i] = (vis[u / 2] >> (16 * (u & 1) + 4 * g + i)) & 1u ? s[u][i] : -INFINITY;
             }
             // online softmax against a reference that trails the maximum
             float psum = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], sc, -m));
-                psum += p[i];
-            }
+            for (int u = 0; u < N; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    p[u][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], sc, -m));
+                    psum += p[u][i];
+                }
             if (__any(!(psum <= kWeightSumMax))) {
-                const float top = row_max<4>(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))) * sc;
-                const float m_new = fmaxf(m, top);
+                float top = -INFINITY;
+#pragma unroll
+                for (int u = 0; u < N; ++u) top = fmaxf(top, fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3])));
+                const float m_new = fmaxf(m, row_max<4>(top) * sc);
                 const float use = m_new == -INFINITY ? 0.f : m_new;
                 const float alpha = __builtin_amdgcn_exp2f(m - use);
 #pragma unroll
@@ -161,37 +203,38 @@ __device__ __forceinline__ bool Tree32<WR, DP>::work(char* buf, uint32_t* flags,
                 m = m_new;
                 psum = 0.f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], sc, -use));
-                    psum += p[i];
-                }
+                for (int u = 0; u < N; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        p[u][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], sc, -use));
+                        psum += p[u][i];
+                    }
             }
             l += psum;
-            const char* const vh = kh + kTileB;
             if (CAREFUL) {
                 // key by key on the vector unit, each only to the rows that see it
+#pragma unroll
+                for (int u = 0; u < N; ++u)
 #pragma unroll 1
-                for (int k = 0; k < 16; ++k) {
-                    const float own = (k & 2) ? ((k & 1) ? p[3] : p[2]) : ((k & 1) ? p[1] : p[0]);
-                    const float w = __shfl(own, ql + 16 * (k >> 2), 64);
-                    const bool seen = (vis >> k) & 1u;
+                    for (int k = 0; k < 16; ++k) {
+                        const float own = (k & 2) ? ((k & 1) ? p[u][3] : p[u][2]) : ((k & 1) ? p[u][1] : p[u][0]);
+                        const float w = __shfl(own, ql + 16 * (k >> 2), 64);
+                        const bool seen = (vis[u / 2] >> (16 * (u & 1) + k)) & 1u;
 #pragma unroll
-                    for (int c = 0; c < J; ++c) {
-                        const f32x4 v = *reinterpret_cast<const f32x4*>(vh + k * ROWB + 16 * piece_v(4 * c + g, k));
+                        for (int c = 0; c < J; ++c) {
+                            const f32x4 v = *reinterpret_cast<const f32x4*>(vh + (16 * u + k) * ROWB + 16 * piece_v(4 * c + g, k));
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) o[c][e] = seen ? __builtin_fmaf(w, v[e], o[c][e]) : o[c][e];
+                            for (int e = 0; e < 4; ++e) o[c][e] = seen ? __builtin_fmaf(w, v[e], o[c][e]) : o[c][e];
+                        }
                     }
-                }
                 continue;
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int key = 4 * g + i;
+            for (int i = 0; i < 4 * N; ++i) {
+                if (i < 4 * N - 1) read_v(i + 1);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int c = 0; c < J; ++c) {
-                    const float v = *reinterpret_cast<const float*>(vh + key * ROWB + 16 * piece_v(4 * c + (ql >> 2), key) + 4 * (ql & 3));
-                    o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[i], o[c], 0, 0, 0);
-                }
+                for (int c = 0; c < J; ++c) o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i & 1][c], p[i / 4][i % 4], o[c], 0, 0, 0);
             }
         }
         b = b == NB - 1 ? 0 : b + 1;
@@ -261,8 +304,10 @@ __device__ __forceinline__ bool Tree32<WR, DP>::work(char* buf, uint32_t* flags,
 template <int DP>
 pa_status launch_rows(const TreeKernelArgs& a, bool merge, int row_waves, hipStream_t stream)
 {
-    if constexpr (DP <= 128)
+    if constexpr (DP <= 128) {
         if (row_waves == 1) return launch_tree_of<Tree32<1, DP>>(a, merge, stream);
+        if (row_waves == 8) return launch_tree_of<Tree32<8, DP>>(a, merge, stream);
+    }
     if (row_waves == 2) return launch_tree_of<Tree32<2, DP>>(a, merge, stream);
     return launch_tree_of<Tree32<4, DP>>(a, merge, stream);
 }

@@ -23,20 +23,25 @@ size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 // 16-bit pools: up to 64 rows a (sequence, KV head) two waves share 32 rows, up to 128 at head_dims up to 128 as well, with eight
 // waves; beyond that a workgroup takes 256 rows (128 above head_dim 128, where a wave's O and Q fill its registers).  fp32 pools: 16 rows a
-// wave, 16, 32 or 64 a workgroup.  The tiles are shared by as many workgroups as the machine holds at once; on contexts of
-// up to kPlainTiles tiles a row block is one workgroup's and there is no merge.
+// wave, 16, 32, 64 or 128 a workgroup.  The tiles are shared by as many workgroups as the machine holds at once; on contexts of
+// up to kPlainTiles tiles a row block is one workgroup's and there is no merge, and row blocks are then made smaller, down to two waves of
+// rows, until there is one for each compute unit (us with / without: bf16 3 x 40 tokens on 400 14.1 / 24.6, 16 x 40 on 350 20.1 / 26.3,
+// fp32 3 x 40 on 400 27.7 / 65; until there are two for each: 32 x 40 on 350 37.9 / 30.7, fp32 8 x 64 on 300 49 / 37.8).
 TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t max_q_len, int32_t max_seq_len, bool f32)
 {
     constexpr int32_t kPlainTiles = 8, kOneTermKeys = 1024;   // (see tree_mfma_impl.h)
     TreePlan p;
     const int64_t rows = (int64_t)max_q_len * (num_q_heads / num_kv_heads);
     const int32_t columns = columns_of(head_dim, f32), wave_rows = f32 ? 16 : 32;
-    if (f32) p.row_waves = rows <= 16 && columns <= 128 ? 1 : rows <= 32 ? 2 : 4;
+    if (f32) p.row_waves = rows <= 16 && columns <= 128 ? 1 : rows <= 32 ? 2 : rows <= 64 || columns > 128 ? 4 : 8;
     else p.row_waves = rows <= 64 ? 2 : rows <= 128 || columns > 128 ? 4 : 8;
-    const int64_t blocks = (rows + wave_rows * p.row_waves - 1) / (wave_rows * p.row_waves);
-    p.row_blocks = blocks < 1 ? 1 : (int32_t)blocks;
+    auto blocks_of = [&](int32_t waves) { return (rows + wave_rows * waves - 1) / (wave_rows * waves); };
     const int32_t tile = f32 && columns > 128 ? 32 : prefill::kBN;
     const int64_t tiles = ((int64_t)max_seq_len + tile - 1) / tile;
+    if (tiles <= kPlainTiles)
+        while (p.row_waves > 2 && (int64_t)batch * num_kv_heads * blocks_of(p.row_waves) < device_cus()) p.row_waves /= 2;
+    const int64_t blocks = blocks_of(p.row_waves);
+    p.row_blocks = blocks < 1 ? 1 : (int32_t)blocks;
     p.two_terms = max_seq_len < kOneTermKeys;
     p.wgs = 0;
     p.part_o_bytes = p.part_lse_bytes = p.cuts_bytes = 0;
