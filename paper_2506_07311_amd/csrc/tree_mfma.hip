@@ -69,6 +69,8 @@ pa_status launch_tree_mfma(const TreeArgs& t, void* workspace, hipStream_t strea
 {
     const TreePlan p = plan_tree(t.batch, t.num_q_heads, t.cache.num_kv_heads, t.cache.head_dim, t.max_q_len, t.max_seq_len,
                                  t.dtype == PA_DTYPE_F32);
+    // (places of a KV head are counted in 32 bits)
+    if ((int64_t)t.batch * p.row_blocks * (t.max_seq_len / 32 + 1 + kTreePieceTiles) > 0x7fffffff) return PA_ERR_UNSUPPORTED;
     TreeKernelArgs a;
     a.cache = t.cache;
     a.q = t.q;

@@ -325,73 +325,77 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
         b = b == NB - 1 ? 0 : b + 1;
     }
 
-    bool again = false;
+    // Vector i of a wave's O is four columns of its rows.  Two waves that share rows exchange halves of theirs through a buffer that no
+    // tile is in (buffers b on, but for the last tile's), so both join and store.
+    l += __shfl_xor(l, 32, 64);
+    constexpr int VECS = 4 * T, MINE = VECS / KW;
+    auto vec = [&](int i) { return float4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]}; };
+    float4* const met = reinterpret_cast<float4*>(buf + (b + rw / 2) % NB * Geo::kBufB) + rw % 2 * (VECS * 64) + lane;
+    float2* const ml = reinterpret_cast<float2*>(buf + NB * Geo::kBufB) + rw * 128 + lane;
     if (!CAREFUL) {
-        bool odd = false;
+        float odd[4] = {0.f, 0.f, 0.f, 0.f};                 // (0 times what is not finite is NaN)
 #pragma unroll
         for (int t = 0; t < T; ++t)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) odd |= !(__builtin_fabsf(o[t][i]) <= 3.402823466e38f);
-        const bool any = __any(odd);
+            for (int i = 0; i < 16; ++i) odd[i % 4] = __builtin_fmaf(o[t][i], 0.f, odd[i % 4]);
+        const bool any = __any(!((odd[0] + odd[1]) + (odd[2] + odd[3]) == 0.f));
         if (lane == 0) flags[wave] = any ? 1u : 0u;
+    }
+    if (KW == 2) {
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+            if (kw == 0) met[(MINE + i) * 64] = vec(VECS - MINE + i);
+            else met[i * 64] = vec(i);
+        }
+        ml[kw * 64] = float2{m, l};
     }
     __syncthreads();                                         // (the tile buffers are free)
     if (!CAREFUL) {
+        bool again = false;
 #pragma unroll
         for (int w = 0; w < NW; ++w) again |= flags[w] != 0;
         if (again) return true;
     }
-    l += __shfl_xor(l, 32, 64);
-    if (KW == 2) {                                           // the two waves of 32 rows meet
-        float4* const po = reinterpret_cast<float4*>(buf) + rw * (T * 4 + 1) * 64;
-        if (kw == 1) {
+    float4 mine[MINE];
 #pragma unroll
-            for (int i = 0; i < 4 * T; ++i)
-                po[i * 64 + lane] = float4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
-            po[4 * T * 64 + lane] = float4{m, l, 0.f, 0.f};
-        }
-        __syncthreads();
-        if (kw == 0) {
-            const float4 ml = po[4 * T * 64 + lane];
-            const float top = fmaxf(m, ml.x), use = top == -INFINITY ? 0.f : top;
-            const float wa = __builtin_amdgcn_exp2f(m - use), wb = __builtin_amdgcn_exp2f(ml.x - use);
-            l = l * wa + ml.y * wb;
-            m = top;
+    for (int i = 0; i < MINE; ++i) {
+        if (KW == 1 || kw == 0) mine[i] = vec(i);
+        else mine[i] = vec(VECS - MINE + i);
+    }
+    if (KW == 2) {
+        const float2 m0 = ml[0], m1 = ml[64];
+        m = fmaxf(m0.x, m1.x);
+        const float use = m == -INFINITY ? 0.f : m;
+        const float w0 = __builtin_amdgcn_exp2f(m0.x - use), w1 = __builtin_amdgcn_exp2f(m1.x - use);
+        l = m0.y * w0 + m1.y * w1;
+        const float wa = kw == 0 ? w0 : w1, wb = kw == 0 ? w1 : w0;
 #pragma unroll
-            for (int i = 0; i < 4 * T; ++i) {
-                const float4 v = po[i * 64 + lane];
-                o[i / 4][4 * (i % 4)] = o[i / 4][4 * (i % 4)] * wa + v.x * wb;
-                o[i / 4][4 * (i % 4) + 1] = o[i / 4][4 * (i % 4) + 1] * wa + v.y * wb;
-                o[i / 4][4 * (i % 4) + 2] = o[i / 4][4 * (i % 4) + 2] * wa + v.z * wb;
-                o[i / 4][4 * (i % 4) + 3] = o[i / 4][4 * (i % 4) + 3] * wa + v.w * wb;
-            }
+        for (int i = 0; i < MINE; ++i) {
+            const float4 v = met[(i + MINE * kw) * 64];
+            mine[i] = float4{mine[i].x * wa + v.x * wb, mine[i].y * wa + v.y * wb, mine[i].z * wa + v.z * wb, mine[i].w * wa + v.w * wb};
         }
         __syncthreads();                                     // (before the next piece of work loads over them)
-        if (kw == 1) return false;
     }
     if (!live) return false;
     const float inv = l > 0.f ? 1.f / l : 0.f;               // (a NaN among the scores is in O as well)
     const float lse2 = l <= 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l);
+    const int first = KW == 1 ? 0 : kw * MINE;
     if (it.slot >= 0) {                                      // a partial, lane by lane: whole lines a store
-        float4* const po = reinterpret_cast<float4*>(a.part_o) + (it.slot * WR + rw) * (4 * T * 64) + lane;
+        float4* const po = reinterpret_cast<float4*>(a.part_o) + (it.slot * WR + rw) * (VECS * 64) + first * 64 + lane;
 #pragma unroll
-        for (int i = 0; i < 4 * T; ++i)
-            po[i * 64] = float4{o[i / 4][4 * (i % 4)] * inv, o[i / 4][4 * (i % 4) + 1] * inv, o[i / 4][4 * (i % 4) + 2] * inv,
-                                o[i / 4][4 * (i % 4) + 3] * inv};
-        if (hh == 0) a.part_lse[it.slot * RB + 32 * rw + ql] = lse2;
+        for (int i = 0; i < MINE; ++i) po[i * 64] = float4{mine[i].x * inv, mine[i].y * inv, mine[i].z * inv, mine[i].w * inv};
+        if (hh == 0 && first == 0) a.part_lse[it.slot * RB + 32 * rw + ql] = lse2;
         return false;
     }
     if (r_lane >= n_rows) return false;
     const int64_t row = (int64_t)(it.row0 + qi) * a.num_q_heads + h;
-    uint16_t* const orow = static_cast<uint16_t*>(a.out) + row * d;
+    uint16_t* const orow = static_cast<uint16_t*>(a.out) + row * d + 8 * first + 4 * hh;
 #pragma unroll
-    for (int i = 0; i < 4 * T; ++i) {
-        if (8 * i >= d) continue;                            // columns behind head_dim
-        *reinterpret_cast<uint2*>(orow + 8 * i + 4 * hh) =
-            uint2{E::pack(o[i / 4][4 * (i % 4)] * inv, o[i / 4][4 * (i % 4) + 1] * inv),
-                  E::pack(o[i / 4][4 * (i % 4) + 2] * inv, o[i / 4][4 * (i % 4) + 3] * inv)};
+    for (int i = 0; i < MINE; ++i) {
+        if (8 * (first + i) >= d) continue;                  // columns behind head_dim
+        *reinterpret_cast<uint2*>(orow + 8 * i) = uint2{E::pack(mine[i].x * inv, mine[i].y * inv), E::pack(mine[i].z * inv, mine[i].w * inv)};
     }
-    if (a.lse && hh == 0) a.lse[row] = lse2 * kLn2;
+    if (a.lse && hh == 0 && first == 0) a.lse[row] = lse2 * kLn2;
     return false;
 }
 
@@ -399,7 +403,7 @@ template <int WR, bool TWO, typename E, int DP>
 struct Tree16 {
     typedef TreeShape<WR, DP> Shape;
     static constexpr int kRows = 32 * WR, kWaveRows = 32, kColumns = DP, kTile = kBN, kWaves = Shape::kWaves, kOcc = Shape::kOcc;
-    static constexpr int kLds = Shape::kBufs * TreeGeo<DP>::kBufB;
+    static constexpr int kLds = Shape::kBufs * TreeGeo<DP>::kBufB + (Shape::kKW - 1) * WR * 1024;   // (maxima and sums of two waves)
     template <bool CAREFUL>
     static __device__ __forceinline__ bool work(char* buf, uint32_t* flags, const TreeKernelArgs& a, const TreeItem& it, int32_t kvh)
     {

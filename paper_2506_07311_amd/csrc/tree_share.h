@@ -97,32 +97,40 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeKernelArgs& a, int32_t i)
 // How a KV head's workgroups share the call's key tiles.  Where they are few, every row block is cut into chunks of about `chunk`
 // tiles, one a workgroup.  Otherwise (chunk == 0) all tiles stand in a row, each row block's behind kTreePieceTiles places for what a
 // piece of work costs besides its tiles, and workgroup x of wgs takes places [x all / wgs, (x + 1) all / wgs).
+// (32-bit numbers: the host refuses calls with more places, and a 64-bit division takes 0.2 us.)
 struct TreeShare {
-    int64_t all;
-    int32_t wgs, chunk;
+    int32_t all, wgs, chunk;
+    uint32_t each, rest;         // all = wgs each + rest
+    __device__ __forceinline__ int32_t begin(int32_t x) const   // floor(x all / wgs)
+    {
+        return (int32_t)((uint32_t)x * each + (uint32_t)x * rest / (uint32_t)wgs);
+    }
 };
 template <typename S>
 __device__ __forceinline__ TreeShare tree_share(const TreeKernelArgs& a, int lane, const TreeSeq& own)   // own: sequence `lane`
 {
-    int64_t tiles = 0, blocks = 0;
+    int32_t tiles = 0, blocks = 0;
     for (int32_t i0 = 0; i0 < a.batch; i0 += 64) {
         const TreeSeq q = i0 == 0 ? own : tree_seq<S>(a, i0 + lane);
         tiles += wave_total_moves(q.blocks * q.tiles);
         blocks += wave_total_moves(q.blocks);
     }
-    TreeShare r = {tiles + kTreePieceTiles * blocks, 1, 0};
+    TreeShare r = {tiles + kTreePieceTiles * blocks, 1, 0, 0, 0};
     if (blocks < a.wgs) {
-        const int64_t c = (tiles + a.wgs - blocks - 1) / (a.wgs - blocks);
-        if (c <= kTreeMaxChunk) r.chunk = (int32_t)(c < kTreeMinTiles ? kTreeMinTiles : c);
+        const uint32_t c = (uint32_t)(tiles + a.wgs - blocks - 1) / (uint32_t)(a.wgs - blocks);
+        if (c <= kTreeMaxChunk) r.chunk = max((int32_t)c, kTreeMinTiles);
     }
-    const int64_t n = r.all / (kTreeMinTiles + kTreePieceTiles);
-    r.wgs = n > a.wgs ? a.wgs : n < 1 ? 1 : (int32_t)n;
+    if (r.chunk == 0) {
+        r.wgs = min(max(r.all / (kTreeMinTiles + kTreePieceTiles), 1), a.wgs);
+        r.each = (uint32_t)r.all / (uint32_t)r.wgs;
+        r.rest = (uint32_t)r.all % (uint32_t)r.wgs;
+    }
     return r;
 }
 // Places of a row block of the sequence: chunks, or tiles and what comes before them.
 __device__ __forceinline__ int32_t tree_places(const TreeShare& r, const TreeSeq& q)
 {
-    return q.blocks == 0 ? 0 : r.chunk > 0 ? (q.tiles + r.chunk - 1) / r.chunk : q.tiles + kTreePieceTiles;
+    return q.blocks == 0 ? 0 : r.chunk > 0 ? (int32_t)((uint32_t)(q.tiles + r.chunk - 1) / (uint32_t)r.chunk) : q.tiles + kTreePieceTiles;
 }
 
 template <typename S>
@@ -141,8 +149,8 @@ __global__ __launch_bounds__(64 * S::kWaves, S::kOcc * S::kWaves / 4) void paged
     const int32_t kvh = (int32_t)(blockIdx.x % (uint32_t)hkv), x = (int32_t)(blockIdx.x / (uint32_t)hkv);
     // this workgroup's places [t, t_end), the sequence of the first and that one's first place
     int32_t s = 0;
-    int64_t t = 0, t_end = 1, first = 0;
-    TreeShare share = {0, 0, 0};
+    int32_t t = 0, t_end = 1, first = 0;
+    TreeShare share = {0, 0, 0, 0, 0};
     TreeSeq q = {0, 0, 0, 0, 0};
     if (a.wgs == 0) {                                        // one row block
         s = x / a.row_blocks;
@@ -156,8 +164,8 @@ __global__ __launch_bounds__(64 * S::kWaves, S::kOcc * S::kWaves / 4) void paged
             t_end = t + 1;
         } else {
             if (x >= share.wgs) return;
-            t = (int64_t)x * share.all / share.wgs;
-            t_end = (int64_t)(x + 1) * share.all / share.wgs;
+            t = share.begin(x);
+            t_end = share.begin(x + 1);
         }
         bool found = false;
         for (int32_t i0 = 0; i0 < a.batch; i0 += 64) {
@@ -194,20 +202,20 @@ __global__ __launch_bounds__(64 * S::kWaves, S::kOcc * S::kWaves / 4) void paged
             t = t_end;
         } else {
             const int32_t places = tree_places(share, q);
-            if (t >= first + (int64_t)q.blocks * places) {   // (nothing, or nothing more, of this one)
-                first += (int64_t)q.blocks * places;
+            if (t >= first + q.blocks * places) {            // (nothing, or nothing more, of this one)
+                first += q.blocks * places;
                 if (++s >= a.batch) return;
                 q = tree_seq<S>(a, s);
                 continue;
             }
-            const int32_t at = (int32_t)((t - first) % places);
-            it.rb = (int32_t)((t - first) / places);
+            it.rb = (int32_t)((uint32_t)(t - first) / (uint32_t)places);
+            const int32_t at = t - first - it.rb * places;
             if (share.chunk > 0) {
-                it.tile_begin = (int32_t)((int64_t)at * q.tiles / places);
-                it.tile_end = (int32_t)((int64_t)(at + 1) * q.tiles / places);
+                it.tile_begin = (int32_t)((uint32_t)(at * q.tiles) / (uint32_t)places);
+                it.tile_end = (int32_t)((uint32_t)((at + 1) * q.tiles) / (uint32_t)places);
                 t = t_end;
             } else {
-                const int32_t to = (int32_t)min((int64_t)places, at + (t_end - t));
+                const int32_t to = min(places, at + (t_end - t));
                 it.tile_begin = max(at - kTreePieceTiles, 0);
                 it.tile_end = max(to - kTreePieceTiles, 0);
                 t += to - at;
@@ -218,6 +226,7 @@ __global__ __launch_bounds__(64 * S::kWaves, S::kOcc * S::kWaves / 4) void paged
             if (it.tile_begin == 0 && threadIdx.x == 0) {    // what the merge has to know: workgroups up to the last tile's
                 int32_t pieces = places;
                 if (share.chunk == 0) {
+                    // (the workgroup of the block's last place y: floor(((y + 1) wgs - 1) / all))
                     const int64_t end = first + (int64_t)(it.rb + 1) * places;
                     pieces = (int32_t)((end * share.wgs - 1) / share.all) - x + 1;
                 }
