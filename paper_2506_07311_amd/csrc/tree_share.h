@@ -240,16 +240,16 @@ __global__ __launch_bounds__(64 * S::kWaves, S::kOcc * S::kWaves / 4) void paged
 // The pieces of a row block that were cut, merged by their log-sum-exps.  Grid (sequences x row blocks x row waves x
 // PARTS, KV heads): a wave's rows and a part of their columns each, in the partials' own order, so that a call of few sequences spreads over the
 // machine as well.  Statistics first, all at once, and their weights into LDS.
-template <typename S, int PARTS>
-__global__ __launch_bounds__(256) void paged_attention_tree_merge_kernel(
+template <typename S, int PARTS, int NW>
+__global__ __launch_bounds__(64 * NW) void paged_attention_tree_merge_kernel(
     TreeKernelArgs a, const int32_t* __restrict__ cu_q_lens, const int32_t* __restrict__ seq_lens)
 {
     a.cu_q_lens = cu_q_lens;
     a.seq_lens = seq_lens;
     constexpr int RB = S::kRows, RW = S::kWaveRows, WR = RB / RW, VECS = RW * S::kColumns / 4, MINE = VECS / PARTS, LINES = MINE / 64;
     extern __shared__ float weight[];                        // [pieces][RW]
-    __shared__ float sm_top[RW], sm_sum[RW], sm_red[256 / RW][RW];
-    __shared__ float4 sm_acc[4][LINES][64];
+    __shared__ float sm_top[RW], sm_sum[RW], sm_red[64 * NW / RW][RW];
+    __shared__ float4 sm_acc[NW][LINES][64];
     const int32_t kvh = blockIdx.y, part = (int32_t)(blockIdx.x % PARTS);
     const int32_t rw = (int32_t)(blockIdx.x / PARTS) % WR;
     const int32_t u = (int32_t)(blockIdx.x / (PARTS * WR)), s = u / a.row_blocks, rb = u % a.row_blocks;
@@ -261,8 +261,7 @@ __global__ __launch_bounds__(256) void paged_attention_tree_merge_kernel(
     if (pieces == 1) return;
     const int64_t slot0 = ((int64_t)kvh * a.wgs + cut.x) * 2;
     auto slot = [&](int32_t k) { return slot0 + 2 * (int64_t)k + (k == 0 ? 1 : 0); };
-    // (256 / RW threads a row)
-    constexpr int GROUPS = 256 / RW;
+    constexpr int GROUPS = 64 * NW / RW;                     // threads a row
     const int32_t srow = threadIdx.x % RW, group = threadIdx.x / RW;
     float top = -INFINITY;
     for (int32_t k0 = group; k0 < pieces; k0 += 8 * GROUPS) {
@@ -297,24 +296,24 @@ __global__ __launch_bounds__(256) void paged_attention_tree_merge_kernel(
         sm_sum[srow] = wsum;
     }
     __syncthreads();
-    // float4 j of a wave's partial: lane j % 64 holds row j % RW, four columns of every 4 * 64 / RW.  Each of the four waves takes
-    // every fourth piece, several pieces at a time; then they meet in LDS.
+    // float4 j of a wave's partial: lane j % 64 holds row j % RW, four columns of every 4 * 64 / RW.  Each of the NW waves takes
+    // every NW-th piece, several pieces at a time; then they meet in LDS.
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane % RW;
     const float4* const po = reinterpret_cast<const float4*>(a.part_o) + rw * VECS + part * MINE + lane;
     float4 acc[LINES];
 #pragma unroll
     for (int i = 0; i < LINES; ++i) acc[i] = float4{0.f, 0.f, 0.f, 0.f};
     constexpr int DEEP = LINES > 2 ? 2 : 8 / LINES;          // pieces at a time
-    for (int32_t k0 = wave; k0 < pieces; k0 += 4 * DEEP) {
+    for (int32_t k0 = wave; k0 < pieces; k0 += NW * DEEP) {
         float4 v[DEEP][LINES];
 #pragma unroll
         for (int k = 0; k < DEEP; ++k)
 #pragma unroll
-            for (int i = 0; i < LINES; ++i) v[k][i] = po[slot(min(k0 + 4 * k, pieces - 1)) * (WR * VECS) + 64 * i];
+            for (int i = 0; i < LINES; ++i) v[k][i] = po[slot(min(k0 + NW * k, pieces - 1)) * (WR * VECS) + 64 * i];
 #pragma unroll
         for (int k = 0; k < DEEP; ++k) {
-            if (k0 + 4 * k >= pieces) break;
-            const float w = weight[(k0 + 4 * k) * RW + row];
+            if (k0 + NW * k >= pieces) break;
+            const float w = weight[(k0 + NW * k) * RW + row];
 #pragma unroll
             for (int i = 0; i < LINES; ++i)
                 acc[i] = float4{__builtin_fmaf(w, v[k][i].x, acc[i].x), __builtin_fmaf(w, v[k][i].y, acc[i].y),
@@ -324,12 +323,12 @@ __global__ __launch_bounds__(256) void paged_attention_tree_merge_kernel(
 #pragma unroll
     for (int i = 0; i < LINES; ++i) sm_acc[wave][i][lane] = acc[i];
     __syncthreads();
-    for (int32_t i = wave; i < LINES; i += 4) {
+    for (int32_t i = wave; i < LINES; i += NW) {
         const int32_t j = part * MINE + 64 * i + lane, c = 4 * (j / RW), r = r0 + row;
         if (r >= n_rows || c >= d) continue;
         float4 x = sm_acc[0][i][lane];
 #pragma unroll
-        for (int k = 1; k < 4; ++k) {
+        for (int k = 1; k < NW; ++k) {
             const float4 y = sm_acc[k][i][lane];
             x = float4{x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w};
         }
@@ -340,11 +339,11 @@ __global__ __launch_bounds__(256) void paged_attention_tree_merge_kernel(
     }
 }
 
-template <typename S, int PARTS>
+template <typename S, int PARTS, int NW>
 void launch_tree_merge(const TreeKernelArgs& a, hipStream_t stream)
 {
     const uint32_t x = (uint32_t)((int64_t)a.batch * a.row_blocks * (S::kRows / S::kWaveRows) * PARTS);
-    hipLaunchKernelGGL((paged_attention_tree_merge_kernel<S, PARTS>), dim3(x, (uint32_t)a.cache.num_kv_heads), dim3(256),
+    hipLaunchKernelGGL((paged_attention_tree_merge_kernel<S, PARTS, NW>), dim3(x, (uint32_t)a.cache.num_kv_heads), dim3(64 * NW),
                        (size_t)a.wgs * S::kWaveRows * sizeof(float), stream, a, a.cu_q_lens, a.seq_lens);
 }
 
@@ -354,15 +353,16 @@ pa_status launch_tree_of(const TreeKernelArgs& a, bool merge, hipStream_t stream
 {
     const int64_t units = (int64_t)a.batch * a.row_blocks;
     const int64_t grid = (a.wgs > 0 ? a.wgs : units) * a.cache.num_kv_heads;
-    // A merging workgroup takes four lines of 64 vectors of a wave's columns (a quarter of them at 128 columns of 32 rows), or one where
-    // there are few (us with four / one: 2 x 8 tokens on 1500, 512 workgroups, 16.1 / 15.3, 1 x 8 on 100000 with 8 / 1
-    // heads 41.6 / 39.3; 8 x 16 on 128 to 2048, 2048 workgroups, 22.1 / 24.4).
+    // A merging workgroup takes four lines of 64 vectors of a wave's columns, or one and with twice the waves where there are few
+    // (us with four / one: 2 x 8 tokens on 1500, 512 workgroups, 16.1 / 15.3; 8 x 16 on 128 to 2048, 2048 workgroups, 22.1 / 24.4;
+    // with one, of four / eight / sixteen waves: 1 x 8 on 100000 with 8 / 1 heads, 32 workgroups and 256 pieces, 38.1 / 29.3 / 25.4,
+    // 2 x 8 on 1500 14.1 / 13.8 / 16.6).
     constexpr int LINES = S::kWaveRows * S::kColumns / 256, PARTS = LINES > 4 ? LINES / 4 : 1;
     const int64_t waves = units * (S::kRows / S::kWaveRows);
     if (grid > 0x7fffffffLL || waves * LINES > 0x7fffffffLL || a.cache.num_kv_heads > 65535) return PA_ERR_UNSUPPORTED;
     if (merge) {
-        if (waves * LINES * a.cache.num_kv_heads <= 512) launch_tree_merge<S, LINES>(a, stream);
-        else launch_tree_merge<S, PARTS>(a, stream);
+        if (waves * LINES * a.cache.num_kv_heads <= 512) launch_tree_merge<S, LINES, 8>(a, stream);
+        else launch_tree_merge<S, PARTS, 4>(a, stream);
     } else {
         hipLaunchKernelGGL((paged_attention_tree_mfma_kernel<S>), dim3((uint32_t)grid), dim3(64 * S::kWaves), 0, stream, a,
                            a.cu_q_lens, a.seq_lens, a.block_table, a.tree_mask);
