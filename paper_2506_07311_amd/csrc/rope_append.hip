@@ -73,34 +73,35 @@ __device__ __forceinline__ float2 turn_of(const RopeKernelArgs& a, int32_t t, in
     return float2{cs * a.mscale, sn * a.mscale};
 }
 
-// 16 bytes at a time, where the turned part divides into such pieces.  A workgroup takes TOKENS tokens, or a part of one's heads where
+// 16 bytes at a time, where the turned part divides into such pieces.  A workgroup takes a token, or a part of one's heads where
 // there are few: cosines and sines once for all heads into LDS, then a thread's pieces: two of a pair of halves, one of neighbours, one to
-// copy.  Bound by reading and writing q, K and V once; a thread's first piece is on its way while the angles are formed.
-template <pa_dtype DT, bool INTER, int TOKENS>
+// copy.  Bound by reading and writing q, K and V once; a thread's first piece is on its way while the angles are formed.  8192 tokens of 32 / 8
+// heads of 128, 201 MB read and written: 34 us (5.9 TB/s) on the same data again, 43 (4.7, as a copy of 4 GiB) on data from memory.  Four
+// tokens a workgroup instead of one: 33.8 / 33.3, 5000 tokens 23.6 / 23.7, 2048 14.7 / 11.1.
+template <pa_dtype DT, bool INTER>
 __global__ __launch_bounds__(kThreads) void paged_rope_append_wide_kernel(RopeKernelArgs a)
 {
     typedef Elem<DT> E;
     typedef typename E::T T;
     constexpr int V = 16 / sizeof(T);
-    __shared__ __attribute__((aligned(16))) float sm_c[TOKENS][128], sm_s[TOKENS][128];
-    __shared__ int64_t sm_slot[TOKENS];
-    const int32_t d = a.head_dim, half = a.half, t0 = (int32_t)blockIdx.x * TOKENS, tokens = min(TOKENS, a.T - t0);
+    __shared__ __attribute__((aligned(16))) float sm_c[128], sm_s[128];   // head_dim is at most 256
+    __shared__ int64_t sm_slot;
+    const int32_t d = a.head_dim, half = a.half;
+    const int64_t t = blockIdx.x;
     const int32_t turned = INTER ? 2 * half / V : half / V;  // pieces of a head that turn, then those to copy
     const int32_t pieces = turned + (d - 2 * half) / V, copies = d / V;
     const int32_t q_tasks = a.q_heads * pieces, k_tasks = a.kv_heads * pieces, all = q_tasks + k_tasks + a.kv_heads * copies;
-    const int32_t mine = (all * tokens + (int32_t)gridDim.y - 1) / (int32_t)gridDim.y, begin = mine * (int32_t)blockIdx.y;
-    const int32_t end = min(begin + mine, all * tokens);
+    const int32_t mine = (all + (int32_t)gridDim.y - 1) / (int32_t)gridDim.y, begin = mine * (int32_t)blockIdx.y;
+    const int32_t end = min(begin + mine, all);
 
     struct Piece {
         const T* src;            // of the piece's first element
-        int32_t token, u;        // u: number of the piece in its head; -1: to copy
+        int32_t u;               // number of the piece in its head; -1: to copy
         int32_t what;            // 0: q, 1: K, 2: V
         int64_t at;              // where it goes within its token
     };
-    auto locate = [&](int32_t i) {
+    auto locate = [&](int32_t j) {
         Piece p;
-        p.token = TOKENS == 1 ? 0 : i / all;
-        int32_t j = i - p.token * all;
         p.what = j < q_tasks ? 0 : j < q_tasks + k_tasks ? 1 : 2;
         j -= p.what == 0 ? 0 : p.what == 1 ? q_tasks : q_tasks + k_tasks;
         const int32_t n = p.what == 2 ? copies : pieces, h = j / n;
@@ -110,7 +111,6 @@ __global__ __launch_bounds__(kThreads) void paged_rope_append_wide_kernel(RopeKe
             if (p.what != 2) first = 2 * half + (p.u - turned) * V;
             p.u = -1;
         }
-        const int64_t t = t0 + p.token;
         const T* const base = p.what == 0 ? (const T*)a.q + t * a.q_stride : p.what == 1 ? (const T*)a.k_new + t * a.k_stride
                                                                                            : (const T*)a.v_new + t * a.v_stride;
         p.src = base + (int64_t)h * d + first;
@@ -134,18 +134,17 @@ __global__ __launch_bounds__(kThreads) void paged_rope_append_wide_kernel(RopeKe
         p = locate(i);
         v = load(p);
     }
-    if (a.kv_heads > 0 && (int)threadIdx.x < tokens) sm_slot[threadIdx.x] = slot_of(a, t0 + threadIdx.x);
-    for (int32_t k = threadIdx.x; k < tokens * half; k += kThreads) {
-        const int32_t t = k / half, pair = k - t * half;
-        const float2 cs = turn_of(a, t0 + t, pair);
-        sm_c[t][pair] = cs.x;
-        sm_s[t][pair] = cs.y;
+    if (a.kv_heads > 0 && threadIdx.x == 0) sm_slot = slot_of(a, (int32_t)t);
+    if ((int)threadIdx.x < half) {
+        const float2 cs = turn_of(a, (int32_t)t, threadIdx.x);
+        sm_c[threadIdx.x] = cs.x;
+        sm_s[threadIdx.x] = cs.y;
     }
     __syncthreads();
     while (i < end) {
         T* dst = nullptr;
-        if (p.what == 0) dst = (T*)a.q_out + (int64_t)(t0 + p.token) * a.q_out_stride + p.at;
-        else if (sm_slot[p.token] >= 0) dst = (T*)(p.what == 1 ? a.k_cache : a.v_cache) + sm_slot[p.token] + p.at;
+        if (p.what == 0) dst = (T*)a.q_out + t * a.q_out_stride + p.at;
+        else if (sm_slot >= 0) dst = (T*)(p.what == 1 ? a.k_cache : a.v_cache) + sm_slot + p.at;
         if (dst) {
             if (p.u >= 0) {
                 T x[V], y[V];
@@ -155,7 +154,7 @@ __global__ __launch_bounds__(kThreads) void paged_rope_append_wide_kernel(RopeKe
                     const int32_t at = p.u * (V / 2);
 #pragma unroll
                     for (int e = 0; e < V; e += 2) {
-                        const float c = sm_c[p.token][at + e / 2], s = sm_s[p.token][at + e / 2];
+                        const float c = sm_c[at + e / 2], s = sm_s[at + e / 2];
                         const float fx = E::get(x[e]), fy = E::get(x[e + 1]);
                         x[e] = E::put(fx * c - fy * s);
                         x[e + 1] = E::put(fx * s + fy * c);
@@ -163,7 +162,7 @@ __global__ __launch_bounds__(kThreads) void paged_rope_append_wide_kernel(RopeKe
                 } else {
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
-                        const float c = sm_c[p.token][p.u * V + e], s = sm_s[p.token][p.u * V + e];
+                        const float c = sm_c[p.u * V + e], s = sm_s[p.u * V + e];
                         const float fx = E::get(x[e]), fy = E::get(y[e]);
                         x[e] = E::put(fx * c - fy * s);
                         y[e] = E::put(fx * s + fy * c);
@@ -230,16 +229,12 @@ void launch_layout(const RopeKernelArgs& a, hipStream_t stream)
         hipLaunchKernelGGL((paged_rope_append_kernel<DT, INTER>), dim3(a.T), dim3(kThreads), 0, stream, a);
         return;
     }
-    // Four tokens a workgroup once that leaves each compute unit four of them; where tokens are few, a thread takes a piece or two.
-    constexpr int kTokens = 4;
-    if (a.T >= 4096) {
-        hipLaunchKernelGGL((paged_rope_append_wide_kernel<DT, INTER, kTokens>), dim3((a.T + kTokens - 1) / kTokens), dim3(kThreads), 0, stream, a);
-        return;
-    }
+    // Where tokens are few, a thread takes a piece or two (us with / without, 32 / 8 heads of 128: 40 tokens 3.9 / 4.6, 300 4.4 / 5.2, 700
+    // 6.0 / 6.3, 2048 11.4 / 11.1).
     const int32_t pieces = (a.q_heads + a.kv_heads) * ((INTER ? 2 * a.half : a.half) / V + (a.head_dim - 2 * a.half) / V) +
                            a.kv_heads * a.head_dim / V;
-    const int32_t parts = a.T >= 512 ? 1 : (pieces + kThreads - 1) / kThreads;
-    hipLaunchKernelGGL((paged_rope_append_wide_kernel<DT, INTER, 1>), dim3(a.T, parts), dim3(kThreads), 0, stream, a);
+    const int32_t parts = a.T >= 1024 ? 1 : (pieces + kThreads - 1) / kThreads;
+    hipLaunchKernelGGL((paged_rope_append_wide_kernel<DT, INTER>), dim3(a.T, parts), dim3(kThreads), 0, stream, a);
 }
 
 template <pa_dtype DT>

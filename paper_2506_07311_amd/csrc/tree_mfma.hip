@@ -24,12 +24,15 @@ size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 // 16-bit pools: up to 64 rows a (sequence, KV head) two waves share 32 rows, up to 128 at head_dims up to 128 as well, with eight
 // waves; beyond that a workgroup takes 256 rows (128 above head_dim 128, where a wave's O and Q fill its registers).  fp32 pools: 16 rows a
 // wave, 16, 32, 64 or 128 a workgroup.  The tiles are shared by as many workgroups as the machine holds at once; on contexts of
-// up to kPlainTiles tiles a row block is one workgroup's and there is no merge, and row blocks are then made smaller, down to two waves of
-// rows, until there is one for each compute unit (us with / without: bf16 3 x 40 tokens on 400 14.1 / 24.6, 16 x 40 on 350 20.1 / 26.3,
+// up to kPlainTiles tiles a row block is one workgroup's and there is no merge (us with 4 / 8 / 16: 16 x 8 tokens on 300 to 400 18.1 /
+// 12.7 / 12.8, 4 x 8 on 800 to 900 15.8 / 15.7 / 20.8); up to kFullTiles where such row blocks alone fill a machine whose compute units
+// hold two (with 8 / 16 / 32: 64 x 8 on 800 to 900 52.4 / 39.6 / 39.9, on 64 to 2000 35.9 / 35.9 / 41.0; of 256 rows, 64 x 64 on 64 to 1000,
+// 76.6 / 81.5). Row blocks of up to kPlainTiles tiles are made smaller, down to two waves of rows, until there is one for
+// each compute unit (us with / without: bf16 3 x 40 tokens on 400 14.1 / 24.6, 16 x 40 on 350 20.1 / 26.3,
 // fp32 3 x 40 on 400 27.7 / 65; until there are two for each: 32 x 40 on 350 37.9 / 30.7, fp32 8 x 64 on 300 49 / 37.8).
 TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t max_q_len, int32_t max_seq_len, bool f32)
 {
-    constexpr int32_t kPlainTiles = 8, kOneTermKeys = 1024;   // (see tree_mfma_impl.h)
+    constexpr int32_t kPlainTiles = 8, kFullTiles = 16, kOneTermKeys = 256;   // (kOneTermKeys: see tree_mfma_impl.h)
     TreePlan p;
     const int64_t rows = (int64_t)max_q_len * (num_q_heads / num_kv_heads);
     const int32_t columns = columns_of(head_dim, f32), wave_rows = f32 ? 16 : 32;
@@ -45,8 +48,9 @@ TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int
     p.two_terms = max_seq_len < kOneTermKeys;
     p.wgs = 0;
     p.part_o_bytes = p.part_lse_bytes = p.cuts_bytes = 0;
-    if (tiles > kPlainTiles) {
-        const int64_t slots = (int64_t)device_cus() * (columns <= 128 && p.row_waves == 2 && !f32 ? 2 : 1);
+    const bool pairs = columns <= 128 && p.row_waves == 2 && !f32;
+    const int64_t slots = (int64_t)device_cus() * (pairs ? 2 : 1);
+    if (tiles > (pairs && batch * num_kv_heads * blocks >= slots ? kFullTiles : kPlainTiles)) {
         const int64_t most = (batch * blocks * tiles + kTreeMinTiles - 1) / kTreeMinTiles;
         int64_t wgs = slots / num_kv_heads;
         if (wgs > most) wgs = most;

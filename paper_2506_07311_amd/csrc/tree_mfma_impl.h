@@ -13,12 +13,12 @@
 //         S^T[key, row] = K Q^T,   O^T[column, row] += V^T P^T.
 //   * Softmax is online in the log2 domain against a reference that trails the maximum: weights are taken with the
 //     reference as it stands, and only where a lane's sum leaves the range that 16-bit operands carry is it raised and O
-//     rescaled.  Up to 64 rows, and in calls for contexts of less than kOneTermKeys, weights enter as two 16-bit terms (p = hi + lo, off by
+//     rescaled.  Up to 64 rows, and in calls for contexts of less than kOneTermKeys = 256, weights enter as two 16-bit terms (p = hi + lo, off by
 //     2^-17 of a weight): the second term's matrix work hides behind the read.  With more rows and longer contexts, where the matrix
 //     cores are the bound (and the card's power: the clock falls to 1.7 GHz), they enter as one, as the prefill kernel's do on long contexts:
 //     the weights' rounding, independent from key to key, then weighs as much as the output's own (error against 64 bits 1.41 times
 //     that of the output's rounding alone).  us with two terms / one: 16 x 16 tokens on 131072, 64 / 8 heads, 1910 / 1530, 32 x 64
-//     on 8000 408 / 318, 8 x 32 on 3600 43.0 / 36.6.
+//     on 8000 408 / 318, 8 x 32 on 3600 43.0 / 36.6, 64 x 64 on 800 131 / 109, 4 x 32 on 700 20.2 / 19.4.
 //   * A key is masked by selection: key len - n + t of a tile is seen by a row if bit t of the row's words is set, 32 bits at a
 //     time; tiles that end in the context take no mask at all.  An infinity or a NaN in a V row that some rows of a tile
 //     do not see would reach them through a product with a weight of zero.  It always leaves its mark on an accumulator, so

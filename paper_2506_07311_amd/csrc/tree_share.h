@@ -35,10 +35,16 @@ namespace {
 
 using namespace prefill;
 
-constexpr int32_t kTreeMinTiles = 2;     // fewest tiles of a workgroup that shares them
-constexpr int32_t kTreePieceTiles = 4;   // what a piece of work costs besides its tiles, in tiles
-constexpr int32_t kTreeMaxChunk = 12;    // most tiles of a workgroup that has one piece of work
-constexpr int32_t kTreeMaxPieces = 256;  // workgroups that share a row block
+// Fewest tiles of a workgroup that shares them.
+constexpr int32_t kTreeMinTiles = 2;
+// What a piece of work costs besides its tiles, in tiles (us with 0 / 4 / 8: 64 x 8 tokens on 64 to 32768 243 / 231 / 236, 16 x 8 on 300
+// to 30000 88.2 / 85.0 / 86.3).
+constexpr int32_t kTreePieceTiles = 4;
+// Most tiles of a workgroup that has one piece of work (with 0 / 12 / 40: 1 x 8 on 20000 26.2 / 25.3 / 25.3, 2 x 40 on 4000 27.7 / 26.3 / 26.4,
+// 16 x 8 on 300 to 30000 86.3 / 85.0 / 89.4, 8 x 64 on 3600 52.9 / 52.7 / 55.7).
+constexpr int32_t kTreeMaxChunk = 12;
+// Workgroups that share a row block; the merge has 32 weights of each in LDS.
+constexpr int32_t kTreeMaxPieces = 256;
 
 // This wave's loads to LDS have landed but for the last N tiles' (LOADS of either pool each).  In order, so what the compiler
 // has issued in between makes it wait for more, not for less.
@@ -119,6 +125,12 @@ __device__ __forceinline__ TreeShare tree_share(const TreeKernelArgs& a, int lan
     if (blocks < a.wgs) {
         const uint32_t c = (uint32_t)(tiles + a.wgs - blocks - 1) / (uint32_t)(a.wgs - blocks);
         if (c <= kTreeMaxChunk) r.chunk = max((int32_t)c, kTreeMinTiles);
+        // A workgroup that has its compute unit to itself is worth up to four tiles (us without / with: 8 x 16 tokens on 128 to 2048
+        // 21.2 / 18.4; four tiles in any case: 2 x 8 on 1500 13.9 / 14.6).
+        if (S::kOcc > 1 && r.chunk > 0 && r.chunk < 4) {
+            const int32_t alone = a.wgs / S::kOcc - blocks;
+            r.chunk = max(r.chunk, alone <= 0 ? 4 : min(4, (int32_t)((uint32_t)(tiles + alone - 1) / (uint32_t)alone)));
+        }
     }
     if (r.chunk == 0) {
         r.wgs = min(max(r.all / (kTreeMinTiles + kTreePieceTiles), 1), a.wgs);

@@ -264,12 +264,12 @@ def check_tree(c, out, lse, what="", bound=None):
     """Half a rounding step of the output; besides, of max |v| (a weighted mean's scale): softmax weights in two 16-bit terms
     (2^-17), their exponentials (scores below 16 in 32 bits: 16 * 2^-23), 32-bit sums and the final division, together below
     3e-5 for 16-bit inputs; with fp32 inputs scores of up to 256 products of 2^-24 each, 1e-5.  lse: scores as there.
-    Calls with more than 64 rows (query, head of a group) for contexts of 1024 keys and more take weights of 16 bits: each is off
+    Calls with more than 64 rows (query, head of a group) for contexts of 256 keys and more take weights of 16 bits: each is off
     by up to half a step of itself, evenly and independently, a deviation of half a step / sqrt(3); six deviations of what
     that does to the output (two in 10^9 are beyond)."""
     dtype, row = c["q"].dtype, 0
     hkv = c["k"].shape[1 if c["head_major"] else 2]
-    one_term = dtype != torch.float32 and max(c["news"]) * c["q"].shape[1] // hkv > 64 and (bound or max(c["host_lens"])) >= 1024
+    one_term = dtype != torch.float32 and max(c["news"]) * c["q"].shape[1] // hkv > 64 and (bound or max(c["host_lens"])) >= 256
     extra = 1e-5 if dtype == torch.float32 else 3e-5
     got, got_lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
     q = c["q"].double().cpu().numpy()

@@ -60,6 +60,17 @@ def test_many_sequences(pa, dtype, d, hq, hkv):  # noqa: F811
         check_tree(c, out, lse, f"{most}")
 
 
+def test_a_full_machine_of_short_contexts(pa):  # noqa: F811
+    """So many row blocks that each is one workgroup's, up to 1024 keys."""
+    rng = np.random.default_rng(15)
+    news = [int(x) for x in rng.integers(1, 3, 70)]
+    lens = [n + int(rng.integers(0, 1000)) for n in news]
+    lens[3] = 1024
+    c = make_tree_call(lens, news, 8, 8, 64, 16, torch.bfloat16, ancestors(7), seed=2)
+    out, lse = run_tree(pa, c)
+    check_tree(c, out, lse)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_bounds_may_be_loose(pa, dtype):  # noqa: F811
     """max_q_len, the masks' words and the rows of q beyond what the sequences bring, as a captured step has them."""
@@ -73,7 +84,7 @@ def test_bounds_may_be_loose(pa, dtype):  # noqa: F811
         out, lse = torch.full_like(c["q"], 9.0), torch.full(c["q"].shape[:2], 7.0, device=DEV)
         pa.paged_attention_tree(c["k"], c["v"], c["q"], c["cu"], max_q, mask, c["table"], c["lens"], longest, c["scale"], out=out,
                                 lse=lse, workspace=ws)
-        # (with bounds of 600 rows and contexts over 1024 the weights are of 16 bits: check_tree's allowance goes by the bound)
+        # (with bounds of 600 rows and of contexts over 255 the weights are of 16 bits: check_tree's allowance goes by the bound)
         if max_q == 7 or dtype == torch.float32:
             check_tree(c, out, lse, f"{max_q}")
         else:
