@@ -146,9 +146,9 @@ __device__ __forceinline__ void plan_sequences(const PlanArgs& a)
     }
 }
 
-// One wave: the rows of sequence s, 64 at a time.  The mask and the depth of a token come from its chain of parents: for
-// up to 64 tokens by doubling (after round k a lane holds the union of the 2^k nearest and points 2^k up: 6 rounds of lane
-// moves), beyond that by walking up, once a word.
+// One wave: the rows of sequence s, 64 at a time.  The mask and the depth of a token come from its chain of parents, among the 64 by
+// doubling (after round k a lane holds the union of the 2^k nearest and points 2^k up: 6 rounds of lane moves); a chain that leaves
+// them goes on with the row of the token that it leaves to, which this wave has written before.
 __device__ __forceinline__ void plan_rows(const PlanArgs& a, int32_t s)
 {
     const int lane = threadIdx.x & 63;
@@ -162,40 +162,27 @@ __device__ __forceinline__ void plan_rows(const PlanArgs& a, int32_t s)
         const int64_t r = (int64_t)start + i;
         const bool live = i < n && r < a.max_rows;
         int32_t depth = i;
-        if (n <= 64 && a.parents) {
-            int32_t up = live ? a.parents[r] : -1;
+        if (a.parents) {
+            int32_t up = live ? a.parents[r] : -1;           // < 0: none, else a number within the sequence
             if (up < 0 || up >= i) up = -1;
             uint64_t bits = 1ull << lane;
-            depth = up >= 0 ? 1 : 0;
-            while (__any(up >= 0)) {
-                const int from = up >= 0 ? up : lane;
+            depth = up >= 0 ? 1 : 0;                         // steps to `up`, or to the root
+            while (__any(up >= base)) {
+                const int from = up >= base ? up - base : lane;
                 const uint64_t b = __shfl((unsigned long long)bits, from, 64);
                 const int32_t d = __shfl(depth, from, 64), u = __shfl(up, from, 64);
-                if (up >= 0) {
+                if (up >= base) {
                     bits |= b;
                     depth += d;
                     up = u;
                 }
             }
-            if (live && a.tree_mask) {
-                a.tree_mask[r * a.mask_words] = bits;
-                for (int32_t w = 1; w < a.mask_words; ++w) a.tree_mask[r * a.mask_words + w] = 0;
-            }
-        } else if (live && a.parents) {
-            auto above = [&](int32_t k) {
-                const int64_t row = (int64_t)start + k;
-                const int32_t u = a.parents[row];
-                return u >= 0 && u < k ? u : -1;
-            };
-            depth = -1;
-            for (int32_t k = i; k >= 0; k = above(k)) ++depth;
-            if (a.tree_mask)
-                for (int32_t w = 0; w < a.mask_words; ++w) {
-                    uint64_t bits = 0;
-                    for (int32_t k = i; k >= 64 * w; k = above(k))
-                        if (k >> 6 == w) bits |= 1ull << (k & 63);
-                    a.tree_mask[r * a.mask_words + w] = bits;
-                }
+            if (base > 0) __threadfence_block();             // (the rows before are there)
+            const int64_t above = (int64_t)start + up;       // < r
+            if (live && up >= 0 && a.rope_positions) depth += a.rope_positions[above] - ctx;
+            if (live && a.tree_mask)
+                for (int32_t w = 0; w < a.mask_words; ++w)
+                    a.tree_mask[r * a.mask_words + w] = w == base >> 6 ? bits : up >= 0 && w < base >> 6 ? a.tree_mask[above * a.mask_words + w] : 0;
         } else if (live && a.tree_mask) {
             for (int32_t w = 0; w < a.mask_words; ++w) {
                 const int32_t k = i - 64 * w;                // bits 0 .. k of the word

@@ -71,6 +71,31 @@ def test_a_full_machine_of_short_contexts(pa):  # noqa: F811
     check_tree(c, out, lse)
 
 
+@pytest.mark.parametrize("how", ["chain", "tree", None])
+def test_plans_of_long_sequences(pa, how):  # noqa: F811
+    """Thousands of new tokens in a sequence, whose chains of parents run through all of them."""
+    new, rng = [2500, 70, 1], np.random.default_rng(4)
+    if how is None:
+        parents = None
+    else:
+        parents = [i - 1 if how == "chain" else int(rng.integers(max(0, i - 200), i)) if i else -1 for n in new for i in range(n)]
+    rows, words, ctx = sum(new), 40, [100, 0, 7]
+    table = torch.full((3, 200), -1, dtype=torch.int32, device=DEV)
+    p = pa.paged_plan_step(ints(ctx), ints(new), table, ints([0] * 3), ints(range(400)), ints([400]), 16, rows, mask_words=words,
+                           parents=None if parents is None else ints(parents))
+    ref = R.plan(ctx, new, parents, table.cpu().numpy() * 0 - 1, [0] * 3, list(range(400)), 16, rows, words)
+    assert p.shortage.tolist() == [0, 0] and p.rope_positions.tolist() == list(ref["rope_positions"])
+    assert torch.equal(p.tree_mask, bits(np.array(ref["tree_mask"], dtype=np.uint64).reshape(rows, words)))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_chunk_of_many_tokens(pa, dtype):  # noqa: F811
+    """As many rows as a chunk of a prompt brings, each with a mask of its own."""
+    c = make_tree_call([650, 90, 300], [400, 3, 300], 4, 2, 64, 16, dtype, any_mask(3), seed=4)
+    out, lse = run_tree(pa, c)
+    check_tree(c, out, lse)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_bounds_may_be_loose(pa, dtype):  # noqa: F811
     """max_q_len, the masks' words and the rows of q beyond what the sequences bring, as a captured step has them."""
