@@ -30,6 +30,9 @@ size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 // 76.6 / 81.5). Row blocks of up to kPlainTiles tiles are made smaller, down to two waves of rows, until there is one for
 // each compute unit (us with / without: bf16 3 x 40 tokens on 400 14.1 / 24.6, 16 x 40 on 350 20.1 / 26.3,
 // fp32 3 x 40 on 400 27.7 / 65; until there are two for each: 32 x 40 on 350 37.9 / 30.7, fp32 8 x 64 on 300 49 / 37.8).
+// Up to 32 rows whose workgroup has its compute unit to itself are four waves', a quarter of a tile of 128 keys each: uncut up to
+// kPlainTiles * 64 keys, to twice as many where that fills half the machine (us with / without: 1 x 8 on 500 11.5 / 13.6, 16 x 8 on 350 11.9 /
+// 12.9, 32 x 8 on 850 24.3 / 33.5, 16 x 8 on 850 19.8 / 21.7; 4 x 8 on 850, 32 workgroups, 17.4 / 15.8, 64 x 8 on 400, 512 workgroups, 29.3 / 22.3).
 TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t max_q_len, int32_t max_seq_len, bool f32)
 {
     constexpr int32_t kPlainTiles = 8, kFullTiles = 16, kOneTermKeys = 256;   // (kOneTermKeys: see tree_mfma_impl.h)
@@ -39,18 +42,21 @@ TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int
     if (f32) p.row_waves = rows <= 16 && columns <= 128 ? 1 : rows <= 32 ? 2 : rows <= 64 || columns > 128 ? 4 : 8;
     else p.row_waves = rows <= 64 ? 2 : rows <= 128 || columns > 128 ? 4 : 8;
     auto blocks_of = [&](int32_t waves) { return (rows + wave_rows * waves - 1) / (wave_rows * waves); };
-    const int32_t tile = f32 && columns > 128 ? 32 : prefill::kBN;
+    const int32_t tile = f32 && columns > 128 ? 32 : 64;
     const int64_t tiles = ((int64_t)max_seq_len + tile - 1) / tile;
-    if (tiles <= kPlainTiles)
-        while (p.row_waves > 2 && (int64_t)batch * num_kv_heads * blocks_of(p.row_waves) < device_cus()) p.row_waves /= 2;
+    const int64_t cus = device_cus(), heads = (int64_t)batch * num_kv_heads;
+    const bool alone = !f32 && rows <= 32 && columns <= 128 && heads <= cus && tiles <= (2 * heads >= cus ? kFullTiles : kPlainTiles);
+    if (alone) p.row_waves = 1;
+    else if (tiles <= kPlainTiles)
+        while (p.row_waves > 2 && heads * blocks_of(p.row_waves) < cus) p.row_waves /= 2;
     const int64_t blocks = blocks_of(p.row_waves);
     p.row_blocks = blocks < 1 ? 1 : (int32_t)blocks;
     p.two_terms = max_seq_len < kOneTermKeys;
     p.wgs = 0;
     p.part_o_bytes = p.part_lse_bytes = p.cuts_bytes = 0;
     const bool pairs = columns <= 128 && p.row_waves == 2 && !f32;
-    const int64_t slots = (int64_t)device_cus() * (pairs ? 2 : 1);
-    if (tiles > (pairs && batch * num_kv_heads * blocks >= slots ? kFullTiles : kPlainTiles)) {
+    const int64_t slots = cus * (pairs ? 2 : 1);
+    if (!alone && tiles > (pairs && heads * blocks >= slots ? kFullTiles : kPlainTiles)) {
         const int64_t most = (batch * blocks * tiles + kTreeMinTiles - 1) / kTreeMinTiles;
         int64_t wgs = slots / num_kv_heads;
         if (wgs > most) wgs = most;

@@ -4,11 +4,12 @@
 // A sequence's n drafted queries and the G query heads of a KV head are n * G rows that all see the context and differ
 // in the last n keys only.  The context's K and V are read once for all of them, so up to about 200 rows the call is bound by
 // that read, not by its 4 * rows * d flops a key; what the kernel is built for is to keep it going.
-//   * A workgroup of four waves owns RB = 32 * WR rows of one (sequence, KV head) and walks keys in tiles of 64, whose K and V
-//     rows the load unit writes straight into LDS through the block table, one tile ahead (two buffers).  Rows are stored in
+//   * A workgroup of four or eight waves owns RB = 32 * WR rows of one (sequence, KV head) and walks keys in tiles, whose K and V
+//     rows the load unit writes straight into LDS through the block table, one to seven tiles ahead.  Rows are stored in
 //     16-byte pieces swizzled so that neither kind of operand read meets a bank conflict.
-//   * WR = 4: a wave takes 32 rows and all 64 keys.  WR = 2 (up to 64 rows): two waves share 32 rows and halve the tile, their
-//     results meet in LDS at the end.
+//   * Beyond 128 rows (64 above 128 columns) a wave takes 32 rows and all 64 keys.  With fewer, two waves share 32 rows and halve the
+//     tile, or on short contexts that leave a compute unit to each workgroup four waves with tiles of 128 keys; their results meet in
+//     LDS at the end.
 //   * Both products are transposed (v_mfma_f32_32x32x16, lane % 32 = row), so softmax statistics are a lane's own:
 //         S^T[key, row] = K Q^T,   O^T[column, row] += V^T P^T.
 //   * Softmax is online in the log2 domain against a reference that trails the maximum: weights are taken with the
@@ -37,8 +38,6 @@ namespace {
 template <int DP>
 struct TreeGeo {
     static constexpr int kRowB = DP > 128 ? 512 : DP > 64 ? 256 : 128;   // bytes of a row in LDS
-    static constexpr int kTileB = kBN * kRowB;                           // K part of a buffer; V follows
-    static constexpr int kBufB = 2 * kTileB;
     static constexpr int kKS = DP / 16;                                  // steps of a score product
     static constexpr int kT = DP / 32;                                   // 32-column blocks of O
 };
@@ -47,11 +46,14 @@ struct TreeGeo {
 // beside the tile being computed has to cover the memory's latency at its full rate, about 100 KB a compute unit.
 template <int WR, int DP>
 struct TreeShape {
-    static constexpr int kKW = WR == 2 || (WR == 4 && DP <= 128) ? 2 : 1;
+    static constexpr int kKW = WR == 1 ? 4 : WR == 2 || (WR == 4 && DP <= 128) ? 2 : 1;
     static constexpr int kWaves = WR * kKW;
-    static constexpr int kOcc = DP <= 128 && kWaves == 4 ? 2 : 1;        // workgroups of a compute unit
-    static constexpr int kBufs = DP > 128 ? 2 : (DP > 64 ? 4 : 8) / kOcc;
-    static constexpr int kLoads = TreeGeo<DP>::kTileB / (1024 * kWaves); // load instructions of a wave and pool a tile
+    static constexpr int kTile = WR == 1 ? 128 : 64;                     // keys
+    static constexpr int kTileB = kTile * TreeGeo<DP>::kRowB;            // K part of a buffer; V follows
+    static constexpr int kBufB = 2 * kTileB;
+    static constexpr int kOcc = DP <= 128 && WR == 2 ? 2 : 1;            // workgroups of a compute unit
+    static constexpr int kBufs = 131072 / (kOcc * kBufB);
+    static constexpr int kLoads = kTileB / (1024 * kWaves);              // load instructions of a wave and pool a tile
 };
 
 // Byte offset inside its LDS row r of logical 16-byte piece L (rows of 512 bytes swizzle each half by itself; of rows of
@@ -151,7 +153,7 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
     typedef TreeGeo<DP> Geo;
     typedef TreeShape<WR, DP> Shape;
     constexpr int RB = 32 * WR, KW = Shape::kKW, NW = Shape::kWaves, NB = Shape::kBufs, ROWB = Geo::kRowB, T = Geo::kT, KS = Geo::kKS;
-    constexpr int HALVES = 2 / KW;                           // 32-key halves of a tile that a wave takes
+    constexpr int TK = Shape::kTile, HALVES = TK / 32 / KW;   // how often a wave takes 32 keys of a tile
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));                            // (what follows from it is not kept across pieces of work)
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -203,16 +205,16 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
             int64_t page_off = ((int64_t)pages[p][i] * a.cache.page_stride + kvh * a.cache.head_stride) * 2;
             asm volatile("" : "+s"(page_off));               // stays in scalar registers
             const uint32_t off = (uint32_t)slot * (uint32_t)(a.cache.token_stride * 2) + lane_off[STEP == 8 ? i & 1 : 0];
-            load_to_lds16(lds0 + b * Geo::kBufB, 1024 * NW * i, reinterpret_cast<const char*>(a.cache.k) + page_off, off);
-            load_to_lds16(lds0 + b * Geo::kBufB, 1024 * NW * i + Geo::kTileB, reinterpret_cast<const char*>(a.cache.v) + page_off, off);
+            load_to_lds16(lds0 + b * Shape::kBufB, 1024 * NW * i, reinterpret_cast<const char*>(a.cache.k) + page_off, off);
+            load_to_lds16(lds0 + b * Shape::kBufB, 1024 * NW * i + Shape::kTileB, reinterpret_cast<const char*>(a.cache.v) + page_off, off);
         }
     };
 
     // The first NB - 1 tiles (a piece of work has a tile at least), the page ids of all of them in one trip.  Q is waited for
     // behind the first of them: what is issued between a load and its wait is waited for as well.
 #pragma unroll
-    for (int i = 0; i < NB - 1; ++i) load_pages(i, min(it.tile_begin + i, it.tile_end - 1) * kBN);
-    fetch(0, 0, it.tile_begin * kBN);
+    for (int i = 0; i < NB - 1; ++i) load_pages(i, min(it.tile_begin + i, it.tile_end - 1) * TK);
+    fetch(0, 0, it.tile_begin * TK);
     // operand offsets: K piece 2 ks + hh of row ql; V pieces of the 32 columns t for the lane's transpose-load row, key 4 hh + j
     // (and 8 on) of a 16-key step, columns 4 qq .. + 3 of the 16-column block dblk
     uint32_t kx[KS], vx[2 * T];
@@ -237,9 +239,9 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
     int32_t ahead = it.tile_begin + 1;                       // the tile to fetch next
 #pragma unroll
     for (int i = 1; i < NB - 1; ++i) {
-        if (ahead < it.tile_end) fetch(i, i, ahead++ * kBN);
+        if (ahead < it.tile_end) fetch(i, i, ahead++ * TK);
     }
-    if (ahead < it.tile_end) load_pages(0, ahead * kBN);
+    if (ahead < it.tile_end) load_pages(0, ahead * TK);
 
     f32x16 o[T];
 #pragma unroll
@@ -256,18 +258,18 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
         else wait_tiles_but<Shape::kLoads, 0>();
         __syncthreads();                                     // tile t is there, and tile t - 1 done with
         if (ahead < it.tile_end) {
-            fetch(b == 0 ? NB - 1 : b - 1, 0, ahead * kBN);
-            if (++ahead < it.tile_end) load_pages(0, ahead * kBN);   // (a tile before they are needed)
+            fetch(b == 0 ? NB - 1 : b - 1, 0, ahead * TK);
+            if (++ahead < it.tile_end) load_pages(0, ahead * TK);   // (a tile before they are needed)
         }
-        const char* const kbuf = buf + b * Geo::kBufB;
+        const char* const kbuf = buf + b * Shape::kBufB;
 #pragma unroll 1
         for (int i = 0; i < HALVES; ++i) {
-            const int half = KW == 2 ? kw : i;
-            const int32_t key0 = t * kBN + 32 * half;
+            const int half = KW > 1 ? kw : i;
+            const int32_t key0 = t * TK + 32 * half;
             if (!live || key0 >= len) continue;              // (wave-uniform)
             f32x16 s = (f32x16)(0.f), p;
             const char* const kh = kbuf + 32 * half * ROWB;
-            const char* const vh = kh + Geo::kTileB;
+            const char* const vh = kh + Shape::kTileB;
             // The operand reads are kept four ahead of their products and V's first step comes behind K's last: left to itself the
             // compiler waits for each read in front of the product that takes it.
             uint4 va[T], vb[T];
@@ -330,8 +332,8 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
     l += __shfl_xor(l, 32, 64);
     constexpr int VECS = 4 * T, MINE = VECS / KW;
     auto vec = [&](int i) { return float4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]}; };
-    float4* const met = reinterpret_cast<float4*>(buf + (b + rw / 2) % NB * Geo::kBufB) + rw % 2 * (VECS * 64) + lane;
-    float2* const ml = reinterpret_cast<float2*>(buf + NB * Geo::kBufB) + rw * 128 + lane;
+    float4* const met = reinterpret_cast<float4*>(buf + (b + rw / 2) % NB * Shape::kBufB) + rw % 2 * (VECS * 64) + lane;
+    float2* const ml = reinterpret_cast<float2*>(buf + NB * Shape::kBufB) + rw * (KW * 64) + lane;
     if (!CAREFUL) {
         float odd[4] = {0.f, 0.f, 0.f, 0.f};                 // (0 times what is not finite is NaN)
 #pragma unroll
@@ -341,14 +343,20 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
         const bool any = __any(!((odd[0] + odd[1]) + (odd[2] + odd[3]) == 0.f));
         if (lane == 0) flags[wave] = any ? 1u : 0u;
     }
+    if (KW == 4) {
+        float4* const all = reinterpret_cast<float4*>(buf + b * Shape::kBufB) + kw * (VECS * 64) + lane;
+#pragma unroll
+        for (int i = 0; i < VECS; ++i)
+            if (i / MINE != kw) all[i * 64] = vec(i);
+    }
     if (KW == 2) {
 #pragma unroll
         for (int i = 0; i < MINE; ++i) {
             if (kw == 0) met[(MINE + i) * 64] = vec(VECS - MINE + i);
             else met[i * 64] = vec(i);
         }
-        ml[kw * 64] = float2{m, l};
     }
+    if (KW > 1) ml[kw * 64] = float2{m, l};
     __syncthreads();                                         // (the tile buffers are free)
     if (!CAREFUL) {
         bool again = false;
@@ -360,7 +368,34 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
 #pragma unroll
     for (int i = 0; i < MINE; ++i) {
         if (KW == 1 || kw == 0) mine[i] = vec(i);
-        else mine[i] = vec(VECS - MINE + i);
+        else if (KW == 2 || kw == 3) mine[i] = vec(VECS - MINE + i);
+        else if (kw == 1) mine[i] = vec(VECS / 4 + i);
+        else mine[i] = vec(VECS / 2 + i);
+    }
+    if (KW == 4) {
+        const float4* const all = reinterpret_cast<const float4*>(buf + b * Shape::kBufB) + MINE * kw * 64 + lane;
+        float2 s[KW];
+#pragma unroll
+        for (int k = 0; k < KW; ++k) s[k] = ml[k * 64];
+        const float own = m;
+        m = fmaxf(fmaxf(s[0].x, s[1].x), fmaxf(s[KW / 2].x, s[KW - 1].x));
+        const float use = m == -INFINITY ? 0.f : m, wo = __builtin_amdgcn_exp2f(own - use);
+        l = 0.f;
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) mine[i] = float4{mine[i].x * wo, mine[i].y * wo, mine[i].z * wo, mine[i].w * wo};
+#pragma unroll
+        for (int k = 0; k < KW; ++k) {
+            const float w = __builtin_amdgcn_exp2f(s[k].x - use);
+            l = __builtin_fmaf(s[k].y, w, l);
+            if (k == kw) continue;
+#pragma unroll
+            for (int i = 0; i < MINE; ++i) {
+                const float4 v = all[(k * VECS + i) * 64];
+                mine[i] = float4{__builtin_fmaf(v.x, w, mine[i].x), __builtin_fmaf(v.y, w, mine[i].y), __builtin_fmaf(v.z, w, mine[i].z),
+                                 __builtin_fmaf(v.w, w, mine[i].w)};
+            }
+        }
+        __syncthreads();                                     // (before the next piece of work loads over them)
     }
     if (KW == 2) {
         const float2 m0 = ml[0], m1 = ml[64];
@@ -402,8 +437,9 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
 template <int WR, bool TWO, typename E, int DP>
 struct Tree16 {
     typedef TreeShape<WR, DP> Shape;
-    static constexpr int kRows = 32 * WR, kWaveRows = 32, kColumns = DP, kTile = kBN, kWaves = Shape::kWaves, kOcc = Shape::kOcc;
-    static constexpr int kLds = Shape::kBufs * TreeGeo<DP>::kBufB + (Shape::kKW - 1) * WR * 1024;   // (maxima and sums of two waves)
+    static constexpr bool kCut = WR > 1;                                 // (one wave of rows is for calls without a cut)
+    static constexpr int kRows = 32 * WR, kWaveRows = 32, kColumns = DP, kTile = Shape::kTile, kWaves = Shape::kWaves, kOcc = Shape::kOcc;
+    static constexpr int kLds = Shape::kBufs * Shape::kBufB + (Shape::kKW - 1) * WR * 1024;   // (maxima and sums of two waves)
     template <bool CAREFUL>
     static __device__ __forceinline__ bool work(char* buf, uint32_t* flags, const TreeKernelArgs& a, const TreeItem& it, int32_t kvh)
     {
@@ -426,6 +462,8 @@ pa_status launch_tree_rows(const TreeKernelArgs& a, bool merge, int row_waves, h
 template <typename E, int DP>
 pa_status launch_tree_type(const TreeKernelArgs& a, bool merge, int row_waves, bool two_terms, hipStream_t stream)
 {
+    if constexpr (DP <= 128)
+        if (row_waves == 1) return launch_tree_of<Tree16<1, true, E, DP>>(a, merge, stream);
     if (row_waves == 2) return launch_tree_of<Tree16<2, true, E, DP>>(a, merge, stream);
     return two_terms ? launch_tree_rows<true, E, DP>(a, merge, row_waves, stream) : launch_tree_rows<false, E, DP>(a, merge, row_waves, stream);
 }

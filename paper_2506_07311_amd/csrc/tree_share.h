@@ -2,7 +2,8 @@
 // kernel around a piece of work, and the merge of what the division cuts.
 //
 // A shape S says what a workgroup does: kRows rows (query, head of the KV head's group) of one sequence at a time, kWaveRows
-// of them a wave, in kColumns columns; tiles of kTile keys; kWaves waves, kOcc workgroups on a compute unit, kLds bytes of LDS; and
+// of them a wave, in kColumns columns; tiles of kTile keys; kWaves waves, kOcc workgroups on a compute unit, kLds bytes of LDS; kCut: its
+// row blocks may be cut; and
 //     work<CAREFUL>(buf, flags, args, item, KV head)   does a piece of work; true: it has to be done again with CAREFUL
 //     store(out, element, float4)                     four output columns
 #pragma once
@@ -164,7 +165,7 @@ __global__ __launch_bounds__(64 * S::kWaves, S::kOcc * S::kWaves / 4) void paged
     int32_t t = 0, t_end = 1, first = 0;
     TreeShare share = {0, 0, 0, 0, 0};
     TreeSeq q = {0, 0, 0, 0, 0};
-    if (a.wgs == 0) {                                        // one row block
+    if (!S::kCut || a.wgs == 0) {                                        // one row block
         s = x / a.row_blocks;
         q = tree_seq<S>(a, s);
         if (x % a.row_blocks >= q.blocks || q.tiles <= 0) return;
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(64 * S::kWaves, S::kOcc * S::kWaves / 4) void paged
         it.row0 = q.row0;
         it.n = q.n;
         it.len = q.len;
-        if (a.wgs == 0) {
+        if (!S::kCut || a.wgs == 0) {
             it.rb = x % a.row_blocks;
             it.tile_begin = 0;
             it.tile_end = q.tiles;
@@ -373,8 +374,10 @@ pa_status launch_tree_of(const TreeKernelArgs& a, bool merge, hipStream_t stream
     const int64_t waves = units * (S::kRows / S::kWaveRows);
     if (grid > 0x7fffffffLL || waves * LINES > 0x7fffffffLL || a.cache.num_kv_heads > 65535) return PA_ERR_UNSUPPORTED;
     if (merge) {
-        if (waves * LINES * a.cache.num_kv_heads <= 512) launch_tree_merge<S, LINES, 8>(a, stream);
-        else launch_tree_merge<S, PARTS, 4>(a, stream);
+        if constexpr (S::kCut) {
+            if (waves * LINES * a.cache.num_kv_heads <= 512) launch_tree_merge<S, LINES, 8>(a, stream);
+            else launch_tree_merge<S, PARTS, 4>(a, stream);
+        }
     } else {
         hipLaunchKernelGGL((paged_attention_tree_mfma_kernel<S>), dim3((uint32_t)grid), dim3(64 * S::kWaves), 0, stream, a,
                            a.cu_q_lens, a.seq_lens, a.block_table, a.tree_mask);
