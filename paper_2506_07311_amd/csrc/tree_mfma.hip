@@ -23,19 +23,25 @@ size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 // 16-bit pools: up to 64 rows a (sequence, KV head) two waves share 32 rows, up to 128 at head_dims up to 128 as well, with eight
 // waves; beyond that a workgroup takes 256 rows (128 above head_dim 128, where a wave's O and Q fill its registers).  fp32 pools: 16 rows a
-// wave, 16, 32, 64 or 128 a workgroup.  The tiles are shared by as many workgroups as the machine holds at once; on contexts of
-// up to kPlainTiles tiles a row block is one workgroup's and there is no merge (us with 4 / 8 / 16: 16 x 8 tokens on 300 to 400 18.1 /
-// 12.7 / 12.8, 4 x 8 on 800 to 900 15.8 / 15.7 / 20.8); up to kFullTiles where such row blocks alone fill a machine whose compute units
-// hold two (with 8 / 16 / 32: 64 x 8 on 800 to 900 52.4 / 39.6 / 39.9, on 64 to 2000 35.9 / 35.9 / 41.0; of 256 rows, 64 x 64 on 64 to 1000,
-// 76.6 / 81.5). Row blocks of up to kPlainTiles tiles are made smaller, down to two waves of rows, until there is one for
-// each compute unit (us with / without: bf16 3 x 40 tokens on 400 14.1 / 24.6, 16 x 40 on 350 20.1 / 26.3,
-// fp32 3 x 40 on 400 27.7 / 65; until there are two for each: 32 x 40 on 350 37.9 / 30.7, fp32 8 x 64 on 300 49 / 37.8).
-// Up to 32 rows whose workgroup has its compute unit to itself are four waves', a quarter of a tile of 128 keys each: uncut up to
-// kPlainTiles * 64 keys, to twice as many where that fills half the machine (us with / without: 1 x 8 on 500 11.5 / 13.6, 16 x 8 on 350 11.9 /
-// 12.9, 32 x 8 on 850 24.3 / 33.5, 16 x 8 on 850 19.8 / 21.7; 4 x 8 on 850, 32 workgroups, 17.4 / 15.8, 64 x 8 on 400, 512 workgroups, 29.3 / 22.3).
+// wave, 16, 32, 64 or 128 a workgroup.  The tiles are shared by as many workgroups as the machine holds at once.
+//
+// On short contexts a row block (a "unit" with its KV head) is one workgroup's and there is no merge:
+//   * up to kPlainTiles tiles (us with 4 / 8 / 16: 16 x 8 tokens on 300 to 400 18.1 / 12.7 / 12.8, 4 x 8 on 800 to 900 15.8 / 15.7 / 20.8);
+//     blocks of more than 64 rows are then made smaller until there is one for each compute unit (with / without: bf16 3 x 40 on 400 14.1 /
+//     24.6, 16 x 40 on 350 20.1 / 26.3, fp32 3 x 40 on 400 27.7 / 65; until there are two: 32 x 40 on 350 37.9 / 30.7);
+//   * 16-bit pools, units for half of the workgroups that the machine holds: up to kFullTiles, and as often as many as there are
+//     rounds of them, since the longest one then is a small part of the call (with / without: 32 x 16 on 800 to 900 27.2 / 38.9, 32 x 64
+//     46.8 / 71.6, 32 x 32 on 700 to 1400 35.8 / 49.7, 200 x 8 on 64 to 2000 116 / 123; where lengths are far apart 32 x 16 on 64 to 1500
+//     29.8 / 26.3, 200 x 8 on 64 to 4000 191 / 184; a quarter of the workgroups, 8 x 64 on 700 to 1400, 48.5 / 32.7); above 128 columns,
+//     where a workgroup holds only two tiles, units for all workgroups and up to 2 kPlainTiles (32 x 16 on 800 to 900, 16 / 8 heads,
+//     44.9 / 60.1; 24 tiles: 100 x 16 on 64 to 3000 201 / 158; half of them: 16 x 16 on 700 to 1400 53.3 / 42.3);
+//   * fp32 pools take kPlainTiles in any case (a matrix core does 1/16 of the work in the time: 8 x 40 on 600 to 900 132 / 89).
+// Up to 32 rows whose workgroup has its compute unit to itself are four waves', a quarter of a tile of 128 keys each, of as many keys
+// (with / without: 1 x 8 on 500 11.5 / 13.6, 16 x 8 on 350 11.9 / 12.9, 32 x 8 on 850 24.3 / 33.5, 16 x 8 on 850 19.8 / 21.7; 4 x 8 on 850, 32
+// workgroups, 17.4 / 15.8, 64 x 8 on 400, 512 workgroups, 29.3 / 22.3).
 TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t max_q_len, int32_t max_seq_len, bool f32)
 {
-    constexpr int32_t kPlainTiles = 8, kFullTiles = 16, kOneTermKeys = 256;   // (kOneTermKeys: see tree_mfma_impl.h)
+    constexpr int32_t kPlainTiles = 8, kFullTiles = 24, kOneTermKeys = 256;   // (kOneTermKeys: see tree_mfma_impl.h)
     TreePlan p;
     const int64_t rows = (int64_t)max_q_len * (num_q_heads / num_kv_heads);
     const int32_t columns = columns_of(head_dim, f32), wave_rows = f32 ? 16 : 32;
@@ -45,18 +51,21 @@ TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int
     const int32_t tile = f32 && columns > 128 ? 32 : 64;
     const int64_t tiles = ((int64_t)max_seq_len + tile - 1) / tile;
     const int64_t cus = device_cus(), heads = (int64_t)batch * num_kv_heads;
-    const bool alone = !f32 && rows <= 32 && columns <= 128 && heads <= cus && tiles <= (2 * heads >= cus ? kFullTiles : kPlainTiles);
-    if (alone) p.row_waves = 1;
-    else if (tiles <= kPlainTiles)
+    if (!f32 && rows <= 32 && columns <= 128 && heads <= cus && tiles <= (2 * heads >= cus ? kFullTiles : kPlainTiles)) {
+        p.row_waves = 1;
+    } else if (tiles <= kPlainTiles) {
         while (p.row_waves > 2 && heads * blocks_of(p.row_waves) < cus) p.row_waves /= 2;
-    const int64_t blocks = blocks_of(p.row_waves);
+    }
+    const int64_t blocks = blocks_of(p.row_waves), units = heads * blocks;
     p.row_blocks = blocks < 1 ? 1 : (int32_t)blocks;
     p.two_terms = max_seq_len < kOneTermKeys;
     p.wgs = 0;
     p.part_o_bytes = p.part_lse_bytes = p.cuts_bytes = 0;
-    const bool pairs = columns <= 128 && p.row_waves == 2 && !f32;
-    const int64_t slots = cus * (pairs ? 2 : 1);
-    if (!alone && tiles > (pairs && heads * blocks >= slots ? kFullTiles : kPlainTiles)) {
+    const int64_t slots = cus * (columns <= 128 && p.row_waves == 2 && !f32 ? 2 : 1);
+    int64_t plain = kPlainTiles;
+    if (!f32 && columns <= 128 && 2 * units >= slots) plain = kFullTiles * (units > slots ? units / slots : 1);
+    if (!f32 && columns > 128 && units >= slots) plain = 2 * kPlainTiles;
+    if (tiles > plain && (f32 || p.row_waves > 1)) {
         const int64_t most = (batch * blocks * tiles + kTreeMinTiles - 1) / kTreeMinTiles;
         int64_t wgs = slots / num_kv_heads;
         if (wgs > most) wgs = most;
