@@ -517,8 +517,9 @@ def pa_rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "
 def _rows(t: torch.Tensor, what: str, shape, dtype) -> torch.Tensor:
     """[T, heads, d] whose tokens may lie apart (a part of one projection) but whose heads are contiguous."""
     if t.dtype != dtype or not t.is_cuda or tuple(t.shape) != tuple(shape) or \
-            (t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]))):
-        raise PagedAttnError(f"{what} must be a {dtype} device tensor {list(shape)} with contiguous heads")
+            (t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]) or
+                            (t.shape[0] > 1 and t.stride(0) < t.shape[1] * t.shape[2]))):
+        raise PagedAttnError(f"{what} must be a {dtype} device tensor {list(shape)} with contiguous heads, tokens apart")
     return t
 
 

@@ -194,6 +194,21 @@ def test_pools_whose_offsets_pass_32_bits(pa, dtype, n, heads, head_major):  # n
         assert torch.equal(a, b)
 
 
+def test_rows_that_share_memory_are_refused(pa):  # noqa: F811
+    """One token's row for all of them (a stride of 0) is not taken for a contiguous tensor, nor are rows that overlap."""
+    k, v = (torch.zeros(4, 16, 2, 64, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    at, inv = ints([0, 1, 2]), torch.ones(32, dtype=torch.float64, device=DEV)
+    good = torch.zeros(3, 2, 64, dtype=torch.bfloat16, device=DEV)
+    same = torch.zeros(1, 2, 64, dtype=torch.bfloat16, device=DEV).expand(3, 2, 64)
+    over = torch.zeros(400, dtype=torch.bfloat16, device=DEV).as_strided((3, 2, 64), (64, 64, 1))
+    table = ints([[0, 1]])
+    for bad in (same, over):
+        for q, kn, vn, out in ((bad, good, good, None), (good, bad, good, None), (good, good, bad, None), (good, good, good, bad)):
+            with pytest.raises(pa.PagedAttnError):
+                pa.paged_rope_append(k, v, q, kn, vn, at, ints([0, 0, 0]), at, table, inv, q_out=out)
+    pa.paged_rope_append(k, v, good, good, good, at, ints([0, 0, 0]), at, table, inv)
+
+
 def test_another_stream_and_prepared_calls(pa):  # noqa: F811
     """Calls run on the stream that they are given or that is current, in its order, and take what their tensors hold then."""
     c = make_tree_call([1500, 90], [8, 3], 8, 2, 128, 16, torch.bfloat16, ancestors(4), seed=5)
