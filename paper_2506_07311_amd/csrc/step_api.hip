@@ -137,7 +137,7 @@ pa_status paged_attention_tree(const pa_kv_cache_desc* cache, const void* q, voi
     if (batch < 0 || total_q < 0 || max_q_len < 0 || mask_words < 0 || max_blocks < 0 || max_seq_len < 0)
         return PA_ERR_INVALID_ARG;
     if (num_q_heads <= 0 || num_q_heads % cache->num_kv_heads != 0 || !(scale == scale)) return PA_ERR_INVALID_ARG;
-    if (batch == 0 || total_q == 0) return PA_OK;
+    if (batch == 0 || total_q == 0 || max_q_len == 0) return PA_OK;
     if (!q || !out || !cu_q_lens || !tree_mask || !block_table || !seq_lens) return PA_ERR_INVALID_ARG;
     if ((int64_t)mask_words * 64 < max_q_len || ((uintptr_t)tree_mask & 7)) return PA_ERR_INVALID_ARG;
     if (((uintptr_t)q | (uintptr_t)out) & 15) return PA_ERR_UNSUPPORTED;

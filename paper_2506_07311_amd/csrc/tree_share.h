@@ -274,6 +274,19 @@ __global__ __launch_bounds__(64 * NW) void paged_attention_tree_merge_kernel(
     if (pieces == 1) return;
     const int64_t slot0 = ((int64_t)kvh * a.wgs + cut.x) * 2;
     auto slot = [&](int32_t k) { return slot0 + 2 * (int64_t)k + (k == 0 ? 1 : 0); };
+    // float4 j of a wave's partial: lane j % 64 holds row j % RW, four columns of every 4 * 64 / RW.  Each of the NW waves takes
+    // every NW-th piece, several pieces at a time, the first of them ahead of their weights; then they meet in LDS.
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane % RW;
+    const float4* const po = reinterpret_cast<const float4*>(a.part_o) + rw * VECS + part * MINE + lane;
+    constexpr int DEEP = LINES > 2 ? 2 : 8 / LINES;          // pieces at a time
+    float4 v[DEEP][LINES];
+    auto read = [&](int32_t k0) {
+#pragma unroll
+        for (int k = 0; k < DEEP; ++k)
+#pragma unroll
+            for (int i = 0; i < LINES; ++i) v[k][i] = po[slot(min(k0 + NW * k, pieces - 1)) * (WR * VECS) + 64 * i];
+    };
+    read(wave);
     constexpr int GROUPS = 64 * NW / RW;                     // threads a row
     const int32_t srow = threadIdx.x % RW, group = threadIdx.x / RW;
     float top = -INFINITY;
@@ -309,20 +322,11 @@ __global__ __launch_bounds__(64 * NW) void paged_attention_tree_merge_kernel(
         sm_sum[srow] = wsum;
     }
     __syncthreads();
-    // float4 j of a wave's partial: lane j % 64 holds row j % RW, four columns of every 4 * 64 / RW.  Each of the NW waves takes
-    // every NW-th piece, several pieces at a time; then they meet in LDS.
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane % RW;
-    const float4* const po = reinterpret_cast<const float4*>(a.part_o) + rw * VECS + part * MINE + lane;
     float4 acc[LINES];
 #pragma unroll
     for (int i = 0; i < LINES; ++i) acc[i] = float4{0.f, 0.f, 0.f, 0.f};
-    constexpr int DEEP = LINES > 2 ? 2 : 8 / LINES;          // pieces at a time
     for (int32_t k0 = wave; k0 < pieces; k0 += NW * DEEP) {
-        float4 v[DEEP][LINES];
-#pragma unroll
-        for (int k = 0; k < DEEP; ++k)
-#pragma unroll
-            for (int i = 0; i < LINES; ++i) v[k][i] = po[slot(min(k0 + NW * k, pieces - 1)) * (WR * VECS) + 64 * i];
+        if (k0 > wave) read(k0);
 #pragma unroll
         for (int k = 0; k < DEEP; ++k) {
             if (k0 + NW * k >= pieces) break;
@@ -368,7 +372,7 @@ pa_status launch_tree_of(const TreeKernelArgs& a, bool merge, hipStream_t stream
     const int64_t grid = (a.wgs > 0 ? a.wgs : units) * a.cache.num_kv_heads;
     // A merging workgroup takes four lines of 64 vectors of a wave's columns, or one and with twice the waves where there are few
     // (us with four / one: 2 x 8 tokens on 1500, 512 workgroups, 16.1 / 15.3; 8 x 16 on 128 to 2048, 2048 workgroups, 22.1 / 24.4;
-    // with one, of four / eight / sixteen waves: 1 x 8 on 100000 with 8 / 1 heads, 32 workgroups and 256 pieces, 38.1 / 29.3 / 25.4,
+    // with one, of four / eight / sixteen waves, before a wave's first pieces were read ahead of their weights (25.5 -> 24.6 on 20000): 1 x 8 on 100000 with 8 / 1 heads, 32 workgroups and 256 pieces, 38.1 / 29.3 / 25.4,
     // 2 x 8 on 1500 14.1 / 13.8 / 16.6).
     constexpr int LINES = S::kWaveRows * S::kColumns / 256, PARTS = LINES > 4 ? LINES / 4 : 1;
     const int64_t waves = units * (S::kRows / S::kWaveRows);

@@ -87,6 +87,7 @@ def test_tree_attention_refusals(lib):
         assert call(fn, a, **bad) == UNSUPPORTED, bad
     assert call(fn, a, ws=NULL) == SMALL and call(fn, a, bytes=size(16)) == SMALL
     assert call(fn, a, batch=i32(0)) == 0 and call(fn, a, total=i32(0)) == 0
+    assert call(fn, a, max_q=i32(0), words=i32(0)) == 0           # no sequence brings a query: nothing to do
 
 
 def test_tree_workspace_bound(lib):
