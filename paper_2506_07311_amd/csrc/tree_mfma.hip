@@ -110,6 +110,7 @@ pa_status launch_tree_mfma(const TreeArgs& t, void* workspace, hipStream_t strea
     a.wgs = p.wgs;
     a.row_blocks = p.row_blocks;
     a.scale = t.scale;
+    a.together = t.cache.head_stride * (t.dtype == PA_DTYPE_F32 ? 4 : 2) % 128 != 0;
     auto launch = [&](bool merge) {
         if (t.dtype == PA_DTYPE_F32) return launch_tree_f32(a, merge, p.row_waves, stream);
         switch (columns_of(t.cache.head_dim, false)) {

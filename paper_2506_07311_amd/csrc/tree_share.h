@@ -29,6 +29,7 @@ struct TreeKernelArgs {
     int32_t mask_words, batch, num_q_heads, max_blocks, group;
     int32_t wgs;                 // workgroups of a KV head that share the tiles; 0: one a (sequence, row block)
     int32_t row_blocks;          // most row blocks of a sequence
+    int32_t together;            // != 0: the KV heads of a share on one chiplet
     float scale;
 };
 
@@ -159,16 +160,24 @@ __global__ __launch_bounds__(64 * S::kWaves, S::kOcc * S::kWaves / 4) void paged
     __shared__ uint32_t flags[8];
     const int lane = threadIdx.x & 63;
     const int32_t hkv = a.cache.num_kv_heads;
-    const int32_t kvh = (int32_t)(blockIdx.x % (uint32_t)hkv), x = (int32_t)(blockIdx.x / (uint32_t)hkv);
+    // Workgroup i runs on chiplet i % 8.  KV heads in a row spread over the chiplets; where their rows share cache lines (160 or 192
+    // bytes a row), the heads of a share stay on one, whose L2 then reads such a line once (us without / with: 8 x 8 tokens on 30000, head_dim
+    // 80 146 / 117, 96 150 / 138; where they do not, 128 181 / 188, 64 112 / 117).
+    int32_t kvh = (int32_t)(blockIdx.x % (uint32_t)hkv), x = (int32_t)(blockIdx.x / (uint32_t)hkv);
+    if (a.together) {
+        kvh = (int32_t)(blockIdx.x / 8 % (uint32_t)hkv);
+        x = (int32_t)(blockIdx.x % 8 + 8 * (blockIdx.x / 8 / (uint32_t)hkv));
+        if (a.wgs > 0 && x >= a.wgs) return;
+    }
     // this workgroup's places [t, t_end), the sequence of the first and that one's first place
     int32_t s = 0;
     int32_t t = 0, t_end = 1, first = 0;
     TreeShare share = {0, 0, 0, 0, 0};
     TreeSeq q = {0, 0, 0, 0, 0};
-    if (!S::kCut || a.wgs == 0) {                                        // one row block
+    if (!S::kCut || a.wgs == 0) {                            // one row block
         s = x / a.row_blocks;
         q = tree_seq<S>(a, s);
-        if (x % a.row_blocks >= q.blocks || q.tiles <= 0) return;
+        if (x % a.row_blocks >= q.blocks || q.tiles <= 0) return;   // (or no sequence's)
     } else {
         const TreeSeq start = tree_seq<S>(a, lane);
         share = tree_share<S>(a, lane, start);
@@ -369,11 +378,11 @@ template <typename S>
 pa_status launch_tree_of(const TreeKernelArgs& a, bool merge, hipStream_t stream)
 {
     const int64_t units = (int64_t)a.batch * a.row_blocks;
-    const int64_t grid = (a.wgs > 0 ? a.wgs : units) * a.cache.num_kv_heads;
+    const int64_t shares = a.wgs > 0 ? a.wgs : units, grid = (a.together ? (shares + 7) / 8 * 8 : shares) * a.cache.num_kv_heads;
     // A merging workgroup takes four lines of 64 vectors of a wave's columns, or one and with twice the waves where there are few
     // (us with four / one: 2 x 8 tokens on 1500, 512 workgroups, 16.1 / 15.3; 8 x 16 on 128 to 2048, 2048 workgroups, 22.1 / 24.4;
-    // with one, of four / eight / sixteen waves, before a wave's first pieces were read ahead of their weights (25.5 -> 24.6 on 20000): 1 x 8 on 100000 with 8 / 1 heads, 32 workgroups and 256 pieces, 38.1 / 29.3 / 25.4,
-    // 2 x 8 on 1500 14.1 / 13.8 / 16.6).
+    // with one, of four / eight / sixteen waves: 1 x 8 on 100000 with 8 / 1 heads, 32 workgroups and 256 pieces, 38.1 / 29.3 / 25.4,
+    // 2 x 8 on 1500 14.1 / 13.8 / 16.6; a wave's first pieces ahead of their weights took 1 to 1.4 off the first).
     constexpr int LINES = S::kWaveRows * S::kColumns / 256, PARTS = LINES > 4 ? LINES / 4 : 1;
     const int64_t waves = units * (S::kRows / S::kWaveRows);
     if (grid > 0x7fffffffLL || waves * LINES > 0x7fffffffLL || a.cache.num_kv_heads > 65535) return PA_ERR_UNSUPPORTED;
