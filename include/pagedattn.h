@@ -345,9 +345,7 @@ pa_status paged_rope_append(const pa_kv_cache_desc* cache, const void* q, int64_
  * tree_mask: uint64[total_q, mask_words], 64 * mask_words >= max_q_len (host upper bound of n).  q, out [total_q, Hq, d],
  * lse NULL or float[total_q, Hq]; rows behind cu_q_lens[batch] are left as they were.  Workspace as for decode, of at least
  * paged_attention_tree_workspace_bytes.  Any cache the library takes.  Results repeat bit for bit with the same arguments.
- * fp32 arithmetic; of 16-bit pools the weights (at most 1) enter the product with V as two 16-bit terms, exact to 2^-16 or
- * better, but with more than 64 rows (max_q_len x query heads of a KV head) and max_seq_len >= 256 as one: each weight is then
- * off by half a step of its type, of a sum whose own rounding to the output is as large.
+ * fp32 arithmetic; of 16-bit pools the weights enter the product with V as two 16-bit terms, exact to 2^-16 or better.
  */
 size_t paged_attention_tree_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                             int32_t total_q, int32_t max_q_len, int32_t max_seq_len);

@@ -302,7 +302,6 @@ pa_status launch_tree_generic(const TreeArgs& a, hipStream_t stream);
 struct TreePlan {
     int32_t row_waves;           // waves of a workgroup beside each other in rows: 2, 4 or 8 of 32 rows; fp32 1, 2 or 4 of 16
     int32_t row_blocks;          // most row blocks of a sequence
-    bool two_terms;              // softmax weights as two 16-bit terms with more than 64 rows, too
     int32_t wgs;                 // workgroups of a KV head that share all key tiles; 0: one a row block, no partials
     size_t part_o_bytes, part_lse_bytes, cuts_bytes;
 };

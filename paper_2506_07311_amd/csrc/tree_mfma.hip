@@ -3,13 +3,13 @@
 
 namespace pa {
 
-pa_status launch_tree_d256(const TreeKernelArgs& a, bool merge, pa_dtype dtype, const TreePlan& p, hipStream_t stream);
-pa_status launch_tree_d128(const TreeKernelArgs& a, bool merge, pa_dtype dtype, const TreePlan& p, hipStream_t stream)
+pa_status launch_tree_d256(const TreeKernelArgs& a, bool merge, pa_dtype dtype, int row_waves, hipStream_t stream);
+pa_status launch_tree_d128(const TreeKernelArgs& a, bool merge, pa_dtype dtype, int row_waves, hipStream_t stream)
 {
-    return launch_tree_dim<128>(a, merge, dtype, p, stream);
+    return launch_tree_dim<128>(a, merge, dtype, row_waves, stream);
 }
-pa_status launch_tree_d96(const TreeKernelArgs& a, bool merge, pa_dtype dtype, const TreePlan& p, hipStream_t stream);
-pa_status launch_tree_d64(const TreeKernelArgs& a, bool merge, pa_dtype dtype, const TreePlan& p, hipStream_t stream);
+pa_status launch_tree_d96(const TreeKernelArgs& a, bool merge, pa_dtype dtype, int row_waves, hipStream_t stream);
+pa_status launch_tree_d64(const TreeKernelArgs& a, bool merge, pa_dtype dtype, int row_waves, hipStream_t stream);
 
 pa_status launch_tree_f32(const TreeKernelArgs& a, bool merge, int row_waves, hipStream_t stream);
 
@@ -41,7 +41,7 @@ size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 // workgroups, 17.4 / 15.8, 64 x 8 on 400, 512 workgroups, 29.3 / 22.3).
 TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t max_q_len, int32_t max_seq_len, bool f32)
 {
-    constexpr int32_t kPlainTiles = 8, kFullTiles = 24, kOneTermKeys = 256;   // (kOneTermKeys: see tree_mfma_impl.h)
+    constexpr int32_t kPlainTiles = 8, kFullTiles = 24;
     TreePlan p;
     const int64_t rows = (int64_t)max_q_len * (num_q_heads / num_kv_heads);
     const int32_t columns = columns_of(head_dim, f32), wave_rows = f32 ? 16 : 32;
@@ -58,7 +58,6 @@ TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int
     }
     const int64_t blocks = blocks_of(p.row_waves), units = heads * blocks;
     p.row_blocks = blocks < 1 ? 1 : (int32_t)blocks;
-    p.two_terms = max_seq_len < kOneTermKeys;
     p.wgs = 0;
     p.part_o_bytes = p.part_lse_bytes = p.cuts_bytes = 0;
     const int64_t slots = cus * (columns <= 128 && p.row_waves == 2 && !f32 ? 2 : 1);
@@ -114,11 +113,11 @@ pa_status launch_tree_mfma(const TreeArgs& t, void* workspace, hipStream_t strea
     auto launch = [&](bool merge) {
         if (t.dtype == PA_DTYPE_F32) return launch_tree_f32(a, merge, p.row_waves, stream);
         switch (columns_of(t.cache.head_dim, false)) {
-            case 64: return launch_tree_d64(a, merge, t.dtype, p, stream);
-            case 96: return launch_tree_d96(a, merge, t.dtype, p, stream);
-            case 128: return launch_tree_d128(a, merge, t.dtype, p, stream);
+            case 64: return launch_tree_d64(a, merge, t.dtype, p.row_waves, stream);
+            case 96: return launch_tree_d96(a, merge, t.dtype, p.row_waves, stream);
+            case 128: return launch_tree_d128(a, merge, t.dtype, p.row_waves, stream);
         }
-        return launch_tree_d256(a, merge, t.dtype, p, stream);
+        return launch_tree_d256(a, merge, t.dtype, p.row_waves, stream);
     };
     {
         ProfileScope prof("paged_attention_tree_mfma_kernel", stream);

@@ -3,9 +3,9 @@
 
 namespace pa {
 
-pa_status launch_tree_d256(const TreeKernelArgs& a, bool merge, pa_dtype dtype, const TreePlan& p, hipStream_t stream)
+pa_status launch_tree_d256(const TreeKernelArgs& a, bool merge, pa_dtype dtype, int row_waves, hipStream_t stream)
 {
-    return launch_tree_dim<256>(a, merge, dtype, p, stream);
+    return launch_tree_dim<256>(a, merge, dtype, row_waves, stream);
 }
 
 }  // namespace pa

@@ -14,12 +14,10 @@
 //         S^T[key, row] = K Q^T,   O^T[column, row] += V^T P^T.
 //   * Softmax is online in the log2 domain against a reference that trails the maximum: weights are taken with the
 //     reference as it stands, and only where a lane's sum leaves the range that 16-bit operands carry is it raised and O
-//     rescaled.  Up to 64 rows, and in calls for contexts of less than kOneTermKeys = 256, weights enter as two 16-bit terms (p = hi + lo, off by
-//     2^-17 of a weight): the second term's matrix work hides behind the read.  With more rows and longer contexts, where the matrix
-//     cores are the bound (and the card's power: the clock falls to 1.7 GHz), they enter as one, as the prefill kernel's do on long contexts:
-//     the weights' rounding, independent from key to key, then weighs as much as the output's own (error against 64 bits 1.41 times
-//     that of the output's rounding alone).  us with two terms / one: 16 x 16 tokens on 131072, 64 / 8 heads, 1910 / 1530, 32 x 64
-//     on 8000 408 / 318, 8 x 32 on 3600 43.0 / 36.6, 64 x 64 on 800 131 / 109, 4 x 32 on 700 20.2 / 19.4.
+//     rescaled.  Weights enter as two 16-bit terms (p = hi + lo), whatever the call's sizes and bounds are: a sequence's weights do
+//     not become coarser because of the others' rows or of a loose bound.  Up to 64 rows the second term's matrix work hides behind the
+//     read; with more it is a third of the matrix work (one term alone, 2^-9 of a weight in bf16: an error against 64 bits 1.41 times that
+//     of the output's rounding, and more where weights cancel).
 //   * A key is masked by selection: key len - n + t of a tile is seen by a row if bit t of the row's words is set, 32 bits at a
 //     time; tiles that end in the context take no mask at all.  An infinity or a NaN in a V row that some rows of a tile
 //     do not see would reach them through a product with a weight of zero.  It always leaves its mark on an accumulator, so
@@ -77,14 +75,13 @@ __device__ __forceinline__ uint4 tree_v_frag(const char* lo, const char* hi)
     return __builtin_bit_cast(uint4, r);
 }
 
-template <typename E, bool TWO>
+template <typename E>
 __device__ __forceinline__ void tree_pack(uint4& w, uint4& wl, const f32x16& p, int r0)
 {
     w.x = E::pack(p[r0 + 0], p[r0 + 1]);
     w.y = E::pack(p[r0 + 2], p[r0 + 3]);
     w.z = E::pack(p[r0 + 4], p[r0 + 5]);
     w.w = E::pack(p[r0 + 6], p[r0 + 7]);
-    if (!TWO) return;
     wl.x = E::pack(p[r0 + 0] - E::lo_of(w.x), p[r0 + 1] - E::hi_of(w.x));
     wl.y = E::pack(p[r0 + 2] - E::lo_of(w.y), p[r0 + 3] - E::hi_of(w.y));
     wl.z = E::pack(p[r0 + 4] - E::lo_of(w.z), p[r0 + 5] - E::hi_of(w.z));
@@ -147,7 +144,7 @@ __device__ __forceinline__ void tree_pv_by_key(f32x16 (&o)[T], f32x16 p, const c
 }
 
 // Returns whether it has to be done again with CAREFUL (the same on every thread).
-template <int WR, bool CAREFUL, bool TWO, typename E, int DP>
+template <int WR, bool CAREFUL, typename E, int DP>
 __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, const TreeKernelArgs& a, const TreeItem& it, int32_t kvh)
 {
     typedef TreeGeo<DP> Geo;
@@ -301,24 +298,24 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
             }
             __builtin_amdgcn_sched_barrier(0);
             uint4 w, wl;
-            tree_pack<E, TWO>(w, wl, p, 0);
+            tree_pack<E>(w, wl, p, 0);
 #pragma unroll
             for (int c = 0; c < T; ++c) {
                 o[c] = E::mfma32(va[c], w, o[c]);
-                if (TWO) o[c] = E::mfma32(va[c], wl, o[c]);
+                o[c] = E::mfma32(va[c], wl, o[c]);
             }
 #pragma unroll
             for (int c = 0; c < T; ++c) vb[c] = tree_v_frag(vh + 16 * ROWB + vx[2 * c], vh + 16 * ROWB + vx[2 * c + 1]);
-            tree_pack<E, TWO>(w, wl, p, 8);
+            tree_pack<E>(w, wl, p, 8);
 #pragma unroll
             for (int c = 0; c < T; ++c) {
                 o[c] = E::mfma32(vb[c], w, o[c]);
-                if (TWO) o[c] = E::mfma32(vb[c], wl, o[c]);
+                o[c] = E::mfma32(vb[c], wl, o[c]);
             }
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
 #pragma unroll
             for (int c = 0; c < 2 * T; ++c) {
-                if (TWO || c < T) __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
                 __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
                 __builtin_amdgcn_sched_group_barrier(0x002, 32 / T, 1);
             }
@@ -434,7 +431,7 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
     return false;
 }
 
-template <int WR, bool TWO, typename E, int DP>
+template <int WR, typename E, int DP>
 struct Tree16 {
     typedef TreeShape<WR, DP> Shape;
     static constexpr bool kCut = WR > 1;                                 // (one wave of rows is for calls without a cut)
@@ -443,7 +440,7 @@ struct Tree16 {
     template <bool CAREFUL>
     static __device__ __forceinline__ bool work(char* buf, uint32_t* flags, const TreeKernelArgs& a, const TreeItem& it, int32_t kvh)
     {
-        return tree_piece_of_work<WR, CAREFUL, TWO, E, DP>(buf, flags, a, it, kvh);
+        return tree_piece_of_work<WR, CAREFUL, E, DP>(buf, flags, a, it, kvh);
     }
     static __device__ __forceinline__ void store(void* out, int64_t at, float4 v)
     {
@@ -451,28 +448,22 @@ struct Tree16 {
     }
 };
 
-template <bool TWO, typename E, int DP>
-pa_status launch_tree_rows(const TreeKernelArgs& a, bool merge, int row_waves, hipStream_t stream)
-{
-    if constexpr (DP <= 128)
-        if (row_waves == 8) return launch_tree_of<Tree16<8, TWO, E, DP>>(a, merge, stream);
-    return launch_tree_of<Tree16<4, TWO, E, DP>>(a, merge, stream);
-}
-
 template <typename E, int DP>
-pa_status launch_tree_type(const TreeKernelArgs& a, bool merge, int row_waves, bool two_terms, hipStream_t stream)
+pa_status launch_tree_type(const TreeKernelArgs& a, bool merge, int row_waves, hipStream_t stream)
 {
-    if constexpr (DP <= 128)
-        if (row_waves == 1) return launch_tree_of<Tree16<1, true, E, DP>>(a, merge, stream);
-    if (row_waves == 2) return launch_tree_of<Tree16<2, true, E, DP>>(a, merge, stream);
-    return two_terms ? launch_tree_rows<true, E, DP>(a, merge, row_waves, stream) : launch_tree_rows<false, E, DP>(a, merge, row_waves, stream);
+    if constexpr (DP <= 128) {
+        if (row_waves == 1) return launch_tree_of<Tree16<1, E, DP>>(a, merge, stream);
+        if (row_waves == 8) return launch_tree_of<Tree16<8, E, DP>>(a, merge, stream);
+    }
+    if (row_waves == 2) return launch_tree_of<Tree16<2, E, DP>>(a, merge, stream);
+    return launch_tree_of<Tree16<4, E, DP>>(a, merge, stream);
 }
 
 template <int DP>
-pa_status launch_tree_dim(const TreeKernelArgs& a, bool merge, pa_dtype dtype, const TreePlan& p, hipStream_t stream)
+pa_status launch_tree_dim(const TreeKernelArgs& a, bool merge, pa_dtype dtype, int row_waves, hipStream_t stream)
 {
-    return dtype == PA_DTYPE_BF16 ? launch_tree_type<ElemBf16, DP>(a, merge, p.row_waves, p.two_terms, stream)
-                                  : launch_tree_type<ElemF16, DP>(a, merge, p.row_waves, p.two_terms, stream);
+    return dtype == PA_DTYPE_BF16 ? launch_tree_type<ElemBf16, DP>(a, merge, row_waves, stream)
+                                  : launch_tree_type<ElemF16, DP>(a, merge, row_waves, stream);
 }
 
 }  // namespace

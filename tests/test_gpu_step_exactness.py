@@ -1,0 +1,74 @@
+"""Attention of drafted trees where its weights and sums could lose something."""
+import numpy as np
+import pytest
+import torch
+
+from tests import step_reference as R
+from tests.test_gpu_step import any_mask, half_step, make_tree_call, pa, run_tree  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def put(c, which, s, keys, value):
+    """K or V ("k", "v") rows of some keys of sequence s of a token-major call: on the device and in the reference's copy."""
+    seq = c["seqs"][s][0 if which == "k" else 1]
+    P, table = c[which].shape[1], c["table"][s].cpu()
+    keys = torch.as_tensor(np.asarray(keys), dtype=torch.int64)
+    seq[keys] = torch.as_tensor(value).to(seq.dtype)
+    c[which][table[keys // P].long().to(c[which].device), (keys % P).to(c[which].device)] = seq[keys].to(c[which].device)
+
+
+def reference(c):
+    """Per sequence: its rows, out and lse in 64 bits, the largest |v|."""
+    row = 0
+    for s, n in enumerate(c["news"]):
+        k, v = (x.double().numpy() for x in c["seqs"][s])
+        q = c["q"][row:row + n].double().cpu().numpy()
+        with np.errstate(invalid="ignore", over="ignore"):
+            out, lse = R.tree_attention(k, v, q, c["masks"][s], c["host_lens"][s] - n, c["scale"])
+        yield slice(row, row + n), out, lse, np.abs(v).max() if v.size else 0.0
+        row += n
+
+
+def causal(s, n):
+    return np.tril(np.ones((n, n)))
+
+
+def awkward(dtype, count):
+    """Numbers a > 0 of the type's own whose e^-a is nearly as far from the type's values as can be."""
+    found = []
+    for a in torch.arange(0.2, 1.0, 1 / 512).to(dtype).unique().double().tolist():
+        w = np.exp(-a)
+        step = half_step(dtype) * 2.0 ** np.floor(np.log2(w))
+        if abs(float(torch.tensor(w).to(dtype).double()) - w) > 0.8 * step:
+            found.append(a)
+    return found[::max(1, len(found) // count)][:count]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("d,G,lens,news,loose", [
+    (128, 1, [300], [5], 0), (128, 2, [1040, 700], [40, 3], 0), (64, 4, [300, 280], [33, 7], 0), (128, 8, [640], [40], 0),
+    (256, 2, [900], [64], 0), (96, 4, [2000], [20], 0), (128, 4, [200], [20], 4096)])
+def test_weights_that_cancel(pa, d, G, lens, news, loose, dtype):  # noqa: F811
+    """Half of the keys weigh 1, with v = 1, the others w, with v = the type's value next to -1 / w: what is left of the sum is
+    about as large as a weight rounded to the type would be off by.  Weights are two terms: 2^-16 and better, with 32-bit sums
+    3e-5 of max |v| together, as for any other call; also where the bound on contexts is loose (`loose`)."""
+    a = awkward(dtype, 4)
+    c = make_tree_call(lens, news, 4 * G, 4, d, 16, dtype, causal, seed=2)
+    c["q"].fill_(1.0)
+    c["scale"] = 1.0 / d
+    for s, n in enumerate(lens):
+        odd = torch.arange(n) % 2 == 1
+        k, v = torch.zeros(n, 4, d), torch.ones(n, 4, d)
+        for h, x in enumerate(a):
+            k[odd, h], v[odd, h] = -x, -float(np.exp(x))
+        put(c, "k", s, np.arange(n), k), put(c, "v", s, np.arange(n), v)
+    if loose:
+        wide = torch.full((len(lens), loose // 16), -1, dtype=torch.int32, device=c["q"].device)
+        wide[:, :c["table"].shape[1]] = c["table"]
+        c["table"] = wide
+    out, lse = run_tree(pa, c, max_len=loose or None)
+    for rows, ref, ref_lse, vmax in reference(c):
+        over = np.abs(out[rows].double().cpu().numpy() - ref) - (half_step(dtype) * np.abs(ref) + 3e-5 * vmax)
+        assert (over <= 0).all(), float(over.max())
+        assert (np.abs(lse[rows].double().cpu().numpy() - ref_lse) <= 2e-5 + 2e-6 * np.abs(ref_lse)).all()
