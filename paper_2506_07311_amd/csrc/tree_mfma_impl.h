@@ -88,8 +88,20 @@ __device__ __forceinline__ void tree_pack(uint4& w, uint4& wl, const f32x16& p, 
     wl.w = E::pack(p[r0 + 6] - E::lo_of(w.w), p[r0 + 7] - E::hi_of(w.w));
 }
 
+// Where the softmax reference stands when it is taken, in powers of two below the largest score, and what a lane's 16 weights may
+// sum to before it is taken anew.  fp16 has steps of 2^-24 at its least: with the reference at the largest score a second term of weights
+// below 2^-9 of the largest loses bits and weights below 2^-25 are 0, while the sum of the weights has them (131072 keys of which one leads by
+// e^18, the others of mean value 1, computed so in numpy: off by nine half steps).  2^11 below, with sums up to the largest fp16 number, a weight is kept
+// to 2^-36 of the largest.  bf16 has the exponents of fp32.
+template <typename E>
+struct TreeReference {
+    static constexpr bool kHalf = E::kDtype == PA_DTYPE_F16;
+    static constexpr float kBelow = kHalf ? 11.f : 0.f, kSumMax = kHalf ? 65504.f : kWeightSumMax;
+    static_assert(!kHalf || 16 * 2048 <= kSumMax, "16 weights of the largest score");
+};
+
 // Weights of 32 keys from their raw scores (-inf: not seen); sc > 0.
-template <int T>
+template <typename R, int T>
 __device__ __forceinline__ void tree_softmax(f32x16& p, const f32x16& s, f32x16 (&o)[T], float& m, float& l, float sc)
 {
     float psum = 0.f;
@@ -98,11 +110,11 @@ __device__ __forceinline__ void tree_softmax(f32x16& p, const f32x16& s, f32x16 
         p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc, -m));
         psum += p[r];
     }
-    if (__any(!(psum <= kWeightSumMax))) {                   // also the NaN or infinity of a fresh reference
+    if (__any(!(psum <= R::kSumMax))) {                      // also the NaN or infinity of a fresh reference
         float top = -INFINITY;
 #pragma unroll
         for (int r = 0; r < 16; ++r) top = fmaxf(top, s[r]);
-        const float m_new = fmaxf(m, row_max<2>(top) * sc);
+        const float m_new = fmaxf(m, row_max<2>(top) * sc - R::kBelow);
         const float use = m_new == -INFINITY ? 0.f : m_new;  // (no key so far)
         const float alpha = __builtin_amdgcn_exp2f(m - use);
 #pragma unroll
@@ -291,7 +303,7 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = (own >> (8 * (r / 4) + r % 4)) & 1u ? s[r] : -INFINITY;
             }
-            tree_softmax<T>(p, s, o, m, l, sc);
+            tree_softmax<TreeReference<E>>(p, s, o, m, l, sc);
             if (CAREFUL) {
                 tree_pv_by_key<E, DP, T>(o, p, vh, vis, ql, hh);
                 continue;

@@ -1,4 +1,5 @@
-"""Attention of drafted trees where its weights and sums could lose something."""
+"""Attention of drafted trees where its weights and sums could lose something: weights that have to cancel, one key far ahead of all
+others."""
 import numpy as np
 import pytest
 import torch
@@ -71,4 +72,26 @@ def test_weights_that_cancel(pa, d, G, lens, news, loose, dtype):  # noqa: F811
     for rows, ref, ref_lse, vmax in reference(c):
         over = np.abs(out[rows].double().cpu().numpy() - ref) - (half_step(dtype) * np.abs(ref) + 3e-5 * vmax)
         assert (over <= 0).all(), float(over.max())
+        assert (np.abs(lse[rows].double().cpu().numpy() - ref_lse) <= 2e-5 + 2e-6 * np.abs(ref_lse)).all()
+
+
+@pytest.mark.parametrize("n", [1, 8, 40])
+@pytest.mark.parametrize("d", [64, 80, 128, 256])
+@pytest.mark.parametrize("lead,at", [(12.0, 0), (17.0, 7000), (17.0, 3)])
+def test_fp16_weights_far_below_the_largest_are_not_lost(pa, d, n, lead, at):  # noqa: F811
+    """One key of 8000 leads all others by e^17: each of them weighs 2^-24.5 of it, together 3e-4, and the leading key's values are
+    0.  A weight is kept to 2^-36 of the largest, 8000 of them to 8000 * 2^-36 of max |v| = 1; exponentials of scores up to 17
+    and 32-bit sums to 2^-17 of the result; then fp16's half step."""
+    length = 8000
+    c = make_tree_call([length, 500], [n, 1], 8, 2, d, 16, torch.float16, causal, seed=3)
+    c["q"].fill_(1.0)
+    c["scale"] = 1.0
+    for s, m in enumerate(c["host_lens"]):
+        put(c, "k", s, np.arange(m), torch.zeros(m, 2, d)), put(c, "v", s, np.arange(m), torch.ones(m, 2, d))
+        put(c, "k", s, [min(at, 400)] if s else [at], lead / d), put(c, "v", s, [min(at, 400)] if s else [at], 0.0)
+    out, lse = run_tree(pa, c)
+    for rows, ref, ref_lse, _ in reference(c):
+        near = (2.0 ** -11 + 2.0 ** -17) * np.abs(ref) + length * 2.0 ** -36
+        tiny = 2.0 ** -25                                         # (half a step of subnormal results)
+        assert (np.abs(out[rows].double().cpu().numpy() - ref) <= np.maximum(near, tiny)).all()
         assert (np.abs(lse[rows].double().cpu().numpy() - ref_lse) <= 2e-5 + 2e-6 * np.abs(ref_lse)).all()
