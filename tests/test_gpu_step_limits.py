@@ -1,0 +1,60 @@
+"""A step's plan and release at their limits."""
+import numpy as np
+import pytest
+import torch
+
+from tests.test_gpu_step import DEV, bits, ints, pa  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def guarded(shape, dtype=torch.int32, guard=4096):
+    """A tensor in the middle of a buffer of -77, and the two ends of that buffer."""
+    n = int(np.prod(shape))
+    buf = torch.full((n + 2 * guard,), -77, dtype=dtype, device=DEV)
+    return buf[guard:guard + n].view(shape), (buf[:guard], buf[guard + n:])
+
+
+@pytest.mark.parametrize("how", ["tree", None])
+@pytest.mark.parametrize("ctx,new,rows", [
+    ([0, 0, 0], [1 << 30, 1 << 30, 5], 20),                       # a sum of 2^31 + 5
+    ([9, 0, 7, 1], [2 ** 31 - 10, 2 ** 31 - 1, 2 ** 31 - 8, 9], 150),   # each length within 31 bits, three times the sum over
+    ([5, 6, 7, 8, 9], [3, 1 << 30, 2 ** 31 - 8, 2 ** 31 - 9, 4], 10),
+    ([1] * 1500, [1 << 30] * 1500, 70),                           # 2^40
+    ([3] * 300, [2] * 299 + [2 ** 31 - 4], 700),
+])
+def test_plans_whose_rows_pass_31_bits(pa, ctx, new, rows, how):  # noqa: F811
+    """Refused on the device, with the state as it was, the rows that there are described and nothing written beyond them."""
+    B, MB, P, words = len(ctx), 4, 16, 3
+    table, num = torch.full((B, MB), -1, dtype=torch.int32, device=DEV), ints([0] * B)
+    free, count = ints(range(8)), ints([8])
+    outs, guards = {}, []
+    for name, shape, dtype in (("seq_lens", (B,), torch.int32), ("cu_q_lens", (B + 1,), torch.int32), ("seq_ids", (rows,), torch.int32),
+                               ("positions", (rows,), torch.int32), ("rope_positions", (rows,), torch.int32),
+                               ("tree_mask", (rows, words), torch.int64), ("shortage", (2,), torch.int32)):
+        outs[name], ends = guarded(shape, dtype)
+        guards += ends
+    parents = None if how is None else ints([max(i - 2, 0) for i in range(rows)])
+    p = pa.paged_plan_step(ints(ctx), ints(new), table, num, free, count, P, rows, parents=parents, **outs)
+    late = sum(-(-(c + n) // P) > MB or n > 64 * words for c, n in zip(ctx, new)) + sum(new) - rows
+    need = sum(-(-(c + n) // P) for c, n in zip(ctx, new)) - 8
+    assert p.shortage.tolist() == [min(need, 2 ** 31 - 1), min(late, 2 ** 31 - 1)]
+    assert p.seq_lens.tolist() == ctx and p.cu_q_lens.tolist() == [0] * (B + 1)
+    assert int(count) == 8 and num.tolist() == [0] * B and bool((table == -1).all())
+    row, at = 0, dict(seq_ids=[], positions=[], rope_positions=[], tree_mask=[])
+    for s, (c, n) in enumerate(zip(ctx, new)):
+        masks, depths = [], []
+        for i in range(min(n, rows - row)):
+            up = i - 1 if how is None else max(row + i - 2, 0)
+            up = up if 0 <= up < i else -1
+            masks.append((masks[up] if up >= 0 else 0) | 1 << i)
+            depths.append(depths[up] + 1 if up >= 0 else 0)
+            at["seq_ids"].append(s), at["positions"].append(c + i), at["rope_positions"].append(c + depths[-1])
+            at["tree_mask"].append([masks[-1] >> 64 * w & (1 << 64) - 1 for w in range(words)])
+        row += len(masks)
+    # (positions past 31 bits are negative)
+    for name in ("seq_ids", "positions", "rope_positions"):
+        assert getattr(p, name).tolist() == [x if x < 2 ** 31 else x - 2 ** 32 for x in at[name]] + [-1 if name != "rope_positions" else 0] * (rows - row)
+    assert torch.equal(p.tree_mask, bits(np.array(at["tree_mask"] + [[0] * words] * (rows - row), dtype=np.uint64)))
+    for g in guards:
+        assert bool((g == -77).all())
