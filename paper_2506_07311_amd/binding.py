@@ -85,6 +85,22 @@ def _stream(stream) -> ctypes.c_void_p:
     return ctypes.c_void_p(stream.cuda_stream)
 
 
+def _new(shape, dtype, device, stream) -> torch.Tensor:
+    """Memory that a call on ``stream`` writes.  Of another stream than the current one it comes from that stream's part of
+    the allocator: whatever used it before and whoever gets it afterwards is then ordered by that stream, on which the
+    call may still be running when the tensor is dropped.  The current stream, whose work may read a result, is told as
+    well."""
+    here = torch.cuda.current_stream(device)
+    if stream is None or stream.cuda_stream == here.cuda_stream:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(here)
+    return t
+
+
 def _i32(t: torch.Tensor, what: str) -> torch.Tensor:
     if t.dtype != torch.int32 or not t.is_contiguous() or not t.is_cuda:
         raise PagedAttnError(f"{what} must be a contiguous int32 device tensor")
@@ -159,8 +175,7 @@ def paged_kv_gather(k_cache, v_cache, block_table, seq_lens, cu_seq_lens, total_
     lib = load_library()
     d = cache_desc(k_cache, v_cache, head_major)
     _i32(block_table, "block_table"), _i32(seq_lens, "seq_lens"), _i32(cu_seq_lens, "cu_seq_lens")
-    out_k = torch.empty((total_tokens, d.num_kv_heads, d.head_dim), dtype=k_cache.dtype, device=k_cache.device)
-    out_v = torch.empty_like(out_k)
+    out_k, out_v = (_new((total_tokens, d.num_kv_heads, d.head_dim), k_cache.dtype, k_cache.device, stream) for _ in range(2))
     st = lib.paged_kv_gather(ctypes.byref(d), _p(out_k), _p(out_v), _p(block_table), _p(seq_lens), _p(cu_seq_lens),
                              ctypes.c_int32(seq_lens.shape[0]), ctypes.c_int32(block_table.shape[1]),
                              ctypes.c_int32(max_seq_len), _stream(stream))
@@ -175,10 +190,8 @@ def paged_attention_workspace_bytes(batch: int, num_q_heads: int, head_dim: int,
         ctypes.c_int32(max_seq_len)))
 
 
-def _workspace(workspace, nbytes, device):
-    if workspace is None:
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    return workspace
+def _workspace(workspace, nbytes, device, stream):
+    return _new(nbytes, torch.uint8, device, stream) if workspace is None else workspace
 
 
 def paged_attention_decode(k_cache, v_cache, q, block_table, seq_lens, max_seq_len: int, scale: float, *,
@@ -198,11 +211,11 @@ def prepare_decode(k_cache, v_cache, q, block_table, seq_lens, max_seq_len: int,
     if hd != d.head_dim or seq_lens.shape[0] != B or block_table.shape[0] != B:
         raise PagedAttnError("q must be [B, Hq, d] with B matching seq_lens and block_table")
     _i32(block_table, "block_table"), _i32(seq_lens, "seq_lens")
-    out = torch.empty_like(q) if out is None else _dense(out, "out", q.dtype)
+    out = _new(q.shape, q.dtype, q.device, stream) if out is None else _dense(out, "out", q.dtype)
     if lse is not None:
         _dense(lse, "lse", torch.float32)
     if workspace is None:   # (a workspace that is passed in is checked by the library itself)
-        workspace = _workspace(None, paged_attention_workspace_bytes(B, Hq, hd, B, max_seq_len), q.device)
+        workspace = _workspace(None, paged_attention_workspace_bytes(B, Hq, hd, B, max_seq_len), q.device, stream)
     args = (ctypes.byref(d), _p(q), _p(out), _p(lse), _p(block_table), _p(seq_lens), ctypes.c_int32(B),
             ctypes.c_int32(Hq), ctypes.c_int32(block_table.shape[1]), ctypes.c_int32(max_seq_len),
             ctypes.c_float(scale), _p(workspace), ctypes.c_size_t(workspace.numel() * workspace.element_size()),
@@ -253,11 +266,11 @@ def prepare_prefill(k_cache, v_cache, q, cu_q_lens, max_q_len: int, block_table,
     if hd != d.head_dim or block_table.shape[0] != B or cu_q_lens.shape[0] != B + 1:
         raise PagedAttnError("q must be [total_q, Hq, d]; cu_q_lens int32[B+1]")
     _i32(block_table, "block_table"), _i32(seq_lens, "seq_lens"), _i32(cu_q_lens, "cu_q_lens")
-    out = torch.empty_like(q) if out is None else _dense(out, "out", q.dtype)
+    out = _new(q.shape, q.dtype, q.device, stream) if out is None else _dense(out, "out", q.dtype)
     if lse is not None:
         _dense(lse, "lse", torch.float32)
     if workspace is None:
-        workspace = _workspace(None, paged_attention_workspace_bytes(B, Hq, hd, total_q, max_seq_len), q.device)
+        workspace = _workspace(None, paged_attention_workspace_bytes(B, Hq, hd, total_q, max_seq_len), q.device, stream)
     args = (ctypes.byref(d), _p(q), _p(out), _p(lse), _p(cu_q_lens), ctypes.c_int32(total_q),
             ctypes.c_int32(max_q_len), _p(block_table), _p(seq_lens), ctypes.c_int32(B), ctypes.c_int32(Hq),
             ctypes.c_int32(block_table.shape[1]), ctypes.c_int32(max_seq_len), ctypes.c_float(scale),
@@ -314,11 +327,11 @@ def paged_attention_decode_mod(k_cache, v_cache, q, block_table, seq_lens, max_s
     if hd != d.head_dim or seq_lens.shape[0] != B or block_table.shape[0] != B:
         raise PagedAttnError("q must be [B, Hq, d] with B matching seq_lens and block_table")
     _i32(block_table, "block_table"), _i32(seq_lens, "seq_lens")
-    out = torch.empty_like(q) if out is None else _dense(out, "out", q.dtype)
+    out = _new(q.shape, q.dtype, q.device, stream) if out is None else _dense(out, "out", q.dtype)
     if lse is not None:
         _dense(lse, "lse", torch.float32)
     mods = _mods(window, softcap, alibi_slopes, doc_ids, Hq, B, user_mod, user_data)
-    workspace = _workspace(workspace, paged_attention_workspace_bytes(B, Hq, hd, B, max_seq_len), q.device)
+    workspace = _workspace(workspace, paged_attention_workspace_bytes(B, Hq, hd, B, max_seq_len), q.device, stream)
     st = lib.paged_attention_decode_mod(ctypes.byref(d), _p(q), _p(out), _p(lse), _p(block_table), _p(seq_lens),
                                         ctypes.c_int32(B), ctypes.c_int32(Hq), ctypes.c_int32(block_table.shape[1]),
                                         ctypes.c_int32(max_seq_len), ctypes.c_float(scale), ctypes.byref(mods),
@@ -344,11 +357,11 @@ def prepare_decode_step(k_cache, v_cache, k_new, v_new, q, block_table, seq_lens
     if tuple(k_new.shape) != (B, d.num_kv_heads, hd) or tuple(v_new.shape) != (B, d.num_kv_heads, hd):
         raise PagedAttnError("k_new / v_new must be [B, Hkv, d]")
     _i32(block_table, "block_table"), _i32(seq_lens, "seq_lens")
-    out = torch.empty_like(q) if out is None else _dense(out, "out", q.dtype)
+    out = _new(q.shape, q.dtype, q.device, stream) if out is None else _dense(out, "out", q.dtype)
     if lse is not None:
         _dense(lse, "lse", torch.float32)
     if workspace is None:
-        workspace = _workspace(None, paged_attention_workspace_bytes(B, Hq, hd, B, max_seq_len), q.device)
+        workspace = _workspace(None, paged_attention_workspace_bytes(B, Hq, hd, B, max_seq_len), q.device, stream)
     m = _mods(window, softcap, alibi_slopes, doc_ids, Hq, B, user_mod, user_data)
     args = (ctypes.byref(d), _p(k_new), _p(v_new), _p(q), _p(out), _p(lse), _p(block_table), _p(seq_lens),
             ctypes.c_int32(B), ctypes.c_int32(Hq), ctypes.c_int32(block_table.shape[1]), ctypes.c_int32(max_seq_len),
@@ -379,11 +392,11 @@ def paged_attention_prefill_mod(k_cache, v_cache, q, cu_q_lens, max_q_len: int, 
     if hd != d.head_dim or block_table.shape[0] != B or cu_q_lens.shape[0] != B + 1:
         raise PagedAttnError("q must be [total_q, Hq, d]; cu_q_lens int32[B+1]")
     _i32(block_table, "block_table"), _i32(seq_lens, "seq_lens"), _i32(cu_q_lens, "cu_q_lens")
-    out = torch.empty_like(q) if out is None else _dense(out, "out", q.dtype)
+    out = _new(q.shape, q.dtype, q.device, stream) if out is None else _dense(out, "out", q.dtype)
     if lse is not None:
         _dense(lse, "lse", torch.float32)
     mods = _mods(window, softcap, alibi_slopes, doc_ids, Hq, B, user_mod, user_data)
-    workspace = _workspace(workspace, paged_attention_workspace_bytes(B, Hq, hd, total_q, max_seq_len), q.device)
+    workspace = _workspace(workspace, paged_attention_workspace_bytes(B, Hq, hd, total_q, max_seq_len), q.device, stream)
     st = lib.paged_attention_prefill_mod(ctypes.byref(d), _p(q), _p(out), _p(lse), _p(cu_q_lens),
                                          ctypes.c_int32(total_q), ctypes.c_int32(max_q_len), _p(block_table),
                                          _p(seq_lens), ctypes.c_int32(B), ctypes.c_int32(Hq),
@@ -421,8 +434,8 @@ def _shaped(t: torch.Tensor, what: str, shape, dtype=torch.int32) -> torch.Tenso
     return t
 
 
-def _or_new(t, what, shape, device, dtype=torch.int32):
-    return torch.empty(shape, dtype=dtype, device=device) if t is None else _shaped(t, what, shape, dtype)
+def _or_new(t, what, shape, device, stream, dtype=torch.int32):
+    return _new(shape, dtype, device, stream) if t is None else _shaped(t, what, shape, dtype)
 
 
 class StepPlan(NamedTuple):
@@ -454,11 +467,11 @@ def prepare_plan_step(ctx_lens, new_lens, block_table, num_blocks, free_pages, f
         _shaped(parents, "parents", (max_rows,))
     if tree_mask is not None:
         mask_words = int(tree_mask.shape[-1])
-    plan = StepPlan(_or_new(seq_lens, "seq_lens", (B,), dev), _or_new(cu_q_lens, "cu_q_lens", (B + 1,), dev),
-                    _or_new(seq_ids, "seq_ids", (max_rows,), dev), _or_new(positions, "positions", (max_rows,), dev),
-                    _or_new(rope_positions, "rope_positions", (max_rows,), dev),
-                    _or_new(tree_mask, "tree_mask", (max_rows, mask_words), dev, torch.int64),
-                    _or_new(shortage, "shortage", (2,), dev))
+    plan = StepPlan(_or_new(seq_lens, "seq_lens", (B,), dev, stream), _or_new(cu_q_lens, "cu_q_lens", (B + 1,), dev, stream),
+                    _or_new(seq_ids, "seq_ids", (max_rows,), dev, stream), _or_new(positions, "positions", (max_rows,), dev, stream),
+                    _or_new(rope_positions, "rope_positions", (max_rows,), dev, stream),
+                    _or_new(tree_mask, "tree_mask", (max_rows, mask_words), dev, stream, torch.int64),
+                    _or_new(shortage, "shortage", (2,), dev, stream))
     args = (_p(ctx_lens), _p(new_lens), ctypes.c_int32(B), _p(parents), ctypes.c_int32(page_size), _p(block_table),
             ctypes.c_int32(block_table.shape[1]), _p(num_blocks), _p(free_pages), _p(free_count), ctypes.c_int32(max_rows),
             _p(plan.seq_lens), _p(plan.cu_q_lens), _p(plan.seq_ids), _p(plan.positions), _p(plan.rope_positions),
@@ -545,7 +558,7 @@ def prepare_rope_append(k_cache, v_cache, q, k_new, v_new, rope_positions, seq_i
     if q is not None:
         Hq = int(q.shape[1]) if q.dim() == 3 else 0
         _rows(q, "q", (T, Hq, d.head_dim), k_cache.dtype)
-        q_out = torch.empty((T, Hq, d.head_dim), dtype=q.dtype, device=dev) if q_out is None else \
+        q_out = _new((T, Hq, d.head_dim), q.dtype, dev, stream) if q_out is None else \
             _rows(q_out, "q_out", (T, Hq, d.head_dim), q.dtype)
     elif q_out is not None:
         raise PagedAttnError("q_out without q")
@@ -603,12 +616,12 @@ def prepare_attention_tree(k_cache, v_cache, q, cu_q_lens, max_q_len: int, tree_
         raise PagedAttnError("tree_mask must be int64[total_q, words]")
     words = int(tree_mask.shape[1])
     _shaped(tree_mask, "tree_mask", (total_q, words), torch.int64)
-    out = torch.empty_like(q) if out is None else _shaped(out, "out", q.shape, q.dtype)
+    out = _new(q.shape, q.dtype, q.device, stream) if out is None else _shaped(out, "out", q.shape, q.dtype)
     if lse is not None:
         _shaped(lse, "lse", (total_q, Hq), torch.float32)
     if workspace is None:
         workspace = _workspace(None, paged_attention_tree_workspace_bytes(B, Hq, d.num_kv_heads, hd, total_q, max_q_len,
-                                                                          max_seq_len), dev)
+                                                                          max_seq_len), dev, stream)
     args = (ctypes.byref(d), _p(q), _p(out), _p(lse), _p(cu_q_lens), ctypes.c_int32(total_q), ctypes.c_int32(max_q_len),
             _p(tree_mask), ctypes.c_int32(words), _p(block_table), _p(seq_lens), ctypes.c_int32(B), ctypes.c_int32(Hq),
             ctypes.c_int32(block_table.shape[1]), ctypes.c_int32(max_seq_len), ctypes.c_float(scale), _p(workspace),
@@ -647,8 +660,8 @@ def prepare_tree_accept(k_cache, v_cache, cu_q_lens, seq_lens, max_q_len: int, b
         for t, what in ((parents, "parents"), (tokens, "tokens"), (targets, "targets")):
             if _i32(t, what).dim() != 1 or t.shape != tokens.shape:
                 raise PagedAttnError("parents, tokens and targets must be int32[rows], equally long")
-        next_tokens = _or_new(next_tokens, "next_tokens", (B,), dev)
-    kept_lens = _or_new(kept_lens, "kept_lens", (B,), dev)
+        next_tokens = _or_new(next_tokens, "next_tokens", (B,), dev, stream)
+    kept_lens = _or_new(kept_lens, "kept_lens", (B,), dev, stream)
     args = (ctypes.byref(d), _p(cu_q_lens), _p(seq_lens), ctypes.c_int32(B), ctypes.c_int32(max_q_len), _p(parents), _p(tokens),
             _p(targets), _p(path), ctypes.c_int32(path.shape[1]), _p(path_lens), _p(next_tokens), _p(kept_lens),
             _p(block_table), ctypes.c_int32(block_table.shape[1]), _stream(stream))
@@ -673,7 +686,7 @@ def pa_debug_check(k_cache, v_cache, block_table, seq_lens, seq_ids=None, positi
     if seq_ids is not None:
         _i32(seq_ids, "seq_ids"), _i32(positions, "positions")
         T = int(seq_ids.shape[0])
-    scratch = torch.empty(4, dtype=torch.int64, device=k_cache.device)
+    scratch = _new(4, torch.int64, k_cache.device, stream)
     counts = (ctypes.c_int64 * 3)()
     st = load_library().pa_debug_check(ctypes.byref(d), _p(block_table), _p(seq_lens),
                                        ctypes.c_int32(block_table.shape[0]), ctypes.c_int32(block_table.shape[1]),
