@@ -141,7 +141,9 @@ __device__ __forceinline__ bool Tree32<WR, DP>::work(char* buf, uint32_t* flags,
             f32x4 kf[AHEAD];
             auto read_k = [&](int i) {                       // 16 keys after 16 keys
                 const int j = i % J;
-                return *reinterpret_cast<const f32x4*>(kh + (16 * (i / J) + ql) * ROWB + 16 * piece_k(4 * j + g, ql));
+                const f32x4 k = *reinterpret_cast<const f32x4*>(kh + (16 * (i / J) + ql) * ROWB + 16 * piece_k(4 * j + g, ql));
+                // (behind head_dim stand other pieces of the row: Q is 0 there, but 0 times an infinity of K is not)
+                return CAREFUL && 16 * j + 4 * g >= d ? (f32x4)(0.f) : k;
             };
             float vf[2][J];
             auto read_v = [&](int i) {

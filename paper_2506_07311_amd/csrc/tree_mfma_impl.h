@@ -21,7 +21,8 @@
 //   * A key is masked by selection: key len - n + t of a tile is seen by a row if bit t of the row's words is set, 32 bits at a
 //     time; tiles that end in the context take no mask at all.  An infinity or a NaN in a V row that some rows of a tile
 //     do not see would reach them through a product with a weight of zero.  It always leaves its mark on an accumulator, so
-//     they are looked at once, at the end, and such a piece of work is done again key by key (CAREFUL).
+//     they are looked at once, at the end, and such a piece of work is done again key by key (CAREFUL).  So is one with an infinity in K
+//     that met the zeros of Q behind head_dim.
 //   * Work is the batch's key tiles in a row (sequence, row block, tile), cut evenly over the workgroups of a KV head whatever the
 //     lengths are; what a cut leaves unfinished goes to the workspace, and a second launch merges it.  On short contexts
 //     a workgroup takes a whole row block and there is no second launch.
@@ -283,7 +284,12 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
             // compiler waits for each read in front of the product that takes it.
             uint4 va[T], vb[T];
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) s = E::mfma32(*reinterpret_cast<const uint4*>(kh + kx[ks]), qf[ks], s);
+            for (int ks = 0; ks < KS; ++ks) {
+                uint4 kf = *reinterpret_cast<const uint4*>(kh + kx[ks]);
+                // (behind head_dim stand other pieces of the row: Q is 0 there, but 0 times an infinity of K is not)
+                if (CAREFUL && 16 * ks + 8 * hh >= d) kf = uint4{0, 0, 0, 0};
+                s = E::mfma32(kf, qf[ks], s);
+            }
             if (!CAREFUL) {
 #pragma unroll
                 for (int c = 0; c < T; ++c) va[c] = tree_v_frag(vh + vx[2 * c], vh + vx[2 * c + 1]);

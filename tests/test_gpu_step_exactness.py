@@ -1,5 +1,5 @@
 """Attention of drafted trees where its weights and sums could lose something: weights that have to cancel, one key far ahead of all
-others."""
+others, infinities in K behind a head_dim that no tile is as wide as."""
 import numpy as np
 import pytest
 import torch
@@ -95,3 +95,30 @@ def test_fp16_weights_far_below_the_largest_are_not_lost(pa, d, n, lead, at):  #
         tiny = 2.0 ** -25                                         # (half a step of subnormal results)
         assert (np.abs(out[rows].double().cpu().numpy() - ref) <= np.maximum(near, tiny)).all()
         assert (np.abs(lse[rows].double().cpu().numpy() - ref_lse) <= 2e-5 + 2e-6 * np.abs(ref_lse)).all()
+
+
+@pytest.mark.parametrize("n", [1, 30])
+@pytest.mark.parametrize("dtype,d", [(t, d) for t in (torch.bfloat16, torch.float16) for d in (40, 64, 72, 80, 112, 128, 200, 256)] +
+                         [(torch.float32, d) for d in (40, 64, 80, 200)])
+@pytest.mark.parametrize("portable", [False, True])
+def test_what_a_query_gets_that_sees_an_infinity_in_k(pa, portable, dtype, d, n):  # noqa: F811
+    """Where the score is -inf the key weighs nothing; where it is inf the result is NaN, as e^(inf - inf) is.  Tiles are wider than
+    most of these head_dims: what stands behind them must not meet the infinity."""
+    from paper_2506_07311_amd import binding
+    for length, at in ((90 + n, 70), (90 + n, 90), (1500 + n, 700)):
+        c = make_tree_call([length, 65], [n, 2], 8, 2, d, 16, dtype, any_mask(5) if n > 1 else causal, seed=d)
+        k = c["seqs"][0][0][at].clone()
+        k[:, 3] = float("inf")
+        put(c, "k", 0, [at], k[None])
+        binding.pa_set_option("force_generic", 1 if portable else 0)
+        try:
+            out, lse = run_tree(pa, c)
+        finally:
+            binding.pa_set_option("force_generic", 0)
+        for rows, ref, ref_lse, vmax in reference(c):
+            got, got_lse = out[rows].double().cpu().numpy(), lse[rows].double().cpu().numpy()
+            bad = np.isnan(ref)
+            assert np.array_equal(np.isnan(got), bad) and np.array_equal(np.isnan(got_lse), np.isnan(ref_lse))
+            assert rows.start > 0 or n == 1 or bad.any() and not bad.all()
+            near = half_step(dtype) * np.abs(ref[~bad]) + 3e-5 * vmax
+            assert (np.abs(got[~bad] - ref[~bad]) <= near).all()
