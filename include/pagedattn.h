@@ -346,7 +346,7 @@ pa_status paged_rope_append(const pa_kv_cache_desc* cache, const void* q, int64_
  * lse NULL or float[total_q, Hq]; rows behind cu_q_lens[batch] are left as they were.  Workspace as for decode, of at least
  * paged_attention_tree_workspace_bytes.  Any cache the library takes.  Results repeat bit for bit with the same arguments.
  * fp32 arithmetic; of 16-bit pools the weights enter the product with V as two 16-bit terms: bf16 exact to 2^-16 or better, fp16 to
- * 2^-21 of the weight or 2^-36 of the row's largest, whichever is more.
+ * 2^-21 of the weight or 2^-36 of the row's largest, whichever is more.  Finite values of V give finite means (of up to 2^24 keys).
  */
 size_t paged_attention_tree_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                             int32_t total_q, int32_t max_q_len, int32_t max_seq_len);

@@ -193,11 +193,11 @@ __device__ __forceinline__ bool Tree32<WR, DP>::work(char* buf, uint32_t* flags,
                     p[u][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], sc, -m));
                     psum += p[u][i];
                 }
-            if (__any(!(psum <= kWeightSumMax))) {
+            if (__any(!(psum <= (CAREFUL ? kCarefulSumMax : kWeightSumMax)))) {
                 float top = -INFINITY;
 #pragma unroll
                 for (int u = 0; u < N; ++u) top = fmaxf(top, fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3])));
-                const float m_new = fmaxf(m, row_max<4>(top) * sc);
+                const float m_new = fmaxf(m, row_max<4>(top) * sc - (CAREFUL ? kCarefulBelow : 0.f));
                 const float use = m_new == -INFINITY ? 0.f : m_new;
                 const float alpha = __builtin_amdgcn_exp2f(m - use);
 #pragma unroll
@@ -275,9 +275,9 @@ __device__ __forceinline__ bool Tree32<WR, DP>::work(char* buf, uint32_t* flags,
             for (int k = 1; k < KW; ++k) {
                 const f32x4 ml = po[at(k) + J * 64];
                 const float top = fmaxf(m, ml[0]), use = top == -INFINITY ? 0.f : top;
-                const float wa = __builtin_amdgcn_exp2f(m - use), wb = __builtin_amdgcn_exp2f(ml[0] - use);
+                const float wa = 0.5f * __builtin_amdgcn_exp2f(m - use), wb = 0.5f * __builtin_amdgcn_exp2f(ml[0] - use);
                 l = l * wa + ml[1] * wb;
-                m = top;
+                m = top + 1.f;                               // (a mean: no sum of the two overflows)
 #pragma unroll
                 for (int c = 0; c < J; ++c) o[c] = o[c] * wa + po[at(k) + c * 64] * wb;
             }

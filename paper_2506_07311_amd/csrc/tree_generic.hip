@@ -13,6 +13,7 @@ namespace {
 constexpr int kWaves = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kShift = 24.f, kLargest = 0x1p-24f;   // weight of the largest score: of up to 2^24 keys no sum of finite values overflows
 
 template <pa_dtype DT>
 __device__ __forceinline__ float load_elem(const void* p, int64_t i)
@@ -70,7 +71,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_attention_tree_generic_kern
         const float top = fmaxf(m, wave_max(x));
         const float use = top == -INFINITY ? 0.f : top;      // (no key so far)
         const float alpha = __builtin_amdgcn_exp2f((m - use) * kLog2e);
-        const float p = seen ? __builtin_amdgcn_exp2f((x - use) * kLog2e) : 0.f;
+        const float p = seen ? kLargest * __builtin_amdgcn_exp2f((x - use) * kLog2e) : 0.f;
         l = l * alpha + wave_sum(p);
         m = top;
         sm_p[wave][lane] = p;
@@ -111,7 +112,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_attention_tree_generic_kern
         store_elem<DT>(out, at + c, x * inv);
     }
     if (lse && threadIdx.x == 0)
-        lse[(int64_t)row * num_q_heads + h] = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum) * kLn2;
+        lse[(int64_t)row * num_q_heads + h] = sum == 0.f ? -INFINITY : top + (__builtin_amdgcn_logf(sum) + kShift) * kLn2;
 }
 
 template <pa_dtype DT>

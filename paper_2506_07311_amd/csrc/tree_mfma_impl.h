@@ -22,7 +22,7 @@
 //     time; tiles that end in the context take no mask at all.  An infinity or a NaN in a V row that some rows of a tile
 //     do not see would reach them through a product with a weight of zero.  It always leaves its mark on an accumulator, so
 //     they are looked at once, at the end, and such a piece of work is done again key by key (CAREFUL).  So is one with an infinity in K
-//     that met the zeros of Q behind head_dim.
+//     that met the zeros of Q behind head_dim, and one whose sums of finite values left the range of fp32 (kCarefulBelow).
 //   * Work is the batch's key tiles in a row (sequence, row block, tile), cut evenly over the workgroups of a KV head whatever the
 //     lengths are; what a cut leaves unfinished goes to the workspace, and a second launch merges it.  On short contexts
 //     a workgroup takes a whole row block and there is no second launch.
@@ -94,11 +94,13 @@ __device__ __forceinline__ void tree_pack(uint4& w, uint4& wl, const f32x16& p, 
 // below 2^-9 of the largest loses bits and weights below 2^-25 are 0, while the sum of the weights has them (131072 keys of which one leads by
 // e^18, the others of mean value 1, computed so in numpy: off by nine half steps).  2^11 below, with sums up to the largest fp16 number, a weight is kept
 // to 2^-36 of the largest.  bf16 has the exponents of fp32.
-template <typename E>
+// CAREFUL: see kCarefulBelow.
+template <typename E, bool CAREFUL>
 struct TreeReference {
     static constexpr bool kHalf = E::kDtype == PA_DTYPE_F16;
-    static constexpr float kBelow = kHalf ? 11.f : 0.f, kSumMax = kHalf ? 65504.f : kWeightSumMax;
-    static_assert(!kHalf || 16 * 2048 <= kSumMax, "16 weights of the largest score");
+    static constexpr float kBelow = CAREFUL ? kCarefulBelow : kHalf ? 11.f : 0.f;
+    static constexpr float kSumMax = CAREFUL ? kCarefulSumMax : kHalf ? 65504.f : kWeightSumMax;
+    static_assert(CAREFUL || !kHalf || 16 * 2048 <= kSumMax, "16 weights of the largest score");
 };
 
 // Weights of 32 keys from their raw scores (-inf: not seen); sc > 0.
@@ -309,7 +311,7 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = (own >> (8 * (r / 4) + r % 4)) & 1u ? s[r] : -INFINITY;
             }
-            tree_softmax<TreeReference<E>>(p, s, o, m, l, sc);
+            tree_softmax<TreeReference<E, CAREFUL>>(p, s, o, m, l, sc);
             if (CAREFUL) {
                 tree_pv_by_key<E, DP, T>(o, p, vh, vis, ql, hh);
                 continue;
@@ -394,13 +396,13 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
         for (int k = 0; k < KW; ++k) s[k] = ml[k * 64];
         const float own = m;
         m = fmaxf(fmaxf(s[0].x, s[1].x), fmaxf(s[KW / 2].x, s[KW - 1].x));
-        const float use = m == -INFINITY ? 0.f : m, wo = __builtin_amdgcn_exp2f(own - use);
+        const float use = m == -INFINITY ? 0.f : m, wo = 0.25f * __builtin_amdgcn_exp2f(own - use);   // (a mean: no sum of the four overflows)
         l = 0.f;
 #pragma unroll
         for (int i = 0; i < MINE; ++i) mine[i] = float4{mine[i].x * wo, mine[i].y * wo, mine[i].z * wo, mine[i].w * wo};
 #pragma unroll
         for (int k = 0; k < KW; ++k) {
-            const float w = __builtin_amdgcn_exp2f(s[k].x - use);
+            const float w = 0.25f * __builtin_amdgcn_exp2f(s[k].x - use);
             l = __builtin_fmaf(s[k].y, w, l);
             if (k == kw) continue;
 #pragma unroll
@@ -410,14 +412,16 @@ __device__ __forceinline__ bool tree_piece_of_work(char* buf, uint32_t* flags, c
                                  __builtin_fmaf(v.w, w, mine[i].w)};
             }
         }
+        m += 2.f;
         __syncthreads();                                     // (before the next piece of work loads over them)
     }
     if (KW == 2) {
         const float2 m0 = ml[0], m1 = ml[64];
         m = fmaxf(m0.x, m1.x);
         const float use = m == -INFINITY ? 0.f : m;
-        const float w0 = __builtin_amdgcn_exp2f(m0.x - use), w1 = __builtin_amdgcn_exp2f(m1.x - use);
+        const float w0 = 0.5f * __builtin_amdgcn_exp2f(m0.x - use), w1 = 0.5f * __builtin_amdgcn_exp2f(m1.x - use);   // (a mean)
         l = m0.y * w0 + m1.y * w1;
+        m += 1.f;
         const float wa = kw == 0 ? w0 : w1, wb = kw == 0 ? w1 : w0;
 #pragma unroll
         for (int i = 0; i < MINE; ++i) {

@@ -47,6 +47,10 @@ constexpr int32_t kTreePieceTiles = 4;
 constexpr int32_t kTreeMaxChunk = 12;
 // Workgroups that share a row block; the merge has 32 weights of each in LDS.
 constexpr int32_t kTreeMaxPieces = 256;
+// Weights are taken against a reference that trails the maximum, so a sum of finite values times weights can leave the range of fp32
+// where their mean does not.  It is then done again (CAREFUL) with the reference 2^24 above the largest score and taken anew
+// where a lane's 16 weights sum to more than 2^-20: of up to 2^24 keys all weights sum to at most 1.  (They are fp32 there.)
+constexpr float kCarefulBelow = -24.f, kCarefulSumMax = 1.f / (1 << 20);
 
 // This wave's loads to LDS have landed but for the last N tiles' (LOADS of either pool each).  In order, so what the compiler
 // has issued in between makes it wait for more, not for less.
@@ -317,7 +321,8 @@ __global__ __launch_bounds__(64 * NW) void paged_attention_tree_merge_kernel(
     const float use = top == -INFINITY ? 0.f : top;
     float wsum = 0.f;
     for (int32_t k = group; k < pieces; k += GROUPS) {       // (the thread's own)
-        const float w = __builtin_amdgcn_exp2f(weight[k * RW + srow] - use);
+        static_assert(kTreeMaxPieces <= 256, "weights of at most 2^-8: no sum of means overflows");
+        const float w = 0x1p-8f * __builtin_amdgcn_exp2f(weight[k * RW + srow] - use);
         weight[k * RW + srow] = w;
         wsum += w;
     }
@@ -327,7 +332,7 @@ __global__ __launch_bounds__(64 * NW) void paged_attention_tree_merge_kernel(
         wsum = 0.f;
 #pragma unroll
         for (int i = 0; i < GROUPS; ++i) wsum += sm_red[i][srow];
-        sm_top[srow] = top;
+        sm_top[srow] = top + 8.f;
         sm_sum[srow] = wsum;
     }
     __syncthreads();

@@ -1,5 +1,5 @@
 """Attention of drafted trees where its weights and sums could lose something: weights that have to cancel, one key far ahead of all
-others, infinities in K behind a head_dim that no tile is as wide as."""
+others, infinities in K behind a head_dim that no tile is as wide as, values near the type's largest."""
 import numpy as np
 import pytest
 import torch
@@ -122,3 +122,35 @@ def test_what_a_query_gets_that_sees_an_infinity_in_k(pa, portable, dtype, d, n)
             assert rows.start > 0 or n == 1 or bad.any() and not bad.all()
             near = half_step(dtype) * np.abs(ref[~bad]) + 3e-5 * vmax
             assert (np.abs(got[~bad] - ref[~bad]) <= near).all()
+
+
+@pytest.mark.parametrize("portable", [False, True])
+@pytest.mark.parametrize("n", [1, 12, 70])
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 64), (torch.bfloat16, 128), (torch.bfloat16, 256), (torch.float32, 64),
+                                     (torch.float32, 128), (torch.float32, 256)])
+@pytest.mark.parametrize("length", [100, 3000])
+def test_means_of_values_near_the_largest_are_finite(pa, length, dtype, d, n, portable):  # noqa: F811
+    """A mean of finite values is finite, however many there are and although later keys outweigh the first ones by e^6.
+    Values: 3e38 for all of a column, of either sign at random in the others."""
+    from paper_2506_07311_amd import binding
+    c = make_tree_call([length + n, 70], [n, 2], 8, 2, d, 16, dtype, causal, seed=5)
+    g = torch.Generator().manual_seed(6)
+    c["q"].fill_(1.0)
+    c["scale"] = 1.0
+    for s, m in enumerate(c["host_lens"]):
+        k = torch.full((m, 2, d), 6.0 / d)
+        k[:m // 3] = 0.0
+        v = 3e38 * torch.randint(0, 2, (m, 2, d), generator=g).mul(2).sub(1)
+        v[..., ::3] = 3e38
+        v[..., 1::3] = -3e38
+        put(c, "k", s, np.arange(m), k), put(c, "v", s, np.arange(m), v)
+    binding.pa_set_option("force_generic", 1 if portable else 0)
+    try:
+        out, lse = run_tree(pa, c)
+    finally:
+        binding.pa_set_option("force_generic", 0)
+    for rows, ref, ref_lse, vmax in reference(c):
+        got = out[rows].double().cpu().numpy()
+        assert np.isfinite(got).all()
+        assert (np.abs(got / vmax - ref / vmax) <= half_step(dtype) * np.abs(ref / vmax) + 3e-5).all()
+        assert (np.abs(lse[rows].double().cpu().numpy() - ref_lse) <= 2e-5 + 2e-6 * np.abs(ref_lse)).all()
