@@ -286,8 +286,9 @@ pa_status paged_plan_step(const int32_t* ctx_lens, const int32_t* new_lens, int3
 /*
  * The way back: sequence s keeps the blocks of its first keep_lens[s] tokens (0: none, a finished sequence), the others'
  * entries become -1 and their pages return to the stack, the last one first, so that a plan for the same
- * blocks takes the same pages again.  max_free: entries of free_pages.  A page that another row maps as well must not be
- * given back (the device's list counts no references).
+ * blocks takes the same pages again.  max_free: entries of free_pages.  Pages for which they have no room stay mapped (of the
+ * blocks in the order of sequences the first ones: num_blocks says how many of a row), to be given back by a later call.  A
+ * page that another row maps as well must not be given back (the device's list counts no references).
  */
 pa_status paged_release_blocks(const int32_t* keep_lens, int32_t batch, int32_t page_size, int32_t* block_table,
                                int32_t max_blocks, int32_t* num_blocks, int32_t* free_pages, int32_t* free_count,

@@ -504,7 +504,8 @@ def prepare_release_blocks(keep_lens, block_table, num_blocks, free_pages, free_
 
 
 def paged_release_blocks(keep_lens, block_table, num_blocks, free_pages, free_count, page_size: int, *, stream=None) -> None:
-    """Gives the pages behind the first keep_lens[s] tokens of each sequence back to the free list, in place."""
+    """Gives the pages behind the first keep_lens[s] tokens of each sequence back to the free list, in place.  Pages that the
+    list has no room for stay mapped."""
     prepare_release_blocks(keep_lens, block_table, num_blocks, free_pages, free_count, page_size, stream=stream)()
 
 

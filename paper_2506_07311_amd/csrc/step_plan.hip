@@ -226,7 +226,8 @@ __global__ __launch_bounds__(N) void paged_plan_step_kernel(PlanArgs a)
 }
 
 // Blocks of a sequence beyond ceil(keep_lens / P) go back to the end of the free list, the last one first: a plan that asks
-// for the same blocks again gets the same pages.  One workgroup: the list is one.  About 4 us, next to all of it
+// for the same blocks again gets the same pages.  Where the list has no room for all of them, its free places go to the last ones, and
+// the rest, a row's first, stay mapped: no page is in neither.  One workgroup: the list is one.  About 4 us, next to all of it
 // the launch and two trips.
 __global__ __launch_bounds__(kReleaseThreads) void paged_release_blocks_kernel(
     const int32_t* __restrict__ keep_lens, int32_t* __restrict__ block_table, int32_t* __restrict__ num_blocks,
@@ -256,15 +257,19 @@ __global__ __launch_bounds__(kReleaseThreads) void paged_release_blocks_kernel(
             const int32_t at = m - (f ? sm_end[f - 1] : 0);
             int32_t* const entry = block_table + (int64_t)(s0 + f) * max_blocks + kept(s0 + f) + at;
             const int64_t to = (int64_t)count + all - 1 - before - m;
-            if (to < max_free) free_pages[to] = *entry;
+            if (to >= max_free) continue;
+            free_pages[to] = *entry;
             *entry = -1;
         }
         __syncthreads();
-        if (mine > 0) num_blocks[s0 + tid] = kept(s0 + tid);
+        if (mine > 0) {
+            const int64_t first = (int64_t)count + all - 1 - before - (sm_end[tid] - mine);   // where this row's first one would go
+            num_blocks[s0 + tid] = kept(s0 + tid) + (int32_t)min(max(first + 1 - max_free, (int64_t)0), (int64_t)mine);
+        }
         before += here;
         __syncthreads();
     }
-    if (tid == 0) free_count[0] = min(count + all, max_free);
+    if (tid == 0) free_count[0] = (int32_t)max(min((int64_t)count + all, (int64_t)max_free), (int64_t)count);
 }
 
 // ---- acceptance ----------------------------------------------------------------------------------------------------

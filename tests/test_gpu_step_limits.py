@@ -58,3 +58,38 @@ def test_plans_whose_rows_pass_31_bits(pa, ctx, new, rows, how):  # noqa: F811
     assert torch.equal(p.tree_mask, bits(np.array(at["tree_mask"] + [[0] * words] * (rows - row), dtype=np.uint64)))
     for g in guards:
         assert bool((g == -77).all())
+
+
+@pytest.mark.parametrize("B,P,room", [(3, 16, 0), (3, 16, 4), (5, 1, 37), (40, 8, 11), (2500, 16, 700), (2500, 16, 0), (2500, 16, 10 ** 6)])
+def test_pages_that_the_free_list_has_no_room_for_stay_mapped(pa, B, P, room):  # noqa: F811
+    """`room` places are left: the last blocks get them, the first ones stay in their rows, and no page is lost.  A later call
+    with room takes them."""
+    rng = np.random.default_rng(B + room)
+    MB = 9
+    have, keep = rng.integers(0, MB + 1, B), rng.integers(0, (MB + 2) * P, B)
+    table = np.full((B, MB), -1)
+    perm = rng.permutation(int(have.sum()) + 5)
+    live, perm = perm[:5].tolist(), perm[5:]
+    at = 0
+    for s in range(B):
+        table[s, :have[s]] = perm[at:at + have[s]]
+        at += have[s]
+    back = [(s, b) for s in range(B) for b in range(-(-int(keep[s]) // P), int(have[s]))]
+    room = min(room, len(back) + 2)
+    stay = max(len(back) - room, 0)
+    want_free = live + [int(table[s, b]) for s, b in back[stay:]][::-1]
+    want_table, want_num = table.copy(), have.copy()
+    for s, b in back[stay:]:
+        want_table[s, b] = -1
+        want_num[s] -= 1
+    t_table, t_num, t_count, t_keep = ints(table), ints(have), ints([5]), ints(keep)
+    t_free, ends = guarded((5 + room,))
+    t_free[:5] = ints(live)
+    pa.paged_release_blocks(t_keep, t_table, t_num, t_free, t_count, P)
+    assert t_table.tolist() == want_table.tolist() and t_num.tolist() == want_num.tolist()
+    assert int(t_count) == len(want_free) and t_free.tolist()[:len(want_free)] == want_free
+    assert all(bool((g == -77).all()) for g in ends)
+    wide = torch.cat([t_free, ints([0] * len(back))]) if len(back) else t_free
+    pa.paged_release_blocks(t_keep, t_table, t_num, wide, t_count, P)
+    assert t_num.tolist() == np.minimum(have, -(-keep // P)).tolist()
+    assert sorted(wide.tolist()[:int(t_count)] + t_table[t_table >= 0].tolist()) == sorted(live + perm.tolist())
