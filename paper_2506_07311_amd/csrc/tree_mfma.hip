@@ -17,6 +17,9 @@ namespace {
 
 int32_t columns_of(int32_t d, bool f32) { return d <= 64 ? 64 : d <= 96 && !f32 ? 96 : d <= 128 ? 128 : 256; }
 
+// Keys of a tile that a cut call's workgroups share.
+int32_t tile_of(int32_t columns, bool f32) { return f32 && columns > 128 ? 32 : 64; }
+
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 }  // namespace
@@ -48,7 +51,7 @@ TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int
     if (f32) p.row_waves = rows <= 16 && columns <= 128 ? 1 : rows <= 32 ? 2 : rows <= 64 || columns > 128 ? 4 : 8;
     else p.row_waves = rows <= 64 ? 2 : rows <= 128 || columns > 128 ? 4 : 8;
     auto blocks_of = [&](int32_t waves) { return (rows + wave_rows * waves - 1) / (wave_rows * waves); };
-    const int32_t tile = f32 && columns > 128 ? 32 : 64;
+    const int32_t tile = tile_of(columns, f32);
     const int64_t tiles = ((int64_t)max_seq_len + tile - 1) / tile;
     const int64_t cus = device_cus(), heads = (int64_t)batch * num_kv_heads;
     if (!f32 && rows <= 32 && columns <= 128 && heads <= cus && tiles <= (2 * heads >= cus ? kFullTiles : kPlainTiles)) {
@@ -80,15 +83,22 @@ TreePlan plan_tree(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int
 bool tree_mfma_supported(const TreeArgs& a)
 {
     // (a lane's offset within a page is one of 32 bits)
-    return a.cache.page_size >= 16 && a.cache.token_stride * a.cache.page_size < ((int64_t)1 << 29);
+    if (a.cache.page_size < 16 || a.cache.token_stride * a.cache.page_size >= ((int64_t)1 << 29)) return false;
+    // Bounds so loose that the places of a KV head pass 31 bits, or a launch 2^32 threads, are the portable kernel's, whose grid goes by
+    // the rows that there are.
+    const bool f32 = a.dtype == PA_DTYPE_F32;
+    const TreePlan p = plan_tree(a.batch, a.num_q_heads, a.cache.num_kv_heads, a.cache.head_dim, a.max_q_len, a.max_seq_len, f32);
+    const int32_t columns = columns_of(a.cache.head_dim, f32), rows = p.row_waves * (f32 ? 16 : 32);
+    const int64_t units = (int64_t)a.batch * p.row_blocks, threads = (int64_t)1 << 32;
+    if ((p.wgs > 0 ? p.wgs + 7 : units + 7) * a.cache.num_kv_heads * 512 >= threads) return false;
+    return p.wgs == 0 || ((a.max_seq_len + (int64_t)tile_of(columns, f32) - 1) / tile_of(columns, f32) + kTreePieceTiles <= 0x7fffffff / units &&
+                          units * rows * columns / 4 < threads);   // (the merge: 256 threads for four lines of 64 vectors)
 }
 
 pa_status launch_tree_mfma(const TreeArgs& t, void* workspace, hipStream_t stream)
 {
     const TreePlan p = plan_tree(t.batch, t.num_q_heads, t.cache.num_kv_heads, t.cache.head_dim, t.max_q_len, t.max_seq_len,
                                  t.dtype == PA_DTYPE_F32);
-    // (places of a KV head are counted in 32 bits)
-    if ((int64_t)t.batch * p.row_blocks * (t.max_seq_len / 32 + 1 + kTreePieceTiles) > 0x7fffffff) return PA_ERR_UNSUPPORTED;
     TreeKernelArgs a;
     a.cache = t.cache;
     a.q = t.q;

@@ -109,7 +109,7 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeKernelArgs& a, int32_t i)
 // How a KV head's workgroups share the call's key tiles.  Where they are few, every row block is cut into chunks of about `chunk`
 // tiles, one a workgroup.  Otherwise (chunk == 0) all tiles stand in a row, each row block's behind kTreePieceTiles places for what a
 // piece of work costs besides its tiles, and workgroup x of wgs takes places [x all / wgs, (x + 1) all / wgs).
-// (32-bit numbers: the host refuses calls with more places, and a 64-bit division takes 0.2 us.)
+// (32-bit numbers: calls with more places are the portable kernel's, and a 64-bit division takes 0.2 us.)
 struct TreeShare {
     int32_t all, wgs, chunk;
     uint32_t each, rest;         // all = wgs each + rest

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_step import DEV, bits, ints, pa  # noqa: F401
+from tests.test_gpu_step import DEV, ancestors, bits, check_tree, ints, make_tree_call, pa  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -93,3 +93,31 @@ def test_pages_that_the_free_list_has_no_room_for_stay_mapped(pa, B, P, room):  
     pa.paged_release_blocks(t_keep, t_table, t_num, wide, t_count, P)
     assert t_num.tolist() == np.minimum(have, -(-keep // P)).tolist()
     assert sorted(wide.tolist()[:int(t_count)] + t_table[t_table >= 0].tolist()) == sorted(live + perm.tolist())
+
+
+@pytest.mark.parametrize("dtype,d,max_q", [(torch.bfloat16, 128, 1 << 17), (torch.float32, 256, 1 << 15)])
+def test_bounds_however_loose_are_taken(pa, dtype, d, max_q):  # noqa: F811
+    """Bounds of millions of tokens on contexts of thousands: on the matrix cores while places and threads fit their counts, else on the
+    portable kernel; the call is not refused."""
+    from paper_2506_07311_amd import binding
+    P, B = 1024, 4
+    c = make_tree_call([3000, 40, 5, 1200], [6, 3, 5, 1], 8, 1, d, P, dtype, ancestors(3), seed=4, pad=2)
+    for bound, kernel in ((1 << 21, "paged_attention_tree_mfma_kernel"), (1 << 22, "paged_attention_tree_%s_kernel" % ("mfma" if d == 128 else "generic")),
+                          (1 << 25, "paged_attention_tree_generic_kernel")):
+        table = torch.full((B, bound // P), -1, dtype=torch.int32, device=DEV)
+        table[:, :c["table"].shape[1]] = c["table"]
+        mask = torch.zeros((c["q"].shape[0], max_q // 64), dtype=torch.int64, device=DEV)
+        mask[:, :1] = c["mask"]
+        ws, ends = guarded((pa.paged_attention_tree_workspace_bytes(B, 8, 1, d, c["q"].shape[0], max_q, bound),), torch.int8)
+        out, lse = torch.full_like(c["q"], 9.0), torch.full(c["q"].shape[:2], 7.0, device=DEV)
+        binding.pa_profile_reset()
+        binding.pa_profile_enable(True)
+        try:
+            pa.paged_attention_tree(c["k"], c["v"], c["q"], c["cu"], max_q, mask, table, c["lens"], bound, c["scale"], out=out, lse=lse,
+                                    workspace=ws)
+            assert binding.pa_profile_read(kernel)[0] == 1
+        finally:
+            binding.pa_profile_enable(False)
+            binding.pa_profile_reset()
+        check_tree(c, out, lse, f"{bound}")
+        assert all(bool((g == -77).all()) for g in ends)
