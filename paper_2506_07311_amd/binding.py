@@ -445,7 +445,7 @@ class StepPlan(NamedTuple):
     seq_ids: torch.Tensor
     positions: torch.Tensor
     rope_positions: torch.Tensor
-    tree_mask: torch.Tensor
+    tree_mask: Optional[torch.Tensor]    # None: left out
     shortage: torch.Tensor
 
 
@@ -453,7 +453,8 @@ def prepare_plan_step(ctx_lens, new_lens, block_table, num_blocks, free_pages, f
                       parents=None, mask_words: int = 1, seq_lens=None, cu_q_lens=None, seq_ids=None, positions=None,
                       rope_positions=None, tree_mask=None, shortage=None, stream=None) -> PreparedCall:
     """paged_plan_step with its arguments marshalled once; the call returns a StepPlan.  Outputs are allocated unless
-    given (tree_mask: int64 [max_rows, mask_words], the bits of the header's uint64)."""
+    given (tree_mask: int64 [max_rows, mask_words], the bits of the header's uint64; mask_words=0 leaves the masks out, as for
+    a prompt, whose tokens may then be more than masks have bits)."""
     lib = load_library()
     dev = _together("paged_plan_step", ctx_lens, new_lens, block_table, num_blocks, free_pages, free_count, parents, seq_lens,
                     cu_q_lens, seq_ids, positions, rope_positions, tree_mask, shortage)
@@ -470,12 +471,12 @@ def prepare_plan_step(ctx_lens, new_lens, block_table, num_blocks, free_pages, f
     plan = StepPlan(_or_new(seq_lens, "seq_lens", (B,), dev, stream), _or_new(cu_q_lens, "cu_q_lens", (B + 1,), dev, stream),
                     _or_new(seq_ids, "seq_ids", (max_rows,), dev, stream), _or_new(positions, "positions", (max_rows,), dev, stream),
                     _or_new(rope_positions, "rope_positions", (max_rows,), dev, stream),
-                    _or_new(tree_mask, "tree_mask", (max_rows, mask_words), dev, stream, torch.int64),
+                    _or_new(tree_mask, "tree_mask", (max_rows, mask_words), dev, stream, torch.int64) if mask_words else None,
                     _or_new(shortage, "shortage", (2,), dev, stream))
     args = (_p(ctx_lens), _p(new_lens), ctypes.c_int32(B), _p(parents), ctypes.c_int32(page_size), _p(block_table),
             ctypes.c_int32(block_table.shape[1]), _p(num_blocks), _p(free_pages), _p(free_count), ctypes.c_int32(max_rows),
             _p(plan.seq_lens), _p(plan.cu_q_lens), _p(plan.seq_ids), _p(plan.positions), _p(plan.rope_positions),
-            _p(plan.tree_mask if max_rows else None), ctypes.c_int32(mask_words), _p(plan.shortage), _stream(stream))
+            _p(plan.tree_mask), ctypes.c_int32(mask_words), _p(plan.shortage), _stream(stream))
     return PreparedCall(lib.paged_plan_step, args, (ctx_lens, new_lens, parents, block_table, num_blocks, free_pages,
                                                     free_count, plan), "paged_plan_step", plan)
 

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from tests import step_reference as R
 from tests.test_gpu_step import DEV, ancestors, bits, check_tree, ints, make_tree_call, pa  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -121,3 +122,18 @@ def test_bounds_however_loose_are_taken(pa, dtype, d, max_q):  # noqa: F811
             binding.pa_profile_reset()
         check_tree(c, out, lse, f"{bound}")
         assert all(bool((g == -77).all()) for g in ends)
+
+
+@pytest.mark.parametrize("parents", [False, True])
+def test_a_plan_without_masks(pa, parents):  # noqa: F811
+    """A prompt's tokens are more than a word of mask has bits; a program that attends causally asks for no masks."""
+    ctx, new, P, rows = [100, 0, 5], [700, 1, 65], 16, 800
+    table = torch.full((3, 60), -1, dtype=torch.int32, device=DEV)
+    up = None if not parents else [max(i - 2, -1) for n in new for i in range(n)] + [-1] * (rows - sum(new))
+    ref = R.plan(ctx, new, up, table.cpu().numpy(), [0] * 3, list(range(90)), P, rows, 64)
+    p = pa.paged_plan_step(ints(ctx), ints(new), table, ints([0] * 3), ints(range(90)), ints([90]), P, rows,
+                           parents=None if up is None else ints(up), mask_words=0)
+    assert p.tree_mask is None and p.shortage.tolist() == [0, 0]
+    for name in ("seq_lens", "cu_q_lens", "seq_ids", "positions", "rope_positions"):
+        assert getattr(p, name).tolist() == list(ref[name]), name
+    assert table.tolist() == ref["block_table"].tolist()
