@@ -137,3 +137,39 @@ def test_a_plan_without_masks(pa, parents):  # noqa: F811
     for name in ("seq_lens", "cu_q_lens", "seq_ids", "positions", "rope_positions"):
         assert getattr(p, name).tolist() == list(ref[name]), name
     assert table.tolist() == ref["block_table"].tolist()
+
+
+@pytest.mark.parametrize("B", [1025, 2500])
+@pytest.mark.parametrize("short", [0, 1])
+@pytest.mark.parametrize("how", ["tree", None])
+def test_plans_and_releases_of_thousands_of_sequences(pa, B, short, how):  # noqa: F811
+    """More sequences than the workgroup that counts has threads: rows, pages and what returns carry over from one block of them to
+    the next, growth and release in each; once granted, once a page short."""
+    rng = np.random.default_rng(B)
+    P, words, pad = 16, 1, 9
+    ctx, new = rng.integers(0, 60, B).tolist(), rng.integers(0, 20, B).tolist()
+    before = [R.blocks(x, P) for x in ctx]
+    MB = 6
+    grow = sum(R.blocks(x + n, P) - k for x, n, k in zip(ctx, new, before))
+    perm = rng.permutation(sum(before) + grow - short + 2 * (1 - short))
+    table, at = np.full((B, MB), -1, np.int64), 0
+    for s in range(B):
+        table[s, :before[s]] = perm[at:at + before[s]]
+        at += before[s]
+    free, rows = perm[at:].tolist(), sum(new) + pad
+    up = None if how is None else [max(0, i - int(rng.integers(1, 4))) if i else -1 for n in new for i in range(n)] + [-1] * pad
+    ref = R.plan(ctx, new, up, table, before, free, P, rows, words)
+    assert ref["shortage"] == [short, 0]
+    t_table, t_num, t_free, t_count = ints(table), ints(before), ints(free + [-7] * (len(perm) - len(free))), ints([len(free)])
+    p = pa.paged_plan_step(ints(ctx), ints(new), t_table, t_num, t_free, t_count, P, rows, parents=None if up is None else ints(up))
+    for name in ("seq_lens", "cu_q_lens", "seq_ids", "positions", "rope_positions", "shortage"):
+        assert getattr(p, name).tolist() == list(ref[name]), name
+    assert torch.equal(p.tree_mask, bits(np.array(ref["tree_mask"], dtype=np.uint64).reshape(rows, words)))
+    assert t_table.tolist() == ref["block_table"].tolist() and t_num.tolist() == ref["num_blocks"]
+    assert t_free.tolist()[:int(t_count)] == ref["free"] and int(t_count) == len(ref["free"])
+    for keep in (rng.integers(0, 60, B).tolist(), [0] * B):
+        back = R.release(keep, t_table.cpu().numpy(), t_num.tolist(), t_free.tolist()[:int(t_count)], P)
+        pa.paged_release_blocks(ints(keep), t_table, t_num, t_free, t_count, P)
+        assert t_table.tolist() == back["block_table"].tolist() and t_num.tolist() == back["num_blocks"]
+        assert t_free.tolist()[:int(t_count)] == [int(x) for x in back["free"]]
+    assert sorted(t_free.tolist()[:int(t_count)]) == sorted(perm.tolist())
