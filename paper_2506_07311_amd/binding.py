@@ -4,6 +4,10 @@ Every function has the name and argument meaning of its C entry point in
 ``include/pagedattn.h``; torch tensors supply device pointers and the current
 HIP stream, nothing else.  There is no CPU fallback: if the HIP library has not
 been built, loading raises.
+
+A call that is given ``stream=`` runs there, and what it allocates is that stream's
+memory; ordering its tensors' other uses around it is the caller's, as for any
+work on another stream.
 """
 from __future__ import annotations
 

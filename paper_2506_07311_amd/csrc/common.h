@@ -300,7 +300,7 @@ struct TreeArgs {
 pa_status launch_tree_generic(const TreeArgs& a, hipStream_t stream);
 // Matrix cores: pages of 16 tokens and more.  The plan is a function of the sizes that the workspace is asked for, and of the type.
 struct TreePlan {
-    int32_t row_waves;           // waves of a workgroup beside each other in rows: 2, 4 or 8 of 32 rows; fp32 1, 2 or 4 of 16
+    int32_t row_waves;           // waves of a workgroup beside each other in rows: 1, 2, 4 or 8, of 32 rows (fp32 pools: of 16)
     int32_t row_blocks;          // most row blocks of a sequence
     int32_t wgs;                 // workgroups of a KV head that share all key tiles; 0: one a row block, no partials
     size_t part_o_bytes, part_lse_bytes, cuts_bytes;

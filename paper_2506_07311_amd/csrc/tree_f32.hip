@@ -73,7 +73,7 @@ __device__ __forceinline__ bool Tree32<WR, DP>::work(char* buf, uint32_t* flags,
         if (16 * j + 4 * g < d) qf[j] = *reinterpret_cast<const f32x4*>(qrow + 16 * j + 4 * g);
     }
 
-    // fetch role: instruction i of a wave fills rows RPI * (wave + 4 i) .. of the tile, a lane the piece at position lane % PPR of its
+    // fetch role: instruction i of a wave fills rows RPI * (wave + NW i) .. of the tile, a lane the piece at position lane % PPR of its
     // row (pieces that head_dim does not have repeat others)
     constexpr int RPI = 1024 / ROWB, PPR = ROWB / 16, STEP = NW * RPI;
     const int frow = RPI * wave + lane / PPR;

@@ -30,12 +30,12 @@ size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 //
 // On short contexts a row block (a "unit" with its KV head) is one workgroup's and there is no merge:
 //   * up to kPlainTiles tiles (us with 4 / 8 / 16: 16 x 8 tokens on 300 to 400 18.1 / 12.7 / 12.8, 4 x 8 on 800 to 900 15.8 / 15.7 / 20.8);
-//     blocks of more than 64 rows are then made smaller until there is one for each compute unit (with / without: bf16 3 x 40 on 400 14.1 /
-//     24.6, 16 x 40 on 350 20.1 / 26.3, fp32 3 x 40 on 400 27.7 / 65; until there are two: 32 x 40 on 350 37.9 / 30.7);
+//     blocks of more than 64 rows are then made smaller until there is one for each compute unit (with / without: bf16 3 x 40 on 400 13.2 /
+//     23.9, 16 x 40 on 350 19.1 / 24.5, fp32 3 x 40 on 400 27.7 / 65; until there are two: 32 x 40 on 350 35.7 / 28.7);
 //   * 16-bit pools, units for half of the workgroups that the machine holds: up to kFullTiles, and as often as many as there are
-//     rounds of them, since the longest one then is a small part of the call (with / without: 32 x 16 on 800 to 900 27.2 / 38.9, 32 x 64
-//     46.8 / 71.6, 32 x 32 on 700 to 1400 35.8 / 49.7, 200 x 8 on 64 to 2000 116 / 123; where lengths are far apart 32 x 16 on 64 to 1500
-//     29.8 / 26.3, 200 x 8 on 64 to 4000 191 / 184; a quarter of the workgroups, 8 x 64 on 700 to 1400, 48.5 / 32.7); above 128 columns,
+//     rounds of them, since the longest one then is a small part of the call (with / without: 32 x 16 on 800 to 900 24.3 / 37.0, 32 x 64
+//     55.0 / 81.7, 32 x 32 on 700 to 1400 41.8 / 54.3, 200 x 8 on 64 to 2000 116 / 123; where lengths are far apart 32 x 16 on 64 to 1500
+//     29.8 / 26.3, 200 x 8 on 64 to 4000 191 / 184; a quarter of the workgroups, 8 x 64 on 700 to 1400, 62.0 / 36.3); above 128 columns,
 //     where a workgroup holds only two tiles, units for all workgroups and up to 2 kPlainTiles (32 x 16 on 800 to 900, 16 / 8 heads,
 //     44.9 / 60.1; 24 tiles: 100 x 16 on 64 to 3000 201 / 158; half of them: 16 x 16 on 700 to 1400 53.3 / 42.3);
 //   * fp32 pools take kPlainTiles in any case (a matrix core does 1/16 of the work in the time: 8 x 40 on 600 to 900 132 / 89).

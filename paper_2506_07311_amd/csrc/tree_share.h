@@ -42,8 +42,8 @@ constexpr int32_t kTreeMinTiles = 2;
 // What a piece of work costs besides its tiles, in tiles (us with 0 / 4 / 8: 64 x 8 tokens on 64 to 32768 243 / 231 / 236, 16 x 8 on 300
 // to 30000 88.2 / 85.0 / 86.3).
 constexpr int32_t kTreePieceTiles = 4;
-// Most tiles of a workgroup that has one piece of work (with 0 / 12 / 40: 1 x 8 on 20000 26.2 / 25.3 / 25.3, 2 x 40 on 4000 27.7 / 26.3 / 26.4,
-// 16 x 8 on 300 to 30000 86.3 / 85.0 / 89.4, 8 x 64 on 3600 52.9 / 52.7 / 55.7).
+// Most tiles of a workgroup that has one piece of work (with 0 / 12 / 40: 1 x 8 on 20000 26.2 / 25.3 / 25.3, 2 x 40 on 4000 31.3 / 29.1 / 29.1,
+// 16 x 8 on 300 to 30000 86.3 / 85.0 / 89.4, 8 x 64 on 3600 63.5 / 63.9 / 67.6).
 constexpr int32_t kTreeMaxChunk = 12;
 // Workgroups that share a row block; the merge has 32 weights of each in LDS.
 constexpr int32_t kTreeMaxPieces = 256;
