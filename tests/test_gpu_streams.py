@@ -74,3 +74,25 @@ def test_attention_on_another_stream_with_memory_of_its_own(pa):  # noqa: F811
         torch.cuda.current_stream().wait_stream(side)
         assert torch.equal(got, want)
     check_tree(c, *run_tree(pa, c))
+
+
+def test_a_captured_call_on_a_forked_stream_with_memory_of_its_own(pa):  # noqa: F811
+    """A stream that joins a capture: what its call allocates lives in the graph, whose replays with the program's own work
+    between repeat the eager result."""
+    c = make_tree_call([3000, 90], [8, 3], 8, 2, 128, 16, torch.bfloat16, ancestors(4), seed=5)
+    args = (c["k"], c["v"], c["q"], c["cu"], 8, c["mask"], c["table"], c["lens"], 3000, c["scale"])
+    side = torch.cuda.Stream()
+    pa.paged_attention_tree(*args)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        out = pa.paged_attention_tree(*args, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+    for turn in range(4):
+        c["q"].copy_(c["q"].roll(1, 0))
+        graph.replay()
+        overwrite([out.numel() * 2, 1 << 20], 2)
+        if turn % 2:
+            torch.cuda.synchronize()
+        assert torch.equal(out, pa.paged_attention_tree(*args))
