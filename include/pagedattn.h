@@ -374,6 +374,118 @@ pa_status paged_tree_accept(const pa_kv_cache_desc* cache, const int32_t* cu_q_l
                             const int32_t* block_table, int32_t max_blocks, void* stream);
 
 /*
+ * ---------------------------------------------------------------------------
+ * Norms of heads, positions of several numbers, and a cache of 4-bit elements.
+ * ---------------------------------------------------------------------------
+ */
+
+/*
+ * Tokens on their way into a cache, for the two calls below.  A head x of q (norm_q != 0) or of k_new (norm_k != 0) becomes
+ *     x / sqrt(mean(x^2) + eps) * (weight_offset + w)
+ * with w = q_weight / k_weight: [head_dim], or with *_weight_heads != 0 [heads, head_dim], DEVICE arrays of type weight_dtype (the
+ * tokens' own or PA_DTYPE_F32), or NULL: no product.  Then its leading rotary_dim elements are turned as by paged_rope_append; of a
+ * position of `axes` numbers (time, height and width of a patch, say), rope_positions int32[axes, T], pair i goes by number pair_axes[i]
+ * (DEVICE int32[rotary_dim / 2], 0 <= pair_axes[i] < axes; NULL: by the first):
+ *     theta = rope_positions[pair_axes[i]][t] * inv_freq[i].
+ * V rows are taken as they are.  fp32 arithmetic (a sum of squares that leaves the range of fp32 in 64 bits, the angle in 64 bits),
+ * rounded once.  The other members, and what may be NULL or one array, are as for paged_rope_append.
+ */
+typedef struct {
+    const void*    q;
+    void*          q_out;
+    const void*    k_new;
+    const void*    v_new;
+    int64_t        q_stride;
+    int64_t        q_out_stride;
+    int64_t        k_stride;
+    int64_t        v_stride;
+    const int32_t* rope_positions;
+    const int32_t* pair_axes;
+    const double*  inv_freq;
+    const void*    q_weight;
+    const void*    k_weight;
+    const int32_t* seq_ids;
+    const int32_t* positions;
+    const int32_t* block_table;
+    int32_t        num_q_heads;
+    int32_t        T;
+    int32_t        batch;
+    int32_t        max_blocks;
+    int32_t        axes;
+    int32_t        rotary_dim;
+    int32_t        interleaved;
+    int32_t        norm_q;
+    int32_t        norm_k;
+    int32_t        q_weight_heads;
+    int32_t        k_weight_heads;
+    pa_dtype       weight_dtype;
+    float          eps;              /* >= 0 */
+    float          weight_offset;
+    float          mscale;
+} pa_norm_rope;
+
+/* Norms, rotary positions, and Algorithm 1, Assign, of the K rows that they leave and the V rows, in one pass. */
+pa_status paged_norm_rope_append(const pa_kv_cache_desc* cache, const pa_norm_rope* tokens, void* stream);
+
+/*
+ * A cache of 4-bit elements: K and V in blocks of 32 elements of a head with a power of two as their common scale.  One
+ * pool of records, a record the page_size tokens of a page and a KV head; page p, head h: records + p * page_stride +
+ * h * head_stride (BYTES, multiples of 16).  A record is, P = page_size, d = head_dim:
+ *     K codes   P d / 2 bytes   [P][d / 2]               the lower element of a byte in its low half
+ *     V codes   P d / 2 bytes   [P / 8][16][8][d / 32]   eight tokens by d / 16 elements, token by token, the same way
+ *     K scales  P d / 32 bytes  [d / 32][P]
+ *     V scales  P d / 32 bytes  [d / 32][P]
+ * A code is sign (bit 3), two bits of exponent and one of mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6.  A scale s stands for
+ * 2^(s - 127), 255 for a block of NaN.  The scale of a block with largest magnitude a is 2^(floor(log2 a) - 2), at least
+ * 2^-127; elements are rounded to nearest, ties to the even mantissa, and end at 6.  A block with an infinity or a NaN is
+ * a block of NaN.  Supported: head_dim 64, 128, 256; page_size a power of two, at least 16.  A page takes 17/64 of its 16-bit size.
+ */
+typedef struct {
+    void*   records;                 /* 16-byte aligned */
+    int64_t page_stride;
+    int64_t head_stride;
+    int32_t num_pages;
+    int32_t page_size;
+    int32_t num_kv_heads;
+    int32_t head_dim;
+} pa_mx4_cache_desc;
+
+/* Bytes of a record (17/16 page_size head_dim); 0 where there is no such cache. */
+size_t pa_mx4_record_bytes(int32_t page_size, int32_t head_dim);
+
+/* paged_norm_rope_append into a 4-bit cache.  q, k_new, v_new, q_out are of type `dtype`; K is rounded once, from fp32 to 4 bits. */
+pa_status paged_norm_rope_append_mx4(const pa_mx4_cache_desc* cache, pa_dtype dtype, const pa_norm_rope* tokens, void* stream);
+
+/* Algorithm 1, Assign, into a 4-bit cache: paged_kv_append's arguments, k_new and v_new of type `dtype`.  A row with positions[t] < 0,
+ * or whose block is not mapped, is not stored. */
+pa_status paged_kv_append_mx4(const pa_mx4_cache_desc* cache, pa_dtype dtype, const void* k_new, const void* v_new,
+                              const int32_t* seq_ids, const int32_t* positions, int32_t T, const int32_t* block_table,
+                              int32_t batch, int32_t max_blocks, void* stream);
+
+/* Algorithm 1, Gather, from a 4-bit cache: tokens [first_lens[s], seq_lens[s]) of sequence s (first_lens NULL: all) to rows
+ * cu_lens[s] .. cu_lens[s + 1] of out_k / out_v [rows, Hkv, d], contiguous, of type `dtype`; cu_lens int32[batch + 1].  max_seq_len:
+ * host upper bound of seq_lens.  Rounded to nearest where the type has fewer exponents. */
+pa_status paged_kv_gather_mx4(const pa_mx4_cache_desc* cache, pa_dtype dtype, void* out_k, void* out_v, const int32_t* block_table,
+                              const int32_t* first_lens, const int32_t* seq_lens, const int32_t* cu_lens, int32_t batch,
+                              int32_t max_blocks, int32_t max_seq_len, void* stream);
+
+/*
+ * Attention over a 4-bit cache, of one or of many new tokens a sequence: rows cu_q_lens[s] .. cu_q_lens[s + 1] of q are the
+ * last tokens of sequence s, whose length seq_lens[s] counts them; row i of n sees keys j <= seq_lens[s] - n + i.  So a decode
+ * step (cu_q_lens 0, 1, 2 ..), drafts in a row, and chunks of prompts are one call.  q, out [total_q, Hq, d] of type `dtype`;
+ * lse float[total_q, Hq] or NULL.  A row that sees no key (seq_lens[s] = 0 in a padded batch) gets out = 0, lse = -inf; rows from
+ * cu_q_lens[batch] on are left as they are.  max_q_len, max_seq_len: host upper bounds.  K and V enter the products exactly,
+ * queries with all their bits, weights with 16 (fp32 queries: 24), sums are fp32.  workspace: 256-byte aligned,
+ * paged_attention_mx4_workspace_bytes(...) with the same sizes; its contents need not be kept between calls.
+ */
+size_t paged_attention_mx4_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                           int32_t total_q, int32_t max_q_len, int32_t max_seq_len);
+pa_status paged_attention_mx4(const pa_mx4_cache_desc* cache, pa_dtype dtype, const void* q, void* out, float* lse,
+                              const int32_t* cu_q_lens, int32_t total_q, int32_t max_q_len, const int32_t* block_table,
+                              const int32_t* seq_lens, int32_t batch, int32_t num_q_heads, int32_t max_blocks,
+                              int32_t max_seq_len, float scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Debug utility: checks on the device the preconditions about device-side CONTENTS that the other entry points
  * assume and do not check.  counts (host, int64[3]) receives
  *   [0] block-table entries among the first ceil(seq_lens[s] / page_size) of a row that lie outside [0, num_pages)

@@ -27,7 +27,9 @@ EXPORTS = (
     "paged_kv_append", "paged_kv_gather", "paged_attention_workspace_bytes", "paged_attention_decode",
     "paged_attention_prefill", "paged_attention_decode_mod", "paged_attention_prefill_mod", "paged_decode_step",
     "paged_attention_decode_static", "paged_plan_step", "paged_release_blocks", "pa_rope_frequencies", "paged_rope_append",
-    "paged_attention_tree_workspace_bytes", "paged_attention_tree", "paged_tree_accept", "pa_debug_check",
+    "paged_attention_tree_workspace_bytes", "paged_attention_tree", "paged_tree_accept", "paged_norm_rope_append",
+    "pa_mx4_record_bytes", "paged_norm_rope_append_mx4", "paged_kv_append_mx4", "paged_kv_gather_mx4",
+    "paged_attention_mx4_workspace_bytes", "paged_attention_mx4", "pa_debug_check",
     "pa_status_string", "pa_set_option", "pa_stream_read", "pa_profile_enable", "pa_profile_reset",
     "pa_profile_read",
     "pa_pool_create", "pa_pool_destroy", "pa_pool_set_growth", "pa_pool_reserve", "pa_pool_release", "pa_pool_share_prefix",
@@ -62,7 +64,8 @@ def load_library():
                 f"{path} is missing: build the HIP library first (python -m paper_2506_07311_amd.build). "
                 "There is no CPU fallback.")
         lib = ctypes.CDLL(path)
-        sizes = ("paged_attention_workspace_bytes", "paged_attention_tree_workspace_bytes")
+        sizes = ("paged_attention_workspace_bytes", "paged_attention_tree_workspace_bytes", "paged_attention_mx4_workspace_bytes",
+                 "pa_mx4_record_bytes")
         for name in sizes:
             getattr(lib, name).restype = ctypes.c_size_t
         lib.pa_status_string.restype = ctypes.c_char_p
@@ -680,6 +683,251 @@ def paged_tree_accept(k_cache, v_cache, cu_q_lens, seq_lens, max_q_len: int, blo
     """Finds what stays of a verified tree and moves its K and V rows together.  Returns (path, path_lens, next_tokens,
     kept_lens); keyword arguments as for prepare_tree_accept."""
     return prepare_tree_accept(k_cache, v_cache, cu_q_lens, seq_lens, max_q_len, block_table, path, path_lens, **kw)()
+
+
+# ---- normalised heads, positions of several numbers, the 4-bit cache (see the block of that name in include/pagedattn.h) -------
+
+class _NormRope(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "q_out", "k_new", "v_new")] + \
+        [(n, ctypes.c_int64) for n in ("q_stride", "q_out_stride", "k_stride", "v_stride")] + \
+        [(n, ctypes.c_void_p) for n in ("rope_positions", "pair_axes", "inv_freq", "q_weight", "k_weight", "seq_ids", "positions",
+                                        "block_table")] + \
+        [(n, ctypes.c_int32) for n in ("num_q_heads", "T", "batch", "max_blocks", "axes", "rotary_dim", "interleaved", "norm_q", "norm_k",
+                                       "q_weight_heads", "k_weight_heads", "weight_dtype")] + \
+        [(n, ctypes.c_float) for n in ("eps", "weight_offset", "mscale")]
+
+
+class _Mx4Desc(ctypes.Structure):
+    _fields_ = [("records", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
+
+
+def pa_mx4_record_bytes(page_size: int, head_dim: int) -> int:
+    return int(load_library().pa_mx4_record_bytes(ctypes.c_int32(page_size), ctypes.c_int32(head_dim)))
+
+
+def pa_mx4_cache(num_pages: int, page_size: int, num_kv_heads: int, head_dim: int, device="cuda") -> torch.Tensor:
+    """An empty 4-bit cache: uint8 [num_pages, num_kv_heads, pa_mx4_record_bytes(page_size, head_dim)]."""
+    size = pa_mx4_record_bytes(page_size, head_dim)
+    if size == 0:
+        raise PagedAttnError("a 4-bit cache has pages of 16 tokens or more, a power of two, and head_dim 64, 128 or 256; "
+                             f"got {page_size} and {head_dim}")
+    return torch.empty((num_pages, num_kv_heads, size), dtype=torch.uint8, device=device)
+
+
+def mx4_desc(cache: torch.Tensor, head_dim: int) -> _Mx4Desc:
+    """Descriptor of a 4-bit cache, uint8 [num_pages, Hkv, record]; its record's size gives the tokens of a page."""
+    if cache.dtype != torch.uint8 or cache.dim() != 3 or not cache.is_cuda or cache.stride(2) != 1:
+        raise PagedAttnError("a 4-bit cache is a uint8 device tensor [num_pages, Hkv, record] with contiguous records")
+    NP, Hkv, size = cache.shape
+    page = size * 16 // (17 * head_dim) if head_dim > 0 else 0
+    if size == 0 or pa_mx4_record_bytes(page, head_dim) != size:
+        raise PagedAttnError(f"records of {size} bytes hold no page of heads of {head_dim}")
+    return _Mx4Desc(cache.data_ptr(), cache.stride(0) if NP > 1 else Hkv * size, cache.stride(1) if Hkv > 1 else size, NP, page, Hkv,
+                    head_dim)
+
+
+def _weights(w, what, heads, d, dtype):
+    """(pointer, [heads, d] and not [d])"""
+    if w is None:
+        return 0, 0
+    if w.dtype not in (dtype, torch.float32) or not w.is_contiguous() or tuple(w.shape) not in ((d,), (heads, d)):
+        raise PagedAttnError(f"{what} must be a contiguous {dtype} or float32 tensor [{d}] or [{heads}, {d}], got {w.dtype} {list(w.shape)}")
+    return w.data_ptr(), int(w.dim() == 2)
+
+
+def _norm_rope(what, caches, Hkv, d, dtype, q, k_new, v_new, rope_positions, seq_ids, positions, block_table, inv_freq, q_weight, k_weight, eps,
+               weight_offset, norm_q, norm_k, pair_axes, interleaved, mscale, q_out, stream):
+    dev = _together(what, *caches, q, k_new, v_new, rope_positions, seq_ids, positions, block_table, inv_freq, q_weight, k_weight, pair_axes,
+                    q_out)
+    if rope_positions.dim() not in (1, 2):
+        raise PagedAttnError("rope_positions must be int32[T] or [axes, T]")
+    T = int(rope_positions.shape[-1])
+    axes = int(rope_positions.shape[0]) if rope_positions.dim() == 2 else 1
+    _shaped(rope_positions, "rope_positions", rope_positions.shape)
+    if inv_freq.dim() != 1:
+        raise PagedAttnError("inv_freq must be float64[rotary_dim / 2]")
+    _shaped(inv_freq, "inv_freq", inv_freq.shape, torch.float64)
+    if pair_axes is not None:
+        _shaped(pair_axes, "pair_axes", inv_freq.shape)
+    elif axes > 1:
+        raise PagedAttnError("positions of several numbers need pair_axes")
+    Hq = 0
+    if q is not None:
+        Hq = int(q.shape[1]) if q.dim() == 3 else 0
+        _rows(q, "q", (T, Hq, d), dtype)
+        q_out = _new((T, Hq, d), dtype, dev, stream) if q_out is None else _rows(q_out, "q_out", (T, Hq, d), dtype)
+    elif q_out is not None:
+        raise PagedAttnError("q_out without q")
+    B = MB = 0
+    if k_new is not None:
+        if v_new is None or seq_ids is None or positions is None or block_table is None:
+            raise PagedAttnError("k_new needs v_new, seq_ids, positions and block_table")
+        _rows(k_new, "k_new", (T, Hkv, d), dtype)
+        _rows(v_new, "v_new", (T, Hkv, d), dtype)
+        _shaped(seq_ids, "seq_ids", (T,)), _shaped(positions, "positions", (T,)), _i32(block_table, "block_table")
+        if block_table.dim() != 2:
+            raise PagedAttnError("block_table must be [batch, max_blocks]")
+        B, MB = block_table.shape
+    elif v_new is not None:
+        raise PagedAttnError("v_new without k_new")
+    qw, qw_heads = _weights(q_weight, "q_weight", Hq, d, dtype)
+    kw, kw_heads = _weights(k_weight, "k_weight", Hkv, d, dtype)
+    kinds = {w.dtype for w in (q_weight, k_weight) if w is not None}
+    if len(kinds) > 1:
+        raise PagedAttnError("q_weight and k_weight must be of one type")
+
+    def ptr(t):
+        return 0 if t is None else t.data_ptr()
+
+    def apart(t):
+        return 0 if t is None or t.shape[0] < 2 else t.stride(0)
+
+    r = _NormRope(ptr(q), ptr(q_out), ptr(k_new), ptr(v_new), apart(q), apart(q_out), apart(k_new), apart(v_new), ptr(rope_positions),
+                  ptr(pair_axes), ptr(inv_freq), qw, kw, ptr(seq_ids), ptr(positions), ptr(block_table), Hq, T, B, MB, axes,
+                  2 * inv_freq.shape[0], int(bool(interleaved)), int(bool(norm_q)), int(bool(norm_k)), qw_heads, kw_heads,
+                  PA_DTYPE[kinds.pop() if kinds else dtype], eps, weight_offset, mscale)
+    keep = (r, caches, q, q_out, k_new, v_new, rope_positions, pair_axes, inv_freq, q_weight, k_weight, seq_ids, positions, block_table)
+    return r, keep, q_out
+
+
+def prepare_norm_rope_append(k_cache, v_cache, q, k_new, v_new, rope_positions, seq_ids, positions, block_table, inv_freq, *, q_weight=None,
+                             k_weight=None, eps: float = 1e-6, weight_offset: float = 0.0, norm_q: bool = True, norm_k: bool = True,
+                             pair_axes=None, interleaved: bool = False, mscale: float = 1.0, q_out=None, head_major=False,
+                             stream=None) -> PreparedCall:
+    """paged_norm_rope_append with its arguments marshalled once; the call returns ``q_out`` (allocated unless given; may be q).
+    rope_positions: int32 [T], or [axes, T] with pair_axes int32 [rotary_dim / 2].  q_weight, k_weight: [d] or [heads, d].  The rest as
+    for prepare_rope_append."""
+    lib = load_library()
+    d = cache_desc(k_cache, v_cache, head_major)
+    r, keep, q_out = _norm_rope("paged_norm_rope_append", (k_cache, v_cache), d.num_kv_heads, d.head_dim, k_cache.dtype, q, k_new, v_new,
+                                rope_positions, seq_ids, positions, block_table, inv_freq, q_weight, k_weight, eps, weight_offset, norm_q,
+                                norm_k, pair_axes, interleaved, mscale, q_out, stream)
+    return PreparedCall(lib.paged_norm_rope_append, (ctypes.byref(d), ctypes.byref(r), _stream(stream)), (d, keep),
+                        "paged_norm_rope_append", q_out)
+
+
+def paged_norm_rope_append(k_cache, v_cache, q, k_new, v_new, rope_positions, seq_ids, positions, block_table, inv_freq, **kw):
+    """Norms of the heads of q and k_new, their rotary positions, K and V into their pages.  Returns ``q_out``; keyword arguments as
+    for prepare_norm_rope_append."""
+    return prepare_norm_rope_append(k_cache, v_cache, q, k_new, v_new, rope_positions, seq_ids, positions, block_table, inv_freq, **kw)()
+
+
+def prepare_norm_rope_append_mx4(cache, q, k_new, v_new, rope_positions, seq_ids, positions, block_table, inv_freq, *, q_weight=None,
+                                 k_weight=None, eps: float = 1e-6, weight_offset: float = 0.0, norm_q: bool = True, norm_k: bool = True,
+                                 pair_axes=None, interleaved: bool = False, mscale: float = 1.0, q_out=None,
+                                 stream=None) -> PreparedCall:
+    """prepare_norm_rope_append into a 4-bit cache (pa_mx4_cache)."""
+    lib = load_library()
+    x = q if q is not None else k_new
+    if x is None or x.dim() != 3 or x.dtype not in PA_DTYPE:
+        raise PagedAttnError("q or k_new must be a float32, bfloat16 or float16 tensor [T, heads, d]")
+    d = mx4_desc(cache, int(x.shape[2]))
+    r, keep, q_out = _norm_rope("paged_norm_rope_append_mx4", (cache,), d.num_kv_heads, d.head_dim, x.dtype, q, k_new, v_new, rope_positions,
+                                seq_ids, positions, block_table, inv_freq, q_weight, k_weight, eps, weight_offset, norm_q, norm_k, pair_axes,
+                                interleaved, mscale, q_out, stream)
+    return PreparedCall(lib.paged_norm_rope_append_mx4, (ctypes.byref(d), ctypes.c_int32(PA_DTYPE[x.dtype]), ctypes.byref(r), _stream(stream)),
+                        (d, keep), "paged_norm_rope_append_mx4", q_out)
+
+
+def paged_norm_rope_append_mx4(cache, q, k_new, v_new, rope_positions, seq_ids, positions, block_table, inv_freq, **kw):
+    """paged_norm_rope_append into a 4-bit cache.  Returns ``q_out``; keyword arguments as for prepare_norm_rope_append_mx4."""
+    return prepare_norm_rope_append_mx4(cache, q, k_new, v_new, rope_positions, seq_ids, positions, block_table, inv_freq, **kw)()
+
+
+def prepare_kv_append_mx4(cache, k_new, v_new, seq_ids, positions, block_table, *, stream=None) -> PreparedCall:
+    """paged_kv_append_mx4 with its arguments marshalled once.  k_new, v_new: [T, Hkv, d], contiguous."""
+    lib = load_library()
+    _together("paged_kv_append_mx4", cache, k_new, v_new, seq_ids, positions, block_table)
+    if k_new.dim() != 3 or k_new.dtype not in PA_DTYPE:
+        raise PagedAttnError("k_new must be a float32, bfloat16 or float16 tensor [T, Hkv, d]")
+    d = mx4_desc(cache, int(k_new.shape[2]))
+    _dense(k_new, "k_new", k_new.dtype), _dense(v_new, "v_new", k_new.dtype)
+    T = int(k_new.shape[0])
+    if k_new.shape[1] != d.num_kv_heads or k_new.shape != v_new.shape:
+        raise PagedAttnError("k_new/v_new must be [T, Hkv, d]")
+    _shaped(seq_ids, "seq_ids", (T,)), _shaped(positions, "positions", (T,)), _i32(block_table, "block_table")
+    if block_table.dim() != 2:
+        raise PagedAttnError("block_table must be [batch, max_blocks]")
+    args = (ctypes.byref(d), ctypes.c_int32(PA_DTYPE[k_new.dtype]), _p(k_new), _p(v_new), _p(seq_ids), _p(positions), ctypes.c_int32(T),
+            _p(block_table), ctypes.c_int32(block_table.shape[0]), ctypes.c_int32(block_table.shape[1]), _stream(stream))
+    return PreparedCall(lib.paged_kv_append_mx4, args, (d, cache, k_new, v_new, seq_ids, positions, block_table), "paged_kv_append_mx4")
+
+
+def paged_kv_append_mx4(cache, k_new, v_new, seq_ids, positions, block_table, *, stream=None) -> None:
+    """K and V rows into their pages of a 4-bit cache."""
+    prepare_kv_append_mx4(cache, k_new, v_new, seq_ids, positions, block_table, stream=stream)()
+
+
+def prepare_kv_gather_mx4(cache, block_table, seq_lens, *, cu_lens, max_seq_len: int, out_k, out_v, first_lens=None,
+                          stream=None) -> PreparedCall:
+    """paged_kv_gather_mx4 with its arguments marshalled once; the call returns (out_k, out_v), [rows, Hkv, d] of a type of the caller's."""
+    lib = load_library()
+    _together("paged_kv_gather_mx4", cache, block_table, first_lens, seq_lens, cu_lens, out_k, out_v)
+    if out_k.dim() != 3 or out_k.dtype not in PA_DTYPE:
+        raise PagedAttnError("out_k must be a float32, bfloat16 or float16 tensor [rows, Hkv, d]")
+    d = mx4_desc(cache, int(out_k.shape[2]))
+    _dense(out_k, "out_k", out_k.dtype), _dense(out_v, "out_v", out_k.dtype)
+    if out_k.shape[1] != d.num_kv_heads or out_k.shape != out_v.shape:
+        raise PagedAttnError("out_k/out_v must be [rows, Hkv, d]")
+    B = int(seq_lens.shape[0])
+    _shaped(seq_lens, "seq_lens", (B,)), _shaped(cu_lens, "cu_lens", (B + 1,)), _i32(block_table, "block_table")
+    if first_lens is not None:
+        _shaped(first_lens, "first_lens", (B,))
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise PagedAttnError("block_table must be [batch, max_blocks]")
+    args = (ctypes.byref(d), ctypes.c_int32(PA_DTYPE[out_k.dtype]), _p(out_k), _p(out_v), _p(block_table), _p(first_lens), _p(seq_lens),
+            _p(cu_lens), ctypes.c_int32(B), ctypes.c_int32(block_table.shape[1]), ctypes.c_int32(max_seq_len), _stream(stream))
+    return PreparedCall(lib.paged_kv_gather_mx4, args, (d, cache, block_table, first_lens, seq_lens, cu_lens, out_k, out_v),
+                        "paged_kv_gather_mx4", (out_k, out_v))
+
+
+def paged_kv_gather_mx4(cache, block_table, seq_lens, *, cu_lens, max_seq_len: int, out_k, out_v, first_lens=None, stream=None):
+    """What a 4-bit cache holds of the sequences (from token first_lens[s] on).  Returns (out_k, out_v)."""
+    return prepare_kv_gather_mx4(cache, block_table, seq_lens, cu_lens=cu_lens, max_seq_len=max_seq_len, out_k=out_k, out_v=out_v,
+                                 first_lens=first_lens, stream=stream)()
+
+
+def paged_attention_mx4_workspace_bytes(batch: int, num_q_heads: int, num_kv_heads: int, head_dim: int, total_q: int, max_q_len: int,
+                                        max_seq_len: int) -> int:
+    return int(load_library().paged_attention_mx4_workspace_bytes(
+        ctypes.c_int32(batch), ctypes.c_int32(num_q_heads), ctypes.c_int32(num_kv_heads), ctypes.c_int32(head_dim),
+        ctypes.c_int32(total_q), ctypes.c_int32(max_q_len), ctypes.c_int32(max_seq_len)))
+
+
+def prepare_attention_mx4(cache, q, cu_q_lens, max_q_len: int, block_table, seq_lens, max_seq_len: int, scale: float, *, out=None, lse=None,
+                          workspace=None, stream=None) -> PreparedCall:
+    """paged_attention_mx4 with its arguments marshalled once; the call returns ``out``."""
+    lib = load_library()
+    dev = _together("paged_attention_mx4", cache, q, cu_q_lens, block_table, seq_lens, out, lse, workspace)
+    if q.dim() != 3 or q.dtype not in PA_DTYPE:
+        raise PagedAttnError("q must be a float32, bfloat16 or float16 tensor [total_q, Hq, d]")
+    _dense(q, "q", q.dtype)
+    d = mx4_desc(cache, int(q.shape[2]))
+    total_q, Hq, hd = q.shape
+    B = int(seq_lens.shape[0])
+    _shaped(seq_lens, "seq_lens", (B,)), _shaped(cu_q_lens, "cu_q_lens", (B + 1,)), _i32(block_table, "block_table")
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise PagedAttnError("block_table must be [batch, max_blocks]")
+    out = _new(q.shape, q.dtype, q.device, stream) if out is None else _shaped(out, "out", q.shape, q.dtype)
+    if lse is not None:
+        _shaped(lse, "lse", (total_q, Hq), torch.float32)
+    if workspace is None:
+        workspace = _workspace(None, paged_attention_mx4_workspace_bytes(B, Hq, d.num_kv_heads, hd, total_q, max_q_len, max_seq_len), dev,
+                               stream)
+    args = (ctypes.byref(d), ctypes.c_int32(PA_DTYPE[q.dtype]), _p(q), _p(out), _p(lse), _p(cu_q_lens), ctypes.c_int32(total_q),
+            ctypes.c_int32(max_q_len), _p(block_table), _p(seq_lens), ctypes.c_int32(B), ctypes.c_int32(Hq),
+            ctypes.c_int32(block_table.shape[1]), ctypes.c_int32(max_seq_len), ctypes.c_float(scale), _p(workspace),
+            ctypes.c_size_t(workspace.numel() * workspace.element_size()), _stream(stream))
+    return PreparedCall(lib.paged_attention_mx4, args, (d, cache, q, out, lse, cu_q_lens, block_table, seq_lens, workspace),
+                        "paged_attention_mx4", out)
+
+
+def paged_attention_mx4(cache, q, cu_q_lens, max_q_len: int, block_table, seq_lens, max_seq_len: int, scale: float, **kw):
+    """Attention of the sequences' last tokens over a 4-bit cache.  Returns ``out`` ([total_q, Hq, d], dtype of q); keyword arguments as
+    for prepare_attention_mx4."""
+    return prepare_attention_mx4(cache, q, cu_q_lens, max_q_len, block_table, seq_lens, max_seq_len, scale, **kw)()
 
 
 def pa_debug_check(k_cache, v_cache, block_table, seq_lens, seq_ids=None, positions=None, *, head_major=False,

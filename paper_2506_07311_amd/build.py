@@ -17,11 +17,13 @@ SOURCES = ["api.hip", "kv_copy.hip", "attention_generic.hip", "attention_f32.hip
            "decode_mfma_d256.hip", "prefill_mfma.hip", "prefill_mfma_d64.hip", "prefill_mfma_d256.hip",
            "prefill_mfma_odd.hip", "jagged_mfma.hip", "page_pool.hip", "step_api.hip", "step_plan.hip",
            "rope_append.hip", "tree_generic.hip", "tree_mfma.hip", "tree_mfma_d64.hip", "tree_mfma_d96.hip", "tree_mfma_d256.hip",
-           "tree_f32.hip"]
+           "tree_f32.hip", "mx4_api.hip", "mx4_gather.hip", "norm_rope_append.hip", "mx4_attention.hip", "mx4_attention_d64.hip",
+           "mx4_attention_d256.hip"]
 HEADERS = [os.path.join(CSRC, "common.h"), os.path.join(CSRC, "prefill_tiles.h"),
            os.path.join(CSRC, "decode_mfma_impl.h"), os.path.join(CSRC, "prefill_mfma_impl.h"),
            os.path.join(HERE, "..", "include", "pagedattn.h"), os.path.join(HERE, "..", "include", "pagedattn_mods.h")]
 TREE_HEADERS = [os.path.join(CSRC, "tree_share.h"), os.path.join(CSRC, "tree_mfma_impl.h")]
+MX4_HEADERS = [os.path.join(CSRC, "mx4.h"), os.path.join(CSRC, "mx4_attention_impl.h"), os.path.join(CSRC, "tree_share.h")]
 # packed-fp32 VALU forms are disabled on purpose (they have produced wrong results on these machines)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang",
          "-packed-fp32-ops", "-Wall", "-Wno-unused-function", "-Wno-unknown-warning-option"]
@@ -37,7 +39,8 @@ def _hipcc() -> str:
 def _compile(src: str, force: bool) -> str:
     obj = os.path.join(OBJ, src.replace(".hip", ".o"))
     path = os.path.join(CSRC, src)
-    deps = [path] + HEADERS + (TREE_HEADERS if src.startswith("tree_") else [])
+    deps = [path] + HEADERS + (TREE_HEADERS if src.startswith("tree_") else []) + \
+        (MX4_HEADERS if src.startswith(("mx4_", "norm_")) else [])
     if not force and os.path.exists(obj) and os.path.getmtime(obj) >= max(os.path.getmtime(p) for p in deps):
         return obj
     cmd = [_hipcc(), *FLAGS, "-c", path, "-o", obj]

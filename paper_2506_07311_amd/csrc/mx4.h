@@ -1,0 +1,81 @@
+// The 4-bit cache (internal header): where a record holds what, and a block's rounding.  The layout is the header's.
+#pragma once
+
+#include "common.h"
+
+namespace pa {
+
+struct Mx4View {
+    char* records;
+    int64_t page_stride, head_stride;   // bytes
+    int32_t log2_page, head_dim, num_kv_heads, num_pages;
+};
+
+inline Mx4View make_view(const pa_mx4_cache_desc* c)
+{
+    Mx4View v = {(char*)c->records, c->page_stride, c->head_stride, 0, c->head_dim, c->num_kv_heads, c->num_pages};
+    while ((1 << v.log2_page) < c->page_size) ++v.log2_page;
+    return v;
+}
+
+#if defined(__HIPCC__)
+
+// Bytes from a record's start.  K codes of a slot.
+__device__ __forceinline__ int32_t mx4_k_codes(int32_t log2_page, int32_t d, int32_t slot) { return slot * (d / 2); }
+// V codes of elements 4 u .. 4 u + 3 of a head.
+__device__ __forceinline__ int32_t mx4_v_codes(int32_t log2_page, int32_t d, int32_t slot, int32_t u)
+{
+    const int32_t w = d / 32;                                // bytes of a cell's row: 2, 4 or 8
+    return ((d / 2) << log2_page) + ((slot >> 3) * 16 + 2 * u / w) * 8 * w + (slot & 7) * w + 2 * u % w;
+}
+// Scale of block b of K (what = 0) or V (1).
+__device__ __forceinline__ int32_t mx4_scale(int32_t log2_page, int32_t d, int32_t slot, int32_t b, int32_t what)
+{
+    return ((d + what * (d / 32) + b) << log2_page) + slot;
+}
+
+// Scale byte of a block from the bits of its largest magnitude (an infinity's or a NaN's are larger than any finite number's).
+__device__ __forceinline__ uint32_t mx4_scale_of(uint32_t top)
+{
+    const int32_t e = (int32_t)(top >> 23) - 2;
+    return top >= 0x7f800000u ? 255u : (uint32_t)max(e, 0);
+}
+
+// Code of x under a scale byte other than 255.  |x| / scale is below 8 and exact; from 1 on its exponent and leading mantissa bit are the
+// code, rounded to nearest even in place, below 1 it is a multiple of 1/2.
+__device__ __forceinline__ uint32_t mx4_code(float x, uint32_t scale)
+{
+    const uint32_t sign = (__float_as_uint(x) >> 31) << 3;
+    const float y = fabsf(x) * __uint_as_float((254u - scale) << 23);
+    uint32_t b = __float_as_uint(y);
+    b = ((b + 0x1fffffu + ((b >> 22) & 1u)) >> 22) - (127u << 1) + 2u;
+    const uint32_t small = (uint32_t)__builtin_rintf(y * 2.f);
+    return sign | (y < 1.f ? small : min(b, 7u));
+}
+
+#endif
+
+pa_status launch_kv_gather_mx4(const pa_mx4_cache_desc* c, pa_dtype dtype, void* out_k, void* out_v, const int32_t* block_table,
+                               const int32_t* first_lens, const int32_t* seq_lens, const int32_t* cu_lens, int32_t batch,
+                               int32_t max_blocks, int32_t max_seq_len, hipStream_t stream);
+// Into a 4-bit cache (to4), or one of the tokens' own type (cache).
+pa_status launch_norm_rope_append(const pa_kv_cache_desc* cache, const pa_mx4_cache_desc* to4, pa_dtype dtype, const pa_norm_rope& r,
+                                  hipStream_t stream);
+
+struct Mx4Args {
+    const pa_mx4_cache_desc* cache;
+    pa_dtype dtype;
+    const void* q;
+    void* out;
+    float* lse;
+    const int32_t* cu_q_lens;
+    const int32_t* seq_lens;
+    const int32_t* block_table;
+    int32_t batch, max_q_len, num_q_heads, max_blocks, max_seq_len;
+    float scale;
+};
+size_t mx4_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t max_q_len,
+                           int32_t max_seq_len);
+pa_status launch_attention_mx4(const Mx4Args& a, void* workspace, hipStream_t stream);
+
+}  // namespace pa

@@ -1,0 +1,116 @@
+// Attention over a cache of 4-bit elements (mx4_attention_impl.h) at head_dim 128, and its plan.
+#include "mx4_attention_impl.h"
+
+namespace pa {
+
+pa_status launch_mx4_d64(const TreeKernelArgs& a, bool merge, pa_dtype dtype, int shape, hipStream_t stream);
+pa_status launch_mx4_d256(const TreeKernelArgs& a, bool merge, pa_dtype dtype, int shape, hipStream_t stream);
+pa_status launch_mx4_d128(const TreeKernelArgs& a, bool merge, pa_dtype dtype, int shape, hipStream_t stream)
+{
+    return launch_mx4_dim<128>(a, merge, dtype, shape, stream);
+}
+
+namespace {
+
+struct Mx4Plan {
+    int shape;                   // launch_mx4_shape's
+    int32_t rows;                // of a workgroup
+    int32_t row_blocks;          // most row blocks of a sequence
+    int32_t wgs;                 // workgroups of a KV head that share all key tiles; 0: one a row block, no partials
+    int32_t tile;                // keys
+    size_t part_o_bytes, part_lse_bytes, cuts_bytes;
+};
+
+size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+
+// `wide`: 16 rows a wave where others take 32 (mx4_attention_impl.h).
+Mx4Plan plan_mx4(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t d, int32_t max_q_len, int32_t max_seq_len, bool f32)
+{
+    const bool wide = d == 256 || f32;
+    Mx4Plan p = {};
+    const int64_t rows = (int64_t)max_q_len * (num_q_heads / num_kv_heads);
+    p.shape = rows <= 16 ? 0 : rows <= 32 ? 1 : rows <= 64 ? 2 : 3;
+    p.rows = p.shape == 0 ? 16 : p.shape == 1 ? 32 : p.shape == 2 || wide ? 64 : 128;
+    p.tile = p.shape == 0 || (p.shape == 1 && !wide) ? 128 : 64;
+    const int64_t blocks = (rows + p.rows - 1) / p.rows;
+    p.row_blocks = blocks < 1 ? 1 : (int32_t)blocks;
+    const int64_t slots = (int64_t)device_cus() * (p.shape == 0 && !wide ? 3 : 2);
+    const int64_t units = (int64_t)batch * num_kv_heads * p.row_blocks;
+    const int64_t tiles = ((int64_t)max_seq_len + p.tile - 1) / p.tile;
+    // Row blocks are cut where they are long, and few or of different lengths.
+    if (tiles > 4 && (p.shape != 3 || units < slots)) {
+        const int64_t most = ((int64_t)batch * p.row_blocks * tiles + kTreeMinTiles - 1) / kTreeMinTiles;
+        int64_t wgs = slots / num_kv_heads;
+        if (wgs > most) wgs = most;
+        p.wgs = wgs < 1 ? 1 : wgs > kTreeMaxPieces ? kTreeMaxPieces : (int32_t)wgs;
+        const size_t part_rows = (size_t)p.wgs * num_kv_heads * 2 * p.rows;
+        p.part_o_bytes = align256(part_rows * d * sizeof(float));
+        p.part_lse_bytes = align256(part_rows * sizeof(float));
+        p.cuts_bytes = align256((size_t)num_kv_heads * batch * p.row_blocks * sizeof(int2));
+    }
+    return p;
+}
+
+}  // namespace
+
+size_t mx4_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t max_q_len,
+                           int32_t max_seq_len)
+{
+    size_t most = 256;                                       // (the type is not known here)
+    for (const bool f32 : {false, true}) {
+        const Mx4Plan p = plan_mx4(batch, num_q_heads, num_kv_heads, head_dim, max_q_len, max_seq_len, f32);
+        const size_t bytes = p.part_o_bytes + p.part_lse_bytes + p.cuts_bytes;
+        if (bytes > most) most = bytes;
+    }
+    return most;
+}
+
+pa_status launch_attention_mx4(const Mx4Args& t, void* workspace, hipStream_t stream)
+{
+    const pa_mx4_cache_desc* const c = t.cache;
+    const Mx4Plan p = plan_mx4(t.batch, t.num_q_heads, c->num_kv_heads, c->head_dim, t.max_q_len, t.max_seq_len, t.dtype == PA_DTYPE_F32);
+    // Places of a KV head stay below 2^31, threads of a launch below 2^32.
+    const int64_t units = (int64_t)t.batch * p.row_blocks, threads = (int64_t)1 << 32;
+    const int64_t tiles = ((int64_t)t.max_seq_len + p.tile - 1) / p.tile;
+    if ((p.wgs > 0 ? p.wgs : units) * c->num_kv_heads * 256 >= threads) return PA_ERR_UNSUPPORTED;
+    if (p.wgs > 0 && (tiles + kTreePieceTiles > 0x7fffffff / units || units * p.rows * c->head_dim / 4 >= threads)) return PA_ERR_UNSUPPORTED;
+    const Mx4View v = make_view(c);
+    TreeKernelArgs a = {};
+    a.cache.k = a.cache.v = v.records;
+    a.cache.page_stride = v.page_stride;
+    a.cache.head_stride = v.head_stride;
+    a.cache.page_size = c->page_size;
+    a.cache.log2_page = v.log2_page;
+    a.cache.num_kv_heads = c->num_kv_heads;
+    a.cache.head_dim = c->head_dim;
+    a.q = t.q;
+    a.out = t.out;
+    a.lse = t.lse;
+    a.cu_q_lens = t.cu_q_lens;
+    a.seq_lens = t.seq_lens;
+    a.block_table = t.block_table;
+    a.part_o = reinterpret_cast<float*>(workspace);
+    a.part_lse = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + p.part_o_bytes);
+    a.cuts = reinterpret_cast<int2*>(reinterpret_cast<char*>(a.part_lse) + p.part_lse_bytes);
+    a.batch = t.batch;
+    a.num_q_heads = t.num_q_heads;
+    a.max_blocks = t.max_blocks;
+    a.group = t.num_q_heads / c->num_kv_heads;
+    a.wgs = p.wgs;
+    a.row_blocks = p.row_blocks;
+    a.scale = t.scale;
+    auto launch = [&](bool merge) {
+        if (c->head_dim == 64) return launch_mx4_d64(a, merge, t.dtype, p.shape, stream);
+        if (c->head_dim == 128) return launch_mx4_d128(a, merge, t.dtype, p.shape, stream);
+        return launch_mx4_d256(a, merge, t.dtype, p.shape, stream);
+    };
+    {
+        ProfileScope prof("paged_attention_mx4_kernel", stream);
+        const pa_status st = launch(false);
+        if (st != PA_OK || p.wgs == 0) return st;
+    }
+    ProfileScope prof("paged_attention_mx4_merge_kernel", stream);
+    return launch(true);
+}
+
+}  // namespace pa

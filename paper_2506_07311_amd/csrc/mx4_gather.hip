@@ -1,0 +1,88 @@
+// Algorithm 1's Gather from a cache of 4-bit elements: the values that codes and scales stand for, in the wanted type.
+#include "mx4.h"
+
+namespace pa {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// Eight tokens of a sequence a workgroup (a V record is laid out so), a thread 8 elements of a token's head at a time: 4 bytes of codes and a
+// scale in, 16 or 32 bytes out.  Bound by the bytes that it writes.
+template <pa_dtype DT>
+__global__ __launch_bounds__(kThreads) void paged_kv_gather_mx4_kernel(Mx4View c, void* out_k, void* out_v,
+                                                                       const int32_t* __restrict__ block_table,
+                                                                       const int32_t* __restrict__ first_lens,
+                                                                       const int32_t* __restrict__ seq_lens,
+                                                                       const int32_t* __restrict__ cu_lens, int32_t max_blocks)
+{
+    const int32_t s = blockIdx.y, d = c.head_dim, lp = c.log2_page;
+    const int32_t from = first_lens ? max(first_lens[s], 0) : 0, row_first = cu_lens[s];
+    const int64_t most = min((int64_t)max_blocks << lp, (int64_t)from + (cu_lens[s + 1] - row_first));
+    const int32_t len = (int32_t)min((int64_t)seq_lens[s], most);
+    const int32_t t0 = ((from >> 3) + (int32_t)blockIdx.x) * 8;
+    if (t0 >= len) return;
+    const int32_t row0 = row_first - from;
+    const int32_t page = block_table[(int64_t)s * max_blocks + (t0 >> lp)];
+    if (page < 0 || page >= c.num_pages) return;
+    const char* const base = c.records + (int64_t)page * c.page_stride;
+    const int32_t slot0 = t0 & ((1 << lp) - 1), pieces = d / 8, each = 8 * c.num_kv_heads * pieces;
+    for (int32_t i = threadIdx.x; i < 2 * each; i += kThreads) {
+        const int32_t what = i >= each, j = what ? i - each : i;
+        const int32_t u = j % pieces, h = j / pieces % c.num_kv_heads, k = j / pieces / c.num_kv_heads, t = t0 + k;
+        if (t < from || t >= len) continue;
+        const char* const rec = base + h * c.head_stride;
+        uint32_t codes;
+        if (what == 0) {
+            codes = *reinterpret_cast<const uint32_t*>(rec + mx4_k_codes(lp, d, slot0 + k) + 4 * u);
+        } else if (d == 64) {
+            codes = *reinterpret_cast<const uint16_t*>(rec + mx4_v_codes(lp, d, slot0 + k, 2 * u)) |
+                    (uint32_t)*reinterpret_cast<const uint16_t*>(rec + mx4_v_codes(lp, d, slot0 + k, 2 * u + 1)) << 16;
+        } else {
+            codes = *reinterpret_cast<const uint32_t*>(rec + mx4_v_codes(lp, d, slot0 + k, 2 * u));
+        }
+        const uint32_t scale = *reinterpret_cast<const uint8_t*>(rec + mx4_scale(lp, d, slot0 + k, u / 4, what));
+        const float unit = __uint_as_float(scale << 23);     // (the conversion reads its exponent alone: 0 is 2^-127, 255 NaN)
+        const int64_t at = ((int64_t)(row0 + t) * c.num_kv_heads + h) * d + 8 * u;
+        typedef __attribute__((ext_vector_type(2))) float f32x2;
+        float x[8];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const f32x2 v = b == 0 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, unit, 0)
+                            : b == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, unit, 1)
+                            : b == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, unit, 2)
+                                     : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, unit, 3);
+            x[2 * b] = v[0];
+            x[2 * b + 1] = v[1];
+        }
+        if (DT == PA_DTYPE_F32) {
+            float4* const dst = reinterpret_cast<float4*>((float*)(what ? out_v : out_k) + at);
+            dst[0] = float4{x[0], x[1], x[2], x[3]};
+            dst[1] = float4{x[4], x[5], x[6], x[7]};
+        } else {
+            typedef typename std::conditional<DT == PA_DTYPE_F16, ElemF16, ElemBf16>::type E;
+            *reinterpret_cast<uint4*>((uint16_t*)(what ? out_v : out_k) + at) =
+                uint4{E::pack(x[0], x[1]), E::pack(x[2], x[3]), E::pack(x[4], x[5]), E::pack(x[6], x[7])};
+        }
+    }
+}
+
+}  // namespace
+
+pa_status launch_kv_gather_mx4(const pa_mx4_cache_desc* c, pa_dtype dtype, void* out_k, void* out_v, const int32_t* block_table,
+                               const int32_t* first_lens, const int32_t* seq_lens, const int32_t* cu_lens, int32_t batch,
+                               int32_t max_blocks, int32_t max_seq_len, hipStream_t stream)
+{
+    const Mx4View v = make_view(c);
+    const dim3 grid((uint32_t)(((int64_t)max_seq_len + 7) / 8), (uint32_t)batch);
+    ProfileScope prof("paged_kv_gather_mx4_kernel", stream);
+    auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, v, out_k, out_v, block_table, first_lens, seq_lens, cu_lens, max_blocks);
+    };
+    if (dtype == PA_DTYPE_F32) launch(paged_kv_gather_mx4_kernel<PA_DTYPE_F32>);
+    else if (dtype == PA_DTYPE_BF16) launch(paged_kv_gather_mx4_kernel<PA_DTYPE_BF16>);
+    else launch(paged_kv_gather_mx4_kernel<PA_DTYPE_F16>);
+    return launch_status();
+}
+
+}  // namespace pa

@@ -26,6 +26,7 @@ typedef mfma_f32x4 f32x4;
 template <int WR, int DP>
 struct Tree32 {
     static constexpr bool kCut = true;
+    static constexpr int kLeastTiles = 0;
     static constexpr int kWaves = WR > 1 && DP <= 128 ? 8 : 4, kOcc = 1, kRows = 16 * WR, kWaveRows = 16, kColumns = DP;
     static constexpr int kTile = DP > 128 ? 32 : 64;
     static constexpr int kKW = kWaves / WR < kTile / 16 ? kWaves / WR : kTile / 16;        // waves that share 16 rows

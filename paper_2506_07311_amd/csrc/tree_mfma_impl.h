@@ -458,6 +458,7 @@ template <int WR, typename E, int DP>
 struct Tree16 {
     typedef TreeShape<WR, DP> Shape;
     static constexpr bool kCut = WR > 1;                                 // (one wave of rows is for calls without a cut)
+    static constexpr int kLeastTiles = 0;
     static constexpr int kRows = 32 * WR, kWaveRows = 32, kColumns = DP, kTile = Shape::kTile, kWaves = Shape::kWaves, kOcc = Shape::kOcc;
     static constexpr int kLds = Shape::kBufs * Shape::kBufB + (Shape::kKW - 1) * WR * 1024;   // (maxima and sums of two waves)
     template <bool CAREFUL>

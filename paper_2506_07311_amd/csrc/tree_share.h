@@ -3,7 +3,7 @@
 //
 // A shape S says what a workgroup does: kRows rows (query, head of the KV head's group) of one sequence at a time, kWaveRows
 // of them a wave, in kColumns columns; tiles of kTile keys; kWaves waves, kOcc workgroups on a compute unit, kLds bytes of LDS; kCut: its
-// row blocks may be cut; and
+// row blocks may be cut; a sequence has kLeastTiles tiles even where it has no key (0: rows of an empty one are left as they are); and
 //     work<CAREFUL>(buf, flags, args, item, KV head)   does a piece of work; true: it has to be done again with CAREFUL
 //     store(out, element, float4)                     four output columns
 #pragma once
@@ -101,7 +101,7 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeKernelArgs& a, int32_t i)
         q.n = a.cu_q_lens[i + 1] - q.row0;
         q.len = a.seq_lens[i];
         q.blocks = q.n > 0 ? min((q.n * a.group + S::kRows - 1) / S::kRows, a.row_blocks) : 0;   // (n keeps to its bound)
-        q.tiles = (q.len + S::kTile - 1) / S::kTile;
+        q.tiles = max((q.len + S::kTile - 1) / S::kTile, S::kLeastTiles);
     }
     return q;
 }
