@@ -877,8 +877,9 @@ def prepare_kv_gather_mx4(cache, block_table, seq_lens, *, cu_lens, max_seq_len:
         _shaped(first_lens, "first_lens", (B,))
     if block_table.dim() != 2 or block_table.shape[0] != B:
         raise PagedAttnError("block_table must be [batch, max_blocks]")
-    args = (ctypes.byref(d), ctypes.c_int32(PA_DTYPE[out_k.dtype]), _p(out_k), _p(out_v), _p(block_table), _p(first_lens), _p(seq_lens),
-            _p(cu_lens), ctypes.c_int32(B), ctypes.c_int32(block_table.shape[1]), ctypes.c_int32(max_seq_len), _stream(stream))
+    args = (ctypes.byref(d), ctypes.c_int32(PA_DTYPE[out_k.dtype]), _p(out_k), _p(out_v),
+            ctypes.c_int32(out_k.shape[0]), _p(block_table), _p(first_lens), _p(seq_lens), _p(cu_lens), ctypes.c_int32(B),
+            ctypes.c_int32(block_table.shape[1]), ctypes.c_int32(max_seq_len), _stream(stream))
     return PreparedCall(lib.paged_kv_gather_mx4, args, (d, cache, block_table, first_lens, seq_lens, cu_lens, out_k, out_v),
                         "paged_kv_gather_mx4", (out_k, out_v))
 

@@ -112,18 +112,19 @@ pa_status paged_kv_append_mx4(const pa_mx4_cache_desc* cache, pa_dtype dtype, co
     return launch_norm_rope_append(nullptr, cache, dtype, r, stream_of(stream));
 }
 
-pa_status paged_kv_gather_mx4(const pa_mx4_cache_desc* cache, pa_dtype dtype, void* out_k, void* out_v, const int32_t* block_table,
-                              const int32_t* first_lens, const int32_t* seq_lens, const int32_t* cu_lens, int32_t batch,
-                              int32_t max_blocks, int32_t max_seq_len, void* stream)
+pa_status paged_kv_gather_mx4(const pa_mx4_cache_desc* cache, pa_dtype dtype, void* out_k, void* out_v, int32_t total_rows,
+                              const int32_t* block_table, const int32_t* first_lens, const int32_t* seq_lens, const int32_t* cu_lens,
+                              int32_t batch, int32_t max_blocks, int32_t max_seq_len, void* stream)
 {
     const pa_status st = check_mx4(cache, dtype);
     if (st != PA_OK) return st;
-    if (batch < 0 || max_blocks < 0 || max_seq_len < 0) return PA_ERR_INVALID_ARG;
-    if (batch == 0 || max_seq_len == 0) return PA_OK;
+    if (total_rows < 0 || batch < 0 || max_blocks < 0 || max_seq_len < 0) return PA_ERR_INVALID_ARG;
+    if (total_rows == 0 || batch == 0 || max_seq_len == 0) return PA_OK;
     if (!out_k || !out_v || !block_table || !seq_lens || !cu_lens || max_blocks == 0) return PA_ERR_INVALID_ARG;
-    if ((((uintptr_t)out_k | (uintptr_t)out_v) & 15) || batch > 65535) return PA_ERR_UNSUPPORTED;
-    return launch_kv_gather_mx4(cache, dtype, out_k, out_v, block_table, first_lens, seq_lens, cu_lens, batch, max_blocks, max_seq_len,
-                                stream_of(stream));
+    if ((((uintptr_t)out_k | (uintptr_t)out_v) & 15) || cache->num_kv_heads > 8192) return PA_ERR_UNSUPPORTED;
+    const int64_t most = (int64_t)batch * max_seq_len;
+    return launch_kv_gather_mx4(cache, dtype, out_k, out_v, total_rows < most ? total_rows : (int32_t)most, block_table, first_lens, seq_lens,
+                                cu_lens, batch, max_blocks, stream_of(stream));
 }
 
 size_t paged_attention_mx4_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,

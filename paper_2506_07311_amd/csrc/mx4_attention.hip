@@ -34,7 +34,7 @@ Mx4Plan plan_mx4(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32
     p.tile = p.shape == 0 || (p.shape == 1 && !wide) ? 128 : 64;
     const int64_t blocks = (rows + p.rows - 1) / p.rows;
     p.row_blocks = blocks < 1 ? 1 : (int32_t)blocks;
-    const int64_t slots = (int64_t)device_cus() * (p.shape == 0 && !wide ? 3 : 2);
+    const int64_t slots = (int64_t)device_cus() * 2;
     const int64_t units = (int64_t)batch * num_kv_heads * p.row_blocks;
     const int64_t tiles = ((int64_t)max_seq_len + p.tile - 1) / p.tile;
     // Row blocks are cut where they are long, and few or of different lengths.

@@ -330,13 +330,22 @@ struct Mx4Shape {
             Keys ring[DEEP];
 #pragma unroll
             for (int i = 0; i < DEEP; ++i) load(ring[i], step0 + KW * min(i, steps - 1));
-            for (int32_t n = 0; n < steps; n += DEEP) {
+            int32_t n = 0;
+            for (; n + 2 * DEEP <= steps; n += DEEP) {
 #pragma unroll
                 for (int i = 0; i < DEEP; ++i) {
-                    if (n + i < steps) compute(ring[i], step0 + KW * (n + i));
-                    load(ring[i], step0 + KW * min(n + i + DEEP, steps - 1));
+                    compute(ring[i], step0 + KW * (n + i));
+                    load(ring[i], step0 + KW * (n + i + DEEP));
                 }
             }
+#pragma unroll
+            for (int i = 0; i < DEEP; ++i) {                 // (fewer than 2 DEEP are left)
+                if (n + i < steps) compute(ring[i], step0 + KW * (n + i));
+                if (n + i + DEEP < steps) load(ring[i], step0 + KW * (n + i + DEEP));
+            }
+#pragma unroll
+            for (int i = 0; i < DEEP; ++i)
+                if (n + i + DEEP < steps) compute(ring[i], step0 + KW * (n + i + DEEP));
         }
         // statistics of whole rows, and whether something has to be done again
         bool bad = false;
@@ -471,7 +480,7 @@ pa_status launch_mx4_shape(const TreeKernelArgs& a, bool merge, int shape, hipSt
 {
     constexpr bool kWide = D == 256 || DT == PA_DTYPE_F32;   // O and Q of 32 rows do not fit a wave's registers
     switch (shape) {
-        case 0: return launch_tree_of<Mx4Shape<DT, D, 1, 1, 4, kWide ? 2 : 3, 2>>(a, merge, stream);
+        case 0: return launch_tree_of<Mx4Shape<DT, D, 1, 1, 4, 2, 2>>(a, merge, stream);
         case 1: return launch_tree_of<Mx4Shape<DT, D, kWide ? 1 : 2, kWide ? 2 : 1, kWide ? 2 : 4, 2, 2>>(a, merge, stream);
         case 2: return launch_tree_of<Mx4Shape<DT, D, kWide ? 1 : 2, kWide ? 4 : 2, kWide ? 1 : 2, 2, 2>>(a, merge, stream);
     }

@@ -7,43 +7,66 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Eight tokens of a sequence a workgroup (a V record is laid out so), a thread 8 elements of a token's head at a time: 4 bytes of codes and a
-// scale in, 16 or 32 bytes out.  Bound by the bytes that it writes.
+// Eight rows a workgroup, a thread 8 elements of a row's head at a time: 4 bytes of codes and a scale in, 16 or 32 bytes out.  Bound by the
+// bytes that it writes.
 template <pa_dtype DT>
-__global__ __launch_bounds__(kThreads) void paged_kv_gather_mx4_kernel(Mx4View c, void* out_k, void* out_v,
+__global__ __launch_bounds__(kThreads) void paged_kv_gather_mx4_kernel(Mx4View c, void* out_k, void* out_v, int32_t rows,
                                                                        const int32_t* __restrict__ block_table,
                                                                        const int32_t* __restrict__ first_lens,
                                                                        const int32_t* __restrict__ seq_lens,
-                                                                       const int32_t* __restrict__ cu_lens, int32_t max_blocks)
+                                                                       const int32_t* __restrict__ cu_lens, int32_t batch, int32_t max_blocks,
+                                                                       uint32_t by_heads)
 {
-    const int32_t s = blockIdx.y, d = c.head_dim, lp = c.log2_page;
-    const int32_t from = first_lens ? max(first_lens[s], 0) : 0, row_first = cu_lens[s];
-    const int64_t most = min((int64_t)max_blocks << lp, (int64_t)from + (cu_lens[s + 1] - row_first));
-    const int32_t len = (int32_t)min((int64_t)seq_lens[s], most);
-    const int32_t t0 = ((from >> 3) + (int32_t)blockIdx.x) * 8;
-    if (t0 >= len) return;
-    const int32_t row0 = row_first - from;
-    const int32_t page = block_table[(int64_t)s * max_blocks + (t0 >> lp)];
-    if (page < 0 || page >= c.num_pages) return;
-    const char* const base = c.records + (int64_t)page * c.page_stride;
-    const int32_t slot0 = t0 & ((1 << lp) - 1), pieces = d / 8, each = 8 * c.num_kv_heads * pieces;
+    constexpr int ROWS = 8;
+    __shared__ int64_t sm_page[ROWS];                        // bytes from the first record on; -1: no such token
+    __shared__ int32_t sm_slot[ROWS];
+    const int32_t d = c.head_dim, lp = c.log2_page, row0 = (int32_t)blockIdx.x * ROWS;
+    const int lane = threadIdx.x & 63;
+    // a wave finds two rows' sequences: the first whose end lies behind the row
+    for (int32_t k = threadIdx.x >> 6; k < ROWS; k += kThreads / 64) {
+        const int32_t r = row0 + k;
+        int32_t s = -1;
+        for (int32_t i0 = 0; i0 < batch && s < 0; i0 += 64) {
+            const uint64_t hit = __ballot(i0 + lane < batch && cu_lens[min(i0 + lane, batch - 1) + 1] > r);
+            if (hit) s = i0 + __ffsll((unsigned long long)hit) - 1;
+        }
+        int64_t at = -1;
+        int32_t slot = 0;
+        if (s >= 0 && r < rows && r >= cu_lens[s]) {
+            const int64_t t = (int64_t)r - cu_lens[s] + (first_lens ? max(first_lens[s], 0) : 0);
+            if (t < seq_lens[s] && t >> lp < max_blocks) {
+                const int32_t page = block_table[(int64_t)s * max_blocks + (t >> lp)];
+                if (page >= 0 && page < c.num_pages) at = (int64_t)page * c.page_stride;
+                slot = (int32_t)t & ((1 << lp) - 1);
+            }
+        }
+        if (lane == 0) {
+            sm_page[k] = at;
+            sm_slot[k] = slot;
+        }
+    }
+    __syncthreads();
+    const int32_t log2_pieces = d == 64 ? 3 : d == 128 ? 4 : 5, pieces = 1 << log2_pieces, each = ROWS * c.num_kv_heads * pieces;
     for (int32_t i = threadIdx.x; i < 2 * each; i += kThreads) {
         const int32_t what = i >= each, j = what ? i - each : i;
-        const int32_t u = j % pieces, h = j / pieces % c.num_kv_heads, k = j / pieces / c.num_kv_heads, t = t0 + k;
-        if (t < from || t >= len) continue;
+        const uint32_t u = j & (pieces - 1), hk = (uint32_t)j >> log2_pieces;
+        const uint32_t k = c.num_kv_heads == 1 ? hk : __umulhi(hk, by_heads), h = hk - k * c.num_kv_heads;
+        if (sm_page[k] < 0) continue;
+        const int32_t slot = sm_slot[k];
+        const char* const base = c.records + sm_page[k];
         const char* const rec = base + h * c.head_stride;
         uint32_t codes;
         if (what == 0) {
-            codes = *reinterpret_cast<const uint32_t*>(rec + mx4_k_codes(lp, d, slot0 + k) + 4 * u);
+            codes = *reinterpret_cast<const uint32_t*>(rec + mx4_k_codes(lp, d, slot) + 4 * u);
         } else if (d == 64) {
-            codes = *reinterpret_cast<const uint16_t*>(rec + mx4_v_codes(lp, d, slot0 + k, 2 * u)) |
-                    (uint32_t)*reinterpret_cast<const uint16_t*>(rec + mx4_v_codes(lp, d, slot0 + k, 2 * u + 1)) << 16;
+            codes = *reinterpret_cast<const uint16_t*>(rec + mx4_v_codes(lp, d, slot, 2 * u)) |
+                    (uint32_t)*reinterpret_cast<const uint16_t*>(rec + mx4_v_codes(lp, d, slot, 2 * u + 1)) << 16;
         } else {
-            codes = *reinterpret_cast<const uint32_t*>(rec + mx4_v_codes(lp, d, slot0 + k, 2 * u));
+            codes = *reinterpret_cast<const uint32_t*>(rec + mx4_v_codes(lp, d, slot, 2 * u));
         }
-        const uint32_t scale = *reinterpret_cast<const uint8_t*>(rec + mx4_scale(lp, d, slot0 + k, u / 4, what));
+        const uint32_t scale = *reinterpret_cast<const uint8_t*>(rec + mx4_scale(lp, d, slot, u / 4, what));
         const float unit = __uint_as_float(scale << 23);     // (the conversion reads its exponent alone: 0 is 2^-127, 255 NaN)
-        const int64_t at = ((int64_t)(row0 + t) * c.num_kv_heads + h) * d + 8 * u;
+        const int64_t at = (((int64_t)row0 + k) * c.num_kv_heads + h) * d + 8 * u;
         typedef __attribute__((ext_vector_type(2))) float f32x2;
         float x[8];
 #pragma unroll
@@ -69,15 +92,18 @@ __global__ __launch_bounds__(kThreads) void paged_kv_gather_mx4_kernel(Mx4View c
 
 }  // namespace
 
-pa_status launch_kv_gather_mx4(const pa_mx4_cache_desc* c, pa_dtype dtype, void* out_k, void* out_v, const int32_t* block_table,
-                               const int32_t* first_lens, const int32_t* seq_lens, const int32_t* cu_lens, int32_t batch,
-                               int32_t max_blocks, int32_t max_seq_len, hipStream_t stream)
+pa_status launch_kv_gather_mx4(const pa_mx4_cache_desc* c, pa_dtype dtype, void* out_k, void* out_v, int32_t rows,
+                               const int32_t* block_table, const int32_t* first_lens, const int32_t* seq_lens, const int32_t* cu_lens,
+                               int32_t batch, int32_t max_blocks, hipStream_t stream)
 {
     const Mx4View v = make_view(c);
-    const dim3 grid((uint32_t)(((int64_t)max_seq_len + 7) / 8), (uint32_t)batch);
+    // x / heads = high word of x ceil(2^32 / heads) while x heads < 2^32; x is below 8 heads
+    const uint32_t by_heads = (uint32_t)((((int64_t)1 << 32) + c->num_kv_heads - 1) / c->num_kv_heads);
+    const dim3 grid((uint32_t)(((int64_t)rows + 7) / 8));
     ProfileScope prof("paged_kv_gather_mx4_kernel", stream);
     auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, v, out_k, out_v, block_table, first_lens, seq_lens, cu_lens, max_blocks);
+        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, v, out_k, out_v, rows, block_table, first_lens, seq_lens, cu_lens, batch,
+                           max_blocks, by_heads);
     };
     if (dtype == PA_DTYPE_F32) launch(paged_kv_gather_mx4_kernel<PA_DTYPE_F32>);
     else if (dtype == PA_DTYPE_BF16) launch(paged_kv_gather_mx4_kernel<PA_DTYPE_BF16>);

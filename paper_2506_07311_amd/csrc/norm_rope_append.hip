@@ -21,6 +21,7 @@ struct NormRopeArgs {
     int64_t page_stride, token_stride, head_stride;          // elements (a 4-bit cache: page and head, bytes)
     int32_t q_heads, kv_heads;                               // (0 heads: that part is absent)
     int32_t d, half, log2_page, num_pages;
+    float by_d;                                              // 1 / d
 };
 
 template <pa_dtype DT>
@@ -29,20 +30,36 @@ template <>
 struct Elem<PA_DTYPE_F32> {
     typedef float T;
     static __device__ __forceinline__ float get(float x) { return x; }
-    static __device__ __forceinline__ float put(float x) { return x; }
+    static __device__ __forceinline__ uint4 pack(const float (&x)[4])
+    {
+        return uint4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+    }
 };
 template <>
 struct Elem<PA_DTYPE_BF16> {
     typedef uint16_t T;
     static __device__ __forceinline__ float get(uint16_t x) { return bf16_bits_to_float(x); }
-    static __device__ __forceinline__ uint16_t put(float x) { return (uint16_t)float_to_bf16_bits(x); }
+    static __device__ __forceinline__ uint4 pack(const float (&x)[8])
+    {
+        return uint4{ElemBf16::pack(x[0], x[1]), ElemBf16::pack(x[2], x[3]), ElemBf16::pack(x[4], x[5]), ElemBf16::pack(x[6], x[7])};
+    }
 };
 template <>
 struct Elem<PA_DTYPE_F16> {
     typedef uint16_t T;
     static __device__ __forceinline__ float get(uint16_t x) { return f16_bits_to_float(x); }
-    static __device__ __forceinline__ uint16_t put(float x) { return (uint16_t)float_to_f16_bits(x); }
+    static __device__ __forceinline__ uint4 pack(const float (&x)[8])
+    {
+        return uint4{ElemF16::pack(x[0], x[1]), ElemF16::pack(x[2], x[3]), ElemF16::pack(x[4], x[5]), ElemF16::pack(x[6], x[7])};
+    }
 };
+
+// Of q, K and V, by values: a choice between variables that a lambda has by reference would put them into memory.
+template <typename X>
+__device__ __forceinline__ X pick(int32_t what, X q, X k, X v)
+{
+    return what == 0 ? q : what == 1 ? k : v;
+}
 
 template <int CTRL>
 __device__ __forceinline__ uint32_t moved(uint32_t x)
@@ -79,43 +96,18 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v)
     return v;
 }
 
-// Elements at .. at + V - 1 of a head: z inv (offset + w).
-template <pa_dtype DT, int V>
-__device__ __forceinline__ void weigh(float (&z)[V], const void* weights, int64_t at, bool f32, float offset, float inv)
-{
-    typedef Elem<DT> E;
-    typedef typename E::T T;
-#pragma unroll
-    for (int e = 0; e < V; ++e) z[e] *= inv;
-    if (!weights) return;
-    if (f32) {
-#pragma unroll
-        for (int e = 0; e < V; e += 4) {
-            const float4 w = *reinterpret_cast<const float4*>((const float*)weights + at + e);
-            z[e] *= offset + w.x;
-            z[e + 1] *= offset + w.y;
-            z[e + 2] *= offset + w.z;
-            z[e + 3] *= offset + w.w;
-        }
-    } else {
-        T raw[V];
-        const uint4 w = *reinterpret_cast<const uint4*>((const T*)weights + at);
-        __builtin_memcpy(raw, &w, 16);
-#pragma unroll
-        for (int e = 0; e < V; ++e) z[e] *= offset + E::get(raw[e]);
-    }
-}
-
-// A head is LANES lanes of a wave (a power of two), 16 bytes each; a workgroup has 256 / LANES heads of one token at a time.  Bound by
-// reading and writing q, K and V once.
+// A head is LANES lanes of a wave (a power of two), 16 bytes each; a workgroup has 256 / LANES heads of one token at a time.  Of an element x
+// with partner y the lane keeps a = m cos t (offset + w) and b = -+ m sin t (offset + w of the partner), the same for all heads where they
+// share weights: a head costs it the sum of squares and x inv a + y inv b.  Bound by reading and writing q, K and V once.
 template <pa_dtype DT, int PAIRS, bool TO4, int LANES>
 __global__ __launch_bounds__(kThreads) void paged_norm_rope_append_kernel(NormRopeArgs a)
 {
     typedef Elem<DT> E;
     typedef typename E::T T;
     constexpr int V = 16 / sizeof(T), HEADS = kThreads / LANES;
-    __shared__ __attribute__((aligned(16))) float sm_c[128], sm_s[128];   // head_dim is at most 256
+    __shared__ __attribute__((aligned(16))) float sm_c[136], sm_s[136];   // pairs (head_dim is at most 256); behind them 1 and 0
     const pa_norm_rope& r = a.r;
+    const float by_d = a.by_d;
     const int32_t d = a.d, half = a.half, u = threadIdx.x % LANES, first = u * V;
     const int64_t t = blockIdx.x;
     const bool live = first < d;
@@ -126,24 +118,44 @@ __global__ __launch_bounds__(kThreads) void paged_norm_rope_append_kernel(NormRo
     const bool turned = first < 2 * half;
     const int32_t partner = PAIRS != kHalves || !turned ? first : first < half ? first + half : first - half;
 
+    const char* const q_weight = (const char*)(r.norm_q ? r.q_weight : nullptr);
+    const char* const k_weight = (const char*)(r.norm_k ? r.k_weight : nullptr);
+    const bool f32 = r.weight_dtype == PA_DTYPE_F32;
+    const T* const q_row = (const T*)r.q + t * r.q_stride;
+    const T* const k_row = (const T*)r.k_new + t * r.k_stride;
+    const T* const v_row = (const T*)r.v_new + t * r.v_stride;
     struct Piece {
         const T* src;            // of the head
         int32_t what, h;         // 0: q, 1: K, 2: V
-        uint4 x, y;
+        uint4 x;
     };
     auto load = [&](int32_t j) {
         Piece p;
         p.what = j < a.q_heads ? 0 : j < a.q_heads + a.kv_heads ? 1 : 2;
-        p.h = j - (p.what == 0 ? 0 : p.what == 1 ? a.q_heads : a.q_heads + a.kv_heads);
-        p.src = (p.what == 0 ? (const T*)r.q + t * r.q_stride : p.what == 1 ? (const T*)r.k_new + t * r.k_stride
-                                                                            : (const T*)r.v_new + t * r.v_stride) + (int64_t)p.h * d;
-        p.x = uint4{0, 0, 0, 0};
-        p.y = p.x;
-        if (live) {
-            p.x = *reinterpret_cast<const uint4*>(p.src + first);
-            if (PAIRS == kHalves && p.what != 2) p.y = *reinterpret_cast<const uint4*>(p.src + partner);
-        }
+        p.h = j - pick(p.what, 0, a.q_heads, a.q_heads + a.kv_heads);
+        p.src = pick(p.what, q_row, k_row, v_row) + (uint32_t)(p.h * d);
+        p.x = *reinterpret_cast<const uint4*>(p.src + (live ? first : 0));
+        if (!live) p.x = uint4{0, 0, 0, 0};
         return p;
+    };
+    // offset + w of the lane's elements
+    auto weights_at = [&](float (&w)[V], const char* weights, int32_t at) {
+        const int32_t i = at + (live ? first : 0);
+        if (DT == PA_DTYPE_F32 || f32) {
+#pragma unroll
+            for (int e = 0; e < V; e += 4) {
+                const float4 x = *reinterpret_cast<const float4*>((const float*)weights + i + e);
+                w[e] = x.x, w[e + 1] = x.y, w[e + 2] = x.z, w[e + 3] = x.w;
+            }
+        } else {
+            T raw[V];
+            const uint4 x = *reinterpret_cast<const uint4*>((const T*)weights + i);
+            __builtin_memcpy(raw, &x, 16);
+#pragma unroll
+            for (int e = 0; e < V; ++e) w[e] = E::get(raw[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) w[e] += r.weight_offset;
     };
     int32_t j = begin + (int32_t)threadIdx.x / LANES;
     Piece p;
@@ -158,6 +170,10 @@ __global__ __launch_bounds__(kThreads) void paged_norm_rope_append_kernel(NormRo
             if (page >= 0 && page < a.num_pages) slot = (int64_t)page * a.page_stride + (TO4 ? 0 : place * a.token_stride);
         }
     }
+    if ((int32_t)threadIdx.x < 136) {
+        sm_c[threadIdx.x] = 1.f;
+        sm_s[threadIdx.x] = 0.f;
+    }
     if ((int32_t)threadIdx.x < half) {
         const int32_t i = threadIdx.x;
         const int32_t axis = r.pair_axes ? min(max(r.pair_axes[i], 0), r.axes - 1) : 0;   // (no read out of range)
@@ -168,8 +184,11 @@ __global__ __launch_bounds__(kThreads) void paged_norm_rope_append_kernel(NormRo
         sm_s[i] = sn * r.mscale;
     }
     __syncthreads();
+    float fa[V], fb[V];
+    int32_t have = -1;           // whose factors these are: q (0), K (1), no one's (-1)
     for (; j < end;) {
-        const bool q = p.what == 0;
+        const int32_t what = p.what, h = p.h;
+        const bool norm = what != 2 && pick(what, r.norm_q, r.norm_k, 0);
         float x[V];
         {
             T raw[V];
@@ -177,17 +196,79 @@ __global__ __launch_bounds__(kThreads) void paged_norm_rope_append_kernel(NormRo
 #pragma unroll
             for (int e = 0; e < V; ++e) x[e] = E::get(raw[e]);
         }
-        if (p.what != 2) {
-            // the norm's factor, and the weights of element i of the head
-            float inv = 1.f;
-            const bool norm = q ? r.norm_q : r.norm_k;
+        if (what != 2 && (norm || half > 0)) {
+            const char* const weights = pick(what, q_weight, k_weight, q_weight);
+            const bool each = weights && pick(what, r.q_weight_heads, r.k_weight_heads, 0);
+            const int from = ((int)threadIdx.x & 63) - u + partner / V;   // the partner's lane
+            if (have != what || each) {
+                float w[V], c[V], s[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) w[e] = 1.f;
+                if (weights) weights_at(w, weights, each ? h * d : 0);
+                if (INTER) {
+                    const int32_t at = live ? first / 2 : 128;
+#pragma unroll
+                    for (int e = 0; e < V; e += 2) {
+                        c[e] = c[e + 1] = sm_c[at + e / 2];
+                        s[e + 1] = sm_s[at + e / 2];
+                        s[e] = -s[e + 1];
+                    }
+                } else if (PAIRS == kHalves) {
+                    const int32_t at = turned ? min(first, partner) : 128;
+                    const float sign = first < half ? -1.f : 1.f;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        c[e] = sm_c[at + e];
+                        s[e] = sm_s[at + e] * sign;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const int32_t i = first + e, at = i < half ? i : i < 2 * half ? i - half : 128;
+                        c[e] = sm_c[at];
+                        s[e] = i < half ? -sm_s[at] : sm_s[at];
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const int32_t i = first + e;
+                    float other = INTER ? w[e ^ 1] : PAIRS == kHalves ? __shfl(w[e], from) : 1.f;
+                    if (PAIRS == kOddHalves && weights && i < 2 * half) {
+                        const int32_t k = (each ? h * d : 0) + (i < half ? i + half : i - half);
+                        other = r.weight_offset + (f32 ? ((const float*)weights)[k] : E::get(((const T*)weights)[k]));
+                    }
+                    fa[e] = c[e] * w[e];
+                    fb[e] = i < 2 * half ? s[e] * other : -0.f;   // (with y = 0: a zero keeps its sign)
+                }
+                have = what;
+            }
+            // partners; 0 where nothing turns
+            float y[V];
+            if (INTER) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) y[e] = first + e < 2 * half ? x[e ^ 1] : 0.f;
+            } else if (PAIRS == kHalves) {
+                T raw[V];
+                const uint4 v = uint4{(uint32_t)__shfl((int)p.x.x, from), (uint32_t)__shfl((int)p.x.y, from),
+                                      (uint32_t)__shfl((int)p.x.z, from), (uint32_t)__shfl((int)p.x.w, from)};
+                __builtin_memcpy(raw, &v, 16);
+#pragma unroll
+                for (int e = 0; e < V; ++e) y[e] = turned ? E::get(raw[e]) : 0.f;
+            } else {
+                // (a wave's lanes have all read before one writes: a head lies within it)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const int32_t i = first + e;
+                    y[e] = i < 2 * half ? E::get(p.src[i < half ? i + half : i - half]) : 0.f;
+                }
+            }
             if (norm) {
                 float sum = 0.f;
 #pragma unroll
-                for (int e = 0; e < V; ++e) sum += x[e] * x[e];
+                for (int e = 0; e < V; ++e) sum = __builtin_fmaf(x[e], x[e], sum);
                 sum = lanes_sum<LANES>(sum);
-                const float mean = sum / (float)d + r.eps;
-                inv = 1.f / __builtin_sqrtf(mean);
+                const float mean = sum * by_d + r.eps;
+                float inv = __builtin_amdgcn_rsqf(mean);     // (a unit in the last place)
                 if (!(sum < 0x1p+120f) || mean < 0x1p-60f) {   // squares that fp32 does not hold
                     double s64 = 0.0;
 #pragma unroll
@@ -196,59 +277,16 @@ __global__ __launch_bounds__(kThreads) void paged_norm_rope_append_kernel(NormRo
                     for (int i = 1; i < LANES; i *= 2) s64 += __shfl_xor(s64, i);
                     inv = (float)(1.0 / sqrt(s64 / d + (double)r.eps));
                 }
-            }
-            const void* const weights = q ? r.q_weight : r.k_weight;
-            const int64_t at = (q ? r.q_weight_heads : r.k_weight_heads) ? (int64_t)p.h * d : 0;
-            const bool f32 = r.weight_dtype == PA_DTYPE_F32;
-            if (live && norm) weigh<DT>(x, weights, at + first, f32, r.weight_offset, inv);
-            if (live && turned) {
-                if (INTER) {
 #pragma unroll
-                    for (int e = 0; e < V; e += 2) {
-                        const int32_t i = (first + e) / 2;
-                        if (i >= half) break;
-                        const float c = sm_c[i], s = sm_s[i], fx = x[e], fy = x[e + 1];
-                        x[e] = fx * c - fy * s;
-                        x[e + 1] = fx * s + fy * c;
-                    }
-                } else if (PAIRS == kHalves) {
-                    float y[V];
-                    T raw[V];
-                    __builtin_memcpy(raw, &p.y, 16);
-#pragma unroll
-                    for (int e = 0; e < V; ++e) y[e] = E::get(raw[e]);
-                    if (norm) weigh<DT>(y, weights, at + partner, f32, r.weight_offset, inv);
-                    const int32_t i = min(first, partner);
-                    const bool lower = first < half;
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const float c = sm_c[i + e], s = sm_s[i + e];
-                        x[e] = x[e] * c + y[e] * (lower ? -s : s);
-                    }
-                } else {
-                    // (a wave's lanes have all read before one writes: a head lies within it)
-                    float y[V];
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const int32_t i = first + e;
-                        y[e] = 0.f;
-                        if (i >= 2 * half) continue;
-                        const int32_t k = i < half ? i + half : i - half;
-                        y[e] = E::get(p.src[k]);
-                        if (norm) y[e] *= inv;
-                        if (norm && weights) y[e] *= r.weight_offset + (f32 ? ((const float*)weights)[at + k] : E::get(((const T*)weights)[at + k]));
-                    }
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const int32_t i = first + e;
-                        if (i >= 2 * half) continue;
-                        const float c = sm_c[i < half ? i : i - half], s = sm_s[i < half ? i : i - half];
-                        x[e] = x[e] * c + y[e] * (i < half ? -s : s);
-                    }
+                for (int e = 0; e < V; ++e) {
+                    x[e] *= inv;
+                    y[e] *= inv;
                 }
             }
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[e] = __builtin_fmaf(y[e], fb[e], x[e] * fa[e]);
         }
-        const int32_t what = p.what, h = p.h;
+        uint4 out = p.x;         // (V as it is)
         j += HEADS;
         if (j < end) p = load(j);
         if (TO4 && what != 0) {
@@ -283,13 +321,9 @@ __global__ __launch_bounds__(kThreads) void paged_norm_rope_append_kernel(NormRo
         }
         T* dst = nullptr;
         if (what == 0) dst = (T*)r.q_out + t * r.q_out_stride + (int64_t)h * d;
-        else if (slot >= 0) dst = (T*)(what == 1 ? a.k_cache : a.v_cache) + slot + h * a.head_stride;
+        else if (slot >= 0) dst = pick(what, (T*)a.k_cache, (T*)a.k_cache, (T*)a.v_cache) + slot + h * a.head_stride;
         if (dst && live) {
-            T raw[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) raw[e] = E::put(x[e]);
-            uint4 out;
-            __builtin_memcpy(&out, raw, 16);
+            if (what != 2) out = E::pack(x);
             *reinterpret_cast<uint4*>(dst + first) = out;
         }
     }
@@ -299,7 +333,9 @@ template <pa_dtype DT, int PAIRS, bool TO4, int LANES>
 void launch_lanes(const NormRopeArgs& a, hipStream_t stream)
 {
     const int32_t heads = a.q_heads + 2 * a.kv_heads, once = kThreads / LANES;
-    const int32_t parts = a.r.T >= 1024 ? 1 : (heads + once - 1) / once;
+    // Few tokens are spread over several workgroups each (us with 512 / 1024 / 2048 in the place of 2048, 32 / 8 heads of 128: 8 tokens 3.8 / 4.1 /
+    // 3.9, 240 4.9 / 4.6 / 4.7; 900 tokens of 32 / 32 heads of 80 10.3 / 10.3 / 9.0, with 4096 9.8).
+    const int32_t parts = min((heads + once - 1) / once, max(1, 2048 / a.r.T));
     hipLaunchKernelGGL((paged_norm_rope_append_kernel<DT, PAIRS, TO4, LANES>), dim3(a.r.T, parts), dim3(kThreads), 0, stream, a);
 }
 
@@ -354,6 +390,7 @@ pa_status launch_norm_rope_append(const pa_kv_cache_desc* cache, const pa_mx4_ca
         a.log2_page = v.log2_page;
         a.num_pages = cache->num_pages;
     }
+    a.by_d = 1.f / (float)a.d;
     ProfileScope prof("paged_norm_rope_append_kernel", stream);
     if (dtype == PA_DTYPE_F32) to4 ? launch_dtype<PA_DTYPE_F32, true>(a, stream) : launch_dtype<PA_DTYPE_F32, false>(a, stream);
     else if (dtype == PA_DTYPE_BF16) to4 ? launch_dtype<PA_DTYPE_BF16, true>(a, stream) : launch_dtype<PA_DTYPE_BF16, false>(a, stream);
