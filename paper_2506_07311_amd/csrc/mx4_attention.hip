@@ -24,21 +24,41 @@ struct Mx4Plan {
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 // `wide`: 16 rows a wave where others take 32 (mx4_attention_impl.h).
-Mx4Plan plan_mx4(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t d, int32_t max_q_len, int32_t max_seq_len, bool f32)
+Mx4Plan plan_mx4(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t d, int32_t max_q_len, int32_t max_seq_len, pa_dtype dtype)
 {
-    const bool wide = d == 256 || f32;
+    const bool f32 = dtype == PA_DTYPE_F32, bf16 = dtype == PA_DTYPE_BF16;
+    const bool wide = d == 256 || f32, whole = d == 256 && !bf16;
     Mx4Plan p = {};
-    const int64_t rows = (int64_t)max_q_len * (num_q_heads / num_kv_heads);
-    p.shape = rows <= 16 ? 0 : rows <= 32 ? 1 : rows <= 64 ? 2 : 3;
-    p.rows = p.shape == 0 ? 16 : p.shape == 1 ? 32 : p.shape == 2 || wide ? 64 : 128;
-    p.tile = p.shape == 0 || (p.shape == 1 && !wide) ? 128 : 64;
+    const int64_t rows = (int64_t)max_q_len * (num_q_heads / num_kv_heads), keys = max_seq_len;
+    const int64_t cus = device_cus(), heads = (int64_t)batch * num_kv_heads;
+    bool cut;
+    if (rows <= 16) {
+        // A row block (a "unit" with its KV head) is one workgroup's where units fill the machine, or contexts are short; otherwise the keys are
+        // shared and merged.  us, 32 / 8 heads of 128, eight waves whole / cut, four waves whole / cut:
+        //     8 x 500..1000 9.6 / 13.3 10.2 / 13.3       8 x 128..2048 13.9 / 13.1 15.5 / 12.2      32 x 2000..4000 24.2 / 28.7 26.6 / 26.7
+        //     64 x 500..1000 19.3 / 19.3 15.0 / 22.4     64 x 2000..4000 42.1 / 45.2 38.1 / 42.8    100 x 300..3000 42.4 / 41.3 39.0 / 36.2
+        //     200 x 500..600 49.2 / 49.2 33.9 / 43.1     400 x 100..2000 110 / 104 76.0 / 81.1      64 x 64..32768 - / 78.1 - / 83.3
+        //     1 x 4000 - / 13.7 - / 12.7                 1 x 100000 - / 28.0 - / 28.5               16 x 131072, 64 heads - / 396 - / 402
+        if (heads <= cus) {
+            p.shape = keys > 128 ? 4 : 0;
+            cut = keys > (4 * heads >= 3 * cus ? 4096 : 1536);
+        } else {
+            p.shape = 0;
+            cut = keys > 4096 * (heads / (2 * cus) > 1 ? heads / (2 * cus) : 1);
+        }
+        if (cut) p.shape = heads * keys >= cus * 2048 ? 4 : 0;
+    } else {
+        p.shape = rows <= 32 ? 1 : rows <= 64 ? 2 : 3;
+        cut = keys > 512;
+    }
+    p.rows = p.shape == 0 || p.shape == 4 ? 16 : p.shape == 1 ? 32 : p.shape == 2 || wide ? 64 : 128;
+    p.tile = p.shape == 4 && !whole ? 256 : p.shape == 0 || p.shape == 4 || (p.shape == 1 && !wide) ? 128 : 64;
     const int64_t blocks = (rows + p.rows - 1) / p.rows;
     p.row_blocks = blocks < 1 ? 1 : (int32_t)blocks;
-    const int64_t slots = (int64_t)device_cus() * 2;
-    const int64_t units = (int64_t)batch * num_kv_heads * p.row_blocks;
+    const int64_t slots = cus * (p.shape == 4 || whole ? 1 : 2);
+    if (p.shape == 3 && heads * p.row_blocks >= slots) cut = false;
     const int64_t tiles = ((int64_t)max_seq_len + p.tile - 1) / p.tile;
-    // Row blocks are cut where they are long, and few or of different lengths.
-    if (tiles > 4 && (p.shape != 3 || units < slots)) {
+    if (cut) {
         const int64_t most = ((int64_t)batch * p.row_blocks * tiles + kTreeMinTiles - 1) / kTreeMinTiles;
         int64_t wgs = slots / num_kv_heads;
         if (wgs > most) wgs = most;
@@ -57,8 +77,8 @@ size_t mx4_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_he
                            int32_t max_seq_len)
 {
     size_t most = 256;                                       // (the type is not known here)
-    for (const bool f32 : {false, true}) {
-        const Mx4Plan p = plan_mx4(batch, num_q_heads, num_kv_heads, head_dim, max_q_len, max_seq_len, f32);
+    for (const pa_dtype dtype : {PA_DTYPE_F32, PA_DTYPE_BF16, PA_DTYPE_F16}) {
+        const Mx4Plan p = plan_mx4(batch, num_q_heads, num_kv_heads, head_dim, max_q_len, max_seq_len, dtype);
         const size_t bytes = p.part_o_bytes + p.part_lse_bytes + p.cuts_bytes;
         if (bytes > most) most = bytes;
     }
@@ -68,11 +88,11 @@ size_t mx4_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_he
 pa_status launch_attention_mx4(const Mx4Args& t, void* workspace, hipStream_t stream)
 {
     const pa_mx4_cache_desc* const c = t.cache;
-    const Mx4Plan p = plan_mx4(t.batch, t.num_q_heads, c->num_kv_heads, c->head_dim, t.max_q_len, t.max_seq_len, t.dtype == PA_DTYPE_F32);
+    const Mx4Plan p = plan_mx4(t.batch, t.num_q_heads, c->num_kv_heads, c->head_dim, t.max_q_len, t.max_seq_len, t.dtype);
     // Places of a KV head stay below 2^31, threads of a launch below 2^32.
     const int64_t units = (int64_t)t.batch * p.row_blocks, threads = (int64_t)1 << 32;
     const int64_t tiles = ((int64_t)t.max_seq_len + p.tile - 1) / p.tile;
-    if ((p.wgs > 0 ? p.wgs : units) * c->num_kv_heads * 256 >= threads) return PA_ERR_UNSUPPORTED;
+    if ((p.wgs > 0 ? p.wgs : units) * c->num_kv_heads * 512 >= threads) return PA_ERR_UNSUPPORTED;
     if (p.wgs > 0 && (tiles + kTreePieceTiles > 0x7fffffff / units || units * p.rows * c->head_dim / 4 >= threads)) return PA_ERR_UNSUPPORTED;
     const Mx4View v = make_view(c);
     TreeKernelArgs a = {};

@@ -27,8 +27,8 @@ namespace pa {
 namespace {
 
 // RT tiles of 16 rows a wave; RW waves beside each other in rows, KW along the keys; OCC workgroups on a compute unit; keys in flight: DEEP
-// steps of 32.
-template <pa_dtype DT, int D, int RT, int RW, int KW, int OCC, int DEEP>
+// steps of 32.  SHARED: four waves of rows, of which each makes operands of a quarter of a tile's codes, in LDS, for all of them.
+template <pa_dtype DT, int D, int RT, int RW, int KW, int OCC, int DEEP, bool SHARED = false>
 struct Mx4Shape {
     static constexpr int kRows = 16 * RT * RW, kWaveRows = 16, kColumns = D;
     static constexpr int kWaves = RW * KW, kOcc = OCC, kTile = KW == 1 ? 64 : 32 * KW, kLeastTiles = 1;
@@ -37,7 +37,9 @@ struct Mx4Shape {
     static constexpr int kPT = DT == PA_DTYPE_F32 ? 3 : 2;                             // terms of a weight
     static constexpr int kLanes = D / 64;                    // float4s of a lane and row quarter
     static constexpr int kJoin = KW > 1 ? RW * KW * RT * D * 16 * 4 : 0;               // bytes in which the waves' results meet
-    static constexpr int kLds = kJoin + kWaves * RT * 16 * 8 + 1024;
+    static constexpr int kTileB = 2 * 64 * D * 2;            // bytes of a tile's operands
+    static constexpr int kLds = SHARED ? 2 * kTileB : kJoin + kWaves * RT * 16 * 8 + 1024;
+    static_assert(!SHARED || (KW == 1 && RW == 4 && D <= 128), "a quarter is 16 keys of K, 32 keys and half of the columns of V");
     static constexpr int kSteps = D / 32, kTiles = D / 16;
     static constexpr int kKDwords = D / 32, kVDwords = D / 16;                         // of a lane: per key, and for its 8 keys
     static constexpr int kKScales = D > 128 ? 2 : 1;
@@ -116,10 +118,56 @@ struct Mx4Shape {
         }
     }
 
+    // Weights of 32 keys from their raw scores (-inf: not seen), as operands; sc > 0.
+    template <bool CAREFUL>
+    static __device__ __forceinline__ void weights(uint4 (&w)[RT][kPT], const mfma_f32x4 (&s)[RT][2], mfma_f32x4 (&o)[RT][kTiles], float (&m)[RT],
+                                                   float (&l)[RT], float sc)
+    {
+        constexpr float kBelow = CAREFUL ? kCarefulBelow : 0.f, kSumMax = CAREFUL ? 0.5f * kCarefulSumMax : kWeightSumMax;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float p[8], psum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][i / 4][i % 4], sc, -m[rt]));
+                psum += p[i];
+            }
+            if (__any(!(psum <= kSumMax))) {         // also the NaN or infinity of a fresh reference
+                float top = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, s[rt][i / 4][i % 4]);
+                const float m_new = fmaxf(m[rt], row_max<4>(top) * sc - kBelow);
+                const float use = m_new == -INFINITY ? 0.f : m_new;   // (no key so far)
+                const float alpha = __builtin_amdgcn_exp2f(m[rt] - use);
+#pragma unroll
+                for (int j = 0; j < kTiles; ++j) o[rt][j] *= alpha;
+                l[rt] *= alpha;
+                m[rt] = m_new;
+                psum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][i / 4][i % 4], sc, -use));
+                    psum += p[i];
+                }
+            }
+            l[rt] += psum;
+#pragma unroll
+            for (int u = 0; u < kPT; ++u) {
+                w[rt][u] = uint4{ElemBf16::pack(p[0], p[1]), ElemBf16::pack(p[2], p[3]), ElemBf16::pack(p[4], p[5]),
+                                 ElemBf16::pack(p[6], p[7])};
+                if (u + 1 < kPT) {
+                    p[0] -= ElemBf16::lo_of(w[rt][u].x), p[1] -= ElemBf16::hi_of(w[rt][u].x);
+                    p[2] -= ElemBf16::lo_of(w[rt][u].y), p[3] -= ElemBf16::hi_of(w[rt][u].y);
+                    p[4] -= ElemBf16::lo_of(w[rt][u].z), p[5] -= ElemBf16::hi_of(w[rt][u].z);
+                    p[6] -= ElemBf16::lo_of(w[rt][u].w), p[7] -= ElemBf16::hi_of(w[rt][u].w);
+                }
+            }
+        }
+    }
+
     template <bool CAREFUL>
     static __device__ __forceinline__ bool work(char* buf, uint32_t* flags, const TreeKernelArgs& a, const TreeItem& item, int32_t kvh)
     {
-        constexpr float kBelow = CAREFUL ? kCarefulBelow : 0.f, kSumMax = CAREFUL ? 0.5f * kCarefulSumMax : kWeightSumMax;
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
         const int kw = wave % KW, rw = wave / KW, row16 = lane & 15, g = lane >> 4;
         const int32_t n_rows = item.n * a.group, lp = a.cache.log2_page, P = 1 << lp;
@@ -169,7 +217,13 @@ struct Mx4Shape {
 #pragma unroll
             for (int j = 0; j < kTiles; ++j) o[rt][j] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        if (steps > 0) {
+        if constexpr (SHARED && !CAREFUL) {
+            // (all waves walk to the end of the workgroup's rows)
+            const int32_t far_row = min(rb * kRows + kRows, n_rows) - 1;
+            const int32_t wg_most = min(max(item.len - item.n + far_row / a.group + 1, 0), item.len);
+            const int32_t tile_end = min(item.tile_end, (wg_most + 63) / 64), tiles = tile_end - item.tile_begin;
+            if (tiles > 0) shared(buf, a, item, kvh, tiles, most, least, sees, q, o, m, l, sc);
+        } else if (steps > 0) {
             const int32_t* const table = a.block_table + (int64_t)item.s * a.max_blocks;
             const char* const base = (const char*)a.cache.k + (int64_t)kvh * a.cache.head_stride;
             const int32_t last_block = (item.len - 1) >> lp;
@@ -180,11 +234,21 @@ struct Mx4Shape {
             const int32_t v_at = ((D / 2) << lp) + vslot * (D / 2) + row16 * (D / 4);
             const int32_t ks_at = ((D + g * (D / 4) / 32) << lp) + kslot;
             const int32_t vs_at = ((D + D / 32 + row16 * (D / 16) / 32) << lp) + vslot;
-            auto load = [&](Keys& x, int32_t step) {
-                const int32_t key0 = 32 * step;
-                const int32_t b0 = key0 >> lp, b1 = min((key0 + 16) >> lp, last_block);
-                const char* const first = base + (int64_t)table[b0] * a.cache.page_stride;
-                const char* const second = base + (int64_t)table[b1] * a.cache.page_stride;
+            // pages of 32 steps at a time, lane 2 n + h those of keys 16 h .. of the wave's n-th step, and of the next 32 (read step by step
+            // they are a trip to memory in front of each: S0T)
+            auto pages_of = [&](int32_t n) {
+                const int32_t key = 32 * (step0 + KW * min(n + (lane >> 1), steps - 1)) + 16 * (lane & 1);
+                return table[min(key >> lp, last_block)];
+            };
+            int32_t pages = pages_of(0), more = pages_of(32);
+            auto load = [&](Keys& x, int32_t n) {
+                if (n > 0 && (n & 31) == 0) {
+                    pages = more;
+                    more = pages_of(n + 32);
+                }
+                const int32_t key0 = 32 * (step0 + KW * n);
+                const char* const first = base + (int64_t)__builtin_amdgcn_readlane(pages, 2 * (n & 31)) * a.cache.page_stride;
+                const char* const second = base + (int64_t)__builtin_amdgcn_readlane(pages, 2 * (n & 31) + 1) * a.cache.page_stride;
                 const int32_t slot = key0 & (P - 1);
                 const char* const kp = (ko >= 2 ? second : first) + slot * (D / 2) + k_at;
                 const char* const vp = (vo >= 2 ? second : first) + slot * (D / 2) + v_at;
@@ -219,20 +283,23 @@ struct Mx4Shape {
                 for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) s[rt][i] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
+                float unit[2][kKScales];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float unit[kKScales];
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int j = 0; j < kKScales; ++j)
-                        unit[j] = __uint_as_float((((i ? x.ks[j].y : x.ks[j].x) >> (8 * (row16 & 3))) & 0xffu) << 23);
+                        unit[i][j] = __uint_as_float((((i ? x.ks[j].y : x.ks[j].x) >> (8 * (row16 & 3))) & 0xffu) << 23);
 #pragma unroll
-                    for (int t = 0; t < kSteps; ++t) {
-                        const uint4 k = bf16_eight(x.k[i][t], unit[kKScales == 2 ? t / 4 : 0]);
+                for (int t = 0; t < kSteps; ++t) {
+                    const uint4 k0 = bf16_eight(x.k[0][t], unit[0][kKScales == 2 ? t / 4 : 0]);
+                    const uint4 k1 = bf16_eight(x.k[1][t], unit[1][kKScales == 2 ? t / 4 : 0]);
 #pragma unroll
-                        for (int rt = 0; rt < RT; ++rt)
+                    for (int u = 0; u < kQT; ++u)
 #pragma unroll
-                            for (int u = 0; u < kQT; ++u) s[rt][i] = ElemBf16::mfma16(k, q[rt][kQT - 1 - u][t], s[rt][i]);
-                    }
+                        for (int rt = 0; rt < RT; ++rt) {
+                            s[rt][0] = ElemBf16::mfma16(k0, q[rt][kQT - 1 - u][t], s[rt][0]);
+                            s[rt][1] = ElemBf16::mfma16(k1, q[rt][kQT - 1 - u][t], s[rt][1]);
+                        }
                 }
                 const bool masked = key0 + 32 > least;       // (the same for the whole wave)
                 if (masked) {
@@ -249,47 +316,8 @@ struct Mx4Shape {
                         x.vs.y &= (uint32_t)(keep >> 32);
                     }
                 }
-                // weights
                 uint4 w[RT][kPT];
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    float p[8], psum = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][i / 4][i % 4], sc, -m[rt]));
-                        psum += p[i];
-                    }
-                    if (__any(!(psum <= kSumMax))) {         // also the NaN or infinity of a fresh reference
-                        float top = -INFINITY;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) top = fmaxf(top, s[rt][i / 4][i % 4]);
-                        const float m_new = fmaxf(m[rt], row_max<4>(top) * sc - kBelow);
-                        const float use = m_new == -INFINITY ? 0.f : m_new;   // (no key so far)
-                        const float alpha = __builtin_amdgcn_exp2f(m[rt] - use);
-#pragma unroll
-                        for (int j = 0; j < kTiles; ++j) o[rt][j] *= alpha;
-                        l[rt] *= alpha;
-                        m[rt] = m_new;
-                        psum = 0.f;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][i / 4][i % 4], sc, -use));
-                            psum += p[i];
-                        }
-                    }
-                    l[rt] += psum;
-#pragma unroll
-                    for (int u = 0; u < kPT; ++u) {
-                        w[rt][u] = uint4{ElemBf16::pack(p[0], p[1]), ElemBf16::pack(p[2], p[3]), ElemBf16::pack(p[4], p[5]),
-                                         ElemBf16::pack(p[6], p[7])};
-                        if (u + 1 < kPT) {
-                            p[0] -= ElemBf16::lo_of(w[rt][u].x), p[1] -= ElemBf16::hi_of(w[rt][u].x);
-                            p[2] -= ElemBf16::lo_of(w[rt][u].y), p[3] -= ElemBf16::hi_of(w[rt][u].y);
-                            p[4] -= ElemBf16::lo_of(w[rt][u].z), p[5] -= ElemBf16::hi_of(w[rt][u].z);
-                            p[6] -= ElemBf16::lo_of(w[rt][u].w), p[7] -= ElemBf16::hi_of(w[rt][u].w);
-                        }
-                    }
-                }
+                weights<CAREFUL>(w, s, o, m, l, sc);
                 if (CAREFUL) {
                     // blocks of NaN count for 0 in the product; rows that see one get NaN in its columns by a product of ones
                     uint4 ones = uint4{0, 0, 0, 0};
@@ -329,19 +357,19 @@ struct Mx4Shape {
             };
             Keys ring[DEEP];
 #pragma unroll
-            for (int i = 0; i < DEEP; ++i) load(ring[i], step0 + KW * min(i, steps - 1));
+            for (int i = 0; i < DEEP; ++i) load(ring[i], min(i, steps - 1));
             int32_t n = 0;
             for (; n + 2 * DEEP <= steps; n += DEEP) {
 #pragma unroll
                 for (int i = 0; i < DEEP; ++i) {
                     compute(ring[i], step0 + KW * (n + i));
-                    load(ring[i], step0 + KW * (n + i + DEEP));
+                    load(ring[i], n + i + DEEP);
                 }
             }
 #pragma unroll
             for (int i = 0; i < DEEP; ++i) {                 // (fewer than 2 DEEP are left)
                 if (n + i < steps) compute(ring[i], step0 + KW * (n + i));
-                if (n + i + DEEP < steps) load(ring[i], step0 + KW * (n + i + DEEP));
+                if (n + i + DEEP < steps) load(ring[i], n + i + DEEP);
             }
 #pragma unroll
             for (int i = 0; i < DEEP; ++i)
@@ -389,7 +417,8 @@ struct Mx4Shape {
             for (int i = 0; i < kWaves; ++i) again |= flags[i] != 0;
         }
         if (!again) {
-            // each of a row tile's KW waves leaves 4 / KW of the lane's column groups: columns (4 g + i) D / 16 + ..
+            // a row tile's KW waves share its columns: unit i kLanes + c is columns (4 g + i) D / 16 + 4 c .. + 3 of each row
+            constexpr int kUnits = 4 * kLanes;
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 float top = m[rt], sum = l[rt], weight[KW];
@@ -407,30 +436,31 @@ struct Mx4Shape {
                     }
                 }
                 const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+                auto leave = [&](int i, int c, float4 x) {
+                    x = float4{x.x * inv, x.y * inv, x.z * inv, x.w * inv};
+                    const int32_t col = (4 * g + i) * (D / 16) + 4 * c;
+                    if (item.slot < 0) {
+                        if (out_row[rt] >= 0) store(a.out, out_row[rt] * D + col, x);
+                    } else {
+                        float4* const part = reinterpret_cast<float4*>(a.part_o) + (item.slot * (kRows / 16) + rw * RT + rt) * (4 * D);
+                        part[col / 4 * 16 + row16] = x;
+                    }
+                };
+                if constexpr (KW == 1) {
 #pragma unroll
-                for (int i4 = 0; i4 < 4 / KW; ++i4) {
-                    const int i = KW > 1 ? kw * (4 / KW) + i4 : i4;
-                    const int32_t col = (4 * g + i) * (D / 16);
+                    for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int c = 0; c < kLanes; ++c) {
-                        float4 x;
-                        if (KW > 1) {
-                            x = float4{0.f, 0.f, 0.f, 0.f};
+                        for (int c = 0; c < kLanes; ++c)
+                            leave(i, c, float4{o[rt][4 * c][i], o[rt][4 * c + 1][i], o[rt][4 * c + 2][i], o[rt][4 * c + 3][i]});
+                } else {
+                    for (int unit = kw; unit < kUnits; unit += KW) {
+                        float4 x = float4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                            for (int k = 0; k < KW; ++k) {
-                                const float4 y = meet[((((rw * RT + rt) * KW + k) * 4 + i) * kLanes + c) * 64 + lane];
-                                x = float4{x.x + weight[k] * y.x, x.y + weight[k] * y.y, x.z + weight[k] * y.z, x.w + weight[k] * y.w};
-                            }
-                        } else {
-                            x = float4{o[rt][4 * c][i4], o[rt][4 * c + 1][i4], o[rt][4 * c + 2][i4], o[rt][4 * c + 3][i4]};
+                        for (int k = 0; k < KW; ++k) {
+                            const float4 y = meet[(((rw * RT + rt) * KW + k) * kUnits + unit) * 64 + lane];
+                            x = float4{x.x + weight[k] * y.x, x.y + weight[k] * y.y, x.z + weight[k] * y.z, x.w + weight[k] * y.w};
                         }
-                        x = float4{x.x * inv, x.y * inv, x.z * inv, x.w * inv};
-                        if (item.slot < 0) {
-                            if (out_row[rt] >= 0) store(a.out, out_row[rt] * D + col + 4 * c, x);
-                        } else {
-                            float4* const part = reinterpret_cast<float4*>(a.part_o) + (item.slot * (kRows / 16) + rw * RT + rt) * (4 * D);
-                            part[(col / 4 + c) * 16 + row16] = x;
-                        }
+                        leave(unit / kLanes, unit % kLanes, x);
                     }
                 }
                 if (g == 0 && kw == 0) {
@@ -444,21 +474,158 @@ struct Mx4Shape {
         return again;
     }
 
+    // The walk of SHARED: operands of a tile of 64 keys are made while the tile before is computed, from codes that were asked for a tile
+    // earlier.
+    static __device__ __forceinline__ void shared(char* buf, const TreeKernelArgs& a, const TreeItem& item, int32_t kvh, int32_t tiles, int32_t most,
+                                                  int32_t least, const int32_t (&sees)[RT], const uint4 (&q)[RT][kQT][kSteps],
+                                                  mfma_f32x4 (&o)[RT][kTiles], float (&m)[RT], float (&l)[RT], float sc)
+    {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        const int row16 = lane & 15, g = lane >> 4, half = wave & 1, sub = wave >> 1;
+        const int32_t lp = a.cache.log2_page, P = 1 << lp;
+        const int32_t* const table = a.block_table + (int64_t)item.s * a.max_blocks;
+        const char* const base = (const char*)a.cache.k + (int64_t)kvh * a.cache.head_stride;
+        const int32_t last_block = (item.len - 1) >> lp;
+        const int ko = row16 >> 2, vo = g;
+        const int32_t kslot = (8 * ko) & (P - 1), vslot = (8 * vo) & (P - 1);
+        const int32_t k_at = (kslot + (row16 & 3) + 4 * half) * (D / 2) + g * (D / 8);
+        const int32_t v_at = ((D / 2) << lp) + vslot * (D / 2) + row16 * (D / 4);
+        const int32_t ks_at = ((D + g * (D / 4) / 32) << lp) + kslot;
+        const int32_t vs_at = ((D + D / 32 + row16 * (D / 16) / 32) << lp) + vslot;
+        uint32_t k[kKDwords], v[kVDwords];
+        uint2 ks, vs;
+        auto load = [&](int32_t tile) {
+            const int32_t key0 = 64 * (item.tile_begin + tile) + 32 * sub;
+            const int32_t b0 = min(key0 >> lp, last_block), b1 = min((key0 + 16) >> lp, last_block);
+            const char* const first = base + (int64_t)table[b0] * a.cache.page_stride;
+            const char* const second = base + (int64_t)table[b1] * a.cache.page_stride;
+            const int32_t slot = key0 & (P - 1);
+            const char* const kp = (ko >= 2 ? second : first) + slot * (D / 2) + k_at;
+            const char* const vp = (vo >= 2 ? second : first) + slot * (D / 2) + v_at;
+            if constexpr (D == 64) {
+                const uint2 w = *reinterpret_cast<const uint2*>(kp);
+                k[0] = w.x, k[1] = w.y;
+            } else {
+                const uint4 w = *reinterpret_cast<const uint4*>(kp);
+                k[0] = w.x, k[1] = w.y, k[2] = w.z, k[3] = w.w;
+            }
+            ks = *reinterpret_cast<const uint2*>((ko >= 2 ? second : first) + slot + ks_at);
+#pragma unroll
+            for (int j = 0; j < kVDwords; j += 4) {
+                const uint4 w = *reinterpret_cast<const uint4*>(vp + 4 * j);
+                v[j] = w.x, v[j + 1] = w.y, v[j + 2] = w.z, v[j + 3] = w.w;
+            }
+            vs = *reinterpret_cast<const uint2*>((vo >= 2 ? second : first) + slot + vs_at);
+        };
+        // [16 keys][step][lane] of K, then [32 keys][column tile][lane] of V
+        auto make = [&](int32_t tile, uint4* to) {
+            const float unit = __uint_as_float((((half ? ks.y : ks.x) >> (8 * (row16 & 3))) & 0xffu) << 23);
+#pragma unroll
+            for (int t = 0; t < kSteps; ++t) to[(wave * kSteps + t) * 64 + lane] = bf16_eight(k[t], unit);
+            // slots behind the sequence may hold anything, NaN among it
+            const int32_t left = item.len - 64 * (item.tile_begin + tile) - 32 * sub - 8 * g;
+            if (left < 8) {
+                const uint64_t keep = left <= 0 ? 0 : ~0ull >> (64 - 8 * left);
+                vs.x &= (uint32_t)keep;
+                vs.y &= (uint32_t)(keep >> 32);
+            }
+            float vu[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) vu[i] = __uint_as_float(scale_bits(vs, i));
+            uint32_t mine[kVDwords];                         // the wave's half of the columns in front
+#pragma unroll
+            for (int j = 0; j < kVDwords; ++j) mine[j] = v[j] >> (half * (D / 8));
+            uint4* const vt = to + 4 * kSteps * 64 + (sub * kTiles + half * (kTiles / 2)) * 64 + lane;
+            halves<0>(vt, mine, vu);
+        };
+        load(0);
+        make(0, reinterpret_cast<uint4*>(buf));
+        if (tiles > 1) load(1);
+        __syncthreads();
+        for (int32_t i = 0; i < tiles; ++i) {
+            if (i + 1 < tiles) make(i + 1, reinterpret_cast<uint4*>(buf + ((i + 1) & 1) * kTileB));
+            if (i + 2 < tiles) load(i + 2);
+            const uint4* const from = reinterpret_cast<const uint4*>(buf + (i & 1) * kTileB);
+#pragma unroll 1
+            for (int u = 0; u < 2; ++u) {
+                const int32_t key0 = 64 * (item.tile_begin + i) + 32 * u;
+                if (key0 >= most) break;
+                mfma_f32x4 s[RT][2];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) s[rt][h] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int t = 0; t < kSteps; ++t) {
+                    const uint4 k0 = from[(2 * u * kSteps + t) * 64 + lane], k1 = from[((2 * u + 1) * kSteps + t) * 64 + lane];
+#pragma unroll
+                    for (int z = 0; z < kQT; ++z)
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) {
+                            s[rt][0] = ElemBf16::mfma16(k0, q[rt][kQT - 1 - z][t], s[rt][0]);
+                            s[rt][1] = ElemBf16::mfma16(k1, q[rt][kQT - 1 - z][t], s[rt][1]);
+                        }
+                }
+                if (key0 + 32 > least) {
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (key0 + 8 * g + e >= sees[rt]) s[rt][e / 4][e % 4] = -INFINITY;
+                }
+                uint4 w[RT][kPT];
+                weights<false>(w, s, o, m, l, sc);
+                const uint4* const vt = from + 4 * kSteps * 64 + u * kTiles * 64 + lane;
+#pragma unroll
+                for (int j = 0; j < kTiles; j += 2) {
+                    const uint4 v0 = vt[j * 64], v1 = vt[(j + 1) * 64];
+#pragma unroll
+                    for (int z = 0; z < kPT; ++z)
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) {
+                            o[rt][j] = ElemBf16::mfma16(v0, w[rt][kPT - 1 - z], o[rt][j]);
+                            o[rt][j + 1] = ElemBf16::mfma16(v1, w[rt][kPT - 1 - z], o[rt][j + 1]);
+                        }
+                }
+            }
+            __syncthreads();
+        }
+    }
+
     template <int B>
-    static __device__ __forceinline__ void columns(const Keys& x, const float (&vu)[8], const uint4 (&w)[RT][kPT], mfma_f32x4 (&o)[RT][kTiles])
+    static __device__ __forceinline__ void halves(uint4* to, const uint32_t (&v)[kVDwords], const float (&vu)[8])
+    {
+        uint4 even, odd;
+        column_pair<B>(even, odd, v, vu);
+        to[2 * B * 64] = even;
+        to[(2 * B + 1) * 64] = odd;
+        if constexpr (B + 1 < D / 64) halves<B + 1>(to, v, vu);
+    }
+
+    // Operands of a lane's columns 2 B and 2 B + 1.
+    template <int B>
+    static __device__ __forceinline__ void column_pair(uint4& ve, uint4& vd, const uint32_t (&v)[kVDwords], const float (&vu)[8])
     {
         uint32_t even[4], odd[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const uint32_t y0 = v_pair<B>(x.v, 2 * k, vu[2 * k]), y1 = v_pair<B>(x.v, 2 * k + 1, vu[2 * k + 1]);
+            const uint32_t y0 = v_pair<B>(v, 2 * k, vu[2 * k]), y1 = v_pair<B>(v, 2 * k + 1, vu[2 * k + 1]);
             even[k] = __builtin_amdgcn_perm(y1, y0, 0x05040100u);
             odd[k] = __builtin_amdgcn_perm(y1, y0, 0x07060302u);
         }
-        const uint4 ve = uint4{even[0], even[1], even[2], even[3]}, vd = uint4{odd[0], odd[1], odd[2], odd[3]};
+        ve = uint4{even[0], even[1], even[2], even[3]};
+        vd = uint4{odd[0], odd[1], odd[2], odd[3]};
+    }
+
+    template <int B>
+    static __device__ __forceinline__ void columns(const Keys& x, const float (&vu)[8], const uint4 (&w)[RT][kPT], mfma_f32x4 (&o)[RT][kTiles])
+    {
+        uint4 ve, vd;
+        column_pair<B>(ve, vd, x.v, vu);
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
+        for (int u = 0; u < kPT; ++u)                        // (products that wait for each other lie apart)
 #pragma unroll
-            for (int u = 0; u < kPT; ++u) {
+            for (int rt = 0; rt < RT; ++rt) {
                 o[rt][2 * B] = ElemBf16::mfma16(ve, w[rt][kPT - 1 - u], o[rt][2 * B]);
                 o[rt][2 * B + 1] = ElemBf16::mfma16(vd, w[rt][kPT - 1 - u], o[rt][2 * B + 1]);
             }
@@ -474,17 +641,21 @@ struct Mx4Shape {
     }
 };
 
-// Workgroups of 16 and 32 rows have four waves along the keys, of 64 two, of more (shape 3) a wave a row tile.
+// Up to 16 rows: shape 0 has four waves along the keys, shape 4 eight.  Up to 32: shape 1, four; up to 64: shape 2, two; beyond: shape 3, a wave a
+// row tile.
 template <pa_dtype DT, int D>
 pa_status launch_mx4_shape(const TreeKernelArgs& a, bool merge, int shape, hipStream_t stream)
 {
     constexpr bool kWide = D == 256 || DT == PA_DTYPE_F32;   // O and Q of 32 rows do not fit a wave's registers
+    constexpr bool kWhole = D == 256 && DT != PA_DTYPE_BF16; // nor those of 16 rows half of a SIMD's
+    constexpr int OCC = kWhole ? 1 : 2, DEEP = 2, DEEP1 = DT == PA_DTYPE_F16 && D < 256 ? 1 : DEEP;
     switch (shape) {
-        case 0: return launch_tree_of<Mx4Shape<DT, D, 1, 1, 4, 2, 2>>(a, merge, stream);
-        case 1: return launch_tree_of<Mx4Shape<DT, D, kWide ? 1 : 2, kWide ? 2 : 1, kWide ? 2 : 4, 2, 2>>(a, merge, stream);
-        case 2: return launch_tree_of<Mx4Shape<DT, D, kWide ? 1 : 2, kWide ? 4 : 2, kWide ? 1 : 2, 2, 2>>(a, merge, stream);
+        case 0: return launch_tree_of<Mx4Shape<DT, D, 1, 1, 4, OCC, DEEP>>(a, merge, stream);
+        case 4: return launch_tree_of<Mx4Shape<DT, D, 1, 1, kWhole ? 4 : 8, 1, DEEP>>(a, merge, stream);
+        case 1: return launch_tree_of<Mx4Shape<DT, D, kWide ? 1 : 2, kWide ? 2 : 1, kWide ? 2 : 4, OCC, DEEP1>>(a, merge, stream);
+        case 2: return launch_tree_of<Mx4Shape<DT, D, kWide ? 1 : 2, kWide ? 4 : 2, kWide ? 1 : 2, OCC, DEEP1>>(a, merge, stream);
     }
-    return launch_tree_of<Mx4Shape<DT, D, kWide ? 1 : 2, 4, 1, 2, 2>>(a, merge, stream);
+    return launch_tree_of<Mx4Shape<DT, D, kWide ? 1 : 2, 4, 1, OCC, DEEP, (D < 256)>>(a, merge, stream);
 }
 
 template <int D>
