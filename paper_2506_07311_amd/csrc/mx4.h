@@ -41,16 +41,22 @@ __device__ __forceinline__ uint32_t mx4_scale_of(uint32_t top)
     return top >= 0x7f800000u ? 255u : (uint32_t)max(e, 0);
 }
 
-// Code of x under a scale byte other than 255.  |x| / scale is below 8 and exact; from 1 on its exponent and leading mantissa bit are the
-// code, rounded to nearest even in place, below 1 it is a multiple of 1/2.
-__device__ __forceinline__ uint32_t mx4_code(float x, uint32_t scale)
+// Codes of eight elements under a scale byte other than 255: the hardware's conversion divides by the power of two, rounds to nearest even
+// and ends at 6, as defined.
+__device__ __forceinline__ uint32_t mx4_codes(const float (&x)[8], uint32_t scale)
 {
-    const uint32_t sign = (__float_as_uint(x) >> 31) << 3;
-    const float y = fabsf(x) * __uint_as_float((254u - scale) << 23);
-    uint32_t b = __float_as_uint(y);
-    b = ((b + 0x1fffffu + ((b >> 22) & 1u)) >> 22) - (127u << 1) + 2u;
-    const uint32_t small = (uint32_t)__builtin_rintf(y * 2.f);
-    return sign | (y < 1.f ? small : min(b, 7u));
+    const float unit = __uint_as_float(scale << 23);         // (its exponent alone is read: 0 is 2^-127)
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0], x[1], unit, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], unit, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], unit, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], unit, 3);
+}
+__device__ __forceinline__ uint32_t mx4_codes(const float (&x)[4], uint32_t scale)
+{
+    const float unit = __uint_as_float(scale << 23);
+    const uint32_t c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0, x[0], x[1], unit, 0);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], unit, 1);
 }
 
 #endif

@@ -294,10 +294,7 @@ __global__ __launch_bounds__(kThreads) void paged_norm_rope_append_kernel(NormRo
 #pragma unroll
             for (int e = 0; e < V; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
             const uint32_t scale = mx4_scale_of(lanes_max<32 / V>(top));
-            uint32_t codes = 0;
-#pragma unroll
-            for (int e = 0; e < V; ++e) codes |= mx4_code(x[e], scale) << 4 * e;
-            if (scale == 255) codes = 0;
+            const uint32_t codes = scale == 255 ? 0u : mx4_codes(x, scale);
             if (slot < 0 || !live) continue;
             char* const rec = (char*)a.k_cache + slot + h * a.head_stride;
             const int32_t lp = a.log2_page;
