@@ -9,7 +9,7 @@ namespace pa {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 
 // Who a pair's elements are: neighbours; halves, a lane's 16 bytes with another lane's; halves of a turned part that does not divide so.
 constexpr int kNeighbours = 0, kHalves = 1, kOddHalves = 2;
@@ -96,9 +96,12 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v)
     return v;
 }
 
-// A head is LANES lanes of a wave (a power of two), 16 bytes each; a workgroup has 256 / LANES heads of one token at a time.  Of an element x
+// A head is LANES lanes of a wave (a power of two), 16 bytes each; a workgroup has 128 / LANES heads of one token at a time.  Of an element x
 // with partner y the lane keeps a = m cos t (offset + w) and b = -+ m sin t (offset + w of the partner), the same for all heads where they
-// share weights: a head costs it the sum of squares and x inv a + y inv b.  Bound by reading and writing q, K and V once.
+// share weights: a head costs it the sum of squares and x inv a + y inv b.  Bound by reading and writing q, K and V once: 8192 tokens of 32 / 8
+// heads of 128, 201 MB, 34.4 us on the same data again (5.9 TB/s, as the rotary append alone), 39 on data from memory.  A token's first wait is for its
+// angles; two waves a workgroup lose least there (64 / 128 / 256 / 512 threads: 38.0 / 34.4 / 35.9 / 51.8).  Two pieces in flight instead of
+// one cost registers and gain nothing (35.9 / 38.0).
 template <pa_dtype DT, int PAIRS, bool TO4, int LANES>
 __global__ __launch_bounds__(kThreads) void paged_norm_rope_append_kernel(NormRopeArgs a)
 {
@@ -170,12 +173,11 @@ __global__ __launch_bounds__(kThreads) void paged_norm_rope_append_kernel(NormRo
             if (page >= 0 && page < a.num_pages) slot = (int64_t)page * a.page_stride + (TO4 ? 0 : place * a.token_stride);
         }
     }
-    if ((int32_t)threadIdx.x < 136) {
-        sm_c[threadIdx.x] = 1.f;
-        sm_s[threadIdx.x] = 0.f;
+    for (int32_t i = half + (int32_t)threadIdx.x; i < 136; i += kThreads) {
+        sm_c[i] = 1.f;
+        sm_s[i] = 0.f;
     }
-    if ((int32_t)threadIdx.x < half) {
-        const int32_t i = threadIdx.x;
+    for (int32_t i = threadIdx.x; i < half; i += kThreads) {
         const int32_t axis = r.pair_axes ? min(max(r.pair_axes[i], 0), r.axes - 1) : 0;   // (no read out of range)
         const double turns = (double)r.rope_positions[(int64_t)axis * r.T + t] * (r.inv_freq[i] * 0.15915494309189535);
         float sn, cs;
@@ -330,9 +332,9 @@ template <pa_dtype DT, int PAIRS, bool TO4, int LANES>
 void launch_lanes(const NormRopeArgs& a, hipStream_t stream)
 {
     const int32_t heads = a.q_heads + 2 * a.kv_heads, once = kThreads / LANES;
-    // Few tokens are spread over several workgroups each (us with 512 / 1024 / 2048 in the place of 2048, 32 / 8 heads of 128: 8 tokens 3.8 / 4.1 /
-    // 3.9, 240 4.9 / 4.6 / 4.7; 900 tokens of 32 / 32 heads of 80 10.3 / 10.3 / 9.0, with 4096 9.8).
-    const int32_t parts = min((heads + once - 1) / once, max(1, 2048 / a.r.T));
+    // Few tokens are spread over several workgroups each (us with 2048 / 4096 in the place of 4096: 8 tokens of 32 / 8 heads of 128 4.0 / 4.0, 240
+    // 4.6 / 4.8, 600 6.2 / 6.4; 900 of 32 / 32 heads of 80 9.8 / 9.0).
+    const int32_t parts = min((heads + once - 1) / once, max(1, 4096 / a.r.T));
     hipLaunchKernelGGL((paged_norm_rope_append_kernel<DT, PAIRS, TO4, LANES>), dim3(a.r.T, parts), dim3(kThreads), 0, stream, a);
 }
 
