@@ -611,6 +611,9 @@ pa_status pa_pool_share_prefix(pa_pool* pool, int32_t dst_seq, int32_t src_seq, 
  * page loses one reference.  A no-op for a private page.  Call before appending into a page that may be shared. */
 pa_status pa_pool_make_writable(pa_pool* pool, const pa_kv_cache_desc* cache, int32_t seq, int32_t position,
                                 void* stream);
+/* The same for the pages of a 4-bit cache. */
+pa_status pa_pool_make_writable_mx4(pa_pool* pool, const pa_mx4_cache_desc* cache, int32_t seq, int32_t position,
+                                    void* stream);
 
 /* Introspection (host, no synchronisation): free pages; blocks of a sequence; copy of a sequence's row into
  * host_row[0 .. capacity) (returns PA_ERR_INVALID_ARG if capacity is too small); references of a page. */

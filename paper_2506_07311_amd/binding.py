@@ -33,7 +33,7 @@ EXPORTS = (
     "pa_status_string", "pa_set_option", "pa_stream_read", "pa_profile_enable", "pa_profile_reset",
     "pa_profile_read",
     "pa_pool_create", "pa_pool_destroy", "pa_pool_set_growth", "pa_pool_reserve", "pa_pool_release", "pa_pool_share_prefix",
-    "pa_pool_make_writable", "pa_pool_num_free", "pa_pool_num_blocks", "pa_pool_get_row", "pa_pool_refcount",
+    "pa_pool_make_writable", "pa_pool_make_writable_mx4", "pa_pool_num_free", "pa_pool_num_blocks", "pa_pool_get_row", "pa_pool_refcount",
 )
 
 
@@ -1037,6 +1037,12 @@ def pa_pool_make_writable(pool, k_cache, v_cache, seq: int, position: int, *, he
     desc = cache_desc(k_cache, v_cache, head_major)
     _check(load_library().pa_pool_make_writable(pool, ctypes.byref(desc), ctypes.c_int32(seq),
                                                 ctypes.c_int32(position), _stream(stream)), "pa_pool_make_writable")
+
+
+def pa_pool_make_writable_mx4(pool, cache, seq: int, position: int, *, head_dim: int, stream=None) -> None:
+    desc = mx4_desc(cache, head_dim)
+    _check(load_library().pa_pool_make_writable_mx4(pool, ctypes.byref(desc), ctypes.c_int32(seq), ctypes.c_int32(position),
+                                                    _stream(stream)), "pa_pool_make_writable_mx4")
 
 
 def pa_pool_num_free(pool) -> int:

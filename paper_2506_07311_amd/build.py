@@ -40,7 +40,7 @@ def _compile(src: str, force: bool) -> str:
     obj = os.path.join(OBJ, src.replace(".hip", ".o"))
     path = os.path.join(CSRC, src)
     deps = [path] + HEADERS + (TREE_HEADERS if src.startswith("tree_") else []) + \
-        (MX4_HEADERS if src.startswith(("mx4_", "norm_")) else [])
+        (MX4_HEADERS if src.startswith(("mx4_", "norm_", "page_pool")) else [])
     if not force and os.path.exists(obj) and os.path.getmtime(obj) >= max(os.path.getmtime(p) for p in deps):
         return obj
     cmd = [_hipcc(), *FLAGS, "-c", path, "-o", obj]

@@ -61,6 +61,8 @@ __device__ __forceinline__ uint32_t mx4_codes(const float (&x)[4], uint32_t scal
 
 #endif
 
+pa_status check_mx4_cache(const pa_mx4_cache_desc* c);
+pa_status launch_mx4_copy_page(const pa_mx4_cache_desc* c, int32_t src_page, int32_t dst_page, hipStream_t stream);
 pa_status launch_kv_gather_mx4(const pa_mx4_cache_desc* c, pa_dtype dtype, void* out_k, void* out_v, int32_t rows,
                                const int32_t* block_table, const int32_t* first_lens, const int32_t* seq_lens, const int32_t* cu_lens,
                                int32_t batch, int32_t max_blocks, hipStream_t stream);
@@ -77,10 +79,10 @@ struct Mx4Args {
     const int32_t* cu_q_lens;
     const int32_t* seq_lens;
     const int32_t* block_table;
-    int32_t batch, max_q_len, num_q_heads, max_blocks, max_seq_len;
+    int32_t batch, total_q, max_q_len, num_q_heads, max_blocks, max_seq_len;
     float scale;
 };
-size_t mx4_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t max_q_len,
+size_t mx4_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t total_q, int32_t max_q_len,
                            int32_t max_seq_len);
 pa_status launch_attention_mx4(const Mx4Args& a, void* workspace, hipStream_t stream);
 

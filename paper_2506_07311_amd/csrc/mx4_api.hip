@@ -4,6 +4,23 @@
 
 using namespace pa;
 
+namespace pa {
+
+pa_status check_mx4_cache(const pa_mx4_cache_desc* c)
+{
+    if (!c || !c->records) return PA_ERR_INVALID_ARG;
+    if (c->num_pages <= 0 || c->num_kv_heads <= 0 || c->head_dim <= 0 || c->page_size <= 0 || (c->page_size & (c->page_size - 1)))
+        return PA_ERR_INVALID_ARG;
+    const size_t record = pa_mx4_record_bytes(c->page_size, c->head_dim);
+    if (record == 0) return PA_ERR_UNSUPPORTED;
+    if (c->head_stride < 0 || (c->num_kv_heads > 1 && c->head_stride < (int64_t)record) || c->page_stride < (int64_t)record)
+        return PA_ERR_INVALID_ARG;
+    if (c->page_stride % 16 || c->head_stride % 16 || ((uintptr_t)c->records & 15)) return PA_ERR_UNSUPPORTED;
+    return PA_OK;
+}
+
+}  // namespace pa
+
 namespace {
 
 inline hipStream_t stream_of(void* s) { return reinterpret_cast<hipStream_t>(s); }
@@ -12,15 +29,8 @@ bool known(pa_dtype t) { return t == PA_DTYPE_F32 || t == PA_DTYPE_BF16 || t == 
 
 pa_status check_mx4(const pa_mx4_cache_desc* c, pa_dtype dtype)
 {
-    if (!c || !c->records) return PA_ERR_INVALID_ARG;
-    if (c->num_pages <= 0 || c->num_kv_heads <= 0 || c->head_dim <= 0 || c->page_size <= 0 || (c->page_size & (c->page_size - 1)))
-        return PA_ERR_INVALID_ARG;
-    const size_t record = pa_mx4_record_bytes(c->page_size, c->head_dim);
-    if (!known(dtype) || record == 0) return PA_ERR_UNSUPPORTED;
-    if (c->page_stride <= 0 || (c->num_kv_heads > 1 && c->head_stride < (int64_t)record)) return PA_ERR_INVALID_ARG;
-    if (c->head_stride < 0 || c->page_stride < (int64_t)record) return PA_ERR_INVALID_ARG;
-    if (c->page_stride % 16 || c->head_stride % 16 || ((uintptr_t)c->records & 15)) return PA_ERR_UNSUPPORTED;
-    return PA_OK;
+    const pa_status st = check_mx4_cache(c);
+    return st != PA_OK || known(dtype) ? st : PA_ERR_UNSUPPORTED;
 }
 
 // What paged_norm_rope_append asks of its tokens; strides of 0 become those of contiguous ones.
@@ -132,7 +142,7 @@ size_t paged_attention_mx4_workspace_bytes(int32_t batch, int32_t num_q_heads, i
 {
     if (batch <= 0 || num_kv_heads <= 0 || num_q_heads < num_kv_heads || head_dim <= 0 || total_q <= 0 || max_q_len <= 0 || max_seq_len < 0)
         return 256;
-    return mx4_workspace_bytes(batch, num_q_heads, num_kv_heads, head_dim, max_q_len, max_seq_len);
+    return mx4_workspace_bytes(batch, num_q_heads, num_kv_heads, head_dim, total_q, max_q_len, max_seq_len);
 }
 
 pa_status paged_attention_mx4(const pa_mx4_cache_desc* cache, pa_dtype dtype, const void* q, void* out, float* lse,
@@ -152,8 +162,8 @@ pa_status paged_attention_mx4(const pa_mx4_cache_desc* cache, pa_dtype dtype, co
                                                                             total_q, max_q_len, max_seq_len))
         return PA_ERR_WORKSPACE_TOO_SMALL;
     if ((uintptr_t)workspace & 255) return PA_ERR_INVALID_ARG;
-    const Mx4Args a = {cache, dtype, q, out, lse, cu_q_lens, seq_lens, block_table, batch, max_q_len, num_q_heads, max_blocks, max_seq_len,
-                       scale};
+    const Mx4Args a = {cache, dtype, q, out, lse, cu_q_lens, seq_lens, block_table, batch, total_q, max_q_len, num_q_heads, max_blocks,
+                       max_seq_len, scale};
     return launch_attention_mx4(a, workspace, stream_of(stream));
 }
 

@@ -24,11 +24,13 @@ struct Mx4Plan {
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 // `wide`: 16 rows a wave where others take 32 (mx4_attention_impl.h).
-Mx4Plan plan_mx4(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t d, int32_t max_q_len, int32_t max_seq_len, pa_dtype dtype)
+Mx4Plan plan_mx4(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t d, int32_t total_q, int32_t max_q_len, int32_t max_seq_len,
+                 pa_dtype dtype)
 {
     const bool f32 = dtype == PA_DTYPE_F32, bf16 = dtype == PA_DTYPE_BF16;
     const bool wide = d == 256 || f32, whole = d == 256 && !bf16;
     Mx4Plan p = {};
+    if (max_q_len > total_q) max_q_len = total_q;            // (a loose bound)
     const int64_t rows = (int64_t)max_q_len * (num_q_heads / num_kv_heads), keys = max_seq_len;
     const int64_t cus = device_cus(), heads = (int64_t)batch * num_kv_heads;
     bool cut;
@@ -56,7 +58,11 @@ Mx4Plan plan_mx4(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32
     const int64_t blocks = (rows + p.rows - 1) / p.rows;
     p.row_blocks = blocks < 1 ? 1 : (int32_t)blocks;
     const int64_t slots = cus * (p.shape == 4 || whole ? 1 : 2);
-    if (p.shape == 3 && heads * p.row_blocks >= slots) cut = false;
+    // Many rows: whole row blocks where the rows that there are fill the machine, once for whole prompts and eight times for chunks behind contexts,
+    // whose lengths may be far apart, and sequences bring about as many each; otherwise the keys are shared (four chunks of 512 tokens behind
+    // 64 to 32768 whole / shared 722 / 417 us).
+    const int64_t filled = num_kv_heads * ((int64_t)total_q * (num_q_heads / num_kv_heads) / p.rows) / slots;
+    if (p.shape == 3 && filled >= (keys <= 2 * (int64_t)max_q_len ? 1 : 8) && 2 * (int64_t)total_q >= (int64_t)batch * max_q_len) cut = false;
     const int64_t tiles = ((int64_t)max_seq_len + p.tile - 1) / p.tile;
     if (cut) {
         const int64_t most = ((int64_t)batch * p.row_blocks * tiles + kTreeMinTiles - 1) / kTreeMinTiles;
@@ -73,12 +79,12 @@ Mx4Plan plan_mx4(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32
 
 }  // namespace
 
-size_t mx4_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t max_q_len,
+size_t mx4_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t total_q, int32_t max_q_len,
                            int32_t max_seq_len)
 {
     size_t most = 256;                                       // (the type is not known here)
     for (const pa_dtype dtype : {PA_DTYPE_F32, PA_DTYPE_BF16, PA_DTYPE_F16}) {
-        const Mx4Plan p = plan_mx4(batch, num_q_heads, num_kv_heads, head_dim, max_q_len, max_seq_len, dtype);
+        const Mx4Plan p = plan_mx4(batch, num_q_heads, num_kv_heads, head_dim, total_q, max_q_len, max_seq_len, dtype);
         const size_t bytes = p.part_o_bytes + p.part_lse_bytes + p.cuts_bytes;
         if (bytes > most) most = bytes;
     }
@@ -88,7 +94,7 @@ size_t mx4_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_he
 pa_status launch_attention_mx4(const Mx4Args& t, void* workspace, hipStream_t stream)
 {
     const pa_mx4_cache_desc* const c = t.cache;
-    const Mx4Plan p = plan_mx4(t.batch, t.num_q_heads, c->num_kv_heads, c->head_dim, t.max_q_len, t.max_seq_len, t.dtype);
+    const Mx4Plan p = plan_mx4(t.batch, t.num_q_heads, c->num_kv_heads, c->head_dim, t.total_q, t.max_q_len, t.max_seq_len, t.dtype);
     // Places of a KV head stay below 2^31, threads of a launch below 2^32.
     const int64_t units = (int64_t)t.batch * p.row_blocks, threads = (int64_t)1 << 32;
     const int64_t tiles = ((int64_t)t.max_seq_len + p.tile - 1) / p.tile;

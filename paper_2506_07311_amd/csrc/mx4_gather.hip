@@ -1,4 +1,4 @@
-// Algorithm 1's Gather from a cache of 4-bit elements: the values that codes and scales stand for, in the wanted type.
+// Algorithm 1's Gather from a cache of 4-bit elements: the values that codes and scales stand for, in the wanted type; and the copy of a page.
 #include "mx4.h"
 
 namespace pa {
@@ -90,7 +90,27 @@ __global__ __launch_bounds__(kThreads) void paged_kv_gather_mx4_kernel(Mx4View c
     }
 }
 
+// A KV head's record a blockIdx.y.
+__global__ __launch_bounds__(kThreads) void paged_mx4_copy_page_kernel(const char* src, char* dst, int64_t head_stride, int32_t record)
+{
+    const int32_t at = ((int32_t)blockIdx.x * kThreads + (int32_t)threadIdx.x) * 16;
+    const int64_t head = (int64_t)blockIdx.y * head_stride;
+    if (at < record) *reinterpret_cast<uint4*>(dst + head + at) = *reinterpret_cast<const uint4*>(src + head + at);
+}
+
 }  // namespace
+
+pa_status launch_mx4_copy_page(const pa_mx4_cache_desc* c, int32_t src_page, int32_t dst_page, hipStream_t stream)
+{
+    if (src_page < 0 || dst_page < 0 || src_page >= c->num_pages || dst_page >= c->num_pages) return PA_ERR_INVALID_ARG;
+    if (c->num_kv_heads > 65535) return PA_ERR_UNSUPPORTED;
+    const int32_t record = (int32_t)pa_mx4_record_bytes(c->page_size, c->head_dim);   // a multiple of 16, at most 2^28 17 / 16
+    const dim3 grid((uint32_t)((record + 16 * kThreads - 1) / (16 * kThreads)), (uint32_t)c->num_kv_heads);
+    ProfileScope prof("paged_mx4_copy_page_kernel", stream);
+    hipLaunchKernelGGL(paged_mx4_copy_page_kernel, grid, dim3(kThreads), 0, stream, (const char*)c->records + src_page * c->page_stride,
+                       (char*)c->records + dst_page * c->page_stride, c->head_stride, record);
+    return launch_status();
+}
 
 pa_status launch_kv_gather_mx4(const pa_mx4_cache_desc* c, pa_dtype dtype, void* out_k, void* out_v, int32_t rows,
                                const int32_t* block_table, const int32_t* first_lens, const int32_t* seq_lens, const int32_t* cu_lens,

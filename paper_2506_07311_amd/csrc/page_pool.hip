@@ -12,7 +12,7 @@
 #include <new>
 #include <vector>
 
-#include "common.h"
+#include "mx4.h"
 
 struct pa_pool {
     int32_t num_pages = 0;
@@ -154,6 +154,33 @@ bool seq_ok(const pa_pool* p, int32_t seq) { return p && seq >= 0 && seq < p->ma
 
 }  // namespace
 
+namespace {
+
+// A private copy of the block that holds `position`, made by copy(from, to), where others share it.
+template <typename Copy>
+pa_status make_writable(pa_pool* p, int32_t page_size, int32_t num_pages, int32_t seq, int32_t position, void* stream, Copy copy)
+{
+    if (page_size != p->page_size || num_pages < p->num_pages) return PA_ERR_INVALID_ARG;
+    const int32_t b = position >> p->log2_page;
+    if (b >= p->num_blocks[seq]) return PA_ERR_INVALID_ARG;
+    int32_t* row = p->host_table + (size_t)seq * p->max_blocks;
+    const int32_t old_page = row[b];
+    if (p->refs[old_page].load(std::memory_order_acquire) <= 1) return PA_OK;   // already private
+    const int32_t page = pop_page(p);
+    if (page < 0) return PA_ERR_OUT_OF_PAGES;
+    p->refs[page].store(1, std::memory_order_release);
+    const pa_status st = copy(old_page, page);
+    if (st != PA_OK) {
+        unref_page(p, page);
+        return st;
+    }
+    row[b] = page;
+    unref_page(p, old_page);
+    return sync_row(p, seq, b, b + 1, stream);
+}
+
+}  // namespace
+
 extern "C" {
 
 pa_status pa_pool_create(pa_pool** out, int32_t num_pages, int32_t page_size, int32_t max_seqs, int32_t max_blocks,
@@ -289,23 +316,19 @@ pa_status pa_pool_make_writable(pa_pool* p, const pa_kv_cache_desc* cache, int32
     if (!seq_ok(p, seq) || position < 0) return PA_ERR_INVALID_ARG;
     const pa_status desc = pa::check_cache(cache);           // dtype, strides, 16-byte alignment of the pools
     if (desc != PA_OK) return desc;
-    if (cache->page_size != p->page_size || cache->num_pages < p->num_pages) return PA_ERR_INVALID_ARG;
-    const int32_t b = position >> p->log2_page;
-    if (b >= p->num_blocks[seq]) return PA_ERR_INVALID_ARG;
-    int32_t* row = p->host_table + (size_t)seq * p->max_blocks;
-    const int32_t old_page = row[b];
-    if (p->refs[old_page].load(std::memory_order_acquire) <= 1) return PA_OK;   // already private
-    const int32_t page = pop_page(p);
-    if (page < 0) return PA_ERR_OUT_OF_PAGES;
-    p->refs[page].store(1, std::memory_order_release);
-    const pa_status st = pa::launch_kv_copy_page(cache, old_page, page, reinterpret_cast<hipStream_t>(stream));
-    if (st != PA_OK) {
-        unref_page(p, page);
-        return st;
-    }
-    row[b] = page;
-    unref_page(p, old_page);
-    return sync_row(p, seq, b, b + 1, stream);
+    return make_writable(p, cache->page_size, cache->num_pages, seq, position, stream, [&](int32_t from, int32_t to) {
+        return pa::launch_kv_copy_page(cache, from, to, reinterpret_cast<hipStream_t>(stream));
+    });
+}
+
+pa_status pa_pool_make_writable_mx4(pa_pool* p, const pa_mx4_cache_desc* cache, int32_t seq, int32_t position, void* stream)
+{
+    if (!seq_ok(p, seq) || position < 0) return PA_ERR_INVALID_ARG;
+    const pa_status desc = pa::check_mx4_cache(cache);
+    if (desc != PA_OK) return desc;
+    return make_writable(p, cache->page_size, cache->num_pages, seq, position, stream, [&](int32_t from, int32_t to) {
+        return pa::launch_mx4_copy_page(cache, from, to, reinterpret_cast<hipStream_t>(stream));
+    });
 }
 
 int32_t pa_pool_num_free(const pa_pool* p) { return p ? p->free_count.load(std::memory_order_relaxed) : -1; }

@@ -441,3 +441,38 @@ def test_a_run_as_a_server_makes_it():
         kept = np.concatenate([v_all[lens[0] - new[0]:lens[0]], v_all[sum(lens) - new[1]:]])
         live = (plan.positions >= 0).cpu().numpy()
         np.testing.assert_array_equal(kept, ref.values(*ref.quantised(v.double().cpu().numpy()[live])))
+
+
+def test_shared_pages_are_copied_before_a_write():
+    """The page manager over a 4-bit cache: a shared prefix, a private copy of its last page, and an append there."""
+    hkv, d, page = 3, 64, 32
+    cache = pa.pa_mx4_cache(10, page, hkv + 1, d)[:, :hkv]
+    cache.fill_(255)
+    table = torch.zeros(2, 5, dtype=torch.int32, device=DEV)
+    pool = pa.pa_pool_create(10, page, 2, 5, table)
+    pa.pa_pool_reserve(pool, 0, 64)
+    k, v = torch.randn(2, 64, hkv, d, device=DEV)
+    pa.paged_kv_append_mx4(cache, k, v, ints(np.zeros(64)), ints(np.arange(64)), table)
+    pa.pa_pool_share_prefix(pool, 1, 0, 64)
+    before = cache.clone()
+    pa.pa_pool_make_writable_mx4(pool, cache, 1, 40, head_dim=d)
+    rows = table.cpu()
+    assert rows[0, 0] == rows[1, 0] and rows[0, 1] != rows[1, 1]
+    assert torch.equal(cache[rows[0, 1]], cache[rows[1, 1]])
+    pa.paged_kv_append_mx4(cache, k[:1], v[:1], ints([1]), ints([40]), table)
+    assert not torch.equal(cache[rows[0, 1]], cache[rows[1, 1]])
+    other = torch.arange(10) != rows[1, 1]
+    assert torch.equal(before[other.to(DEV)], cache[other.to(DEV)])
+    pa.pa_pool_make_writable_mx4(pool, cache, 1, 40, head_dim=d)   # private already
+    assert torch.equal(rows, table.cpu())
+    with pytest.raises(PagedAttnError):
+        pa.pa_pool_make_writable_mx4(pool, cache, 1, 40, head_dim=128)
+    with pytest.raises(PagedAttnError):
+        pa.pa_pool_make_writable_mx4(pool, cache, 1, 64, head_dim=d)
+    pa.pa_pool_destroy(pool)
+
+
+def test_prompts_beside_decode_steps():
+    """Rows of one sequence, a bound for all: the work is shared by keys."""
+    c = Cache([1500, 900, 2000, 64, 700], 2, 128, seed=18).fill()
+    attend(c, [1, 300, 1, 64, 1], 8)

@@ -123,13 +123,15 @@ def test_attention_refusals(lib):
     assert call(fn, a, ws=NULL) == SMALL and call(fn, a, bytes=size(16)) == SMALL
     assert call(fn, a, batch=i32(0)) == 0 and call(fn, a, total=i32(0)) == 0 and call(fn, a, max_q=i32(0)) == 0
     # bounds whose places pass 31 bits
-    assert call(fn, a, batch=i32(1 << 20), max_q=i32(1 << 20), max_len=i32(1 << 30), max_blocks=i32(1 << 26)) == UNSUPPORTED
+    assert call(fn, a, batch=i32(1 << 10), total=i32(1 << 24), max_q=i32(1 << 24), max_len=i32(1 << 30), max_blocks=i32(1 << 26)) == UNSUPPORTED
 
 
 def test_workspace_bound(lib):
     for args in ((1, 8, 8, 64, 5, 5, 128), (64, 32, 8, 128, 300, 8, 32768), (0, 8, 8, 64, 0, 0, 0), (16, 64, 8, 256, 256, 16, 131072)):
         n = pa.paged_attention_mx4_workspace_bytes(*args)
         assert n > 0 and n % 256 == 0
+    # a bound on a sequence's queries beyond all queries asks for nothing more
+    assert pa.paged_attention_mx4_workspace_bytes(4, 32, 8, 128, 9, 9, 5000) == pa.paged_attention_mx4_workspace_bytes(4, 32, 8, 128, 9, 10 ** 9, 5000)
 
 
 def test_binding_refuses_host_tensors_and_odd_records(lib):
