@@ -112,7 +112,10 @@ __global__ __launch_bounds__(kThreads) void paged_norm_rope_append_kernel(NormRo
     const pa_norm_rope& r = a.r;
     const float by_d = a.by_d;
     const int32_t d = a.d, half = a.half, u = threadIdx.x % LANES, first = u * V;
-    const int64_t t = blockIdx.x;
+    // Workgroup i runs on chiplet i % 8: 16 tokens in a row on one, since up to 8 tokens share cache lines of a record (us without / with, 6000
+    // tokens into 4 bits and out again 23.7 / 20.7, 16000 47.5 / 38.2).
+    int64_t t = blockIdx.x;
+    if (TO4 && (t | 127) < (int64_t)gridDim.x) t = (t & ~127) | (t & 7) << 4 | (t >> 3 & 15);
     const bool live = first < d;
     const int32_t heads = a.q_heads + 2 * a.kv_heads;
     const int32_t mine = (heads + (int32_t)gridDim.y - 1) / (int32_t)gridDim.y;
