@@ -708,22 +708,27 @@ def pa_mx4_record_bytes(page_size: int, head_dim: int) -> int:
 
 
 def pa_mx4_cache(num_pages: int, page_size: int, num_kv_heads: int, head_dim: int, device="cuda") -> torch.Tensor:
-    """An empty 4-bit cache: uint8 [num_pages, num_kv_heads, pa_mx4_record_bytes(page_size, head_dim)]."""
+    """An empty 4-bit cache: uint8 [num_pages, num_kv_heads, page_size, 17/16 head_dim], a page's record of a KV head in the last two
+    dimensions (not token by token: the layout is the header's).  A shape that calls check against their tensors'."""
     size = pa_mx4_record_bytes(page_size, head_dim)
     if size == 0:
         raise PagedAttnError("a 4-bit cache has pages of 16 tokens or more, a power of two, and head_dim 64, 128 or 256; "
                              f"got {page_size} and {head_dim}")
-    return torch.empty((num_pages, num_kv_heads, size), dtype=torch.uint8, device=device)
+    return torch.empty((num_pages, num_kv_heads, page_size, size // page_size), dtype=torch.uint8, device=device)
 
 
 def mx4_desc(cache: torch.Tensor, head_dim: int) -> _Mx4Desc:
-    """Descriptor of a 4-bit cache, uint8 [num_pages, Hkv, record]; its record's size gives the tokens of a page."""
-    if cache.dtype != torch.uint8 or cache.dim() != 3 or not cache.is_cuda or cache.stride(2) != 1:
-        raise PagedAttnError("a 4-bit cache is a uint8 device tensor [num_pages, Hkv, record] with contiguous records")
-    NP, Hkv, size = cache.shape
-    page = size * 16 // (17 * head_dim) if head_dim > 0 else 0
+    """Descriptor of a 4-bit cache: uint8 [num_pages, Hkv, page_size, 17/16 head_dim] as of pa_mx4_cache, or [num_pages, Hkv, record],
+    whose record's size gives the tokens of a page once the head_dim is known."""
+    if cache.dtype != torch.uint8 or cache.dim() not in (3, 4) or not cache.is_cuda or cache.stride(-1) != 1 or \
+            (cache.dim() == 4 and cache.stride(2) != cache.shape[3]):
+        raise PagedAttnError("a 4-bit cache is a uint8 device tensor [num_pages, Hkv, page_size, 17/16 head_dim] or "
+                             "[num_pages, Hkv, record] with contiguous records")
+    NP, Hkv = cache.shape[:2]
+    size = cache.shape[2] if cache.dim() == 3 else cache.shape[2] * cache.shape[3]
+    page = (size * 16 // (17 * head_dim) if head_dim > 0 else 0) if cache.dim() == 3 else cache.shape[2]
     if size == 0 or pa_mx4_record_bytes(page, head_dim) != size:
-        raise PagedAttnError(f"records of {size} bytes hold no page of heads of {head_dim}")
+        raise PagedAttnError(f"records of {size} bytes, {list(cache.shape)}, hold no page of heads of {head_dim}")
     return _Mx4Desc(cache.data_ptr(), cache.stride(0) if NP > 1 else Hkv * size, cache.stride(1) if Hkv > 1 else size, NP, page, Hkv,
                     head_dim)
 
@@ -1039,7 +1044,12 @@ def pa_pool_make_writable(pool, k_cache, v_cache, seq: int, position: int, *, he
                                                 ctypes.c_int32(position), _stream(stream)), "pa_pool_make_writable")
 
 
-def pa_pool_make_writable_mx4(pool, cache, seq: int, position: int, *, head_dim: int, stream=None) -> None:
+def pa_pool_make_writable_mx4(pool, cache, seq: int, position: int, *, head_dim: Optional[int] = None, stream=None) -> None:
+    """head_dim: of a cache [num_pages, Hkv, record], whose shape does not say it."""
+    if head_dim is None:
+        if cache.dim() != 4:
+            raise PagedAttnError("pa_pool_make_writable_mx4: a cache [num_pages, Hkv, record] needs head_dim")
+        head_dim = cache.shape[3] * 16 // 17
     desc = mx4_desc(cache, head_dim)
     _check(load_library().pa_pool_make_writable_mx4(pool, ctypes.byref(desc), ctypes.c_int32(seq), ctypes.c_int32(position),
                                                     _stream(stream)), "pa_pool_make_writable_mx4")

@@ -318,7 +318,7 @@ def test_cache_views_and_far_pages():
     """A part of a larger cache, and pages beyond 2^32 bytes."""
     size = pa.pa_mx4_record_bytes(16, 128)
     pages = (1 << 32) // (2 * size) + 4000
-    big = torch.empty((pages, 2, size), dtype=torch.uint8, device=DEV)
+    big = pa.pa_mx4_cache(pages, 16, 2, 128).view(pages, 2, size)
     c = Cache([500, 90], 2, 128, seed=14).fill()
     far = pages - c.cache.shape[0]
     big[far:] = c.cache
@@ -446,7 +446,7 @@ def test_a_run_as_a_server_makes_it():
 def test_shared_pages_are_copied_before_a_write():
     """The page manager over a 4-bit cache: a shared prefix, a private copy of its last page, and an append there."""
     hkv, d, page = 3, 64, 32
-    cache = pa.pa_mx4_cache(10, page, hkv + 1, d)[:, :hkv]
+    cache = pa.pa_mx4_cache(10, page, hkv + 1, d)[:, :hkv]        # (a part of a larger one)
     cache.fill_(255)
     table = torch.zeros(2, 5, dtype=torch.int32, device=DEV)
     pool = pa.pa_pool_create(10, page, 2, 5, table)
@@ -463,7 +463,7 @@ def test_shared_pages_are_copied_before_a_write():
     assert not torch.equal(cache[rows[0, 1]], cache[rows[1, 1]])
     other = torch.arange(10) != rows[1, 1]
     assert torch.equal(before[other.to(DEV)], cache[other.to(DEV)])
-    pa.pa_pool_make_writable_mx4(pool, cache, 1, 40, head_dim=d)   # private already
+    pa.pa_pool_make_writable_mx4(pool, cache, 1, 40)              # private already
     assert torch.equal(rows, table.cpu())
     with pytest.raises(PagedAttnError):
         pa.pa_pool_make_writable_mx4(pool, cache, 1, 40, head_dim=128)
@@ -476,3 +476,78 @@ def test_prompts_beside_decode_steps():
     """Rows of one sequence, a bound for all: the work is shared by keys."""
     c = Cache([1500, 900, 2000, 64, 700], 2, 128, seed=18).fill()
     attend(c, [1, 300, 1, 64, 1], 8)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("new", [1, 12])
+def test_many_sequences(dtype, new):
+    """More than a wave looks at in one go, and units for the whole machine."""
+    rng = np.random.default_rng(1)
+    lens = [int(x) for x in rng.integers(0, 150, 140)]
+    c = Cache(lens, 2, 64, seed=19).fill()
+    attend(c, [min(n, int(rng.integers(0, new + 1))) if i % 7 else min(n, new) for i, n in enumerate(lens)], 4, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_one_long_context_among_short_ones(dtype, d):
+    c = Cache([9000, 10, 700, 1, 33, 2000, 0, 64], 8, d, page=32, seed=20).fill()
+    attend(c, [1] * 6 + [0, 1], 16, dtype)
+
+
+def test_calls_beside_each_other():
+    """Two streams, each with its workspace."""
+    c = Cache([4000, 300], 2, 128, seed=21).fill()
+    q = [torch.randn(2 * n, 8, 128, device=DEV).bfloat16() for n in (1, 5)]
+    args = [(x, ints([0, n, 2 * n]), n, c.table, ints(c.lens), 4000, 0.1) for x, n in zip(q, (1, 5))]
+    want = [pa.paged_attention_mx4(c.cache, *a) for a in args]
+    streams = [torch.cuda.Stream() for _ in args]
+    torch.cuda.synchronize()
+    outs = [torch.zeros_like(w) for w in want]
+    torch.cuda.synchronize()
+    calls = [pa.prepare_attention_mx4(c.cache, *a, out=o, stream=s) for a, o, s in zip(args, outs, streams)]
+    for _ in range(20):
+        for call in calls:
+            call()
+    torch.cuda.synchronize()
+    for o, w in zip(outs, want):
+        assert torch.equal(o, w)
+
+
+def test_refusals():
+    c = Cache([40, 9], 2, 128).fill(torch.bfloat16)
+    q = torch.zeros(2, 4, 128, dtype=torch.bfloat16, device=DEV)
+    good = dict(cache=c.cache, q=q, cu=ints([0, 1, 2]), max_q=1, table=c.table, lens=ints(c.lens), max_len=40, scale=0.1)
+    pa.paged_attention_mx4(*good.values())
+    for change in (dict(q=q.double()), dict(q=q[:, :3]), dict(q=q.transpose(0, 1)), dict(cu=ints([0, 1])),
+                   dict(lens=ints([40])), dict(table=c.table[:1]), dict(table=c.table.long()), dict(cache=c.cache[..., :-16]),
+                   dict(cache=c.cache.cpu()), dict(cache=c.cache.to(torch.int32)), dict(max_len=100000), dict(scale=float("nan")),
+                   dict(max_q=-1)):
+        with pytest.raises(PagedAttnError):
+            pa.paged_attention_mx4(*dict(good, **change).values())
+    # a shape that says the page's tokens: heads of another size are refused (a record of 16 x 128 is as large as one of 32 x 64)
+    four = c.cache.view(c.cache.shape[0], 2, 16, 136)
+    assert torch.equal(pa.paged_attention_mx4(*dict(good, cache=four).values()), pa.paged_attention_mx4(*good.values()))
+    for change in (dict(q=q[..., :64].contiguous()), dict(cache=four[:, :, :8]), dict(cache=four[..., :68]), dict(cache=four.transpose(2, 3))):
+        with pytest.raises(PagedAttnError):
+            pa.paged_attention_mx4(*dict(dict(good, cache=four), **change).values())
+    with pytest.raises(PagedAttnError):
+        pa.paged_attention_mx4(*good.values(), workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
+    with pytest.raises(PagedAttnError):
+        pa.paged_attention_mx4(*good.values(), out=torch.empty(2, 4, 128, device=DEV))
+    k = torch.zeros(3, 2, 128, dtype=torch.bfloat16, device=DEV)
+    for args in ((k, k[:2], ints([0] * 3), ints([0] * 3), c.table), (k, k.float(), ints([0] * 3), ints([0] * 3), c.table),
+                 (k, k, ints([0] * 2), ints([0] * 3), c.table), (k[:, :1], k[:, :1], ints([0] * 3), ints([0] * 3), c.table),
+                 (k.int(), k.int(), ints([0] * 3), ints([0] * 3), c.table), (k, k, ints([0] * 3), ints([0] * 3), c.table[0])):
+        with pytest.raises(PagedAttnError):
+            pa.paged_kv_append_mx4(c.cache, *args)
+    for change in (dict(out_v=k[:2]), dict(out_k=k.int()), dict(cu_lens=ints([0, 1])), dict(first_lens=ints([0])), dict(out_k=k[:, :1])):
+        kw = dict(dict(cu_lens=ints([0, 1, 3]), max_seq_len=40, out_k=k, out_v=k.clone(), first_lens=None), **change)
+        with pytest.raises(PagedAttnError):
+            pa.paged_kv_gather_mx4(c.cache, c.table, ints(c.lens), **kw)
+    rope = ints([0, 1])
+    with pytest.raises(PagedAttnError):
+        pa.paged_norm_rope_append_mx4(c.cache, None, None, None, rope, None, None, None, torch.zeros(64, dtype=torch.float64, device=DEV))
+    with pytest.raises(PagedAttnError):
+        pa.paged_norm_rope_append_mx4(c.cache, q[..., :96].contiguous(), None, None, rope, None, None, None,
+                                      torch.zeros(16, dtype=torch.float64, device=DEV))
