@@ -453,7 +453,9 @@ typedef struct {
 /* Bytes of a record (17/16 page_size head_dim); 0 where there is no such cache. */
 size_t pa_mx4_record_bytes(int32_t page_size, int32_t head_dim);
 
-/* paged_norm_rope_append into a 4-bit cache.  q, k_new, v_new, q_out are of type `dtype`; K is rounded once, from fp32 to 4 bits. */
+/* paged_norm_rope_append into a 4-bit cache.  q, k_new, v_new, q_out are of type `dtype`.  K goes from fp32 to 4 bits, without a rounding to
+ * `dtype` in between; each step before it is an fp32 operation of its own (mean of squares, root, product with the weight, two products
+ * and a sum of the rotation). */
 pa_status paged_norm_rope_append_mx4(const pa_mx4_cache_desc* cache, pa_dtype dtype, const pa_norm_rope* tokens, void* stream);
 
 /* Algorithm 1, Assign, into a 4-bit cache: paged_kv_append's arguments, k_new and v_new of type `dtype`.  A row with positions[t] < 0,

@@ -2,7 +2,11 @@
 // of the tokens' own type or of 4-bit elements.
 //
 //     y = x rsqrt(mean(x^2) + eps) (offset + w),   (y_i, y_j) -> m (y_i cos t - y_j sin t, y_i sin t + y_j cos t)
-// with t = p[axis of the pair] f_pair, the angle in 64 bits as turns (rope_append.hip).  Everything is 32-bit and rounded once.
+// with t = p[axis of the pair] f_pair, the angle in 64 bits as turns (rope_append.hip), and so its sine and cosine.  The rest is 32-bit and
+// rounded once.  K on its way to 4 bits takes the steps one by one, each rounded: squares, their sum in fours and then in pairs of neighbours, y,
+// the weight, the products of the rotation, their sum.  A last bit of it can decide between two codes, a third of the value apart; so it
+// is what any program gets that takes the same steps.  (In 64 bits throughout it costs the registers of three waves of seven, 4096 tokens with their
+// gather 31 -> 36 us, these steps 31.5; 64 bits where a border is near, 39: the last of those heads ends late.)
 #include "mx4.h"
 
 namespace pa {
@@ -22,6 +26,7 @@ struct NormRopeArgs {
     int32_t q_heads, kv_heads;                               // (0 heads: that part is absent)
     int32_t d, half, log2_page, num_pages;
     float by_d;                                              // 1 / d
+    double by_d64;
 };
 
 template <pa_dtype DT>
@@ -88,12 +93,72 @@ __device__ __forceinline__ float lanes_sum(float v)
     return v;
 }
 template <int LANES>
+__device__ __forceinline__ double lanes_sum(double v)
+{
+    auto step = [&](auto move) {
+        const uint64_t b = (uint64_t)__double_as_longlong(v);
+        v += __longlong_as_double((long long)((uint64_t)move((uint32_t)(b >> 32)) << 32 | move((uint32_t)b)));
+    };
+    if (LANES > 1) step([](uint32_t x) { return other<1>(x); });
+    if (LANES > 2) step([](uint32_t x) { return other<2>(x); });
+    if (LANES > 4) step([](uint32_t x) { return other<4>(x); });
+    if (LANES > 8) step([](uint32_t x) { return other<8>(x); });
+    if (LANES > 16) step([](uint32_t x) { return other<16>(x); });
+    if (LANES > 32) step([](uint32_t x) { return other<32>(x); });
+    return v;
+}
+template <int LANES>
 __device__ __forceinline__ uint32_t lanes_max(uint32_t v)
 {
     v = max(v, other<1>(v));
     v = max(v, other<2>(v));
     if (LANES > 4) v = max(v, other<4>(v));
     return v;
+}
+
+// 1 / sqrt(x) in 64 bits: the hardware's 32-bit root and a step of Newton's method, or what the library does where 32 bits do not hold x.
+__device__ __forceinline__ double root_of_inverse(double x)
+{
+    if (!(x > 0x1p-100 && x < 0x1p+100)) return 1.0 / sqrt(x);
+    double r = (double)__builtin_amdgcn_rsqf((float)x);      // (to 2^-22: after the step to 2^-43, after another to the last bits)
+    r = r * fma(-0.5 * x * r, r, 1.5);
+    return r * fma(-0.5 * x * r, r, 1.5);
+}
+
+// Products and sums that are rounded each by itself.
+__device__ __forceinline__ float times(float x, float y)
+{
+#pragma clang fp contract(off)
+    return x * y;
+}
+__device__ __forceinline__ float plus(float x, float y)
+{
+#pragma clang fp contract(off)
+    return x + y;
+}
+
+// Sine and cosine of so many turns, in 64 bits: an eighth of a turn at most is left to the Taylor series, whose next terms are below 2^-45.
+__device__ __forceinline__ void sine_cosine(double turns, double& sn, double& cs)
+{
+    turns -= rint(turns);
+    const double quarter = rint(4.0 * turns);
+    const double x = 6.283185307179586 * (turns - 0.25 * quarter), z = x * x;
+    double s = 1.0 / 6227020800.0, c = 1.0 / 479001600.0;    // 1 / 13!, 1 / 12!
+    s = fma(s, z, -1.0 / 39916800.0);
+    c = fma(c, z, -1.0 / 3628800.0);
+    s = fma(s, z, 1.0 / 362880.0);
+    c = fma(c, z, 1.0 / 40320.0);
+    s = fma(s, z, -1.0 / 5040.0);
+    c = fma(c, z, -1.0 / 720.0);
+    s = fma(s, z, 1.0 / 120.0);
+    c = fma(c, z, 1.0 / 24.0);
+    s = fma(s, z, -1.0 / 6.0);
+    c = fma(c, z, -0.5);
+    s = fma(s * z, x, x);
+    c = fma(c, z, 1.0);
+    const int q = (int)quarter;
+    sn = q == 0 ? s : q == 1 ? c : q == -1 ? -c : -s;
+    cs = q == 0 ? c : q == 1 ? -s : q == -1 ? s : -c;
 }
 
 // A head is LANES lanes of a wave (a power of two), 16 bytes each; a workgroup has 128 / LANES heads of one token at a time.  Of an element x
@@ -103,12 +168,13 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v)
 // angles; two waves a workgroup lose least there (64 / 128 / 256 / 512 threads: 38.0 / 34.4 / 35.9 / 51.8).  Two pieces in flight instead of
 // one cost registers and gain nothing (35.9 / 38.0).
 template <pa_dtype DT, int PAIRS, bool TO4, int LANES>
-__global__ __launch_bounds__(kThreads) void paged_norm_rope_append_kernel(NormRopeArgs a)
+__global__ __launch_bounds__(kThreads, TO4 && PAIRS != kOddHalves ? 6 : 1) void paged_norm_rope_append_kernel(NormRopeArgs a)
 {
     typedef Elem<DT> E;
     typedef typename E::T T;
     constexpr int V = 16 / sizeof(T), HEADS = kThreads / LANES;
-    __shared__ __attribute__((aligned(16))) float sm_c[136], sm_s[136];   // pairs (head_dim is at most 256); behind them 1 and 0
+    // cosines and sines of the pairs (head_dim is at most 256), behind them 1 and 0
+    __shared__ __attribute__((aligned(16))) float sm_c[136], sm_s[136];
     const pa_norm_rope& r = a.r;
     const float by_d = a.by_d;
     const int32_t d = a.d, half = a.half, u = threadIdx.x % LANES, first = u * V;
@@ -144,7 +210,7 @@ __global__ __launch_bounds__(kThreads) void paged_norm_rope_append_kernel(NormRo
         if (!live) p.x = uint4{0, 0, 0, 0};
         return p;
     };
-    // offset + w of the lane's elements
+    // w of the lane's elements
     auto weights_at = [&](float (&w)[V], const char* weights, int32_t at) {
         const int32_t i = at + (live ? first : 0);
         if (DT == PA_DTYPE_F32 || f32) {
@@ -160,9 +226,51 @@ __global__ __launch_bounds__(kThreads) void paged_norm_rope_append_kernel(NormRo
 #pragma unroll
             for (int e = 0; e < V; ++e) w[e] = E::get(raw[e]);
         }
-#pragma unroll
-        for (int e = 0; e < V; ++e) w[e] += r.weight_offset;
     };
+    const int from = ((int)threadIdx.x & 63) - u + partner / V;   // the partner's lane
+    // weights of the lane's elements and of their partners, offset not yet added (1 in all without weights)
+    auto both_weights = [&](float (&w)[V], float (&other)[V], const char* weights, int32_t at_head) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) w[e] = 1.f;
+        if (weights) weights_at(w, weights, at_head);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const int32_t i = first + e;
+            other[e] = INTER ? w[e ^ 1] : PAIRS == kHalves ? __shfl(w[e], from) : 1.f;
+            if (PAIRS == kOddHalves && weights && i < 2 * half) {
+                const int32_t k = at_head + (i < half ? i + half : i - half);
+                other[e] = f32 ? ((const float*)weights)[k] : E::get(((const T*)weights)[k]);
+            }
+        }
+    };
+    // the partners of a piece's elements; 0 where nothing turns
+    auto partners = [&](float (&y)[V], const float (&x)[V], const Piece& p) {
+        if (INTER) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) y[e] = first + e < 2 * half ? x[e ^ 1] : 0.f;
+        } else if (PAIRS == kHalves) {
+            T raw[V];
+            const uint4 v = uint4{(uint32_t)__shfl((int)p.x.x, from), (uint32_t)__shfl((int)p.x.y, from),
+                                  (uint32_t)__shfl((int)p.x.z, from), (uint32_t)__shfl((int)p.x.w, from)};
+            __builtin_memcpy(raw, &v, 16);
+#pragma unroll
+            for (int e = 0; e < V; ++e) y[e] = turned ? E::get(raw[e]) : 0.f;
+        } else {
+            // (a wave's lanes have all read before one writes: a head lies within it)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const int32_t i = first + e;
+                y[e] = i < 2 * half ? E::get(p.src[i < half ? i + half : i - half]) : 0.f;
+            }
+        }
+    };
+    // where element e's cosine and sine stand, and whether it is a pair's first
+    const int32_t at_halves = turned ? min(first, partner) : 128, at_pairs = live ? first / 2 : 128;
+    auto pair_of = [&](int e) {
+        const int32_t i = first + e;
+        return INTER ? at_pairs + e / 2 : PAIRS == kHalves ? at_halves + e : i < half ? i : i < 2 * half ? i - half : 128;
+    };
+    auto is_first = [&](int e) { return INTER ? e % 2 == 0 : first + e < half; };
     int32_t j = begin + (int32_t)threadIdx.x / LANES;
     Piece p;
     if (j < end) p = load(j);
@@ -183,13 +291,13 @@ __global__ __launch_bounds__(kThreads) void paged_norm_rope_append_kernel(NormRo
     for (int32_t i = threadIdx.x; i < half; i += kThreads) {
         const int32_t axis = r.pair_axes ? min(max(r.pair_axes[i], 0), r.axes - 1) : 0;   // (no read out of range)
         const double turns = (double)r.rope_positions[(int64_t)axis * r.T + t] * (r.inv_freq[i] * 0.15915494309189535);
-        float sn, cs;
-        sincospif((float)(2.0 * (turns - rint(turns))), &sn, &cs);
-        sm_c[i] = cs * r.mscale;
-        sm_s[i] = sn * r.mscale;
+        double sn, cs;
+        sine_cosine(turns, sn, cs);
+        sm_c[i] = (float)(cs * r.mscale);
+        sm_s[i] = (float)(sn * r.mscale);
     }
     __syncthreads();
-    float fa[V], fb[V];
+    float fa[V], fb[V];          // a and b; on the way to 4 bits the weights alone
     int32_t have = -1;           // whose factors these are: q (0), K (1), no one's (-1)
     for (; j < end;) {
         const int32_t what = p.what, h = p.h;
@@ -204,92 +312,54 @@ __global__ __launch_bounds__(kThreads) void paged_norm_rope_append_kernel(NormRo
         if (what != 2 && (norm || half > 0)) {
             const char* const weights = pick(what, q_weight, k_weight, q_weight);
             const bool each = weights && pick(what, r.q_weight_heads, r.k_weight_heads, 0);
-            const int from = ((int)threadIdx.x & 63) - u + partner / V;   // the partner's lane
+            const int32_t at_head = each ? h * d : 0;
+            float y[V];
+            partners(y, x, p);
+            auto in_64 = [&] {                               // of squares that fp32 does not hold
+                double sum = 0.0;
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum = fma((double)x[e], (double)x[e], sum);
+                return (float)root_of_inverse(lanes_sum<LANES>(sum) * a.by_d64 + (double)r.eps);
+            };
             if (have != what || each) {
-                float w[V], c[V], s[V];
-#pragma unroll
-                for (int e = 0; e < V; ++e) w[e] = 1.f;
-                if (weights) weights_at(w, weights, each ? h * d : 0);
-                if (INTER) {
-                    const int32_t at = live ? first / 2 : 128;
-#pragma unroll
-                    for (int e = 0; e < V; e += 2) {
-                        c[e] = c[e + 1] = sm_c[at + e / 2];
-                        s[e + 1] = sm_s[at + e / 2];
-                        s[e] = -s[e + 1];
-                    }
-                } else if (PAIRS == kHalves) {
-                    const int32_t at = turned ? min(first, partner) : 128;
-                    const float sign = first < half ? -1.f : 1.f;
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        c[e] = sm_c[at + e];
-                        s[e] = sm_s[at + e] * sign;
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const int32_t i = first + e, at = i < half ? i : i < 2 * half ? i - half : 128;
-                        c[e] = sm_c[at];
-                        s[e] = i < half ? -sm_s[at] : sm_s[at];
-                    }
-                }
+                both_weights(fa, fb, weights, at_head);
+                const float offset = weights ? r.weight_offset : 0.f;
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const int32_t i = first + e;
-                    float other = INTER ? w[e ^ 1] : PAIRS == kHalves ? __shfl(w[e], from) : 1.f;
-                    if (PAIRS == kOddHalves && weights && i < 2 * half) {
-                        const int32_t k = (each ? h * d : 0) + (i < half ? i + half : i - half);
-                        other = r.weight_offset + (f32 ? ((const float*)weights)[k] : E::get(((const T*)weights)[k]));
-                    }
-                    fa[e] = c[e] * w[e];
-                    fb[e] = i < 2 * half ? s[e] * other : -0.f;   // (with y = 0: a zero keeps its sign)
+                    fa[e] += offset;
+                    fb[e] += offset;
+                    if (TO4) continue;
+                    const int32_t at = pair_of(e);
+                    const float sn = sm_s[at] * fb[e];
+                    fa[e] *= sm_c[at];
+                    fb[e] = first + e >= 2 * half ? -0.f : is_first(e) ? -sn : sn;   // (with y = 0: a zero keeps its sign)
                 }
                 have = what;
             }
-            // partners; 0 where nothing turns
-            float y[V];
-            if (INTER) {
-#pragma unroll
-                for (int e = 0; e < V; ++e) y[e] = first + e < 2 * half ? x[e ^ 1] : 0.f;
-            } else if (PAIRS == kHalves) {
-                T raw[V];
-                const uint4 v = uint4{(uint32_t)__shfl((int)p.x.x, from), (uint32_t)__shfl((int)p.x.y, from),
-                                      (uint32_t)__shfl((int)p.x.z, from), (uint32_t)__shfl((int)p.x.w, from)};
-                __builtin_memcpy(raw, &v, 16);
-#pragma unroll
-                for (int e = 0; e < V; ++e) y[e] = turned ? E::get(raw[e]) : 0.f;
-            } else {
-                // (a wave's lanes have all read before one writes: a head lies within it)
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const int32_t i = first + e;
-                    y[e] = i < 2 * half ? E::get(p.src[i < half ? i + half : i - half]) : 0.f;
-                }
-            }
+            float inv = 1.f;
             if (norm) {
-                float sum = 0.f;
+                float four[V / 4];
 #pragma unroll
-                for (int e = 0; e < V; ++e) sum = __builtin_fmaf(x[e], x[e], sum);
+                for (int e = 0; e < V; ++e)
+                    four[e / 4] = e % 4 == 0 ? times(x[e], x[e]) : TO4 ? plus(four[e / 4], times(x[e], x[e])) : __builtin_fmaf(x[e], x[e], four[e / 4]);
+                float sum = four[0];
+                if (V == 8) sum = plus(four[0], four[V / 4 - 1]);
                 sum = lanes_sum<LANES>(sum);
-                const float mean = sum * by_d + r.eps;
-                float inv = __builtin_amdgcn_rsqf(mean);     // (a unit in the last place)
-                if (!(sum < 0x1p+120f) || mean < 0x1p-60f) {   // squares that fp32 does not hold
-                    double s64 = 0.0;
-#pragma unroll
-                    for (int e = 0; e < V; ++e) s64 += (double)x[e] * (double)x[e];
-#pragma unroll
-                    for (int i = 1; i < LANES; i *= 2) s64 += __shfl_xor(s64, i);
-                    inv = (float)(1.0 / sqrt(s64 / d + (double)r.eps));
-                }
+                const float mean = plus(times(sum, by_d), r.eps);
+                inv = __builtin_amdgcn_rsqf(mean);           // (a unit in the last place)
+                if (!(sum < 0x1p+120f) || mean < 0x1p-60f) inv = in_64();
+            }
+            if constexpr (TO4) {
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    x[e] *= inv;
-                    y[e] *= inv;
+                    const int32_t at = pair_of(e);
+                    const float z = times(times(x[e], inv), fa[e]), zc = times(z, sm_c[at]), zs = times(times(times(y[e], inv), fb[e]), sm_s[at]);
+                    x[e] = first + e >= 2 * half ? z : plus(zc, is_first(e) ? -zs : zs);
                 }
-            }
+            } else {
 #pragma unroll
-            for (int e = 0; e < V; ++e) x[e] = __builtin_fmaf(y[e], fb[e], x[e] * fa[e]);
+                for (int e = 0; e < V; ++e) x[e] = __builtin_fmaf(y[e] * inv, fb[e], x[e] * inv * fa[e]);
+            }
         }
         uint4 out = p.x;         // (V as it is)
         j += HEADS;
@@ -393,6 +463,7 @@ pa_status launch_norm_rope_append(const pa_kv_cache_desc* cache, const pa_mx4_ca
         a.num_pages = cache->num_pages;
     }
     a.by_d = 1.f / (float)a.d;
+    a.by_d64 = 1.0 / a.d;
     ProfileScope prof("paged_norm_rope_append_kernel", stream);
     if (dtype == PA_DTYPE_F32) to4 ? launch_dtype<PA_DTYPE_F32, true>(a, stream) : launch_dtype<PA_DTYPE_F32, false>(a, stream);
     else if (dtype == PA_DTYPE_BF16) to4 ? launch_dtype<PA_DTYPE_BF16, true>(a, stream) : launch_dtype<PA_DTYPE_BF16, false>(a, stream);
