@@ -21,7 +21,7 @@ inline Mx4View make_view(const pa_mx4_cache_desc* c)
 #if defined(__HIPCC__)
 
 // Bytes from a record's start.  K codes of a slot.
-__device__ __forceinline__ int32_t mx4_k_codes(int32_t log2_page, int32_t d, int32_t slot) { return slot * (d / 2); }
+__device__ __forceinline__ int32_t mx4_k_codes(int32_t d, int32_t slot) { return slot * (d / 2); }
 // V codes of elements 4 u .. 4 u + 3 of a head.
 __device__ __forceinline__ int32_t mx4_v_codes(int32_t log2_page, int32_t d, int32_t slot, int32_t u)
 {

@@ -33,7 +33,7 @@ Mx4Plan plan_mx4(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32
     if (max_q_len > total_q) max_q_len = total_q;            // (a loose bound)
     const int64_t rows = (int64_t)max_q_len * (num_q_heads / num_kv_heads), keys = max_seq_len;
     const int64_t cus = device_cus(), heads = (int64_t)batch * num_kv_heads;
-    bool cut;
+    int64_t whole_keys;                                      // longest contexts whose row blocks stay whole
     if (rows <= 16) {
         // A row block (a "unit" with its KV head) is one workgroup's where units fill the machine, or contexts are short; otherwise the keys are
         // shared and merged.  us, 32 / 8 heads of 128, eight waves whole / cut, four waves whole / cut:
@@ -43,26 +43,35 @@ Mx4Plan plan_mx4(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32
         //     1 x 4000 - / 13.7 - / 12.7                 1 x 100000 - / 28.0 - / 28.5               16 x 131072, 64 heads - / 396 - / 402
         if (heads <= cus) {
             p.shape = keys > 128 ? 4 : 0;
-            cut = keys > (4 * heads >= 3 * cus ? 4096 : 1536);
+            whole_keys = 4 * heads >= 3 * cus ? 4096 : 1536;
         } else {
             p.shape = 0;
-            cut = keys > 4096 * (heads / (2 * cus) > 1 ? heads / (2 * cus) : 1);
+            whole_keys = 4096 * (heads / (2 * cus) > 1 ? heads / (2 * cus) : 1);
         }
-        if (cut) p.shape = heads * keys >= cus * 2048 ? 4 : 0;
+        if (keys > whole_keys) p.shape = heads * keys >= cus * 2048 ? 4 : 0;
     } else {
         p.shape = rows <= 32 ? 1 : rows <= 64 ? 2 : 3;
-        cut = keys > 512;
     }
     p.rows = p.shape == 0 || p.shape == 4 ? 16 : p.shape == 1 ? 32 : p.shape == 2 || wide ? 64 : 128;
     p.tile = p.shape == 4 && !whole ? 256 : p.shape == 0 || p.shape == 4 || (p.shape == 1 && !wide) ? 128 : 64;
     const int64_t blocks = (rows + p.rows - 1) / p.rows;
     p.row_blocks = blocks < 1 ? 1 : (int32_t)blocks;
     const int64_t slots = cus * (p.shape == 4 || whole ? 1 : 2);
-    // Many rows: whole row blocks where the rows that there are fill the machine, once for whole prompts and eight times for chunks behind contexts,
-    // whose lengths may be far apart, and sequences bring about as many each; otherwise the keys are shared (four chunks of 512 tokens behind
-    // 64 to 32768 whole / shared 722 / 417 us).
-    const int64_t filled = num_kv_heads * ((int64_t)total_q * (num_q_heads / num_kv_heads) / p.rows) / slots;
-    if (p.shape == 3 && filled >= (keys <= 2 * (int64_t)max_q_len ? 1 : 8) && 2 * (int64_t)total_q >= (int64_t)batch * max_q_len) cut = false;
+    // More rows, the same way (us whole / cut: 16 x 8 on 500..1000 13.8 / 16.8, 4 x 16 19.8 / 16.4, 16 x 16 20.0 / 26.3, 32 x 8 on 1500..3000 26.6 / 33.9,
+    // 32 x 16 44.8 / 49.5, 64 x 16 72.9 / 80.5, on 300..6000 99.4 / 74.4; 16 x 32 on 500..1000 36.5 / 32.7, 32 x 32 39.0 / 48.2, on 1500..3000 96.5 / 76.7,
+    // 64 x 32 129 / 133).
+    if (p.shape == 1) whole_keys = heads >= cus ? 4096 : 1024;
+    if (p.shape == 2) whole_keys = heads >= cus ? 4096 : 2 * heads >= cus ? 1024 : 512;
+    if (p.shape == 3) {
+        // Whole, too, where the rows that there are fill the machine, once for whole prompts and eight times for chunks behind contexts, whose lengths
+        // may be far apart; but shared where sequences do not bring about as many rows each (four chunks of 512 tokens behind 64 to 32768 whole /
+        // shared 722 / 417 us).
+        const int64_t units = num_kv_heads * ((int64_t)total_q * (num_q_heads / num_kv_heads) / p.rows);
+        whole_keys = units >= 2 * cus ? 4096 : units >= cus ? 1536 : 512;
+        if (units >= slots * (keys <= 2 * (int64_t)max_q_len ? 1 : 8)) whole_keys = keys;
+        if (2 * (int64_t)total_q < (int64_t)batch * max_q_len) whole_keys = 512;
+    }
+    const bool cut = keys > whole_keys;
     const int64_t tiles = ((int64_t)max_seq_len + p.tile - 1) / p.tile;
     if (cut) {
         const int64_t most = ((int64_t)batch * p.row_blocks * tiles + kTreeMinTiles - 1) / kTreeMinTiles;

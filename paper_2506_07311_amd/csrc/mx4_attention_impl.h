@@ -70,7 +70,7 @@ struct Mx4Shape {
     {
         return uint4{bf16_pair<0>(codes, unit), bf16_pair<1>(codes, unit), bf16_pair<2>(codes, unit), bf16_pair<3>(codes, unit)};
     }
-    // Bytes w of a lane's V codes are elements of key w % .. of its 8
+    // A lane's V codes are d / 32 bytes of each of its 8 keys, in their order.
     template <int B>
     static __device__ __forceinline__ uint32_t v_pair(const uint32_t (&v)[kVDwords], int key, float unit)   // elements 2 B, 2 B + 1
     {
@@ -234,8 +234,7 @@ struct Mx4Shape {
             const int32_t v_at = ((D / 2) << lp) + vslot * (D / 2) + row16 * (D / 4);
             const int32_t ks_at = ((D + g * (D / 4) / 32) << lp) + kslot;
             const int32_t vs_at = ((D + D / 32 + row16 * (D / 16) / 32) << lp) + vslot;
-            // pages of 32 steps at a time, lane 2 n + h those of keys 16 h .. of the wave's n-th step, and of the next 32 (read step by step
-            // they are a trip to memory in front of each: S0T)
+            // pages of 32 steps at a time, lane 2 n + h those of keys 16 h .. of the wave's n-th step, and of the next 32
             auto pages_of = [&](int32_t n) {
                 const int32_t key = 32 * (step0 + KW * min(n + (lane >> 1), steps - 1)) + 16 * (lane & 1);
                 return table[min(key >> lp, last_block)];

@@ -56,7 +56,7 @@ __global__ __launch_bounds__(kThreads) void paged_kv_gather_mx4_kernel(Mx4View c
         const char* const rec = base + h * c.head_stride;
         uint32_t codes;
         if (what == 0) {
-            codes = *reinterpret_cast<const uint32_t*>(rec + mx4_k_codes(lp, d, slot) + 4 * u);
+            codes = *reinterpret_cast<const uint32_t*>(rec + mx4_k_codes(d, slot) + 4 * u);
         } else if (d == 64) {
             codes = *reinterpret_cast<const uint16_t*>(rec + mx4_v_codes(lp, d, slot, 2 * u)) |
                     (uint32_t)*reinterpret_cast<const uint16_t*>(rec + mx4_v_codes(lp, d, slot, 2 * u + 1)) << 16;

@@ -374,7 +374,7 @@ __global__ __launch_bounds__(kThreads, TO4 && PAIRS != kOddHalves ? 6 : 1) void 
             char* const rec = (char*)a.k_cache + slot + h * a.head_stride;
             const int32_t lp = a.log2_page;
             if (what == 1) {
-                char* const dst = rec + mx4_k_codes(lp, d, place) + u * (V / 2);
+                char* const dst = rec + mx4_k_codes(d, place) + u * (V / 2);
                 if (V == 8) *reinterpret_cast<uint32_t*>(dst) = codes;
                 else *reinterpret_cast<uint16_t*>(dst) = (uint16_t)codes;
             } else {
