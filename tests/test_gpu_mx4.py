@@ -405,8 +405,7 @@ def test_norm_rope_append_into_four_bits(dtype, d, inter):
 
 
 def test_a_run_as_a_server_makes_it():
-    """Plan, norms and positions into the 4-bit cache, attention: a prompt, then three steps of one or several tokens, two sequences, one
-    captured graph for each width."""
+    """Plan, norms and positions into the 4-bit cache, attention: a prompt, then three steps of one or several tokens, two sequences."""
     hq, hkv, d, page = 8, 2, 128, 16
     g = torch.Generator().manual_seed(5)
     cache = pa.pa_mx4_cache(80, page, hkv, d)
@@ -551,3 +550,68 @@ def test_refusals():
     with pytest.raises(PagedAttnError):
         pa.paged_norm_rope_append_mx4(c.cache, q[..., :96].contiguous(), None, None, rope, None, None, None,
                                       torch.zeros(16, dtype=torch.float64, device=DEV))
+
+
+def test_a_captured_decode_loop():
+    """One graph of plan, norms and positions into the cache, attention and the lengths' step, replayed with eager work in between: each
+    replay as the calls one by one on a cache of their own."""
+    hq, hkv, d, page, B = 8, 2, 128, 16, 3
+    g = torch.Generator().manual_seed(6)
+    freq = pa.pa_rope_frequencies(d)[0].to(DEV)
+    qw, kw = (1 + 0.1 * torch.randn(2, d, generator=g)).bfloat16().to(DEV)
+    q_in, out = torch.zeros(B, hq, d, dtype=torch.bfloat16, device=DEV), torch.zeros(B, hq, d, dtype=torch.bfloat16, device=DEV)
+    k_in, v_in = (torch.zeros(B, hkv, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    new = ints([1] * B)
+
+    class Side:
+        def __init__(self):
+            self.cache = pa.pa_mx4_cache(60, page, hkv, d)
+            self.cache.fill_(255)
+            self.table, self.num = ints(np.full((B, 20), -1)), ints([0] * B)
+            self.free, self.count, self.ctx = ints(np.arange(60)), ints([60]), ints([0] * B)
+            self.cu, self.lens, self.ids, self.at, self.rope = (ints(np.zeros(n)) for n in (B + 1, B, B, B, B))
+            self.short, self.q = ints([0, 0]), torch.zeros_like(q_in)
+            self.ws = torch.empty(pa.paged_attention_mx4_workspace_bytes(B, hq, hkv, d, B, 1, 20 * page), dtype=torch.uint8, device=DEV)
+
+        def step(self, o):
+            pa.paged_plan_step(self.ctx, new, self.table, self.num, self.free, self.count, page, B, mask_words=0, seq_lens=self.lens,
+                               cu_q_lens=self.cu, seq_ids=self.ids, positions=self.at, rope_positions=self.rope, shortage=self.short)
+            pa.paged_norm_rope_append_mx4(self.cache, q_in, k_in, v_in, self.rope, self.ids, self.at, self.table, freq, q_weight=qw, k_weight=kw,
+                                          q_out=self.q)
+            pa.paged_attention_mx4(self.cache, self.q, self.cu, 1, self.table, self.lens, 20 * page, d ** -0.5, out=o, workspace=self.ws)
+            self.ctx.add_(new)
+
+    one, other = Side(), Side()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        one.step(out)
+    want = torch.zeros_like(out)
+    for i in range(40):
+        for x in (q_in, k_in, v_in):
+            x.copy_(torch.randn(x.shape, generator=g).bfloat16())
+        graph.replay()
+        other.step(want)
+        torch.cuda.synchronize()
+        assert one.ctx.tolist() == [i + 1] * B and one.short.tolist() == [0, 0]
+        assert torch.equal(out, want) and torch.equal(one.cache, other.cache) and bool(torch.isfinite(out.float()).all())
+
+
+def test_captured_append_and_gather():
+    c = Cache([300, 77, 5], 2, 128, seed=22)
+    k, v = (torch.zeros(382, 2, 128, device=DEV) for _ in range(2))
+    lens, cu = ints(c.lens), ints(np.cumsum([0, *c.lens]))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        pa.paged_kv_append_mx4(c.cache, c.k_new, c.v_new, c.ids, c.places, c.table)
+        pa.paged_kv_gather_mx4(c.cache, c.table, lens, cu_lens=cu, max_seq_len=300, out_k=k, out_v=v)
+    for i in range(3):
+        c.k_new.mul_(-1.5), c.v_new.add_(0.1)
+        k.zero_(), v.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, x in ((k, c.k_new), (v, c.v_new)):
+            np.testing.assert_array_equal(got.cpu().numpy(), ref.values(*ref.quantised(x.double().cpu().numpy())))
