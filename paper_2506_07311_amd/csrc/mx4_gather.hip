@@ -78,13 +78,13 @@ __global__ __launch_bounds__(kThreads) void paged_kv_gather_mx4_kernel(Mx4View c
             x[2 * b + 1] = v[1];
         }
         if (DT == PA_DTYPE_F32) {
-            float4* const dst = reinterpret_cast<float4*>((float*)(what ? out_v : out_k) + at);
-            dst[0] = float4{x[0], x[1], x[2], x[3]};
-            dst[1] = float4{x[4], x[5], x[6], x[7]};
+            float* const dst = (float*)(what ? out_v : out_k) + at;
+            store_past_cache(dst, __builtin_bit_cast(uint4, float4{x[0], x[1], x[2], x[3]}));
+            store_past_cache(dst + 4, __builtin_bit_cast(uint4, float4{x[4], x[5], x[6], x[7]}));
         } else {
             typedef typename std::conditional<DT == PA_DTYPE_F16, ElemF16, ElemBf16>::type E;
-            *reinterpret_cast<uint4*>((uint16_t*)(what ? out_v : out_k) + at) =
-                uint4{E::pack(x[0], x[1]), E::pack(x[2], x[3]), E::pack(x[4], x[5]), E::pack(x[6], x[7])};
+            store_past_cache((uint16_t*)(what ? out_v : out_k) + at,
+                             uint4{E::pack(x[0], x[1]), E::pack(x[2], x[3]), E::pack(x[4], x[5]), E::pack(x[6], x[7])});
         }
     }
 }

@@ -396,7 +396,7 @@ __global__ __launch_bounds__(kThreads, TO4 && PAIRS != kOddHalves ? 6 : 1) void 
         else if (slot >= 0) dst = pick(what, (T*)a.k_cache, (T*)a.k_cache, (T*)a.v_cache) + slot + h * a.head_stride;
         if (dst && live) {
             if (what != 2) out = E::pack(x);
-            *reinterpret_cast<uint4*>(dst + first) = out;
+            store_past_cache(dst + first, out);
         }
     }
 }
