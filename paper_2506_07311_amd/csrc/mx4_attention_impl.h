@@ -51,6 +51,18 @@ struct Mx4Shape {
         uint2 ks[kKScales], vs;
     };
 
+    // Codes are read once where no other wave has rows beside: past the caches (us from memory without / so: 16 x 131072 tokens 398 / 365, 6.25 TB/s, as a
+    // plain read; 64 on 64 to 32768 81 / 76, 16 x 8000..9000 38.9 / 35.1, head_dim 64 27.9 / 25.9; 256 x 1000 that share 512, which the last-level cache still holds, 39.5 / 42.2.
+    // At head_dim 256, where a lane's two pieces of a line come by two loads, 66.6 / 84.6).
+    typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+    template <typename T, typename V>
+    static __device__ __forceinline__ T read(const char* p)
+    {
+        if (RW == 1 && D <= 128) return __builtin_bit_cast(T, __builtin_nontemporal_load(reinterpret_cast<const V*>(p)));
+        return *reinterpret_cast<const T*>(p);
+    }
+
     static __device__ __forceinline__ uint32_t scale_bits(uint2 s, int i)   // scale of key i of 8, as a float's bits
     {
         const uint32_t w = i < 4 ? s.x : s.y;
@@ -256,12 +268,12 @@ struct Mx4Shape {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     if constexpr (D == 64) {
-                        const uint2 w = *reinterpret_cast<const uint2*>(kp + i * (4 * D / 2));
+                        const uint2 w = read<uint2, u32x2>(kp + i * (4 * D / 2));
                         x.k[i][0] = w.x, x.k[i][1] = w.y;
                     } else {
 #pragma unroll
                         for (int j = 0; j < kKDwords; j += 4) {
-                            const uint4 w = *reinterpret_cast<const uint4*>(kp + i * (4 * D / 2) + 4 * j);
+                            const uint4 w = read<uint4, u32x4>(kp + i * (4 * D / 2) + 4 * j);
                             x.k[i][j] = w.x, x.k[i][j + 1] = w.y, x.k[i][j + 2] = w.z, x.k[i][j + 3] = w.w;
                         }
                     }
@@ -270,7 +282,7 @@ struct Mx4Shape {
                 for (int j = 0; j < kKScales; ++j) x.ks[j] = *reinterpret_cast<const uint2*>(ksp + (j << lp));
 #pragma unroll
                 for (int j = 0; j < kVDwords; j += 4) {
-                    const uint4 w = *reinterpret_cast<const uint4*>(vp + 4 * j);
+                    const uint4 w = read<uint4, u32x4>(vp + 4 * j);
                     x.v[j] = w.x, x.v[j + 1] = w.y, x.v[j + 2] = w.z, x.v[j + 3] = w.w;
                 }
                 x.vs = *reinterpret_cast<const uint2*>(vsp);
