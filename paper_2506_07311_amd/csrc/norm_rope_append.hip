@@ -164,7 +164,7 @@ __device__ __forceinline__ void sine_cosine(double turns, double& sn, double& cs
 // A head is LANES lanes of a wave (a power of two), 16 bytes each; a workgroup has 128 / LANES heads of one token at a time.  Of an element x
 // with partner y the lane keeps a = m cos t (offset + w) and b = -+ m sin t (offset + w of the partner), the same for all heads where they
 // share weights: a head costs it the sum of squares and x inv a + y inv b.  Bound by reading and writing q, K and V once: 8192 tokens of 32 / 8
-// heads of 128, 201 MB, 35.3 us on the same data again (5.7 TB/s), 46 on data from memory (4.3; a copy of 4 GiB 4.7).  A token's first wait is for
+// heads of 128, 201 MB, 36 us on the same data again (5.6 TB/s), 42.8 on data from memory (4.7, as a copy of 4 GiB).  A token's first wait is for
 // its angles; two waves a workgroup lose least there (64 / 128 / 256 / 512 threads: 38.0 / 34.4 / 35.9 / 51.8, before sine and cosine were
 // 64-bit, 0.9 more).  Two pieces in flight instead of one cost registers and gain nothing (35.9 / 38.0).
 template <pa_dtype DT, int PAIRS, bool TO4, int LANES>
