@@ -424,7 +424,7 @@ typedef struct {
     float          mscale;
 } pa_norm_rope;
 
-/* Norms, rotary positions, and Algorithm 1, Assign, of the K rows that they leave and the V rows, in one pass. */
+/* Norms, rotary positions, and Algorithm 1, Assign, of the K rows that they leave and the V rows, in one pass.  T is below 2^25. */
 pa_status paged_norm_rope_append(const pa_kv_cache_desc* cache, const pa_norm_rope* tokens, void* stream);
 
 /*
@@ -467,7 +467,7 @@ pa_status paged_kv_append_mx4(const pa_mx4_cache_desc* cache, pa_dtype dtype, co
 /* Algorithm 1, Gather, from a 4-bit cache: tokens [first_lens[s], seq_lens[s]) of sequence s (first_lens NULL: all) to rows
  * cu_lens[s] .. cu_lens[s + 1] of out_k / out_v [total_rows, Hkv, d], contiguous, of type `dtype`; cu_lens int32[batch + 1].  max_seq_len:
  * host upper bound of seq_lens.  Rounded to nearest where the type has fewer exponents; rows behind the last sequence, and of
- * blocks that are not mapped, are left as they are. */
+ * blocks that are not mapped, are left as they are.  Rows stay below 2^27 - 7. */
 pa_status paged_kv_gather_mx4(const pa_mx4_cache_desc* cache, pa_dtype dtype, void* out_k, void* out_v, int32_t total_rows,
                               const int32_t* block_table, const int32_t* first_lens, const int32_t* seq_lens, const int32_t* cu_lens,
                               int32_t batch, int32_t max_blocks, int32_t max_seq_len, void* stream);

@@ -56,6 +56,7 @@ pa_status check_tokens(pa_norm_rope& r, pa_dtype dtype, int32_t kv_heads, int32_
     if (r.v_stride == 0) r.v_stride = kv_row;
     if (r.q && (r.q_stride < q_row || r.q_out_stride < q_row || (r.q == r.q_out && r.q_stride != r.q_out_stride))) return PA_ERR_INVALID_ARG;
     if (r.k_new && (r.k_stride < kv_row || r.v_stride < kv_row)) return PA_ERR_INVALID_ARG;
+    if (r.T >= 1 << 25) return PA_ERR_UNSUPPORTED;           // (128 threads a token: those of a launch stay below 2^32)
     if (r.q_stride % epv || r.q_out_stride % epv || r.k_stride % epv || r.v_stride % epv) return PA_ERR_UNSUPPORTED;
     if (((uintptr_t)r.q | (uintptr_t)r.q_out | (uintptr_t)r.k_new | (uintptr_t)r.v_new | (uintptr_t)r.q_weight | (uintptr_t)r.k_weight) & 15)
         return PA_ERR_UNSUPPORTED;
@@ -133,7 +134,9 @@ pa_status paged_kv_gather_mx4(const pa_mx4_cache_desc* cache, pa_dtype dtype, vo
     if (!out_k || !out_v || !block_table || !seq_lens || !cu_lens || max_blocks == 0) return PA_ERR_INVALID_ARG;
     if ((((uintptr_t)out_k | (uintptr_t)out_v) & 15) || cache->num_kv_heads > 8192) return PA_ERR_UNSUPPORTED;
     const int64_t most = (int64_t)batch * max_seq_len;
-    return launch_kv_gather_mx4(cache, dtype, out_k, out_v, total_rows < most ? total_rows : (int32_t)most, block_table, first_lens, seq_lens,
+    const int32_t rows = total_rows < most ? total_rows : (int32_t)most;
+    if (rows > (1 << 27) - 8) return PA_ERR_UNSUPPORTED;     // (256 threads for 8 rows: those of a launch stay below 2^32)
+    return launch_kv_gather_mx4(cache, dtype, out_k, out_v, rows, block_table, first_lens, seq_lens,
                                 cu_lens, batch, max_blocks, stream_of(stream));
 }
 

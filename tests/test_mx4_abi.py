@@ -107,6 +107,18 @@ def test_cache_refusals(lib):
     assert call(lib.paged_kv_gather_mx4, gather, rows=i32(0)) == 0
 
 
+def test_calls_of_more_threads_than_a_launch_has(lib):
+    for fn, first in ((lib.paged_norm_rope_append, dict(cache=plain())), (lib.paged_norm_rope_append_mx4, dict(cache=desc(), dtype=i32(1)))):
+        for T in (1 << 25, (1 << 31) - 1):
+            assert call(fn, dict(first, tokens=tokens(T=T), stream=NULL)) == UNSUPPORTED
+    append = dict(cache=desc(), dtype=i32(1), k=P, v=P, ids=P, pos=P, T=i32(1 << 25), table=P, batch=i32(2), max_blocks=i32(4), stream=NULL)
+    assert call(lib.paged_kv_append_mx4, append) == UNSUPPORTED
+    gather = dict(cache=desc(), dtype=i32(1), k=P, v=P, rows=i32((1 << 31) - 1), table=P, first=NULL, lens=P, cu=P, batch=i32(1 << 10),
+                  max_blocks=i32(1 << 14), max_len=i32(1 << 18), stream=NULL)
+    assert call(lib.paged_kv_gather_mx4, gather) == UNSUPPORTED
+    assert call(lib.paged_kv_gather_mx4, gather, rows=i32((1 << 27) - 7)) == UNSUPPORTED
+
+
 def attention_args():
     return dict(cache=desc(), dtype=i32(1), q=P, out=P, lse=NULL, cu=P, total=i32(6), max_q=i32(3), table=P, lens=P, batch=i32(2), hq=i32(32),
                 max_blocks=i32(4), max_len=i32(64), scale=f32(0.1), ws=ctypes.c_void_p(0x10000), bytes=size(1 << 40), stream=NULL)
