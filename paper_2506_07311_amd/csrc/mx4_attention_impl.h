@@ -39,6 +39,7 @@ struct Mx4Shape {
     static constexpr int kJoin = KW > 1 ? RW * KW * RT * D * 16 * 4 : 0;               // bytes in which the waves' results meet
     static constexpr int kTileB = 2 * 64 * D * 2;            // bytes of a tile's operands
     static constexpr int kLds = SHARED ? 2 * kTileB : kJoin + kWaves * RT * 16 * 8 + 1024;
+    static_assert(KW == 1 || KW == 2 || KW == 4 || KW == 8, "their join knows log2 of it");
     static_assert(!SHARED || (KW == 1 && RW == 4 && D <= 128), "a quarter is 16 keys of K, 32 keys and half of the columns of V");
     static constexpr int kSteps = D / 32, kTiles = D / 16;
     static constexpr int kKDwords = D / 32, kVDwords = D / 16;                         // of a lane: per key, and for its 8 keys
@@ -442,9 +443,11 @@ struct Mx4Shape {
                     sum = 0.f;
 #pragma unroll
                     for (int k = 0; k < KW; ++k) {
-                        weight[k] = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stats[at + 16 * k] - top);
+                        // (a mean: no sum of the waves' overflows)
+                        weight[k] = top == -INFINITY ? 0.f : (1.f / KW) * __builtin_amdgcn_exp2f(stats[at + 16 * k] - top);
                         sum += stats[kStats + at + 16 * k] * weight[k];
                     }
+                    top += KW == 8 ? 3.f : KW == 4 ? 2.f : 1.f;
                 }
                 const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
                 auto leave = [&](int i, int c, float4 x) {
