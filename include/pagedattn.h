@@ -465,9 +465,10 @@ pa_status paged_kv_append_mx4(const pa_mx4_cache_desc* cache, pa_dtype dtype, co
                               int32_t batch, int32_t max_blocks, void* stream);
 
 /* Algorithm 1, Gather, from a 4-bit cache: tokens [first_lens[s], seq_lens[s]) of sequence s (first_lens NULL: all) to rows
- * cu_lens[s] .. cu_lens[s + 1] of out_k / out_v [total_rows, Hkv, d], contiguous, of type `dtype`; cu_lens int32[batch + 1].  max_seq_len:
- * host upper bound of seq_lens.  Rounded to nearest where the type has fewer exponents; rows behind the last sequence, and of
- * blocks that are not mapped, are left as they are.  Rows stay below 2^27 - 7. */
+ * cu_lens[s] .. cu_lens[s + 1] of out_k / out_v [total_rows, Hkv, d], contiguous, of type `dtype`; cu_lens int32[batch + 1] does not fall.
+ * A sequence's rows may be more than its tokens, or fewer (its first ones are taken).  max_seq_len: host upper bound of
+ * seq_lens (0: nothing is taken).  Rounded to nearest where the type has fewer exponents; rows without a token, and of blocks that are not
+ * mapped, are left as they are.  total_rows or batch * max_seq_len stays below 2^27 - 7. */
 pa_status paged_kv_gather_mx4(const pa_mx4_cache_desc* cache, pa_dtype dtype, void* out_k, void* out_v, int32_t total_rows,
                               const int32_t* block_table, const int32_t* first_lens, const int32_t* seq_lens, const int32_t* cu_lens,
                               int32_t batch, int32_t max_blocks, int32_t max_seq_len, void* stream);

@@ -74,7 +74,7 @@ pa_status check_mx4_cache(const pa_mx4_cache_desc* c);
 pa_status launch_mx4_copy_page(const pa_mx4_cache_desc* c, int32_t src_page, int32_t dst_page, hipStream_t stream);
 pa_status launch_kv_gather_mx4(const pa_mx4_cache_desc* c, pa_dtype dtype, void* out_k, void* out_v, int32_t rows,
                                const int32_t* block_table, const int32_t* first_lens, const int32_t* seq_lens, const int32_t* cu_lens,
-                               int32_t batch, int32_t max_blocks, hipStream_t stream);
+                               int32_t batch, int32_t max_blocks, int32_t max_seq_len, hipStream_t stream);
 // Into a 4-bit cache (to4), or one of the tokens' own type (cache).
 pa_status launch_norm_rope_append(const pa_kv_cache_desc* cache, const pa_mx4_cache_desc* to4, pa_dtype dtype, const pa_norm_rope& r,
                                   hipStream_t stream);

@@ -1,5 +1,7 @@
 // C ABI of normalised heads, positions of several numbers and the 4-bit cache: argument validation and dispatch.  Every check is a host
 // check made before the first launch; nothing here touches device memory.
+#include <algorithm>
+
 #include "mx4.h"
 
 using namespace pa;
@@ -133,11 +135,10 @@ pa_status paged_kv_gather_mx4(const pa_mx4_cache_desc* cache, pa_dtype dtype, vo
     if (total_rows == 0 || batch == 0 || max_seq_len == 0) return PA_OK;
     if (!out_k || !out_v || !block_table || !seq_lens || !cu_lens || max_blocks == 0) return PA_ERR_INVALID_ARG;
     if ((((uintptr_t)out_k | (uintptr_t)out_v) & 15) || cache->num_kv_heads > 8192) return PA_ERR_UNSUPPORTED;
-    const int64_t most = (int64_t)batch * max_seq_len;
-    const int32_t rows = total_rows < most ? total_rows : (int32_t)most;
-    if (rows > (1 << 27) - 8) return PA_ERR_UNSUPPORTED;     // (256 threads for 8 rows: those of a launch stay below 2^32)
-    return launch_kv_gather_mx4(cache, dtype, out_k, out_v, rows, block_table, first_lens, seq_lens,
-                                cu_lens, batch, max_blocks, stream_of(stream));
+    // (256 threads for 8 rows that may have a token: those of a launch stay below 2^32)
+    if (std::min((int64_t)total_rows, (int64_t)batch * max_seq_len) > (1 << 27) - 8) return PA_ERR_UNSUPPORTED;
+    return launch_kv_gather_mx4(cache, dtype, out_k, out_v, total_rows, block_table, first_lens, seq_lens, cu_lens, batch, max_blocks,
+                                max_seq_len, stream_of(stream));
 }
 
 size_t paged_attention_mx4_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
