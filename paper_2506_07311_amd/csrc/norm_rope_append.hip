@@ -319,7 +319,16 @@ __global__ __launch_bounds__(kThreads, TO4 && PAIRS != kOddHalves ? 6 : 1) void 
                 double sum = 0.0;
 #pragma unroll
                 for (int e = 0; e < V; ++e) sum = fma((double)x[e], (double)x[e], sum);
-                return (float)root_of_inverse(lanes_sum<LANES>(sum) * a.by_d64 + (double)r.eps);
+                const double root = root_of_inverse(lanes_sum<LANES>(sum) * a.by_d64 + (double)r.eps);
+                if (!(root > 0x1p+100)) return (float)root;
+                // (subnormal heads: the inverse of a root below 2^-128 is none of fp32's numbers; 2^64 of it goes into the factors)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    fa[e] *= 0x1p+64f;
+                    fb[e] *= 0x1p+64f;
+                }
+                have = -1;
+                return (float)(root * 0x1p-64);
             };
             if (have != what || each) {
                 both_weights(fa, fb, weights, at_head);
