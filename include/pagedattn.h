@@ -454,8 +454,9 @@ typedef struct {
 size_t pa_mx4_record_bytes(int32_t page_size, int32_t head_dim);
 
 /* paged_norm_rope_append into a 4-bit cache.  q, k_new, v_new, q_out are of type `dtype`.  K goes from fp32 to 4 bits, without a rounding to
- * `dtype` in between; each step before it is an fp32 operation of its own (mean of squares, root, product with the weight, two products
- * and a sum of the rotation). */
+ * `dtype` in between; each step before it is an fp32 operation of its own: squares; their sum, ((x0^2 + x1^2) + x2^2) + x3^2 of every
+ * four and then of neighbours in pairs; the product with 1 / head_dim; + eps; the inverse root, to a unit in the last place (a sum that
+ * leaves the range of fp32: from 64 bits); x times it; times (weight_offset + w); the products with mscale cos and mscale sin; their sum. */
 pa_status paged_norm_rope_append_mx4(const pa_mx4_cache_desc* cache, pa_dtype dtype, const pa_norm_rope* tokens, void* stream);
 
 /* Algorithm 1, Assign, into a 4-bit cache: paged_kv_append's arguments, k_new and v_new of type `dtype`.  A row with positions[t] < 0,

@@ -3,10 +3,12 @@
 //
 //     y = x rsqrt(mean(x^2) + eps) (offset + w),   (y_i, y_j) -> m (y_i cos t - y_j sin t, y_i sin t + y_j cos t)
 // with t = p[axis of the pair] f_pair, the angle in 64 bits as turns (rope_append.hip), and so its sine and cosine.  The rest is 32-bit and
-// rounded once.  K on its way to 4 bits takes the steps one by one, each rounded: squares, their sum in fours and then in pairs of neighbours, y,
-// the weight, the products of the rotation, their sum.  A last bit of it can decide between two codes, a third of the value apart; so it
-// is what any program gets that takes the same steps.  (In 64 bits throughout it costs the registers of three waves of seven, 4096 tokens with their
-// gather 31 -> 36 us, these steps 31.5; 64 bits where a border is near, 39: the last of those heads ends late.)
+// rounded once.  K on its way to 4 bits takes the steps one by one, each rounded to fp32: squares, their sum in fours and then of neighbours, its product
+// with 1 / d, eps, an inverse root (a unit in the last place), the products with it and with the weight, those with cosine and sine (64-bit, mscale
+// in them, rounded once), their sum.  A last bit of it can decide between two codes, a third of the value apart; so the header names the steps, and
+// a program that takes them gets the same codes but where the two roots differ.  It is not nearer to the definition than fused products are.
+// (In 64 bits throughout it costs the registers of three waves of seven, 4096 tokens with their gather 31 -> 36 us, these steps 31.5; 64
+// bits where a border is near, 39: the last of those heads ends late.)
 #include "mx4.h"
 
 namespace pa {
@@ -137,7 +139,8 @@ __device__ __forceinline__ float plus(float x, float y)
     return x + y;
 }
 
-// Sine and cosine of so many turns, in 64 bits: an eighth of a turn at most is left to the Taylor series, whose next terms are below 2^-45.
+// Sine and cosine of so many turns, in 64 bits: an eighth of a turn at most is left to the Taylor series, whose next terms are below 2^-45 (sine) and
+// 2^-41 (cosine); both are then rounded to 2^-25.
 __device__ __forceinline__ void sine_cosine(double turns, double& sn, double& cs)
 {
     turns -= rint(turns);

@@ -78,3 +78,98 @@ def test_norms_of_subnormal_numbers_into_four_bits(dtype, size):
     ends = [ref.values(*ref.quantised(want + s * 2.0 ** -19 * size)) for s in (-1, 0, 1)]   # (the bound on an element that the other tests take)
     got = c.held()[0][0]
     assert ((got >= np.minimum.reduce(ends)) & (got <= np.maximum.reduce(ends))).all()
+
+
+F = np.float32
+
+
+def steps_of_rotation(a, b, c, s):
+    """(a c - b s, a s + b c) in fp32, each product and sum rounded by itself."""
+    return a * c - b * s, a * s + b * c
+
+
+def next_to_borders(rng, c, s):
+    """Per element of c and s (fp32) a pair (a, b) of fp32 numbers whose a c - b s lies so near to a border between two codes of scale 1 that
+    the separately rounded steps are on one side of it, or on it, and both fused forms on the other.  (0, 0) where none was found."""
+    borders = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5])
+    best = np.zeros((2, *c.shape), F)
+
+    def code(x):
+        return ref.quantised(np.concatenate([x[..., None], np.full((*x.shape, 31), 6.0)], -1))[0][..., 0]
+
+    for _ in range(60):
+        a = rng.uniform(4, 60, c.shape).astype(F)
+        border = rng.choice(borders, c.shape)
+        b = ((a.astype(np.float64) * c - border) / s).astype(F)
+        for step in range(-6, 7):
+            y = (b.view(np.int32) + step).view(F)
+            apart = a * c - y * s
+            first = (a.astype(np.float64) * c - (y * s)).astype(F)     # a product of two 24-bit numbers is exact in 64 bits
+            second = ((a * c) - y.astype(np.float64) * s).astype(F)
+            hit = (code(apart) != code(first)) & (code(apart) != code(second)) & (np.abs(apart) < 4)
+            best[0], best[1] = np.where(hit, a, best[0]), np.where(hit, y, best[1])
+    return best
+
+
+def test_rotation_on_the_way_to_four_bits_rounds_each_step():
+    """Codes are those of products and sums in fp32 that are rounded one by one: elements next to borders, where a fused product would give
+    other ones."""
+    T, d = 64, 64
+    rng = np.random.default_rng(4)
+    position = rng.integers(1, 60, T)
+    freq = np.geomspace(1.0, 0.02, d // 2)
+    angle = position[:, None] * freq
+    c, s = np.cos(angle).astype(F), np.sin(angle).astype(F)
+    s_safe = np.where(np.abs(s) < 0.05, F(1), s)
+    k = np.zeros((T, 1, d), F)
+    k[:, 0, :d // 2], k[:, 0, d // 2:] = next_to_borders(rng, c, s_safe)
+    k[:, 0][:, np.r_[0, d // 2]] = 0.0
+    lost = np.concatenate([np.abs(s) < 0.05] * 2, 1)
+    k[:, 0][lost] = 0.0
+    k[:, 0, 0], k[:, 0, d // 2] = 5.5 * c[:, 0], -5.5 * s[:, 0]        # (the first pair: about 5.5, which makes the scale 1)
+    left, right = steps_of_rotation(k[:, 0, :d // 2], k[:, 0, d // 2:], c, s)
+    found = (k[:, 0, 1:d // 2] != 0)
+    assert found.mean() > 0.8
+    cache = Cache([T], 1, d, seed=1)
+    k_dev = torch.from_numpy(k).to(DEV)
+    pa.paged_norm_rope_append_mx4(cache.cache, None, k_dev, k_dev, ints(position), cache.ids, cache.places, cache.table,
+                                  torch.from_numpy(freq).to(DEV), norm_k=False)
+    got = cache.held()[0][0][:, 0]
+    want = ref.values(*ref.quantised(np.concatenate([left, right], 1).astype(np.float64)))
+    np.testing.assert_array_equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d,inter", [(64, True), (128, False), (256, False)])
+def test_norms_on_the_way_to_four_bits_round_each_step(dtype, d, inter):
+    """Codes of whole heads are those of fp32 steps, rounded one by one: squares summed in fours, then neighbours, the mean and eps, an inverse
+    root to a unit in the last place, the products with it, with the weight (its offset added), with cosine and sine, their sum."""
+    T, hkv, t = 200, 2, TYPES[dtype]
+    g = torch.Generator().manual_seed(d)
+    rng = np.random.default_rng(d)
+    k = torch.randn(T, hkv, d, generator=g).to(t)
+    w = (0.2 * torch.randn(hkv, d, generator=g)).to(t)
+    position = rng.integers(0, 60, T)
+    freq = np.geomspace(1.0, 0.02, d // 2)
+    cache = Cache([T], hkv, d, seed=2)
+    k_dev = k.to(DEV)
+    pa.paged_norm_rope_append_mx4(cache.cache, None, k_dev, k_dev, ints(position), cache.ids, cache.places, cache.table,
+                                  torch.from_numpy(freq).to(DEV), k_weight=w.to(DEV), weight_offset=1.0, eps=1e-5, interleaved=inter)
+    got = cache.held()[0][0]
+    x = k.float().numpy()
+    sq = (x * x).reshape(T, hkv, d // 4, 4)
+    total = ((sq[..., 0] + sq[..., 1]) + sq[..., 2]) + sq[..., 3]
+    while total.shape[-1] > 1:
+        total = total[..., 0::2] + total[..., 1::2]
+    mean = total * F(1.0 / d) + F(1e-5)
+    angle = position[:, None] * freq
+    c, s = (f(angle).astype(F)[:, None] for f in (np.cos, np.sin))
+    root = (1.0 / np.sqrt(mean.astype(np.float64))).astype(F)
+    ok = np.zeros((T, hkv), bool)
+    for step in (-1, 0, 1):
+        z = x * (root.view(np.int32) + step).view(F) * (w.float().numpy() + F(1))
+        lead = (slice(0, None, 2), slice(1, None, 2)) if inter else (slice(0, d // 2), slice(d // 2, None))
+        turned = np.empty_like(z)
+        turned[..., lead[0]], turned[..., lead[1]] = steps_of_rotation(z[..., lead[0]], z[..., lead[1]], c, s)
+        ok |= (ref.values(*ref.quantised(turned.astype(np.float64))) == got).all(-1)
+    assert ok.all(), int((~ok).sum())
