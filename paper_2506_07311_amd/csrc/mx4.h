@@ -20,8 +20,8 @@ inline Mx4View make_view(const pa_mx4_cache_desc* c)
 
 #if defined(__HIPCC__)
 
-// 16 bytes of whole cache lines that this kernel's L2 has no further use for (us on data from memory, with plain stores / so: 17000 tokens of 8 KV
-// heads of 256 taken out, 140 MB, behind 3000 stored 61 / 40).
+// 16 bytes of cache lines that the wave fills whole, by one store or two behind each other, and that this kernel's L2 has no further use for (us on
+// data from memory, with plain stores / so: 17000 tokens of 8 KV heads of 256 taken out, 140 MB, behind 3000 stored 61 / 40).
 __device__ __forceinline__ void store_past_cache(void* dst, uint4 x)
 {
     typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;

@@ -139,6 +139,7 @@ pa_status launch_attention_mx4(const Mx4Args& t, void* workspace, hipStream_t st
         if (c->head_dim == 128) return launch_mx4_d128(a, merge, t.dtype, p.shape, stream);
         return launch_mx4_d256(a, merge, t.dtype, p.shape, stream);
     };
+    // (A profiler shows both launches under the names of the kernels around a piece of work, paged_attention_tree_*_kernel<Mx4Shape>.)
     {
         ProfileScope prof("paged_attention_mx4_kernel", stream);
         const pa_status st = launch(false);

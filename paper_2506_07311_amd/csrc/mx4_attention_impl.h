@@ -4,12 +4,14 @@
 // lane % 16 = row), so softmax statistics are a lane's own:
 //     S^T[key, row] = K Q^T,   O^T[column, row] += V^T P^T.
 //   * A wave walks keys 32 at a time and takes what it needs of a record straight into registers: a lane's K codes are a
-//     quarter of a key's, its V codes 8 keys by head_dim / 16 elements, which the record holds in one piece; 17 KB of 16-bit K
-//     and V are 4.25 KB in seven loads.  No LDS is involved until the end.
+//     quarter of a key's, its V codes 8 keys by head_dim / 16 elements, which the record holds in one piece; 16 KB of 16-bit K
+//     and V (head_dim 128) are 4.25 KB in six loads.  No LDS is involved until the end, but where waves share operands (SHARED).
 //   * Codes become bf16, exactly, by the hardware's conversion under a block's scale, two elements at a time.  For K those are the operand as
 //     it stands; a lane's V pairs are elements of one key and are exchanged with the next key's by two byte permutes.
-//   * Queries enter with all their bits: bf16 as they are, fp16 as two bf16 terms, fp32 as three.  Weights enter as two terms (2^-17 of a
-//     weight), with fp32 queries as three.
+//   * Queries enter with all their bits: bf16 as they are, fp16 as two bf16 terms (since K is made bf16, whatever its scales), fp32 as three.
+//     Weights enter as two terms (2^-17 of a weight, below the half step of a 16-bit output; about one bf16 output in 500 is the neighbour of
+//     what fp32 weights give), with fp32 queries as three.  A third term for all costs, us: 4 prompts of 2047 234 -> 269, 1000 tokens
+//     behind 31000 689 -> 826, one token on 16 x 8000..9000 36.2 -> 42.8.
 //   * Softmax is online in the log2 domain against a reference that trails the maximum; only where a lane's weights sum to more
 //     than they may is it raised and O rescaled.
 //   * Keys are masked by selection.  A V block of NaN that some rows of a tile do not see would reach them through a product with

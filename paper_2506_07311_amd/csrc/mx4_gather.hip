@@ -10,7 +10,8 @@ namespace {
 constexpr int kThreads = 256;
 
 // ROWS rows a workgroup at a time, a thread 8 elements of a row's head at a time: 4 bytes of codes and a scale in, 16 or 32 bytes out.  Bound by
-// the bytes that it writes.  MORE: the grid does not reach all rows, and a workgroup goes on (without that loop 320000 tokens of 8 heads of 128 take
+// the bytes that it writes: 4096 tokens of 8 heads of 256, 43 MB in 16 bits, 14.0 us, 76 MB in 32 19.2 (there a lane's two stores fill a line's two halves in
+// turn).  MORE: the grid does not reach all rows, and a workgroup goes on (without that loop 320000 tokens of 8 heads of 128 take
 // 399 us, with it 411).
 template <pa_dtype DT, int ROWS, bool MORE>
 __global__ __launch_bounds__(kThreads) void paged_kv_gather_mx4_kernel(Mx4View c, void* out_k, void* out_v, int32_t rows,
