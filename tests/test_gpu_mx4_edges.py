@@ -51,6 +51,48 @@ def test_gather_into_rows_with_room_between_sequences(dtype, starts, rows, part)
     assert torch.equal(k.cpu(), want[0]) and torch.equal(v.cpu(), want[1])
 
 
+def test_gather_of_many_sequences():
+    """More sequences than a wave looks at in one go, empty ones among them; few and many rows."""
+    rng = np.random.default_rng(3)
+    for most in (9, 60):
+        lens = [int(x) for x in rng.integers(0, most, 200)]
+        lens[0] = lens[63] = lens[64] = lens[199] = 0
+        c = Cache(lens, 2, 64, seed=most).fill()
+        k, v = (torch.full((sum(lens) + 1, 2, 64), 7.0, device=DEV) for _ in range(2))
+        pa.paged_kv_gather_mx4(c.cache, c.table, ints(lens), cu_lens=ints(np.cumsum([0, *lens])), max_seq_len=most, out_k=k, out_v=v)
+        for got, i in ((k, 0), (v, 1)):
+            want = np.concatenate([x[i] for x in c.held()])
+            assert np.array_equal(got[:-1].cpu().numpy(), want.astype(np.float32)) and (got[-1] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("new", [1, 5, 12, 40])
+@pytest.mark.parametrize("size", [2.0 ** 10, 2.0 ** 20, 2.0 ** 25])
+@pytest.mark.parametrize("n", [300, 3000])
+def test_large_scores(dtype, new, size, n):
+    """Scores are multiples of size / 2 up to 6 size, exact in fp32, with one largest a row: its V row comes out.  (The two steps of a weight
+    and its sum, a product and a quotient: 2^-15 of V.  The score times log2 e is rounded before a logarithm of at most 2^24 is added.)"""
+    d, hq = 64, 4
+    c = Cache([n], 1, d, seed=9)
+    g = torch.Generator().manual_seed(n + new)
+    grid = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0])
+    k = torch.zeros(n, 1, d)
+    k[:, 0, :hq] = grid[torch.randint(0, 7, (n, hq), generator=g)] * torch.where(torch.rand(n, hq, generator=g) < 0.5, -1.0, 1.0)
+    k[:, 0, hq:] = 4.0                                            # (every block's scale is 1)
+    best = torch.arange(hq) * 37 + 50
+    k[best, 0] = 0.0
+    k[best, 0, torch.arange(hq)] = 6.0
+    c.k_new = k.to(DEV)
+    c.fill()
+    q = torch.zeros(new, hq, d, device=DEV)
+    q[:, torch.arange(hq), torch.arange(hq)] = size
+    out, lse, _ = attend(c, [new], hq, dtype, q=q.to(TYPES[dtype]), scale=1.0, expect=False)
+    v = torch.from_numpy(c.held()[0][1][best.numpy(), 0])
+    err = (out.double().cpu() - v).abs()
+    assert (err <= (2.0 ** -15 + torch.finfo(TYPES[dtype]).eps / 2) * v.abs()).all()
+    assert ((lse.double().cpu() - 6 * size).abs() <= 2.0 ** -22 * 6 * size + 2.0 ** -18).all()
+
+
 @pytest.mark.parametrize("dtype,size", [("fp32", 3e38), ("fp32", 1e-39), ("fp32", 3e-43), ("bf16", 3e38), ("bf16", 1e-39)])
 @pytest.mark.parametrize("d,rot,inter", [(128, 128, False), (80, 20, False), (256, 128, True)])
 def test_norms_of_the_largest_and_of_subnormal_numbers(dtype, size, d, rot, inter):
