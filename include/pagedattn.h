@@ -438,7 +438,8 @@ pa_status paged_norm_rope_append(const pa_kv_cache_desc* cache, const pa_norm_ro
  * A code is sign (bit 3), two bits of exponent and one of mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6.  A scale s stands for
  * 2^(s - 127), 255 for a block of NaN.  The scale of a block with largest magnitude a is 2^(floor(log2 a) - 2), at least
  * 2^-127; elements are rounded to nearest, ties to the even mantissa, and end at 6.  A block with an infinity or a NaN is
- * a block of NaN.  (So 252 is the largest scale of numbers; attention expects no 253 or 254, whose values may leave fp32.)  Supported: head_dim 64, 128, 256; page_size a power of two, at least 16.  A page takes 17/64 of its 16-bit size.
+ * a block of NaN.  (So 252 is the largest scale of numbers; attention expects no 253 or 254, whose values may leave fp32.)
+ * Supported: head_dim 64, 128, 256; page_size a power of two, at least 16.  A page takes 17/64 of its 16-bit size.
  */
 typedef struct {
     void*   records;                 /* 16-byte aligned */
@@ -481,8 +482,8 @@ pa_status paged_kv_gather_mx4(const pa_mx4_cache_desc* cache, pa_dtype dtype, vo
  * lse float[total_q, Hq] or NULL.  A row that sees no key (seq_lens[s] = 0 in a padded batch) gets out = 0, lse = -inf; rows from
  * cu_q_lens[batch] on are left as they are.  max_q_len, max_seq_len: host upper bounds.  K and V enter the products exactly,
  * queries with all their bits, weights with 16 (fp32 queries: 24), sums are fp32.  Scores are to stay below 2^28 in magnitude.  Finite values of V give
- * finite means (of up to 2^24 keys); blocks of NaN reach the rows that see them.  Results repeat bit for bit with the same arguments.  workspace: 256-byte aligned,
- * paged_attention_mx4_workspace_bytes(...) with the same sizes; its contents need not be kept between calls.
+ * finite means (of up to 2^24 keys); blocks of NaN reach the rows that see them.  Results repeat bit for bit with the same arguments.
+ * workspace: 256-byte aligned, paged_attention_mx4_workspace_bytes(...) with the same sizes; its contents need not be kept between calls.
  */
 size_t paged_attention_mx4_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                            int32_t total_q, int32_t max_q_len, int32_t max_seq_len);

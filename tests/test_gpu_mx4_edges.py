@@ -108,6 +108,19 @@ def test_norms_of_the_largest_and_of_subnormal_numbers(dtype, size, d, rot, inte
                                                         interleaved=inter), eps=0.0, interleaved=inter)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("per_head", [False, True])
+def test_norms_of_heads_far_apart(dtype, per_head):
+    """Subnormal, ordinary and very large heads in turn and in any order, several of a token in the same lanes."""
+    t = TYPES[dtype]
+    c = norms.Case(t, T=4100, hq=20, hkv=4, d=128, per_head=per_head, seed=9)
+    g = torch.Generator().manual_seed(4)
+    for x in (c.q, c.k):
+        size = torch.tensor([1e-39, 1.0, 1e30], dtype=torch.float64)[torch.randint(0, 3, (*x.shape[:2], 1), generator=g)]
+        x.copy_((x.double().cpu() * size).to(t))
+    norms.check(c, t, lambda: pa.paged_norm_rope_append(c.k_cache, c.v_cache, *c.tokens(), q_weight=c.qw, k_weight=c.kw, eps=0.0), eps=0.0)
+
+
 @pytest.mark.parametrize("dtype,size", [("fp32", 1e-39), ("bf16", 1e-39), ("fp32", 3e38)])
 def test_norms_of_subnormal_numbers_into_four_bits(dtype, size):
     t, d = TYPES[dtype], 128
